@@ -308,6 +308,131 @@ int sj_lsh_plan(double p1, double p2, uint64_t n, uint32_t tile, double recall, 
 int sj_jl(sj_ctx *ctx, int dtype, const void *X, uint32_t n, uint32_t d, uint32_t levels,
           const uint32_t *shape, const float *A, float *Y);
 
+/* ---------------------------------------------------------------------------
+ * A cache of key and value rows, and attention over it.
+ *
+ * Attention is the softened join of query rows with a table of key rows: where
+ * a join reports the rows j with <x, k_j> >= s, attention weighs every row by
+ * exp(scale <x, k_j>) / sum and answers with the weighted mean of the value rows
+ * v_j.  The same blocked product feeds both, and again no score matrix is
+ * stored.  The calls below keep the table (rows appended with their rotary
+ * positions, rows evicted by the weight they have drawn) and query it.
+ *
+ * Unlike the joins these calls only put work on the context's stream and
+ * return: no result comes back to the host, so nothing is waited for.  Their
+ * device scratch grows on demand; a call that does not grow it may be captured
+ * into a HIP graph, and its grid does not depend on the lengths, which are read
+ * on the device.  sj_get_stats describes the joins only and is left alone.
+ *
+ * Numbers on the device (lengths, tables, masks) are not read back to be
+ * checked; whatever they hold, no access leaves the described arrays: lengths
+ * are clamped to [0, width * page], and rows whose page number is outside
+ * [0, pages) do not exist (they are not attended to, appended or evicted
+ * to, and are read as zeros where they are evicted from).
+ *
+ * A cache is a pool of `pages` pages of `page` rows for `heads` heads of d
+ * elements, k and v apart, each with strides of its own in elements (elements of
+ * one row and head are adjacent).  Row n of sequence b is row n % page of page
+ * table[b * table_row + n / page]; a sequence has room for width * page rows.
+ * Without a table (NULL) sequence b is page b and width is 1. */
+typedef struct sj_cache {
+    int dtype;                      /* SJ_F16 or SJ_BF16 */
+    uint32_t heads, d;              /* d <= 256 */
+    uint32_t pages, page;           /* pages in the pool, rows in a page */
+    uint32_t batch, width;          /* sequences, pages of a sequence in the table */
+    int64_t table_row;              /* elements from one sequence's table row to the next */
+    const int32_t *table;           /* device, or NULL */
+    void *k, *v;                    /* device, caller-owned */
+    int64_t k_page, k_row, k_head;  /* strides in elements, >= 0 */
+    int64_t v_page, v_row, v_head;
+} sj_cache;
+
+/* Rotary layouts: pair i of a head is elements (i, i + rot / 2) or (2 i, 2 i + 1). */
+enum sj_layout { SJ_HALF = 0, SJ_INTERLEAVED = 1 };
+
+/* Flags of the calls on caches. */
+enum sj_cache_flags {
+    SJ_FLAG_INVERSE = 16u  /* sj_rotary: turn back (the transposed map: the gradient) */
+};
+
+/* Rotary positions: y = x with its first rot = 2 n_pairs elements of every
+ * head turned by the token's position, pair i by the angle pos * f_i and scaled by
+ * `factor`: (a, b) -> factor (a cos - b sin, b cos + a sin); elements from rot on
+ * are copied.  The frequency f_i is given in turns a position as the fixed-point
+ * fraction turns[i] = f_i / (2 pi) * 2^64 (device, int64), so that whole turns
+ * drop out of the 64-bit product pos * turns[i] and far positions lose no
+ * precision.  x and y are n tokens x heads x d elements of dtype with
+ * strides {token, head} in elements (host arrays; adjacent elements within a
+ * head); pos (device) holds n int32 positions, any sign.  y may be x with the
+ * same strides; otherwise the two must not overlap.  SJ_FLAG_INVERSE turns by -pos * f_i,
+ * which is the gradient of the call without it.  Errors as the joins';
+ * SJ_E_INVAL also for 2 n_pairs > d or a negative stride. */
+int sj_rotary(sj_ctx *ctx, int dtype, const void *x, const int64_t x_stride[2], void *y,
+              const int64_t y_stride[2], uint32_t n, uint32_t heads, uint32_t d,
+              const int32_t *pos, const int64_t *turns, uint32_t n_pairs, int layout, double factor,
+              unsigned flags);
+
+/* Appends t rows to every sequence: row len[b] + u of sequence b receives key
+ * (b, u), turned as sj_rotary turns it by pos[b * t + u], and value (b, u) as it is, for
+ * u < count[b] (count NULL: u < t).  key and value are batch x t x heads x d with strides
+ * {sequence, token, head}; q, when given, is batch x t x q_heads x d, and its
+ * turned rows (all t of a sequence) go to q_out with strides q_out_stride.  With n_pairs = 0 nothing is turned (pos and turns may
+ * be NULL).  len (device, int32 per sequence) is not changed.  Rows past the
+ * sequence's room or in pages that do not exist are dropped.  The rows of one
+ * call must be distinct rows of the pool.  key, value and q must not overlap
+ * the cache or q_out (q_out may be q with the same strides). */
+int sj_cache_append(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, const int32_t *count,
+                    uint32_t t, const void *key, const int64_t key_stride[3], const void *value,
+                    const int64_t value_stride[3], const int32_t *pos, const int64_t *turns,
+                    uint32_t n_pairs, int layout, double factor, const void *q,
+                    const int64_t q_stride[3], uint32_t q_heads, void *q_out,
+                    const int64_t q_out_stride[3]);
+
+/* Attention of t tokens of every sequence over its rows in the cache.  Token u of
+ * sequence b (u < count[b], or u < t without count) sees the rows n < len[b] and, of
+ * the rows len[b] + w of the tokens themselves (w < count[b], appended
+ * before the call), those that its mask names: bit w % 64 of word w / 64 of
+ * tree[b * tree_stride[0] + u * tree_stride[1] + ...], ceil(t / 64) words a token.
+ * With tree NULL the tokens are a chain: w <= u.  Query head i reads cache head
+ * i / (q_heads / heads).  For every token and query head, over the rows n it sees,
+ *   s_n = scale <q, k_n>,  lse = log sum_n exp(s_n),  out = sum_n exp(s_n - lse) v_n,
+ * and for every cache head the weight that row n draws from all its query heads
+ * and tokens, w_out[b, head, n] = w_in[b, head, n] + sum exp(s_n - lse).
+ * A row that sees nothing has out = 0, lse = -inf and adds no weight, as have the tokens from
+ * count[b] on; what a mask or a length hides (NaN and infinities in keys and values
+ * included) changes nothing.
+ * q is batch x t x q_heads x d with strides {sequence, token, head};
+ * out (batch x t x q_heads x d of dtype) and lse (batch x t x q_heads fp32, or NULL) are
+ * contiguous; w_in and w_out (batch x heads x w_cols fp32, contiguous; w_in NULL:
+ * zeros) may be the same array; w_out NULL: no weights.
+ * Arithmetic: fp32 sums of 16-bit products on the matrix cores; softmax statistics
+ * and weights in fp32; exp(s_n - running maximum) enters the product with v as
+ * 16-bit values.  Results do not depend on timing (no atomics).
+ * Errors as the joins'; SJ_E_INVAL also when heads does not divide q_heads or for a NaN
+ * scale; SJ_E_UNSUPPORTED for d > 256, width * page or t * q_heads / heads >= 2^31. */
+int sj_attend(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, const int32_t *count,
+              uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
+              const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,
+              float *lse, const float *w_in, float *w_out, uint64_t w_cols);
+
+/* Eviction by accumulated weight: copies the rows worth keeping of every
+ * sequence of `src` into `dst` (same dtype, heads, d and batch; other pages),
+ * closed up and in their order.  Of n = len[b] rows the kept ones are all if n <=
+ * keep, else the first `sink`, the last `recent` and, of those between, the keep -
+ * sink - recent of largest weight: ties go to the lower row, -0 equals 0, and a NaN ranks with
+ * -inf.  weight is batch x sets x w_cols fp32 (contiguous; columns past w_cols count as
+ * 0): sets = heads chooses for each head by itself, sets = 1 for all heads together.
+ * index (batch x sets x keep int32, contiguous) receives the kept row numbers
+ * in ascending order, then -1; new_len (int32 per sequence) min(n, keep); w_out (batch x sets x
+ * w_out_cols fp32, contiguous, or NULL) the kept weights, then zeros.  Rows of dst past
+ * new_len are left alone.  dst must not share rows with src, w_out none with weight.
+ * Errors as the joins'; SJ_E_INVAL also for sink + recent > keep, caches that do not match or
+ * sets other than 1 and heads; SJ_E_UNSUPPORTED for keep above dst's room or >= 2^31. */
+int sj_cache_evict(sj_ctx *ctx, const sj_cache *src, const int32_t *len, const float *weight,
+                   uint32_t sets, uint64_t w_cols, uint32_t keep, uint32_t sink, uint32_t recent,
+                   const sj_cache *dst, int32_t *index, int32_t *new_len, float *w_out,
+                   uint64_t w_out_cols);
+
 /* Free the context and its scratch; NULL is a no-op. */
 void sj_destroy(sj_ctx *ctx);
 

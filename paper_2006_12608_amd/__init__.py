@@ -6,7 +6,8 @@ sj_join_ip, sj_join_l2, sj_count, sj_join_noalloc, sj_normalize,
 sj_join_hamming, sj_join_lsh, sj_lsh_sort, sj_lsh_collision, sj_lsh_plan, sj_jl, sj_destroy,
 sj_get_stats, sj_last_error) with plain integer pointers; `join_ip`, `join_l2`, `count` and
 `join_lsh` (the LSH-bucketed join of Theorem 3) are conveniences over PyTorch
-device tensors.  This module only marshals
+device tensors, as are `rotary`, `cache_append`, `attend` and `cache_evict` around a
+cache of key and value rows (`kv_cache`).  This module only marshals
 arguments: every step of the join runs in the library's HIP kernels.  Import
 fails when libsj.so has not been built (python paper_2006_12608_amd/build.py).
 """
@@ -22,6 +23,8 @@ SJ_F16, SJ_BF16, SJ_I8 = 1, 2, 3
 SJ_IP, SJ_L2 = 0, 1
 SJ_OK, SJ_E_INVAL, SJ_E_OVERFLOW, SJ_E_NOMEM, SJ_E_HIP, SJ_E_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 SJ_FLAG_TWO_PASS, SJ_FLAG_TIMING, SJ_FLAG_RECOMPUTE, SJ_FLAG_COSINE = 1, 2, 4, 8
+SJ_FLAG_INVERSE = 16
+SJ_HALF, SJ_INTERLEAVED = 0, 1
 
 STATUS_NAMES = {0: "SJ_OK", -1: "SJ_E_INVAL", -2: "SJ_E_OVERFLOW", -3: "SJ_E_NOMEM",
                 -4: "SJ_E_HIP", -5: "SJ_E_UNSUPPORTED"}
@@ -40,6 +43,15 @@ class sj_stats(ctypes.Structure):
                 ("ms_scan", ctypes.c_double), ("ms_emit", ctypes.c_double),
                 ("kernel", ctypes.c_uint32), ("timed", ctypes.c_uint32),
                 ("emit_from_bits", ctypes.c_uint32), ("lsh_rows", ctypes.c_uint64)]
+
+
+class sj_cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("heads", ctypes.c_uint32), ("d", ctypes.c_uint32),
+                ("pages", ctypes.c_uint32), ("page", ctypes.c_uint32), ("batch", ctypes.c_uint32),
+                ("width", ctypes.c_uint32), ("table_row", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_page", ctypes.c_int64), ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64),
+                ("v_page", ctypes.c_int64), ("v_row", ctypes.c_int64), ("v_head", ctypes.c_int64)]
 
 
 # allocation of an output half-way through a call, once its size is known
@@ -91,6 +103,20 @@ def _load():
     lib.sj_lsh_plan.restype = i32
     lib.sj_jl.argtypes = [vp, i32, vp, u32, u32, u32, vp, vp, vp]
     lib.sj_jl.restype = i32
+    strides = ctypes.POINTER(ctypes.c_int64)
+    cache = ctypes.POINTER(sj_cache)
+    lib.sj_rotary.argtypes = [vp, i32, vp, strides, vp, strides, u32, u32, u32, vp, vp, u32, i32,
+                              dbl, ctypes.c_uint]
+    lib.sj_rotary.restype = i32
+    lib.sj_cache_append.argtypes = [vp, cache, vp, vp, u32, vp, strides, vp, strides, vp, vp, u32,
+                                    i32, dbl, vp, strides, u32, vp, strides]
+    lib.sj_cache_append.restype = i32
+    lib.sj_attend.argtypes = [vp, cache, vp, vp, u32, vp, strides, u32, vp, strides, dbl, vp, vp,
+                              vp, vp, u64]
+    lib.sj_attend.restype = i32
+    lib.sj_cache_evict.argtypes = [vp, cache, vp, vp, u32, u64, u32, u32, u32, cache, vp, vp, vp,
+                                   u64]
+    lib.sj_cache_evict.restype = i32
     lib.sj_destroy.argtypes = [vp]
     lib.sj_destroy.restype = None
     lib.sj_get_stats.argtypes = [vp, ctypes.POINTER(sj_stats)]
@@ -198,6 +224,46 @@ def sj_jl(ctx, dtype, X, n, d, levels, shape, A, Y):
     flat = [int(v) for s in shape for v in s]
     arr = (ctypes.c_uint32 * max(len(flat), 1))(*flat)
     return lib.sj_jl(ctx, dtype, X, n, d, levels, arr, A, Y)
+
+
+def _strides(*values):
+    """Element strides as the C array the calls on caches take."""
+    return (ctypes.c_int64 * len(values))(*values)
+
+
+def sj_rotary(ctx, dtype, x, x_stride, y, y_stride, n, heads, d, pos, turns, n_pairs, layout,
+              factor, flags=0):
+    """Returns the status; strides are sequences of element strides, the other
+    arrays device addresses."""
+    return lib.sj_rotary(ctx, dtype, x, _strides(*x_stride), y, _strides(*y_stride), n, heads, d,
+                         pos, turns, n_pairs, layout, factor, flags)
+
+
+def sj_cache_append(ctx, cache, length, count, t, key, key_stride, value, value_stride, pos, turns,
+                    n_pairs, layout, factor, q=None, q_stride=(0, 0, 0), q_heads=0, q_out=None,
+                    q_out_stride=(0, 0, 0)):
+    """Returns the status; cache is an sj_cache structure (or None)."""
+    return lib.sj_cache_append(ctx, None if cache is None else ctypes.byref(cache), length, count,
+                               t, key, _strides(*key_stride), value, _strides(*value_stride), pos,
+                               turns, n_pairs, layout, factor, q, _strides(*q_stride), q_heads,
+                               q_out, _strides(*q_out_stride))
+
+
+def sj_attend(ctx, cache, length, count, t, q, q_stride, q_heads, tree, tree_stride, scale, out,
+              lse, w_in=None, w_out=None, w_cols=0):
+    """Returns the status; cache is an sj_cache structure (or None)."""
+    return lib.sj_attend(ctx, None if cache is None else ctypes.byref(cache), length, count, t, q,
+                         _strides(*q_stride), q_heads, tree, _strides(*tree_stride), scale, out,
+                         lse, w_in, w_out, w_cols)
+
+
+def sj_cache_evict(ctx, src, length, weight, sets, w_cols, keep, sink, recent, dst, index, new_len,
+                   w_out=None, w_out_cols=0):
+    """Returns the status; src and dst are sj_cache structures (or None)."""
+    return lib.sj_cache_evict(ctx, None if src is None else ctypes.byref(src), length, weight,
+                              sets, w_cols, keep, sink, recent,
+                              None if dst is None else ctypes.byref(dst), index, new_len, w_out,
+                              w_out_cols)
 
 
 def sj_get_stats(ctx) -> sj_stats:
@@ -491,3 +557,236 @@ def jl_transform(X, shapes, As, ctx=None):
     if st != SJ_OK:
         raise SjError(st, sj_last_error())
     return Y
+
+
+# ------------------------------------------- a cache of key and value rows
+
+_LAYOUTS = {"half": SJ_HALF, "interleaved": SJ_INTERLEAVED}
+
+
+def _layout_code(layout: str) -> int:
+    if layout not in _LAYOUTS:
+        raise ValueError(f"layout must be 'half' or 'interleaved', not {layout!r}")
+    return _LAYOUTS[layout]
+
+
+def _check_rows(name, x, shape, dtype, device):
+    """x: a device tensor of `shape` (None: any size) and dtype whose last
+    dimension is adjacent."""
+    if x.dtype != dtype or x.device != device or x.dim() != len(shape) or \
+            any(s is not None and s != n for s, n in zip(shape, x.shape)):
+        raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}, expected "
+                         f"{tuple('any' if s is None else s for s in shape)} {dtype} on {device}")
+    if x.stride(-1) != 1 and x.shape[-1] > 1:
+        raise ValueError(f"{name}: the elements of its last dimension must be adjacent")
+
+
+def _check_whole(name, x, shape, dtype, device):
+    _check_rows(name, x, shape, dtype, device)
+    if not x.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _ptr(x):
+    return None if x is None or x.numel() == 0 else x.data_ptr()
+
+
+class kv_cache:
+    """A cache of key and value rows over tensors the caller owns: k and v are
+    (pages, page, heads, d) float16 or bfloat16 device tensors, views of any strides with
+    adjacent elements in a row; table is a (sequences, pages of a sequence)
+    int32 device tensor of page numbers (rows of a page number that does not
+    exist, as -1, do not exist), or None when sequence b is page b.  Row n of
+    sequence b is row n % page of page table[b, n // page]."""
+
+    def __init__(self, k, v, table=None):
+        import torch
+        if k.dtype not in (torch.float16, torch.bfloat16) or not k.is_cuda:
+            raise ValueError("k must be a float16 or bfloat16 device tensor")
+        _check_rows("k", k, (None,) * 4, k.dtype, k.device)
+        _check_rows("v", v, tuple(k.shape), k.dtype, k.device)
+        pages, page, heads, d = k.shape
+        if table is not None:
+            _check_rows("table", table, (None, None), torch.int32, k.device)
+        self.k, self.v, self.table = k, v, table
+        self.dtype, self.device = k.dtype, k.device
+        self.heads, self.d, self.page = heads, d, page
+        self.batch, self.width = (pages, 1) if table is None else table.shape
+        self.raw = sj_cache(dtype_code(k), heads, d, pages, page, self.batch, self.width,
+                            0 if table is None else table.stride(0),
+                            None if table is None else (table.data_ptr() or None),
+                            _ptr(k), _ptr(v), *k.stride()[:3], *v.stride()[:3])
+
+    @property
+    def room(self) -> int:
+        """Rows a sequence may hold."""
+        return self.width * self.page
+
+
+def rotary_turns(rot: int, base: float = 10000.0, *, linear: float = 1.0, ramp=None, device="cuda"):
+    """The frequencies of rotary positions over the first `rot` elements of a
+    head, as the calls below take them: an int64 tensor of rot / 2 fixed-point
+    fractions, turns a position in units of 2^-64.  Pair i has base^(-2 i / rot)
+    radians a position.  Long contexts: `linear` divides every frequency;
+    ramp = (s, length, low, high) divides by s the pairs that turn less than
+    `low` times within `length` positions, leaves those that turn more than `high`
+    times, and blends linearly between."""
+    import math
+    import torch
+    if rot < 0 or rot % 2 or not base > 0 or not linear > 0:
+        raise ValueError("rot must be even, base and linear positive")
+    out = []
+    for i in range(rot // 2):
+        f = base ** (-2.0 * i / rot) / linear
+        if ramp is not None:
+            s, length, low, high = ramp
+            g = min(max((length * f / (2 * math.pi) - low) / (high - low), 0.0), 1.0)
+            f = f / s * (1.0 - g) + f * g
+        out.append(round(f / (2 * math.pi) * 2.0 ** 64) % 2 ** 64)
+    return torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in out], dtype=torch.int64,
+                        device=device)
+
+
+def rotary(x, pos, turns, *, layout: str = "half", factor: float = 1.0, inverse: bool = False,
+           out=None, ctx=None):
+    """Rotary positions (sj_rotary): x (tokens, heads, d) with the first
+    2 len(turns) elements of every head turned by the token's position (pos: int32
+    per token) and scaled by `factor`; layout "half" pairs elements i and i +
+    len(turns), "interleaved" 2 i and 2 i + 1.  inverse=True turns back: the
+    gradient with respect to x of the call without it, given the gradient of its result.
+    out may be x."""
+    import torch
+    code = _layout_code(layout)
+    if x.dtype not in (torch.float16, torch.bfloat16) or not x.is_cuda:
+        raise ValueError("x must be a float16 or bfloat16 device tensor")
+    _check_rows("x", x, (None,) * 3, x.dtype, x.device)
+    n, heads, d = x.shape
+    _check_whole("pos", pos, (n,), torch.int32, x.device)
+    _check_whole("turns", turns, (None,), torch.int64, x.device)
+    if out is None:
+        out = torch.empty((n, heads, d), dtype=x.dtype, device=x.device)
+    _check_rows("out", out, tuple(x.shape), x.dtype, x.device)
+    st = sj_rotary(ctx or context(x.device.index), dtype_code(x), _ptr(x), x.stride()[:2], _ptr(out),
+                   out.stride()[:2], n, heads, d, _ptr(pos), _ptr(turns), turns.shape[0], code,
+                   factor, SJ_FLAG_INVERSE if inverse else 0)
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+    return out
+
+
+def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, layout: str = "half",
+                 factor: float = 1.0, counts=None, q_out=None, ctx=None):
+    """Appends rows to a cache (sj_cache_append): row lengths[b] + u of sequence
+    b receives key[b, u], turned by position pos[b, u] where turns are given (see
+    rotary), and value[b, u]; with counts only u < counts[b].  key and value
+    are (sequences, tokens, heads, d); lengths and counts int32 per sequence, pos
+    int32 (sequences, tokens).  q (sequences, tokens, query heads, d), when
+    given, is turned by the same positions and returned (in q_out, which may be
+    q)."""
+    import torch
+    code = _layout_code(layout)
+    B, dev = cache.batch, cache.device
+    _check_rows("key", key, (B, None, cache.heads, cache.d), cache.dtype, dev)
+    _check_rows("value", value, tuple(key.shape), cache.dtype, dev)
+    _check_whole("lengths", lengths, (B,), torch.int32, dev)
+    if counts is not None:
+        _check_whole("counts", counts, (B,), torch.int32, dev)
+    t = key.shape[1]
+    if (pos is None) != (turns is None):
+        raise ValueError("pos and turns go together")
+    if turns is not None:
+        _check_whole("pos", pos, (B, t), torch.int32, dev)
+        _check_whole("turns", turns, (None,), torch.int64, dev)
+    args = ()
+    if q is not None:
+        _check_rows("q", q, (B, t, None, cache.d), cache.dtype, dev)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        _check_rows("q_out", q_out, tuple(q.shape), q.dtype, dev)
+        if q.numel():
+            args = (q.data_ptr(), q.stride()[:3], q.shape[2], q_out.data_ptr(), q_out.stride()[:3])
+    st = sj_cache_append(ctx or context(dev.index), cache.raw, _ptr(lengths), _ptr(counts), t,
+                         _ptr(key), key.stride()[:3], _ptr(value), value.stride()[:3], _ptr(pos),
+                         _ptr(turns), 0 if turns is None else turns.shape[0], code, factor, *args)
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+    return q_out
+
+
+def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=None, weight=None,
+           weight_out=None, out=None, ctx=None):
+    """Attention of a few tokens of every sequence over its rows in the cache
+    (sj_attend).  q is (sequences, tokens, query heads, d); query head i reads cache head
+    i // (query heads / cache heads).  Token u of sequence b sees the
+    lengths[b] rows before the call's tokens and, of the tokens' own rows (which
+    follow them, appended beforehand), those that its mask names: bit w % 64 of
+    tree[b, u, w // 64] for token w (tree: int64 (sequences or 1, tokens,
+    ceil(tokens / 64))), or tokens up to itself without a tree.  counts (int32
+    per sequence): tokens that exist.  scale defaults to 1 / sqrt(d).
+    Returns (out, lse): out as q, lse (sequences, tokens, query heads) float32; a
+    token that sees nothing has out 0 and lse -inf.  With weight (float32
+    (sequences, cache heads, columns)) the softmax weight that every row drew from all
+    tokens and query heads is added to it in place; weight_out receives the sum instead
+    where given (with weight None, of this call alone)."""
+    import torch
+    B, dev = cache.batch, cache.device
+    _check_rows("q", q, (B, None, None, cache.d), cache.dtype, dev)
+    _check_whole("lengths", lengths, (B,), torch.int32, dev)
+    if counts is not None:
+        _check_whole("counts", counts, (B,), torch.int32, dev)
+    t, q_heads = q.shape[1], q.shape[2]
+    tree_stride = (0, 0)
+    if tree is not None:
+        words = (t + 63) // 64
+        _check_rows("tree", tree, (1 if tree.shape[0] == 1 else B, t, words), torch.int64, dev)
+        tree_stride = (0 if tree.shape[0] == 1 else tree.stride(0), tree.stride(1))
+    if weight is not None:
+        _check_whole("weight", weight, (B, cache.heads, None), torch.float32, dev)
+        if weight_out is None:
+            weight_out = weight
+    cols = 0
+    if weight_out is not None:
+        cols = weight_out.shape[-1]
+        _check_whole("weight_out", weight_out, (B, cache.heads, cols if weight is None else
+                                                weight.shape[2]), torch.float32, dev)
+    if out is None:
+        out = torch.empty((B, t, q_heads, cache.d), dtype=cache.dtype, device=dev)
+    _check_whole("out", out, (B, t, q_heads, cache.d), cache.dtype, dev)
+    lse = torch.empty((B, t, q_heads), dtype=torch.float32, device=dev)
+    st = sj_attend(ctx or context(dev.index), cache.raw, _ptr(lengths), _ptr(counts), t, _ptr(q),
+                   q.stride()[:3], q_heads, _ptr(tree), tree_stride,
+                   cache.d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse),
+                   _ptr(weight), _ptr(weight_out), cols)
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+    return out, lse
+
+
+def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recent: int = 0,
+                weight_out=None, ctx=None):
+    """Eviction by accumulated weight (sj_cache_evict): of every sequence's rows
+    the first `sink`, the last `recent` and the heaviest of the others stay, `keep`
+    in all; they are copied, closed up and in order, into the cache `into` (other
+    pages).  weight is (sequences, 1 or heads, columns) float32: one choice for
+    all heads, or one for each.  Returns (index, lengths, weight): index
+    (sequences, 1 or heads, keep) int32, the kept rows in ascending order, then
+    -1; the new lengths (int32); and the kept weights, then zeros (weight_out where
+    given, else as wide as index)."""
+    import torch
+    B, dev = cache.batch, cache.device
+    _check_whole("lengths", lengths, (B,), torch.int32, dev)
+    _check_whole("weight", weight, (B, None, None), torch.float32, dev)
+    sets = weight.shape[1]
+    if keep < 0 or sink < 0 or recent < 0:
+        raise ValueError("keep, sink and recent must not be negative")
+    index = torch.empty((B, sets, keep), dtype=torch.int32, device=dev)
+    new = torch.empty((B,), dtype=torch.int32, device=dev)
+    if weight_out is None:
+        weight_out = torch.empty((B, sets, keep), dtype=torch.float32, device=dev)
+    _check_whole("weight_out", weight_out, (B, sets, None), torch.float32, dev)
+    st = sj_cache_evict(ctx or context(dev.index), cache.raw, _ptr(lengths), _ptr(weight), sets,
+                        weight.shape[2], keep, sink, recent, into.raw, _ptr(index), _ptr(new),
+                        _ptr(weight_out), weight_out.shape[2])
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+    return index, new, weight_out

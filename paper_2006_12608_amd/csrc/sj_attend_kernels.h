@@ -1,0 +1,624 @@
+// sj_attend_kernels.h -- attention of a few tokens of every sequence over its rows in
+// the cache (sj_attend), for one element type per translation unit.
+//
+// For a query row q and the rows n it sees, with s_n = scale <q, k_n>:
+//   m = max s_n, l = sum exp(s_n - m), out = sum exp(s_n - m) v_n / l, lse = m + log l.
+// One pass over the rows keeps (m, l, sum) and rescales them when m grows;
+// results over disjoint sets of rows join by the same rule.
+#pragma once
+
+#include "sj_cache.h"
+
+namespace sjc {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<sjk::DT_F16> {
+    typedef _Float16 one;
+    typedef f16x8 eight;
+    static constexpr uint32_t EXP = 0x7c00u;   // exponent bits: all set = not finite
+    static __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                      __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Elem<sjk::DT_BF16> {
+    typedef __bf16 one;
+    typedef bf16x8 eight;
+    static constexpr uint32_t EXP = 0x7f80u;
+    static __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+
+__device__ __forceinline__ float bits_to_float(uint16_t x, int dt)
+{
+    return dt == sjk::DT_F16 ? (float)__builtin_bit_cast(_Float16, x)
+                             : __uint_as_float((uint32_t)x << 16);
+}
+
+// 2^x, 2^-inf = 0.
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ __forceinline__ int64_t shfl64(int64_t v, int lane)
+{
+    const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane);
+    const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), lane);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// Rows of sequence b: those before the call's tokens, the tokens there are, and the
+// end of the tokens' rows.
+struct Rows {
+    uint32_t len, count, end;
+};
+
+__device__ __forceinline__ Rows rows_of(const Attend &a, uint32_t b)
+{
+    Rows r;
+    r.len = clamp_rows(a.len[b], a.c.room);
+    r.count = a.count ? clamp_rows(a.count[b], a.t) : a.t;
+    r.end = r.len + r.count < a.c.room ? r.len + r.count : a.c.room;
+    return r;
+}
+
+// Whether token u sees row n of its sequence (n < r.end).
+__device__ __forceinline__ bool sees(const Attend &a, uint32_t b, const Rows &r, uint32_t u,
+                                     uint32_t n)
+{
+    if (n < r.len)
+        return true;
+    const uint32_t w = n - r.len;
+    if (!a.tree)
+        return w <= u;
+    return (a.tree[(int64_t)b * a.tree_seq + (int64_t)u * a.tree_tok + (w >> 6)] >> (w & 63)) & 1;
+}
+
+// The share of the work that a workgroup takes: blocks [first, last) of
+// AT_ROWS rows of sequence b, number `share` of its `shares`.
+struct Share {
+    uint32_t b, share, shares, first, last;
+    Rows rows;
+};
+
+// Finds share number `slot` of the batch.  All sequences' blocks together are cut
+// into about target / (heads * tiles) shares of equal size, each sequence into
+// whole shares of its own and at least one; every workgroup computes the cut
+// from the lengths on the device, so the grid does not depend on them.  Returns
+// false when there are fewer shares.  Called by whole waves.
+__device__ __forceinline__ bool find_share(const Attend &a, uint32_t slot, Share *out)
+{
+    const uint32_t lane = threadIdx.x & 63, B = a.c.batch;
+    unsigned long long total = 0;
+    for (uint32_t b0 = 0; b0 < B; b0 += 64)
+        if (b0 + lane < B)
+            total += (rows_of(a, b0 + lane).end + AT_ROWS - 1) / AT_ROWS;
+    for (int o = 1; o < 64; o <<= 1)
+        total += __shfl_xor(total, o);
+    const uint32_t want = a.target / (a.c.heads * a.tiles) > 0 ? a.target / (a.c.heads * a.tiles) : 1;
+    unsigned long long size = (total + want - 1) / want;
+    size = size < AT_WAVES ? AT_WAVES : size;   // (a block per wave at least)
+    uint32_t base = 0;
+    for (uint32_t b0 = 0; b0 < B; b0 += 64) {
+        uint32_t blocks = 0, shares = 0;
+        if (b0 + lane < B) {
+            blocks = (rows_of(a, b0 + lane).end + AT_ROWS - 1) / AT_ROWS;
+            shares = (uint32_t)((blocks + size - 1) / size);
+            shares = shares ? shares : 1;
+        }
+        uint32_t incl = shares;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t y = __shfl_up(incl, o);
+            incl += (int)lane >= o ? y : 0;
+        }
+        const uint32_t sum = __shfl(incl, 63);
+        if (slot < base + sum) {
+            const int who = __ffsll((unsigned long long)__ballot(slot < base + incl)) - 1;
+            const uint32_t mine = __shfl(shares, who), nb = __shfl(blocks, who);
+            out->b = b0 + who;
+            out->shares = mine;
+            out->share = slot - (base + __shfl(incl, who) - mine);
+            out->first = (uint32_t)((unsigned long long)nb * out->share / mine);
+            out->last = (uint32_t)((unsigned long long)nb * (out->share + 1) / mine);
+            out->rows = rows_of(a, out->b);
+            return true;
+        }
+        base += sum;
+    }
+    return false;
+}
+
+// ------------------------------------------------------------- the split kernel
+//
+// A workgroup takes one share of a sequence's rows for one cache head and one
+// tile of QT = 16 NQ query rows (row r = token r / group, query head r % group: all
+// that read this cache head, so that a cache row is loaded once for all of them).
+// Its four waves take blocks of 32 rows in turn, each with running statistics
+// of its own; they join at the end through LDS.
+//
+// A block on a wave: S^T = K Q^T as 16 x 16 x 32 tiles with K's rows from global
+// memory straight in operand layout (lane l: row l % 16, elements 8 (l / 16) ..
+// + 7 of each 32), so that lane l holds the scores of query l % 16 with rows
+// 4 (l / 16) .. + 3 of both 16-row halves: the statistics of a query need two
+// exchanges, and the exponentials are, without moving, the operand of
+// O^T = V^T P^T in the order of rows {4g .. 4g + 3, 16 + 4g .. 16 + 4g + 3} of lane group g.
+// V goes through the wave's own LDS and comes back transposed (ds_read_b64_tr_b16:
+// each 16-lane group reads 4 rows x 16 columns, lane l receives column l) in
+// the same order of rows.  LDS rows are padded by 32 bytes: the 4 rows x 32 bytes that a
+// lane group reads then lie in different banks.
+// The next block's K and V are loaded while this one is worked on.
+template <int DT, int DC, int NQ, bool EXACT>
+__global__ void __launch_bounds__(256) attend_split(const Attend a)
+{
+    typedef Elem<DT> E;
+    constexpr int QT = AT_Q * NQ, D = 32 * DC;
+    constexpr int RS = 2 * D + 32;              // bytes of a V row in LDS
+    constexpr int OS = D + 4;                   // floats of a query's sums in LDS
+    constexpr int NV = 2 * DC;                  // 16-byte loads of V per lane and block
+    constexpr int VR = 16 / DC;                 // rows of V per load
+    constexpr int WAVE_LDS = AT_ROWS * RS;
+    static_assert(AT_Q * OS * 4 <= WAVE_LDS, "the sums of a query tile fit in the wave's V");
+    __shared__ __align__(16) uint8_t lds[AT_WAVES * WAVE_LDS];
+    __shared__ float stat[AT_WAVES][QT][2];
+
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t units = a.c.heads * a.tiles;
+    const uint32_t unit = blockIdx.x % units, slot = blockIdx.x / units;
+    const uint32_t h = unit / a.tiles, tile = unit % a.tiles;
+    Share sh;
+    if (!find_share(a, slot, &sh))
+        return;
+    const uint32_t b = __builtin_amdgcn_readfirstlane(sh.b);
+    const uint32_t first = __builtin_amdgcn_readfirstlane(sh.first);
+    const uint32_t last = __builtin_amdgcn_readfirstlane(sh.last);
+    const uint32_t shares = __builtin_amdgcn_readfirstlane(sh.shares);
+    const Rows rows = {(uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.len),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.count),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.end)};
+    if (unit == 0 && sh.share == 0 && threadIdx.x == 0) {
+        a.plan[2 * b] = slot;
+        a.plan[2 * b + 1] = shares;
+    }
+
+    const uint32_t q16 = lane & 15, g4 = lane >> 4;
+    const uint32_t d = a.c.d;
+    const uint32_t q_rows = a.t * a.group;
+
+    // queries: lane l holds query l % 16 of each tile in operand layout
+    i32x4 Q[NQ][DC];
+    uint32_t tok[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        const uint32_t r = tile * QT + AT_Q * j + q16;
+        const bool there = r < q_rows && r / a.group < rows.count;
+        tok[j] = there ? r / a.group : 0;
+        const uint16_t *p = a.q + (int64_t)b * a.q_seq + (int64_t)tok[j] * a.q_tok +
+                            (int64_t)(h * a.group + (there ? r % a.group : 0)) * a.q_head + 8 * g4;
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+            Q[j][c] = there ? load8(p + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4))
+                            : i32x4{0, 0, 0, 0};
+    }
+
+    f32x4 O[NQ][NV];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        m[j] = -INFINITY;
+        l[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            O[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const uint16_t *kb = a.c.k + (int64_t)h * a.c.k_head, *vb = a.c.v + (int64_t)h * a.c.v_head;
+    uint8_t *const my = lds + wave * WAVE_LDS;
+
+    // place of row lane % 32 of a block: absent rows read page 0, row 0 (their
+    // scores and values are replaced below)
+    auto place = [&](uint32_t blk) -> Place {
+        const uint32_t n = blk * AT_ROWS + (lane & 31);
+        return blk < last && n < rows.end ? place_of(a.c, b, n) : Place{-1, 0u};
+    };
+    i32x4 K[2][DC], V[NV];
+    auto load_k = [&](const Place &p) {
+        const int64_t off = p.page < 0 ? 0
+                                       : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint16_t *r = kb + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
+#pragma unroll
+            for (int c = 0; c < DC; ++c)
+                K[t][c] = load8(r + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4));
+        }
+    };
+    const uint32_t v_row = lane / (4 * DC), v_col = 8 * (lane % (4 * DC));
+    auto load_v = [&](const Place &p) {
+        const int64_t off = p.page < 0 ? 0
+                                       : (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint16_t *r = vb + shfl64(off, VR * i + (int)v_row) + v_col;
+            V[i] = load8(r, EXACT ? 8 : (int)d - (int)v_col);
+        }
+    };
+
+    uint32_t blk = first + wave;
+    Place cur = place(blk);
+    if (blk < last) {
+        load_k(cur);
+        load_v(cur);
+    }
+    Place nxt = place(blk + AT_WAVES);
+    for (; blk < last; blk += AT_WAVES) {
+        const Place aft = place(blk + 2 * AT_WAVES);
+        // bit r: row r of the block exists
+        const uint32_t there = (uint32_t)__ballot(cur.page >= 0);
+        const bool tail = blk * AT_ROWS + AT_ROWS > rows.len;
+
+        f32x4 s[NQ][2];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    s[j][t] = E::mma(K[t][c], Q[j][c], s[j][t]);
+            }
+        if (blk + AT_WAVES < last)
+            load_k(nxt);
+
+        // V to LDS; rows that do not exist as zeros (0 x NaN would reach every query)
+        uint32_t odd = 0;       // not finite in a row that a mask may hide
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (there != 0xffffffffu && !((there >> (VR * i + v_row)) & 1))
+                V[i] = i32x4{0, 0, 0, 0};
+            if (tail)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t x = (uint32_t)V[i][e];
+                    odd |= (uint32_t)((x & E::EXP) == E::EXP) |
+                           (uint32_t)(((x >> 16) & E::EXP) == E::EXP);
+                }
+            *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = V[i];
+        }
+        if (blk + AT_WAVES < last)
+            load_v(nxt);
+
+        // scores to exponentials
+        i32x4 P[NQ];
+        float pf[NQ][8];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    float x = s[j][t][r] * a.scale2;
+                    if (tail || there != 0xffffffffu) {
+                        const uint32_t i = 16 * t + 4 * g4 + r, n = blk * AT_ROWS + i;
+                        if (!((there >> i) & 1) || !sees(a, b, rows, tok[j], n))
+                            x = -INFINITY;
+                    }
+                    pf[j][4 * t + r] = x;
+                    top = fmaxf(top, x);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m_new = fmaxf(m[j], top);
+            // nothing seen yet: any finite maximum will do
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float shrink = exp2_(m[j] - m_use);
+            m[j] = m_new;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                pf[j][e] = exp2_(pf[j][e] - m_use);
+                sum += pf[j][e];
+            }
+            l[j] = l[j] * shrink + sum;     // this lane's rows only; joined at the end
+            typename E::eight p8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                p8[e] = (typename E::one)pf[j][e];
+            P[j] = __builtin_bit_cast(i32x4, p8);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                O[j][i] *= shrink;
+        }
+
+        if (__builtin_expect(!__any((int)odd), 1)) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint8_t *at = my + (4 * g4 + (q16 >> 2)) * RS + 32 * i + 8 * (q16 & 3);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4 *)at);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4 *)(at + 16 * RS));
+                const i32x4 vt = {__builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7))};
+#pragma unroll
+                for (int j = 0; j < NQ; ++j)
+                    O[j][i] = E::mma(vt, P[j], O[j][i]);
+            }
+        } else {
+            // infinities or NaN among the tokens' own values: only rows that a query
+            // sees may reach it, one product at a time
+#pragma unroll
+            for (int j = 0; j < NQ; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+                    for (uint32_t g = 0; g < 4; ++g) {
+                        const uint32_t i = 16 * (e >> 2) + 4 * g + (e & 3);
+                        const float p = __shfl(pf[j][e], (int)(16 * g + q16));
+                        const uint32_t n = blk * AT_ROWS + i;
+                        if (!((there >> i) & 1) || !sees(a, b, rows, tok[j], n))
+                            continue;
+#pragma unroll
+                        for (int x = 0; x < NV; ++x)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                O[j][x][r] += p * bits_to_float(
+                                    *(const uint16_t *)(my + i * RS + 2 * (16 * x + 4 * g4 + r)), DT);
+                    }
+        }
+        cur = nxt;
+        nxt = aft;
+    }
+
+    // join the lanes of a query, then the waves
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        l[j] += __shfl_xor(l[j], 16);
+        l[j] += __shfl_xor(l[j], 32);
+        if (g4 == 0) {
+            stat[wave][AT_Q * j + q16][0] = m[j];
+            stat[wave][AT_Q * j + q16][1] = l[j];
+        }
+    }
+    __syncthreads();
+    const uint64_t part = (uint64_t)slot * units + unit;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+        float top = -INFINITY;
+#pragma unroll
+        for (uint32_t w = 0; w < AT_WAVES; ++w)
+            top = fmaxf(top, stat[w][AT_Q * j + q16][0]);
+        const float f = exp2_(m[j] - (top == -INFINITY ? 0.f : top));
+        if (j)
+            __syncthreads();
+        float *mine = (float *)my + q16 * OS;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            *(f32x4 *)(mine + 16 * i + 4 * g4) = O[j][i] * f;
+        __syncthreads();
+        // 256 threads: query threadIdx.x / 16, columns 4 (threadIdx.x % 16) + 64 k
+        const uint32_t qi = threadIdx.x >> 4, c0 = 4 * (threadIdx.x & 15);
+        float tot = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (uint32_t w = 0; w < AT_WAVES; ++w)
+            tot = fmaxf(tot, stat[w][AT_Q * j + qi][0]);
+        const float base = tot == -INFINITY ? 0.f : tot;
+#pragma unroll
+        for (uint32_t w = 0; w < AT_WAVES; ++w)
+            sum += stat[w][AT_Q * j + qi][1] * exp2_(stat[w][AT_Q * j + qi][0] - base);
+        const uint32_t r = tile * QT + AT_Q * j + qi;
+        const uint32_t u = r / a.group;
+        if (r < q_rows) {
+            const bool live = u < rows.count;
+            const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r % a.group;
+#pragma unroll
+            for (uint32_t c = c0; c < (uint32_t)D; c += 64) {
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (uint32_t w = 0; w < AT_WAVES; ++w)
+                    o += *(const f32x4 *)((const float *)(lds + w * WAVE_LDS) + qi * OS + c);
+                if (shares > 1) {
+                    *(f32x4 *)(a.part_o + (part * QT + AT_Q * j + qi) * D + c) = o;
+                } else {
+                    const float inv = live && tot != -INFINITY ? 1.f / sum : 0.f;
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e)
+                        if (EXACT || c + e < d)
+                            a.out[row * d + c + e] = __builtin_bit_cast(
+                                uint16_t, (typename E::one)(live && tot != -INFINITY ? o[e] * inv : 0.f));
+                }
+            }
+            if (c0 == 0) {
+                if (shares > 1) {
+                    a.part_ml[(part * QT + AT_Q * j + qi) * 2] = tot;
+                    a.part_ml[(part * QT + AT_Q * j + qi) * 2 + 1] = sum;
+                } else {
+                    a.lse[row] = live && tot != -INFINITY
+                                     ? (tot + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f
+                                     : -INFINITY;
+                }
+            }
+        }
+    }
+}
+
+// Joins the shares of every query row that has more than one: a wave a row,
+// lanes over the row's elements.
+template <int DT>
+__global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, uint32_t D)
+{
+    typedef Elem<DT> E;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t row = (uint64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t n_rows = (uint64_t)a.c.batch * a.t * a.q_heads;
+    if (row >= n_rows)
+        return;
+    const uint32_t head = (uint32_t)(row % a.q_heads);
+    const uint32_t u = (uint32_t)(row / a.q_heads % a.t), b = (uint32_t)(row / a.q_heads / a.t);
+    const uint32_t slot = a.plan[2 * b], shares = a.plan[2 * b + 1];
+    if (shares <= 1)
+        return;
+    const uint32_t h = head / a.group, r = u * a.group + head % a.group;
+    const uint32_t units = a.c.heads * a.tiles, unit = h * a.tiles + r / QT;
+    auto at = [&](uint32_t s) { return ((uint64_t)(slot + s) * units + unit) * QT + r % QT; };
+    float top = -INFINITY;
+    for (uint32_t s = lane; s < shares; s += 64)
+        top = fmaxf(top, a.part_ml[2 * at(s)]);
+    for (int o = 1; o < 64; o <<= 1)
+        top = fmaxf(top, __shfl_xor(top, o));
+    const bool live = u < rows_of(a, b).count && top != -INFINITY;
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+    for (uint32_t s = lane; s < shares; s += 64)
+        sum += a.part_ml[2 * at(s) + 1] * exp2_(a.part_ml[2 * at(s)] - base);
+    for (int o = 1; o < 64; o <<= 1)
+        sum += __shfl_xor(sum, o);
+    const float inv = live ? 1.f / sum : 0.f;
+    for (uint32_t c = 2 * lane; c < D; c += 128) {
+        f32x2 o = {0.f, 0.f};
+        for (uint32_t s = 0; s < shares; ++s) {
+            const float f = exp2_(a.part_ml[2 * at(s)] - base);
+            const f32x2 x = *(const f32x2 *)(a.part_o + at(s) * D + c);
+            o += x * f;
+        }
+        for (uint32_t e = 0; e < 2; ++e)
+            if (c + e < a.c.d)
+                a.out[row * a.c.d + c + e] =
+                    __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[e] * inv : 0.f));
+    }
+    if (lane == 0)
+        a.lse[row] = live ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
+}
+
+// Weights: w_out[b, h, n] = w_in[b, h, n] + sum over the query rows r that read head h of
+// exp(s_rn - lse_r).  A wave holds 16 x 2 key rows in operand layout and runs
+// through the query rows, S = Q K^T: lane l holds key row l % 16 with query rows
+// 4 (l / 16) .. + 3, so the sum stays in the lane until the end.
+template <int DT, int DC, bool EXACT>
+__global__ void __launch_bounds__(256) attend_weights(const Attend a)
+{
+    typedef Elem<DT> E;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t q16 = lane & 15, g4 = lane >> 4, d = a.c.d;
+    const uint32_t h = blockIdx.y % a.c.heads, b = blockIdx.y / a.c.heads;
+    const uint32_t row0 = (blockIdx.x * AT_WAVES + wave) * AT_ROWS;
+    if (row0 >= a.w_cols)
+        return;
+    const Rows rows = rows_of(a, b);
+    float w[2] = {0.f, 0.f};
+    if (row0 < rows.end) {
+        const uint32_t n = row0 + (lane & 31);
+        const Place p = n < rows.end ? place_of(a.c, b, n) : Place{-1, 0u};
+        const uint32_t there = (uint32_t)__ballot(p.page >= 0);
+        const bool tail = row0 + AT_ROWS > rows.len;
+        const int64_t off =
+            p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
+        i32x4 K[2][DC];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint16_t *r = a.c.k + (int64_t)h * a.c.k_head + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
+#pragma unroll
+            for (int c = 0; c < DC; ++c)
+                K[t][c] = load8(r + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4));
+        }
+        const uint32_t q_rows = rows.count * a.group;
+        for (uint32_t r0 = 0; r0 < q_rows; r0 += AT_Q) {
+            const uint32_t r = r0 + q16 < q_rows ? r0 + q16 : q_rows - 1;
+            const uint16_t *p16 = a.q + (int64_t)b * a.q_seq + (int64_t)(r / a.group) * a.q_tok +
+                                  (int64_t)(h * a.group + r % a.group) * a.q_head + 8 * g4;
+            i32x4 Q[DC];
+#pragma unroll
+            for (int c = 0; c < DC; ++c)
+                Q[c] = load8(p16 + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4));
+            f32x4 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    s[t] = E::mma(Q[c], K[t][c], s[t]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t x = r0 + 4 * g4 + e;
+                if (x >= q_rows)
+                    continue;
+                const uint32_t u = x / a.group;
+                const float lse2 = a.lse[((uint64_t)b * a.t + u) * a.q_heads + h * a.group +
+                                         x % a.group] * 1.4426950408889634f;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bool ok = true;
+                    if (tail || there != 0xffffffffu) {
+                        const uint32_t i = 16 * t + q16;
+                        ok = ((there >> i) & 1) && sees(a, b, rows, u, row0 + i);
+                    }
+                    if (ok)
+                        w[t] += exp2_(s[t][e] * a.scale2 - lse2);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        w[t] += __shfl_xor(w[t], 16);
+        w[t] += __shfl_xor(w[t], 32);
+        const uint64_t n = (uint64_t)row0 + 16 * t + q16;
+        if (g4 == 0 && n < a.w_cols) {
+            const uint64_t at = ((uint64_t)b * a.c.heads + h) * a.w_cols + n;
+            a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + w[t];
+        }
+    }
+}
+
+template <int DT, int DC, bool EXACT>
+hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
+{
+    const uint32_t qt = attend_tile_rows(a.t * a.group, a.c.d);
+    const uint64_t rows = (uint64_t)a.c.batch * a.t * a.q_heads;
+    hipError_t e;
+    if (rows) {
+        const dim3 grid(a.slots * a.c.heads * a.tiles);
+        if (qt == 16)
+            attend_split<DT, DC, 1, EXACT><<<grid, 256, 0, s>>>(a);
+        else
+            attend_split<DT, DC, 2, EXACT><<<grid, 256, 0, s>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        attend_join<DT><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, s>>>(a, qt, 32 * DC);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+    }
+    if (!a.w_out || !a.w_cols)
+        return hipSuccess;
+    const dim3 wg((uint32_t)((a.w_cols + AT_WAVES * AT_ROWS - 1) / (AT_WAVES * AT_ROWS)),
+                  a.c.batch * a.c.heads);
+    attend_weights<DT, DC, EXACT><<<wg, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_attend(const Attend &a, hipStream_t s)
+{
+    const uint32_t d = a.c.d;
+    if (d <= 64)
+        return d == 64 ? launch_attend_dc<DT, 2, true>(a, s) : launch_attend_dc<DT, 2, false>(a, s);
+    if (d <= 128)
+        return d == 128 ? launch_attend_dc<DT, 4, true>(a, s) : launch_attend_dc<DT, 4, false>(a, s);
+    return d == 256 ? launch_attend_dc<DT, 8, true>(a, s) : launch_attend_dc<DT, 8, false>(a, s);
+}
+
+}  // namespace sjc

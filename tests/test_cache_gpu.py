@@ -1,0 +1,724 @@
+"""The calls on a cache of key and value rows on the GPU against their
+definitions in 64 bits (oracle.cache).
+
+Tolerances.  With u the unit roundoff of the 16-bit type (2^-8 bf16, 2^-11 fp16), one
+rounding of a value y costs u |y| (and 2^-25 where fp16 is subnormal).
+  rotary: one rounding, plus sines and two products in fp32: 2^-20 (|a| + |b|).
+  scores: an fp32 sum of d products, |error| <= (d + 4) 2^-24 scale sum |q k| =: e.
+  lse: 2 e + n 2^-24 + 2^-20 (1 + |lse|).
+  a normalised weight: relative rho = 4 e + n 2^-23 + 2^-19 (score, maximum, sum and
+  exponentials in fp32); their sum over R query rows: (rho + (R + 2) 2^-24) times itself,
+  and 2^-23 of the value it is added to.
+  out: one rounding of each exponential (u sum p |v|; fp16: 2^-25 max |v| a row on top),
+  rho sum p |v|, and the final rounding u |out|.
+"""
+import numpy as np
+import pytest
+
+from oracle import cache as ref
+
+pytestmark = pytest.mark.gpu
+
+U = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def say(*a):
+    print("[case]", *a, flush=True)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2006_12608_amd  # noqa: F401  (fails loudly when libsj.so is missing)
+    yield
+    torch.cuda.synchronize()
+
+
+def tdtype(dtype):
+    import torch
+    return {"f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+
+
+def dev(x, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(x)).to("cuda")
+    return t if dtype is None else t.to(tdtype(dtype))
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def chain_tree(rng, B, T):
+    """Random ancestor masks, every token with itself."""
+    words = np.zeros((B, T, (T + 63) // 64), np.uint64)
+    for b in range(B):
+        masks = []
+        for t in range(T):
+            parent = int(rng.integers(-1, t)) if t else -1
+            masks.append((masks[parent] if parent >= 0 else 0) | 1 << t)
+            for w in range(words.shape[2]):
+                words[b, t, w] = (masks[t] >> (64 * w)) & (2 ** 64 - 1)
+    return words
+
+
+class Case:
+    """A cache with random rows, more of them than any sequence uses, and queries.
+    Rows that no sequence holds are NaN."""
+
+    def __init__(self, seed, dtype, B, T, heads, group, d, page, lens, order="rows", table="mixed",
+                 counts=None, hole=None):
+        import torch
+        import paper_2006_12608_amd as sj
+        rng = self.rng = np.random.default_rng(seed)
+        self.dtype, self.T, self.B, self.page = dtype, T, B, page
+        self.lens = np.array(lens, np.int32)
+        self.counts = None if counts is None else np.array(counts, np.int32)
+        width = max(1, -(-(max(max(lens), 0) + T) // page)) if table else 1
+        if not table:
+            page = self.page = max(max(lens), 0) + T
+        pages = B * width + 3
+        if table:
+            self.table = rng.permutation(pages)[:B * width].reshape(B, width).astype(np.int32)
+        else:
+            pages, self.table = B, None
+        if hole is not None:
+            self.table[hole] = [-1, pages, -2 ** 31, 2 ** 31 - 1][seed % 4]
+        shape = (pages, page, heads, d)
+        full = np.full(shape, np.nan)
+        self.k, self.v = full.copy(), full.copy()
+        for b in range(B):
+            t = T if counts is None else min(max(counts[b], 0), T)
+            for n in range(min(max(lens[b], 0) + t, width * page)):
+                r = ref.row_of(self.table, page, pages, b, n)
+                if r is not None:
+                    self.k[r] = rng.standard_normal((heads, d))
+                    self.v[r] = rng.standard_normal((heads, d))
+        self.q = rng.standard_normal((B, T, heads * group, d)) * 1.5
+
+        def put(x):
+            t = dev(x, dtype)
+            if order == "heads":        # (pages, heads, page, d) in memory
+                t = t.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+            elif order == "wide":       # rows in a wider tensor, at an odd place
+                big = torch.full((pages, page, heads, 2 * d + 3), float("nan"), dtype=t.dtype,
+                                 device="cuda")
+                big[..., 1:d + 1] = t
+                t = big[..., 1:d + 1]
+            return t
+        self.dk, self.dv = put(self.k), put(self.v)
+        self.dq = dev(self.q, dtype)
+        self.k, self.v, self.q = host(self.dk), host(self.dv), host(self.dq)
+        self.cache = sj.kv_cache(self.dk, self.dv, None if self.table is None else dev(self.table))
+
+
+def check_attend(c, tree=None, weight=None, scale=None, dq=None):
+    import torch
+    import paper_2006_12608_amd as sj
+    B, T, q_heads, d = c.q.shape
+    scale = d ** -0.5 if scale is None else scale
+    out, lse, w, mag, dots = ref.attend(c.k, c.v, c.table, c.lens, c.q, tree, scale, c.counts)
+    w_out = None
+    kw = {}
+    if weight is not None:
+        w_out = torch.full(weight.shape, float("nan"), device="cuda")
+        kw = dict(weight=dev(weight), weight_out=w_out)
+    got, got_lse = sj.attend(c.cache, dev(c.lens), c.dq if dq is None else dq,
+                             None if tree is None else dev(tree.view(np.int64)), scale=scale,
+                             counts=None if c.counts is None else dev(c.counts), **kw)
+    got, got_lse = host(got), host(got_lse)
+    u = U[c.dtype]
+    n = c.cache.room
+    e = (d + 4) * 2.0 ** -24 * dots
+    assert np.array_equal(np.isinf(lse), np.isinf(got_lse)) and not np.isnan(got_lse).any()
+    seen = np.isfinite(lse)
+    tol = 2 * e + n * 2.0 ** -24 + 2.0 ** -20 * (1 + np.abs(np.where(seen, lse, 0)))
+    assert (np.abs(got_lse - lse)[seen] <= tol[seen]).all(), np.abs(got_lse - lse)[seen].max()
+    rho = 4 * e + n * 2.0 ** -23 + 2.0 ** -19
+    tol = u * np.abs(out) + (u + rho[..., None]) * mag + 2.0 ** -25
+    if c.dtype == "f16":
+        top = np.nanmax(np.abs(c.v)) if np.isfinite(c.v).any() else 0.0
+        tol = tol + n * 2.0 ** -25 * top
+    bad = ~(np.abs(got - out) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], out[bad][:3], tol[bad][:3])
+    if weight is not None:
+        cols = weight.shape[2]
+        full = np.zeros((B, c.k.shape[2], max(cols, w.shape[2])))
+        full[..., :w.shape[2]] = w
+        w = full[..., :cols]
+        R = T * q_heads // c.k.shape[2]
+        tol = (rho.max() + (R + 2) * 2.0 ** -24) * w + 2.0 ** -23 * np.abs(weight + w) + 1e-30
+        bad = ~(np.abs(host(w_out) - (weight + w)) <= tol)
+        assert not bad.any(), (np.argwhere(bad)[:3], host(w_out)[bad][:3], (weight + w)[bad][:3])
+
+
+SHAPES = [
+    # B, T, heads, group, d, page, lens
+    (1, 1, 1, 1, 64, 16, [1]),
+    (1, 1, 2, 4, 64, 16, [0]),
+    (3, 1, 2, 4, 128, 16, [0, 1, 517]),
+    (2, 5, 3, 3, 80, 48, [37, 300]),
+    (2, 16, 2, 4, 128, 64, [63, 700]),
+    (1, 64, 1, 4, 128, 64, [333]),
+    (2, 70, 1, 1, 64, 7, [5, 129]),
+    (2, 2, 1, 7, 33, 1, [40, 3]),
+    (1, 3, 2, 2, 1, 5, [33]),
+    (2, 4, 1, 8, 256, 100, [250, 31]),
+    (1, 33, 2, 1, 200, 16, [90]),
+    (70, 1, 1, 2, 64, 16, [(7 * b) % 90 for b in range(70)]),
+    (1, 1, 1, 4, 128, 256, [5000]),
+    (3, 130, 1, 2, 96, 32, [0, 64, 31]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:6])))
+@pytest.mark.parametrize("mask", ["chain", "tree"])
+def test_attend(dtype, shape, mask):
+    B, T, heads, group, d, page, lens = shape
+    say("attend", dtype, shape[:6], mask)
+    c = Case(B + T + d, dtype, B, T, heads, group, d, page, lens)
+    tree = chain_tree(c.rng, B, T) if mask == "tree" else None
+    weight = c.rng.random((B, heads, c.cache.room + 5)).astype(np.float32)
+    check_attend(c, tree, weight)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("order", ["heads", "wide"])
+@pytest.mark.parametrize("table", ["mixed", None])
+@pytest.mark.parametrize("d", [64, 72, 128])
+def test_attend_strides(dtype, order, table, d):
+    say("attend strides", dtype, order, table, d)
+    c = Case(11, dtype, 2, 3, 2, 3, d, 16, [50, 7], order=order, table=table)
+    # queries inside a fused projection's output, and in another order of dimensions
+    import torch
+    wide = torch.full((2, 3, 13, d + 1), float("nan"), dtype=c.dq.dtype, device="cuda")
+    wide[:, :, 2:8, 1:] = c.dq
+    weight = np.zeros((2, 2, c.cache.room), np.float32)
+    check_attend(c, chain_tree(c.rng, 2, 3), weight, dq=wide[:, :, 2:8, 1:])
+    check_attend(c, None, weight, dq=c.dq.permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("mask", ["chain", "tree", "nothing", "some"])
+def test_attend_counts_and_empty_rows(dtype, mask):
+    """Sequences with fewer tokens than the call (and with more than fit, or a
+    negative number), masks that hide everything where there is no history,
+    lengths outside the cache."""
+    say("attend empty", dtype, mask)
+    c = Case(3, dtype, 6, 9, 2, 2, 64, 16, [0, 40, 0, 9, -5, 100], counts=[9, 4, 0, 20, 3, -1])
+    tree = None
+    if mask != "chain":
+        tree = chain_tree(c.rng, 6, 9)
+        if mask == "nothing":
+            tree[:] = 0
+        if mask == "some":
+            tree[:, ::2] = 0
+    check_attend(c, tree, np.ones((6, 2, c.cache.room), np.float32))
+
+
+def test_attend_length_beyond_the_room():
+    say("attend beyond")
+    c = Case(4, "bf16", 2, 4, 1, 2, 64, 16, [60, 30])
+    c.lens[:] = [10 ** 6, 62]
+    for b in range(2):      # every row of the room now belongs to the sequence
+        for n in range(c.cache.room):
+            r = ref.row_of(c.table, c.page, c.k.shape[0], b, n)
+            c.k[r], c.v[r] = 0.25, n % 5
+    c.dk.copy_(dev(c.k, "bf16"))
+    c.dv.copy_(dev(c.v, "bf16"))
+    check_attend(c, None, np.zeros((2, 1, c.cache.room), np.float32))
+
+
+@pytest.mark.parametrize("hole", [(0, 0), (1, 2), (1, slice(0, 3))])
+def test_attend_pages_that_do_not_exist(hole):
+    say("attend hole", hole)
+    c = Case(5 + sum(map(ord, str(hole))), "f16", 2, 6, 2, 2, 64, 16, [40, 38], hole=hole)
+    check_attend(c, chain_tree(c.rng, 2, 6), np.zeros((2, 2, c.cache.room), np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("group", [1, 12])
+def test_attend_hidden_rows_may_hold_anything(dtype, bad, group):
+    """A drafted token whose key and value are not finite reaches only the tokens
+    that see it."""
+    import paper_2006_12608_amd as sj
+    say("attend hidden", dtype, bad, group)
+    T = 6
+    c = Case(21, dtype, 1, T, 2, group, 64, 16, [20])
+    tree = np.zeros((1, T, 1), np.uint64)
+    for t in range(T):
+        tree[0, t, 0] = sum(1 << w for w in range(t + 1) if w != 2 or t == 2)
+    weight = np.zeros((1, 2, c.cache.room), np.float32)
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, 22)
+    for x in (c.dk, c.dv):
+        x[r[0], r[1]] = bad
+    c.k[r], c.v[r] = 0.0, 0.0           # the oracle's hidden row is plain
+    want, want_lse, _, mag, dots = ref.attend(c.k, c.v, c.table, c.lens, c.q, tree, 0.125, None)
+    import torch
+    w = torch.zeros(weight.shape, device="cuda")
+    got, lse = sj.attend(c.cache, dev(c.lens), c.dq, dev(tree.view(np.int64)), weight_out=w)
+    got, lse = host(got), host(lse)
+    others = [0, 1, 3, 4, 5]
+    assert np.isfinite(got[:, others]).all() and np.isfinite(lse[:, others]).all()
+    u = U[dtype]
+    rho = 4 * 68 * 2.0 ** -24 * dots.max() + 40 * 2.0 ** -23 + 2.0 ** -19
+    tol = u * np.abs(want) + (u + rho) * mag + 40 * 2.0 ** -25 * 6
+    assert (np.abs(got - want)[:, others] <= tol[:, others]).all()
+    # token 2 sees the row: what is not finite shows
+    assert not np.isfinite(got[:, 2]).all()
+
+
+def test_attend_visible_infinite_values_reach_their_queries():
+    """An infinite value in a token's own row appears, with its sign, in the
+    outputs of the tokens that see it and in no other."""
+    import paper_2006_12608_amd as sj
+    say("attend visible inf")
+    c = Case(22, "bf16", 1, 4, 1, 2, 64, 16, [17])
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, 18)
+    c.dv[r[0], r[1], 0, 5] = float("inf")
+    c.dv[r[0], r[1], 0, 60] = float("-inf")
+    tree = np.array([[[1], [3], [5], [11]]], np.uint64)       # tokens 1 and 3 see token 1
+    got = host(sj.attend(c.cache, dev(c.lens), c.dq, dev(tree.view(np.int64)))[0])
+    assert np.isfinite(got[0, [0, 2]]).all()
+    for t in (1, 3):
+        assert (got[0, t, :, 5] == np.inf).all() and (got[0, t, :, 60] == -np.inf).all()
+        assert np.isfinite(np.delete(got[0, t], [5, 60], axis=-1)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attend_scores_of_every_size(dtype):
+    """Scores so large that all but one exponential vanish, all equal, and a
+    negative and a zero scale."""
+    say("attend scores", dtype)
+    for scale in (8.0, -0.5, 0.0, 1e-6):
+        c = Case(31, dtype, 2, 3, 1, 4, 64, 16, [700, 64])
+        check_attend(c, None, np.zeros((2, 1, c.cache.room), np.float32), scale=scale)
+
+
+def test_attend_weight_in_place_and_absent():
+    import torch
+    import paper_2006_12608_amd as sj
+    say("attend weight")
+    c = Case(41, "bf16", 2, 4, 2, 2, 128, 16, [90, 20])
+    _, _, w, _, _ = ref.attend(c.k, c.v, c.table, c.lens, c.q, None, 128 ** -0.5, None)
+    acc = torch.ones((2, 2, c.cache.room), device="cuda")
+    for _ in range(3):
+        sj.attend(c.cache, dev(c.lens), c.dq, weight=acc)
+    assert np.allclose(host(acc), 1 + 3 * w, rtol=1e-4, atol=1e-6)
+    fresh = torch.full_like(acc, float("nan"))
+    sj.attend(c.cache, dev(c.lens), c.dq, weight_out=fresh)
+    assert np.allclose(host(fresh), w, rtol=1e-4, atol=1e-6)
+    narrow = torch.zeros((2, 2, 17), device="cuda")     # fewer columns than rows
+    sj.attend(c.cache, dev(c.lens), c.dq, weight=narrow)
+    assert np.allclose(host(narrow), w[..., :17], rtol=1e-4, atol=1e-6)
+
+
+def test_attend_offsets_past_32_bits():
+    """Pages further than 2^32 bytes and 2^31 elements into the pool."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("attend far pages")
+    page, heads, d = 64, 8, 128
+    pages = 2 ** 31 // (page * heads * d) + 70
+    k = torch.zeros((pages, page, heads, d), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    far = [pages - 1, 3, pages - 40, pages - 7]
+    small = torch.randn((4, page, heads, d), generator=g, device="cuda").bfloat16()
+    for i, p in enumerate(far):
+        k[p] = small[i]
+    q = torch.randn((1, 2, 16, d), generator=g, device="cuda").bfloat16()
+    lens = torch.tensor([220], dtype=torch.int32, device="cuda")
+    w = torch.zeros((1, heads, 256), device="cuda")
+    w2 = torch.zeros_like(w)
+    table = torch.tensor([far], dtype=torch.int32, device="cuda")
+    near = torch.arange(4, dtype=torch.int32, device="cuda")[None]
+    a = sj.attend(sj.kv_cache(k, k, table), lens, q, weight=w)
+    b = sj.attend(sj.kv_cache(small, small, near), lens, q, weight=w2)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and torch.equal(w, w2)
+    # the same rows evicted from there and appended back
+    small2 = torch.zeros_like(small)
+    index, n, _ = sj.cache_evict(sj.kv_cache(k, k, table), lens, w, sj.kv_cache(small2, small2.clone(), near),
+                                 keep=220)
+    assert int(n) == 220 and torch.equal(small2.flatten(0, 1)[:220], small.flatten(0, 1)[:220])
+    row = torch.randn((1, 1, heads, d), generator=g, device="cuda").bfloat16()
+    sj.cache_append(sj.kv_cache(k, k, table), lens, row, row)
+    assert torch.equal(k[far[3], 220 - 192], row[0, 0])
+
+
+# ------------------------------------------------------------- rotary, append
+
+SCALINGS = [{}, {"linear": 4.0}, {"ramp": (8.0, 4096.0, 1.0, 32.0)}]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("n,heads,d,rot", [(1, 1, 2, 2), (5, 3, 64, 64), (300, 2, 128, 64),
+                                           (33, 7, 80, 40), (17, 2, 33, 18), (9, 1, 256, 256),
+                                           (4, 2, 7, 0), (2, 40, 128, 128), (3, 2, 600, 510)])
+def test_rotary(dtype, layout, n, heads, d, rot):
+    import torch
+    import paper_2006_12608_amd as sj
+    say("rotary", dtype, layout, n, heads, d, rot)
+    rng = np.random.default_rng(n + d)
+    x = dev(rng.standard_normal((n, heads, d)) * 3, dtype)
+    pos = rng.integers(0, 10 ** 6, n).astype(np.int32)
+    pos[0] = -7 if n > 1 else 12345678
+    for kw in SCALINGS:
+        for inverse in (False, True):
+            turns = sj.rotary_turns(rot, 10000.0, **kw)
+            y = sj.rotary(x, dev(pos), turns, layout=layout, factor=1.25, inverse=inverse)
+            f = ref.frequencies(rot, 10000.0, **kw) if rot else np.zeros(0)
+            want = ref.rotary(host(x), pos, f, layout, 1.25, inverse)
+            pair = np.abs(host(x))
+            tol = U[dtype] * np.abs(want) + 2.0 ** -20 * 2 * 1.25 * pair.max() + 2.0 ** -25
+            assert (np.abs(host(y) - want) <= tol).all(), np.abs(host(y) - want).max()
+            assert torch.equal(y[..., rot:], x[..., rot:])
+    # strided input and output, and in place
+    wide = torch.zeros((n, heads + 2, d + 3), dtype=x.dtype, device="cuda")
+    wide[:, 1:-1, 1:d + 1] = x
+    view = wide[:, 1:-1, 1:d + 1]
+    turns = sj.rotary_turns(rot)
+    want = sj.rotary(x, dev(pos), turns, layout=layout)
+    out = torch.zeros((heads, n, d), dtype=x.dtype, device="cuda").transpose(0, 1)
+    sj.rotary(view, dev(pos), turns, layout=layout, out=out)
+    assert torch.equal(out, want)
+    sj.rotary(view, dev(pos), turns, layout=layout, out=view)
+    assert torch.equal(view, want) and wide[:, 0].eq(0).all() and wide[..., 0].eq(0).all() \
+        and wide[..., d + 1:].eq(0).all()
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotary_gradient_against_differences(layout):
+    """<g, rotary(x + h e) - rotary(x - h e)> / 2h = (inverse of g)_e.  The map is linear, so
+    the differences are exact up to the roundings: with h a power of two and x = 0 only
+    those of h times a sine (u h each, over the two elements of a pair)."""
+    import paper_2006_12608_amd as sj
+    say("rotary gradient", layout)
+    n, heads, d, rot = 3, 2, 12, 8
+    rng = np.random.default_rng(6)
+    pos, turns = dev(np.array([0, 5, 70001], np.int32)), sj.rotary_turns(rot)
+    g = dev(rng.standard_normal((n, heads, d)), "f16")
+    grad = host(sj.rotary(g, pos, turns, layout=layout, factor=1.5, inverse=True))
+    gh = host(g)
+    for e in range(d):
+        x = np.zeros((n, heads, d))
+        x[..., e] = 2.0
+        up = host(sj.rotary(dev(x, "f16"), pos, turns, layout=layout, factor=1.5))
+        down = host(sj.rotary(dev(-x, "f16"), pos, turns, layout=layout, factor=1.5))
+        slope = (gh * (up - down)).sum(-1) / 4.0
+        tol = U["f16"] * (1.5 * np.abs(gh).sum(-1) + np.abs(grad[..., e])) + 1e-5
+        assert (np.abs(slope - grad[..., e]) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("B,T,heads,group,d,rot,page,lens,counts",
+                         [(1, 1, 1, 1, 64, 64, 16, [0], None),
+                          (3, 4, 2, 3, 80, 40, 7, [0, 13, 6], [4, 0, 3]),
+                          (2, 9, 3, 0, 33, 10, 1, [5, 2], None),
+                          (2, 70, 1, 4, 128, 128, 64, [63, 1], [99, -3])])
+def test_append(dtype, layout, B, T, heads, group, d, rot, page, lens, counts):
+    import torch
+    import paper_2006_12608_amd as sj
+    say("append", dtype, layout, B, T, heads, d, rot, page)
+    c = Case(9, dtype, B, T, heads, max(group, 1), d, page, lens, counts=counts, order="wide")
+    key, value = (dev(c.rng.standard_normal((B, T, heads, d)), dtype) for _ in range(2))
+    pos = c.rng.integers(0, 50000, (B, T)).astype(np.int32)
+    turns = sj.rotary_turns(rot)
+    k0, v0 = c.dk.clone(), c.dv.clone()
+    q = sj.cache_append(c.cache, dev(c.lens), key, value, pos=dev(pos), turns=turns,
+                        q=c.dq if group else None, layout=layout,
+                        counts=None if counts is None else dev(c.counts))
+    flat = dev(pos.reshape(-1))
+    want_k = sj.rotary(key.reshape(-1, heads, d), flat, turns, layout=layout).view(B, T, heads, d)
+    for b in range(B):
+        t = T if counts is None else min(max(counts[b], 0), T)
+        for u in range(t):
+            r = ref.row_of(c.table, page, c.k.shape[0], b, lens[b] + u)
+            k0[r[0], r[1]], v0[r[0], r[1]] = want_k[b, u], value[b, u]
+    bits = torch.int16
+    assert torch.equal(c.dk.contiguous().view(bits), k0.contiguous().view(bits))
+    assert torch.equal(c.dv.contiguous().view(bits), v0.contiguous().view(bits))
+    if group:
+        want = sj.rotary(c.dq.reshape(-1, heads * group, d), flat, turns, layout=layout)
+        assert torch.equal(q.view(-1, heads * group, d), want)
+        q2 = c.dq.clone()
+        sj.cache_append(c.cache, dev(c.lens), key, value, pos=dev(pos), turns=turns, q=q2, q_out=q2,
+                        layout=layout)
+        assert torch.equal(q2, q)
+    # unturned
+    sj.cache_append(c.cache, dev(c.lens), key, value)
+    r = ref.row_of(c.table, page, c.k.shape[0], 0, lens[0])
+    assert torch.equal(c.dk[r[0], r[1]], key[0, 0])
+
+
+def test_append_drops_rows_without_room():
+    import torch
+    import paper_2006_12608_amd as sj
+    say("append no room")
+    k, v = (torch.zeros((3, 4, 1, 8), dtype=torch.float16, device="cuda") for _ in range(2))
+    table = torch.tensor([[0, 7], [-1, 2]], dtype=torch.int32, device="cuda")
+    c = sj.kv_cache(k, v, table)
+    x = torch.ones((2, 5, 1, 8), dtype=torch.float16, device="cuda")
+    sj.cache_append(c, torch.tensor([2, 2], dtype=torch.int32, device="cuda"), x, x)
+    # sequence 0: rows 2, 3 on page 0, rows 4 .. on page 7, which is not there;
+    # sequence 1: rows 2, 3 on no page, rows 4 .. 6 on page 2
+    want = torch.zeros((3, 4), dtype=torch.bool)
+    want[0, 2:] = True
+    want[2, :3] = True
+    assert torch.equal((k[:, :, 0, 0] != 0).cpu(), want)
+    sj.cache_append(c, torch.tensor([-3, 10 ** 9], dtype=torch.int32, device="cuda"), x, x * 2)
+    want[0, :2] = True
+    assert torch.equal((v[:, :, 0, 0] != 0).cpu(), want)
+
+
+# -------------------------------------------------------------------- eviction
+
+def check_evict(c, weight, keep, sink, recent, page2=None, order="rows"):
+    import torch
+    import paper_2006_12608_amd as sj
+    B, heads, d = c.B, c.k.shape[2], c.k.shape[3]
+    sets = weight.shape[1]
+    page2 = page2 or c.page
+    width = max(1, -(-min(keep, c.cache.room) // page2))
+    k2, v2 = (torch.full((B * width + 1, page2, heads, d), 7.0, dtype=c.dk.dtype, device="cuda")
+              for _ in range(2))
+    table2 = dev(c.rng.permutation(B * width + 1)[:B * width].reshape(B, width).astype(np.int32))
+    into = sj.kv_cache(k2, v2, table2)
+    index, n, w = sj.cache_evict(c.cache, dev(c.lens), dev(weight), into, keep=keep, sink=sink,
+                                 recent=recent)
+    index, n, w = index.cpu().numpy(), n.cpu().numpy(), w.cpu().numpy()
+    touched = np.zeros((B * width + 1, page2), bool)
+    hk, hv, hk2, hv2 = host(c.dk), host(c.dv), host(k2), host(v2)
+    for b in range(B):
+        rows = min(max(int(c.lens[b]), 0), c.cache.room)
+        m = min(rows, keep)
+        assert n[b] == m
+        for s in range(sets):
+            want = ref.evict(weight[b, s].astype(np.float64), rows, keep, sink, recent)
+            assert np.array_equal(index[b, s, :m], want) and (index[b, s, m:] == -1).all()
+            full = np.zeros(max(rows, 1), np.float32)
+            full[:min(rows, weight.shape[2])] = weight[b, s, :rows]
+            assert np.array_equal(w[b, s, :m], full[want], equal_nan=True) and \
+                (w[b, s, m:] == 0).all()
+        for j in range(m):
+            to = ref.row_of(table2.cpu().numpy(), page2, B * width + 1, b, j)
+            touched[to] = True
+            for h in range(heads):
+                fr = ref.row_of(c.table, c.page, c.k.shape[0], b, index[b, h if sets > 1 else 0, j])
+                for x, y in ((hk, hk2), (hv, hv2)):
+                    assert np.array_equal(y[to][h], x[fr][h] if fr else np.zeros(d))
+    assert (hk2[~touched] == 7).all() and (hv2[~touched] == 7).all()
+
+
+@pytest.mark.parametrize("dtype,heads,d,page,page2,lens,keep,sink,recent",
+                         [("bf16", 2, 64, 16, 16, [100, 3, 0, 40], 40, 4, 8),
+                          ("f16", 3, 33, 7, 5, [61, 60, 59], 60, 0, 0),
+                          ("bf16", 1, 128, 64, 64, [1500], 300, 4, 100),
+                          ("f16", 2, 8, 1, 3, [20, 9], 5, 2, 3),
+                          ("f16", 1, 8, 16, 16, [50], 0, 0, 0),
+                          ("f16", 1, 8, 16, 16, [50], 1, 0, 0),
+                          ("bf16", 1, 8, 16, 16, [50], 9, 9, 0),
+                          ("bf16", 1, 16, 16, 16, [5000, 4097], 1000, 4, 64)])
+@pytest.mark.parametrize("kind", ["spread", "ties", "odd"])
+@pytest.mark.parametrize("joint", [False, True])
+def test_evict(dtype, heads, d, page, page2, lens, keep, sink, recent, kind, joint):
+    say("evict", dtype, heads, d, page, lens, keep, kind, joint)
+    c = Case(len(lens) + d, dtype, len(lens), 0, heads, 1, d, page, lens)
+    shape = (len(lens), 1 if joint else heads, c.cache.room)
+    if kind == "spread":
+        w = np.exp(2 * c.rng.standard_normal(shape))
+    elif kind == "ties":
+        w = c.rng.integers(0, 3, shape) / 4.0
+    else:   # signs, zeros of both signs, denormals, infinities and NaN
+        w = c.rng.choice([0.0, -0.0, 1e-42, -1e-42, 1.0, -1.0, np.inf, -np.inf, np.nan, 3.0], shape)
+    check_evict(c, w.astype(np.float32), keep, sink, recent, page2)
+
+
+def test_evict_narrow_weights_and_missing_pages():
+    say("evict narrow")
+    c = Case(8, "f16", 2, 0, 2, 1, 16, 16, [100, 90], hole=(1, 2))
+    w = np.abs(c.rng.standard_normal((2, 2, 33))).astype(np.float32)
+    check_evict(c, w, 50, 2, 4)
+
+
+def test_evict_many_rows():
+    """More rows than one pass of a workgroup, one choice and one for each head."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("evict many")
+    n, keep = 70001, 20000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for sets in (1, 2):
+        w = torch.randint(0, 5000, (1, sets, n), generator=g, device="cuda").float() / 64
+        k = torch.randn((1, n, 2, 8), generator=g, device="cuda").half()
+        k2, v2 = torch.zeros((1, keep, 2, 8), dtype=k.dtype, device="cuda"), \
+            torch.zeros((1, keep, 2, 8), dtype=k.dtype, device="cuda")
+        index, m, kept = sj.cache_evict(sj.kv_cache(k, -k), torch.tensor([n], dtype=torch.int32, device="cuda"), w,
+                                        sj.kv_cache(k2, v2), keep=keep, sink=7, recent=100)
+        assert int(m) == keep
+        wh = w.cpu().numpy()
+        for s in range(sets):
+            at = np.arange(n)
+            forced = (at < 7) | (at >= n - 100)
+            want = np.sort(np.lexsort((at, -wh[0, s], ~forced))[:keep])
+            assert np.array_equal(index[0, s].cpu().numpy(), want)
+            assert np.array_equal(kept[0, s].cpu().numpy(), wh[0, s][want])
+            for h in range(2):
+                if sets == 1 or h == s:
+                    assert torch.equal(k2[0, :, h], k[0, torch.from_numpy(want).cuda(), h])
+                    assert torch.equal(v2[0, :, h], -k[0, torch.from_numpy(want).cuda(), h])
+
+
+# ------------------------------------------------------------ streams, refusals
+
+def test_another_stream_and_a_graph():
+    """A context per stream; a captured step whose lengths change between replays."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("streams and graphs")
+    c = Case(51, "bf16", 3, 2, 2, 4, 128, 16, [500, 33, 0])
+    lens = dev(c.lens)
+    w = torch.zeros((3, 2, c.cache.room), device="cuda")
+    want = sj.attend(c.cache, lens, c.dq, weight_out=torch.empty_like(w))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = sj.attend(c.cache, lens, c.dq, weight_out=torch.empty_like(w))
+        side.synchronize()
+        out = torch.empty_like(c.dq)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            lse = sj.attend(c.cache, lens, c.dq, weight=w, out=out)[1]
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    total = torch.zeros_like(w)
+    for new in ([500, 33, 0], [20, 40, 1], [499, 0, 7], [500, 33, 0]):
+        lens.copy_(dev(np.array(new, np.int32)))
+        torch.cuda.synchronize()
+        fresh = torch.empty_like(w)
+        a, b = sj.attend(c.cache, lens, c.dq, weight_out=fresh)
+        total += fresh
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        seen = torch.isfinite(a)
+        assert torch.equal(seen, torch.isfinite(out)) and torch.equal(out[seen], a[seen])
+        assert torch.equal(lse.nan_to_num(), b.nan_to_num())
+        assert torch.allclose(w.nan_to_num(), total.nan_to_num(), rtol=1e-5, atol=1e-7)
+
+
+def test_results_do_not_depend_on_timing():
+    import torch
+    import paper_2006_12608_amd as sj
+    say("repeatable")
+    c = Case(61, "f16", 4, 8, 2, 4, 64, 16, [3000, 17, 800, 0])
+    w = torch.empty((4, 2, c.cache.room), device="cuda")
+    first = sj.attend(c.cache, dev(c.lens), c.dq, weight_out=w)
+    for _ in range(5):
+        w2 = torch.empty_like(w)
+        again = sj.attend(c.cache, dev(c.lens), c.dq, weight_out=w2)
+        assert all(torch.equal(x, y) for x, y in zip(first, again)) and torch.equal(w, w2)
+
+
+def test_no_sequences_no_tokens():
+    import torch
+    import paper_2006_12608_amd as sj
+    say("empty calls")
+    k = torch.zeros((4, 16, 2, 64), dtype=torch.float16, device="cuda")
+    none = sj.kv_cache(k, k.clone(), torch.zeros((0, 3), dtype=torch.int32, device="cuda"))
+    lens0 = torch.zeros((0,), dtype=torch.int32, device="cuda")
+    out, lse = sj.attend(none, lens0, k.new_zeros((0, 2, 4, 64)))
+    assert out.shape == (0, 2, 4, 64) and lse.shape == (0, 2, 4)
+    c = sj.kv_cache(k, k.clone(), torch.zeros((2, 2), dtype=torch.int32, device="cuda"))
+    lens = torch.tensor([5, 0], dtype=torch.int32, device="cuda")
+    w = torch.ones((2, 2, 8), device="cuda")
+    w2 = torch.zeros_like(w)
+    sj.attend(c, lens, k.new_zeros((2, 0, 4, 64)), weight=w, weight_out=w2)
+    assert torch.equal(w, w2)
+    sj.cache_append(c, lens, k.new_zeros((2, 0, 2, 64)), k.new_zeros((2, 0, 2, 64)))
+    empty = sj.kv_cache(k[:0], k[:0], torch.zeros((2, 2), dtype=torch.int32, device="cuda"))
+    out, lse = sj.attend(empty, lens, k.new_ones((2, 1, 4, 64)))
+    assert (out == 0).all() and torch.isinf(lse).all()
+    assert sj.rotary(k[0][:0], lens0, sj.rotary_turns(8)).shape == (0, 2, 64)
+
+
+def test_refusals():
+    import torch
+    import paper_2006_12608_amd as sj
+    say("refusals")
+    k = torch.zeros((4, 16, 2, 64), dtype=torch.float16, device="cuda")
+    table = torch.zeros((2, 2), dtype=torch.int32, device="cuda")
+    c = sj.kv_cache(k, k.clone(), table)
+    lens = torch.zeros((2,), dtype=torch.int32, device="cuda")
+    q = k.new_zeros((2, 3, 4, 64))
+    for bad in (lambda: sj.kv_cache(k.float(), k.float()), lambda: sj.kv_cache(k.cpu(), k.cpu()),
+                lambda: sj.kv_cache(k, k[..., :32]), lambda: sj.kv_cache(k, k, table.long()),
+                lambda: sj.kv_cache(k.transpose(2, 3), k.transpose(2, 3)),
+                lambda: sj.attend(c, lens.long(), q), lambda: sj.attend(c, lens[:1], q),
+                lambda: sj.attend(c, lens, q.float()), lambda: sj.attend(c, lens, q[..., :32]),
+                lambda: sj.attend(c, lens, q, torch.zeros((2, 3, 2), dtype=torch.int64,
+                                                         device="cuda")),
+                lambda: sj.attend(c, lens, q, weight=torch.zeros((2, 1, 8), device="cuda")),
+                lambda: sj.rotary(k[0], lens, sj.rotary_turns(8)),
+                lambda: sj.rotary(k[0], torch.zeros(16, dtype=torch.int32, device="cuda"),
+                                  sj.rotary_turns(8), layout="other"),
+                lambda: sj.rotary_turns(7),
+                lambda: sj.cache_append(c, lens, q[:, :, :2], q[:, :, :2], pos=lens),
+                lambda: sj.cache_evict(c, lens, torch.zeros((2, 2, 9), device="cuda"), c, keep=-1)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad, status in (
+            (lambda: sj.attend(c, lens, q[:, :, :3]), sj.SJ_E_INVAL),
+            (lambda: sj.attend(c, lens, q, scale=float("nan")), sj.SJ_E_INVAL),
+            (lambda: sj.attend(sj.kv_cache(k.new_zeros((2, 4, 1, 264)), k.new_zeros((2, 4, 1, 264))),
+                               lens, k.new_zeros((2, 1, 1, 264))), sj.SJ_E_UNSUPPORTED),
+            (lambda: sj.rotary(k[0], torch.zeros(16, dtype=torch.int32, device="cuda"),
+                               sj.rotary_turns(66)), sj.SJ_E_INVAL),
+            (lambda: sj.cache_evict(c, lens, torch.zeros((2, 2, 9), device="cuda"), c, keep=4),
+             sj.SJ_E_INVAL),
+            (lambda: sj.cache_evict(c, lens, torch.zeros((2, 2, 9), device="cuda"),
+                                    sj.kv_cache(k.clone(), k.clone(), table), keep=4, sink=3,
+                                    recent=2), sj.SJ_E_INVAL),
+            (lambda: sj.cache_evict(c, lens, torch.zeros((2, 2, 9), device="cuda"),
+                                    sj.kv_cache(k.clone(), k.clone(), table[:, :1]), keep=20),
+             sj.SJ_E_UNSUPPORTED)):
+        with pytest.raises(sj.SjError) as e:
+            bad()
+        assert e.value.status == status and str(e.value)
+    # at the C boundary: host memory, short arrays, bad codes
+    ctx = sj.context(0)
+    a = (ctx, c.raw, lens.data_ptr(), None, 3, q.data_ptr(), q.stride()[:3], 4, None, (0, 0), 1.0)
+    out = torch.empty_like(q)
+    assert sj.sj_attend(*a, out.data_ptr(), None) == sj.SJ_OK
+    assert sj.sj_attend(*a, None, None) == sj.SJ_E_INVAL
+    assert sj.sj_attend(*a, out.cpu().data_ptr(), None) == sj.SJ_E_INVAL
+    assert sj.sj_attend(*a, out.data_ptr(), None, lens.data_ptr(), None, 1) == sj.SJ_E_INVAL
+    assert sj.sj_attend(*a[:6], (-1, 64, 64), *a[7:], out.data_ptr(), None) == sj.SJ_E_INVAL
+    assert sj.sj_attend(*a[:6], (2 ** 38, 64, 64), *a[7:], out.data_ptr(), None) == sj.SJ_E_INVAL
+    assert sj.sj_attend(*a[:8], lens.data_ptr() + 4, (0, 1), 1.0, out.data_ptr(), None) == sj.SJ_E_INVAL
+    raw = sj.sj_cache.from_buffer_copy(c.raw)
+    raw.pages = 2 ** 20
+    assert sj.sj_attend(ctx, raw, *a[2:], out.data_ptr(), None) == sj.SJ_E_INVAL
+    raw = sj.sj_cache.from_buffer_copy(c.raw)
+    raw.dtype = sj.SJ_I8
+    assert sj.sj_attend(ctx, raw, *a[2:], out.data_ptr(), None) == sj.SJ_E_INVAL
+    raw = sj.sj_cache.from_buffer_copy(c.raw)
+    raw.k_row = -1
+    assert sj.sj_attend(ctx, raw, *a[2:], out.data_ptr(), None) == sj.SJ_E_INVAL
+    raw = sj.sj_cache.from_buffer_copy(c.raw)
+    raw.width = 2 ** 31 - 1
+    assert sj.sj_attend(ctx, raw, *a[2:], out.data_ptr(), None) == sj.SJ_E_UNSUPPORTED
+    x = k.data_ptr()
+    assert sj.sj_rotary(ctx, sj.SJ_I8, x, (1, 1), x, (1, 1), 1, 1, 1, None, None, 0, 0, 1.0) == \
+        sj.SJ_E_INVAL
+    assert sj.sj_rotary(ctx, sj.SJ_F16, x, (64, 64), x, (64, 64), 1, 1, 64, None, None, 4, 0, 1.0) == \
+        sj.SJ_E_INVAL
+    assert sj.sj_rotary(ctx, sj.SJ_F16, x, (64, 64), x, (64, 64), 1, 1, 64, None, None, 0, 7, 1.0) == \
+        sj.SJ_E_INVAL
+    assert sj.sj_rotary(ctx, sj.SJ_F16, x, (64, 64), x, (64, 64), 1, 1, 64, None, None, 0, 0, 1.0,
+                        1) == sj.SJ_E_INVAL

@@ -3,7 +3,14 @@
 
 namespace sjc {
 
-uint32_t attend_tile_rows(uint32_t rows, uint32_t) { return rows <= AT_Q ? AT_Q : 2 * AT_Q; }
+uint32_t attend_tile_rows(uint32_t rows, uint32_t d)
+{
+    if (rows <= 32)
+        return rows <= 16 ? 16 : 32;
+    if (rows <= 64)
+        return d <= 128 ? 64 : 32;
+    return 128;
+}
 
 hipError_t launch_attend_f16(const Attend &a, hipStream_t s)
 {

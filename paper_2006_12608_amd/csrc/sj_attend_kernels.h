@@ -13,6 +13,7 @@ namespace sjc {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -30,6 +31,11 @@ struct Elem<sjk::DT_F16> {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
                                                       __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ f32x16 mma(i32x4 a, i32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                      __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
 };
 template <>
 struct Elem<sjk::DT_BF16> {
@@ -41,12 +47,46 @@ struct Elem<sjk::DT_BF16> {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                        __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ f32x16 mma(i32x4 a, i32x4 b, f32x16 c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
 };
 
 __device__ __forceinline__ float bits_to_float(uint16_t x, int dt)
 {
     return dt == sjk::DT_F16 ? (float)__builtin_bit_cast(_Float16, x)
                              : __uint_as_float((uint32_t)x << 16);
+}
+
+// The eight elements with zeros in the place of infinities and NaN; returns whether there
+// were any.
+template <int DT>
+__device__ __forceinline__ uint32_t drop_odd8(i32x4 &v)
+{
+    constexpr uint32_t EXP = Elem<DT>::EXP;
+    uint32_t odd = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t x = (uint32_t)v[e];
+        const uint32_t lo = (x & EXP) == EXP ? 0xffffu : 0u;
+        const uint32_t hi = ((x >> 16) & EXP) == EXP ? 0xffff0000u : 0u;
+        v[e] = (int)(x & ~(lo | hi));
+        odd |= lo | hi;
+    }
+    return odd;
+}
+
+// Eight 16-bit values down a column of LDS rows: each group of 16 lanes reads 4 rows x 16
+// columns at lo and 4 more at hi (lane l passes the address of columns 4 (l % 4) .. + 3 of row
+// (l / 4) % 4) and lane l receives column l % 16 of both.
+__device__ __forceinline__ i32x4 column8(const uint8_t *lo, const uint8_t *hi)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)lo);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)hi);
+    return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // 2^x, 2^-inf = 0.
@@ -84,6 +124,52 @@ __device__ __forceinline__ bool sees(const Attend &a, uint32_t b, const Rows &r,
     if (!a.tree)
         return w <= u;
     return (a.tree[(int64_t)b * a.tree_seq + (int64_t)u * a.tree_tok + (w >> 6)] >> (w & 63)) & 1;
+}
+
+// Which of the 64 rows from row0 on token u sees, bit by bit, among rows that exist.
+__device__ __forceinline__ uint64_t seen64(const Attend &a, uint32_t b, const Rows &r, uint32_t u,
+                                           uint32_t row0)
+{
+    const int64_t o = (int64_t)row0 - r.len;     // of the tokens' own rows
+    const uint64_t before = o >= 0 ? 0 : (o <= -64 ? ~(uint64_t)0 : ((uint64_t)1 << -o) - 1);
+    if (!a.tree) {
+        const int64_t n = (int64_t)u + 1 - o;    // a chain: the rows below this one
+        return n <= 0 ? 0 : (n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1);
+    }
+    if (o <= -64)
+        return before;
+    const uint64_t *t = a.tree + (int64_t)b * a.tree_seq + (int64_t)u * a.tree_tok;
+    if (o < 0)
+        return before | t[0] << -o;
+    const uint32_t words = (a.t + 63) / 64, w = (uint32_t)(o >> 6), sh = (uint32_t)(o & 63);
+    uint64_t v = w < words ? t[w] >> sh : 0;
+    if (sh && w + 1 < words)
+        v |= t[w + 1] << (64 - sh);
+    return v;
+}
+
+// Calls f(row of values) for the tokens' own rows in [from, to) that token u sees.  The
+// products leave out what is not finite in these rows, since 0 x inf and 0 x NaN would
+// reach the queries that do not see them; added up afterwards, what a query does
+// see of them decides its output whatever the weights are.
+template <class F>
+__device__ __forceinline__ void own_rows(const Attend &a, uint32_t b, uint32_t h, const Rows &r,
+                                         uint32_t u, uint32_t from, uint32_t to, F f)
+{
+#pragma unroll 1
+    for (uint32_t n = from > r.len ? from : r.len; n < to; ++n) {
+        const Place p = place_of(a.c, b, n);
+        if (p.page >= 0 && sees(a, b, r, u, n))
+            f(a.c.v + (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row +
+              (int64_t)h * a.c.v_head);
+    }
+}
+
+// x where it is infinite or NaN, else 0.
+template <int DT>
+__device__ __forceinline__ float odd_part(uint16_t x)
+{
+    return (x & Elem<DT>::EXP) == Elem<DT>::EXP ? bits_to_float(x, DT) : 0.f;
 }
 
 // The share of the work that a workgroup takes: blocks [first, last) of
@@ -172,6 +258,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     static_assert(AT_Q * OS * 4 <= WAVE_LDS, "the sums of a query tile fit in the wave's V");
     __shared__ __align__(16) uint8_t lds[AT_WAVES * WAVE_LDS];
     __shared__ float stat[AT_WAVES][QT][2];
+    __shared__ uint32_t odd_any;      // infinities or NaN among the tokens' own values
 
     const uint32_t lane = threadIdx.x & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -193,6 +280,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         a.plan[2 * b + 1] = shares;
     }
 
+    const uint32_t to = last * AT_ROWS < rows.end ? last * AT_ROWS : rows.end;
     const uint32_t q16 = lane & 15, g4 = lane >> 4;
     const uint32_t d = a.c.d;
     const uint32_t q_rows = a.t * a.group;
@@ -256,6 +344,9 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         }
     };
 
+    if (threadIdx.x == 0)
+        odd_any = 0;
+    __syncthreads();
     uint32_t blk = first + wave;
     Place cur = place(blk);
     if (blk < last) {
@@ -283,18 +374,13 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             load_k(nxt);
 
         // V to LDS; rows that do not exist as zeros (0 x NaN would reach every query)
-        uint32_t odd = 0;       // not finite in a row that a mask may hide
+        uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (there != 0xffffffffu && !((there >> (VR * i + v_row)) & 1))
                 V[i] = i32x4{0, 0, 0, 0};
             if (tail)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t x = (uint32_t)V[i][e];
-                    odd |= (uint32_t)((x & E::EXP) == E::EXP) |
-                           (uint32_t)(((x >> 16) & E::EXP) == E::EXP);
-                }
+                odd |= drop_odd8<DT>(V[i]);
             *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = V[i];
         }
         if (blk + AT_WAVES < last)
@@ -303,19 +389,18 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         // scores to exponentials
         i32x4 P[NQ];
         float pf[NQ][8];
+        uint32_t seen[NQ];
 #pragma unroll
         for (int j = 0; j < NQ; ++j) {
+            seen[j] = there & (tail ? (uint32_t)seen64(a, b, rows, tok[j], blk * AT_ROWS) : ~0u);
             float top = -INFINITY;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     float x = s[j][t][r] * a.scale2;
-                    if (tail || there != 0xffffffffu) {
-                        const uint32_t i = 16 * t + 4 * g4 + r, n = blk * AT_ROWS + i;
-                        if (!((there >> i) & 1) || !sees(a, b, rows, tok[j], n))
-                            x = -INFINITY;
-                    }
+                    if (tail || there != 0xffffffffu)
+                        x = (seen[j] >> (16 * t + 4 * g4 + r)) & 1 ? x : -INFINITY;
                     pf[j][4 * t + r] = x;
                     top = fmaxf(top, x);
                 }
@@ -343,40 +428,15 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                 O[j][i] *= shrink;
         }
 
-        if (__builtin_expect(!__any((int)odd), 1)) {
+        if (odd)
+            odd_any = 1;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const uint8_t *at = my + (4 * g4 + (q16 >> 2)) * RS + 32 * i + 8 * (q16 & 3);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4 *)at);
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4 *)(at + 16 * RS));
-                const i32x4 vt = {__builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7))};
-#pragma unroll
-                for (int j = 0; j < NQ; ++j)
-                    O[j][i] = E::mma(vt, P[j], O[j][i]);
-            }
-        } else {
-            // infinities or NaN among the tokens' own values: only rows that a query
-            // sees may reach it, one product at a time
+        for (int i = 0; i < NV; ++i) {
+            const uint8_t *at = my + (4 * g4 + (q16 >> 2)) * RS + 32 * i + 8 * (q16 & 3);
+            const i32x4 vt = column8(at, at + 16 * RS);
 #pragma unroll
             for (int j = 0; j < NQ; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-#pragma unroll 1
-                    for (uint32_t g = 0; g < 4; ++g) {
-                        const uint32_t i = 16 * (e >> 2) + 4 * g + (e & 3);
-                        const float p = __shfl(pf[j][e], (int)(16 * g + q16));
-                        const uint32_t n = blk * AT_ROWS + i;
-                        if (!((there >> i) & 1) || !sees(a, b, rows, tok[j], n))
-                            continue;
-#pragma unroll
-                        for (int x = 0; x < NV; ++x)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                O[j][x][r] += p * bits_to_float(
-                                    *(const uint16_t *)(my + i * RS + 2 * (16 * x + 4 * g4 + r)), DT);
-                    }
+                O[j][i] = E::mma(vt, P[j], O[j][i]);
         }
         cur = nxt;
         nxt = aft;
@@ -429,6 +489,13 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 #pragma unroll
                 for (uint32_t w = 0; w < AT_WAVES; ++w)
                     o += *(const f32x4 *)((const float *)(lds + w * WAVE_LDS) + qi * OS + c);
+                if (odd_any && live)
+                    own_rows(a, b, h, rows, u, first * AT_ROWS, to, [&](const uint16_t *v) {
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e)
+                            if (c + e < d)
+                                o[e] += odd_part<DT>(v[c + e]);
+                    });
                 if (shares > 1) {
                     *(f32x4 *)(a.part_o + (part * QT + AT_Q * j + qi) * D + c) = o;
                 } else {
@@ -450,6 +517,321 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                                      : -INFINITY;
                 }
             }
+        }
+    }
+}
+
+// ------------------------------------------------------------- the tiled kernel
+//
+// For more query rows than 32: QW groups of 32 query rows share tiles of BN cache rows
+// in LDS (32 x 32 x 16 products).  With QW = 4 every wave takes 32 queries and all rows of a tile,
+// with QW = 2 two waves share 32 queries and take half of its rows each.  As above
+// S^T = K Q^T leaves query l % 32 in lane l with rows 8 (r / 4) + 4 (l / 32) + r % 4 in
+// register r, which is, register by register, the operand of O^T = V^T P^T for steps of 16
+// rows in the order {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3} of lane half h.
+// Two buffers; the next tile's loads go to registers while a tile is worked on
+// and to LDS at the start of the next, one barrier a tile.  The 16-byte
+// chunks of a row are permuted by the row (swz) so that neither the K reads (16
+// rows, one chunk) nor the transposed V reads (4 rows, 4 chunks) meet in a bank.
+template <int DC>
+__device__ __forceinline__ uint32_t swz(uint32_t row, uint32_t chunk)
+{
+    if constexpr (DC == 2)
+        return chunk ^ ((((row >> 1) & 1) << 2) | ((row >> 2) & 3));
+    else
+        return chunk ^ (((row & 3) << 2) | ((row >> 2) & 3));
+}
+
+template <int DT, int DC, int QW, bool EXACT>
+__global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Attend a)
+{
+    typedef Elem<DT> E;
+    constexpr uint32_t D = 32 * DC, QT = 32 * QW, RW = 4 / QW;
+    constexpr uint32_t BN = DC == 8 ? 32 : 64;      // rows of a tile
+    constexpr uint32_t WR = BN / RW;                // of these, one wave's
+    constexpr int SR = WR / 32;                     // 32-row products of a wave
+    constexpr uint32_t CPR = 4 * DC;                // 16-byte chunks of a row
+    constexpr int NL = BN * CPR / 256;              // loads per thread of K, of V
+    constexpr uint32_t RPL = 256 / CPR;             // rows per load of the workgroup
+    constexpr uint32_t TILE = BN * D * 2;           // bytes
+    static_assert(WR % 32 == 0, "whole products");
+    __shared__ __align__(16) uint8_t lds[4 * TILE]; // K, V of two tiles
+    __shared__ float stat[4][32][2];
+    __shared__ uint32_t odd_any;
+
+    const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t qw = wave % QW, rw = wave / QW;
+    const uint32_t units = a.c.heads * a.tiles;
+    // neighbours in (share, head, tile) on one XCD: the tiles of a head read the same rows
+    const uint32_t per = gridDim.x / 8, id = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    const uint32_t unit = id % units, slot = id / units;
+    const uint32_t h = unit / a.tiles, tile = unit % a.tiles;
+    Share sh;
+    if (slot >= a.slots || !find_share(a, slot, &sh))
+        return;
+    const uint32_t b = __builtin_amdgcn_readfirstlane(sh.b);
+    const uint32_t shares = __builtin_amdgcn_readfirstlane(sh.shares);
+    const Rows rows = {(uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.len),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.count),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.end)};
+    const uint32_t from = __builtin_amdgcn_readfirstlane(sh.first) * AT_ROWS;
+    const uint32_t last = __builtin_amdgcn_readfirstlane(sh.last) * AT_ROWS;
+    const uint32_t to = last < rows.end ? last : rows.end;      // rows [from, to)
+    if (unit == 0 && sh.share == 0 && tid == 0) {
+        a.plan[2 * b] = slot;
+        a.plan[2 * b + 1] = shares;
+    }
+
+    const uint32_t q32 = lane & 31, half = lane >> 5, g = lane >> 4, l16 = lane & 15;
+    const uint32_t d = a.c.d, q_rows = a.t * a.group;
+    const uint32_t r_mine = tile * QT + 32 * qw + q32;
+    const bool live = r_mine < q_rows && r_mine / a.group < rows.count;
+    const uint32_t tok = live ? r_mine / a.group : 0;
+    i32x4 Q[2 * DC];
+    {
+        const uint16_t *p = a.q + (int64_t)b * a.q_seq + (int64_t)tok * a.q_tok +
+                            (int64_t)(h * a.group + (live ? r_mine % a.group : 0)) * a.q_head +
+                            8 * half;
+#pragma unroll
+        for (int k = 0; k < 2 * DC; ++k)
+            Q[k] = live ? load8(p + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half))
+                        : i32x4{0, 0, 0, 0};
+    }
+    f32x16 O[DC];
+#pragma unroll
+    for (int i = 0; i < DC; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            O[i][r] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    const uint16_t *kb = a.c.k + (int64_t)h * a.c.k_head, *vb = a.c.v + (int64_t)h * a.c.v_head;
+    // places in a tile: chunk 2 k + half of row q32 of K (the same for every 32 rows), and of V
+    // columns 32 z + 16 (g % 2) + 4 (l16 % 4) .. of rows 4 half + l16 / 4 and 8 further (the same
+    // for every 16 rows)
+    uint32_t k_at[2 * DC], v_at[DC][2];
+#pragma unroll
+    for (uint32_t k = 0; k < 2 * DC; ++k)
+        k_at[k] = (rw * WR + q32) * (2 * D) + 16 * swz<DC>(q32, 2 * k + half);
+#pragma unroll
+    for (uint32_t z = 0; z < DC; ++z)
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x) {
+            const uint32_t r = 4 * half + (l16 >> 2) + 8 * x;
+            v_at[z][x] = TILE + (rw * WR + r) * (2 * D) +
+                         16 * swz<DC>(r, 4 * z + 2 * (g & 1) + ((l16 & 3) >> 1)) + 8 * (l16 & 1);
+        }
+    const uint32_t n_tiles = from < to ? (to - from + BN - 1) / BN : 0;
+    const uint32_t row_at = tid / CPR, chunk = tid % CPR;
+    auto place = [&](uint32_t i) -> Place {
+        const uint32_t n = from + i * BN + (lane & (BN - 1));
+        return i < n_tiles && n < to ? place_of(a.c, b, n) : Place{-1, 0u};
+    };
+    i32x4 kr[NL], vr[NL];
+    auto fetch = [&](const Place &p) {      // absent rows read page 0, row 0
+        const int64_t ko =
+            p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
+        const int64_t vo =
+            p.page < 0 ? 0 : (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row;
+        const int left = EXACT ? 8 : (int)d - (int)(8 * chunk);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            kr[i] = load8(kb + shfl64(ko, RPL * i + row_at) + 8 * chunk, left);
+            vr[i] = load8(vb + shfl64(vo, RPL * i + row_at) + 8 * chunk, left);
+        }
+    };
+    auto stash = [&](uint32_t i, uint64_t there) {
+        uint8_t *kt = lds + (i & 1) * 2 * TILE, *vt = kt + TILE;
+        uint32_t odd = 0;
+        const bool tail = from + i * BN + BN > rows.len;
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+            const uint32_t r = RPL * x + row_at, at = r * (2 * D) + 16 * swz<DC>(r, chunk);
+            if (!((there >> r) & 1))
+                vr[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
+            if (tail)
+                odd |= drop_odd8<DT>(vr[x]);
+            *(i32x4 *)(kt + at) = kr[x];
+            *(i32x4 *)(vt + at) = vr[x];
+        }
+        if (odd)
+            odd_any = 1;
+    };
+
+    if (tid == 0)
+        odd_any = 0;
+    __syncthreads();
+    Place nxt = place(0);
+    uint64_t there = __ballot(nxt.page >= 0), there_nxt = 0;
+    if (n_tiles > 0) {
+        fetch(nxt);
+        nxt = place(1);
+        stash(0, there);
+        there_nxt = __ballot(nxt.page >= 0);
+        if (n_tiles > 1)
+            fetch(nxt);
+        nxt = place(2);
+    }
+    __syncthreads();
+    for (uint32_t i = 0; i < n_tiles; ++i) {
+        uint64_t there_aft = 0;
+        if (i + 1 < n_tiles) {
+            stash(i + 1, there_nxt);
+            there_aft = __ballot(nxt.page >= 0);
+            if (i + 2 < n_tiles)
+                fetch(nxt);
+            nxt = place(i + 3);
+        }
+        uint8_t *const kt = lds + (i & 1) * 2 * TILE;
+        const uint32_t row0 = from + i * BN;
+        const bool tail = row0 + BN > rows.len;
+        const bool masked = tail || there != ~(uint64_t)0;
+        uint32_t seen[SR];      // bit 8 (r / 4) + r % 4: this lane's row in register r
+        if (masked) {
+            const uint64_t v = (there & (tail ? seen64(a, b, rows, tok, row0) : ~(uint64_t)0)) >>
+                               (rw * WR + 4 * half);
+#pragma unroll
+            for (int x = 0; x < SR; ++x)
+                seen[x] = (uint32_t)(v >> (32 * x));
+        }
+
+        f32x16 s[SR];
+#pragma unroll
+        for (int x = 0; x < SR; ++x) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                s[x][e] = 0.f;
+#pragma unroll
+            for (uint32_t k = 0; k < 2 * DC; ++k)
+                s[x] = E::mma(*(const i32x4 *)(kt + k_at[k] + 32 * x * 2 * D), Q[k], s[x]);
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < SR; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float y = s[x][e] * a.scale2;
+                if (masked)
+                    y = seen[x] & (1u << (8 * (e >> 2) + (e & 3))) ? y : -INFINITY;
+                s[x][e] = y;
+                top = fmaxf(top, y);
+            }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (__any(top > m)) {
+            const float m_new = fmaxf(m, top);
+            const float shrink = exp2_(m - (m_new == -INFINITY ? 0.f : m_new));
+            m = m_new;
+            l *= shrink;
+#pragma unroll
+            for (int y = 0; y < DC; ++y)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    O[y][e] *= shrink;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        i32x4 P[SR][2];
+#pragma unroll
+        for (int x = 0; x < SR; ++x) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[x][e] = exp2_(s[x][e] - base);
+                l += s[x][e];
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                typename E::eight p8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    p8[e] = (typename E::one)s[x][8 * y + e];
+                P[x][y] = __builtin_bit_cast(i32x4, p8);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < SR; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int z = 0; z < DC; ++z) {
+                    const uint8_t *at = kt + (32 * x + 16 * y) * 2 * D;
+                    O[z] = E::mma(column8(at + v_at[z][0], at + v_at[z][1]), P[x][y], O[z]);
+                }
+        there = there_nxt;
+        there_nxt = there_aft;
+        __syncthreads();
+    }
+
+    // join the halves of a query, then (QW = 2) the two waves of its rows
+    l += __shfl_xor(l, 32);
+    if constexpr (RW == 2) {
+        if (half == 0) {
+            stat[wave][q32][0] = m;
+            stat[wave][q32][1] = l;
+        }
+        float *sums = (float *)lds + qw * (16 * DC * 64);
+        __syncthreads();
+        const float m2 = stat[wave ^ QW][q32][0], l2 = stat[wave ^ QW][q32][1];
+        const float all = fmaxf(m, m2), base = all == -INFINITY ? 0.f : all;
+        const float f = exp2_(m - base);
+        l = l * f + l2 * exp2_(m2 - base);
+        m = all;
+#pragma unroll
+        for (int z = 0; z < DC; ++z)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                O[z][e] *= f;
+                if (rw == 1)
+                    sums[(16 * z + e) * 64 + lane] = O[z][e];
+            }
+        __syncthreads();
+        if (rw == 1)
+            return;
+#pragma unroll
+        for (int z = 0; z < DC; ++z)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                O[z][e] += sums[(16 * z + e) * 64 + lane];
+    }
+    if (r_mine >= q_rows)
+        return;
+    const uint32_t u = r_mine / a.group;
+    const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r_mine % a.group;
+    const uint64_t part = ((uint64_t)slot * units + unit) * QT + 32 * qw + q32;
+    if (odd_any && live)
+        own_rows(a, b, h, rows, tok, from, to, [&](const uint16_t *v) {
+#pragma unroll
+            for (int z = 0; z < DC; ++z)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t c = 32 * z + 8 * (e >> 2) + 4 * half + (e & 3);
+                    if (EXACT || c < d)
+                        O[z][e] += odd_part<DT>(v[c]);
+                }
+        });
+    const bool some = live && m != -INFINITY;
+    const float inv = some ? 1.f / l : 0.f;
+#pragma unroll
+    for (int z = 0; z < DC; ++z)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t c = 32 * z + 8 * x + 4 * half;
+            const f32x4 o = {O[z][4 * x], O[z][4 * x + 1], O[z][4 * x + 2], O[z][4 * x + 3]};
+            if (shares > 1) {
+                *(f32x4 *)(a.part_o + part * D + c) = o;
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (EXACT || c + e < d)
+                        a.out[row * d + c + e] = __builtin_bit_cast(
+                            uint16_t, (typename E::one)(some ? o[e] * inv : 0.f));
+            }
+        }
+    if (half == 0) {
+        if (shares > 1) {
+            a.part_ml[part * 2] = m;
+            a.part_ml[part * 2 + 1] = l;
+        } else {
+            a.lse[row] = some ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
         }
     }
 }
@@ -503,81 +885,109 @@ __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, 
 }
 
 // Weights: w_out[b, h, n] = w_in[b, h, n] + sum over the query rows r that read head h of
-// exp(s_rn - lse_r).  A wave holds 16 x 2 key rows in operand layout and runs
-// through the query rows, S = Q K^T: lane l holds key row l % 16 with query rows
-// 4 (l / 16) .. + 3, so the sum stays in the lane until the end.
+// exp(s_rn - lse_r).  A wave holds 32 WT key rows in operand layout and runs
+// through the query rows, 64 of them in LDS at a time: S = Q K^T leaves key row l % 32 in
+// lane l with query rows 8 (r / 4) + 4 (l / 32) + r % 4 in register r, so the sum stays in
+// the lane until the end.
 template <int DT, int DC, bool EXACT>
 __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 {
     typedef Elem<DT> E;
+    constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QS = 64, WT = DC == 8 ? 1 : 2;
+    constexpr uint32_t WROWS = 32 * WT;
+    __shared__ __align__(16) uint8_t qs[QS * D * 2];
+    __shared__ __align__(16) float lse2[QS];
     const uint32_t lane = threadIdx.x & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t q16 = lane & 15, g4 = lane >> 4, d = a.c.d;
+    const uint32_t l32 = lane & 31, half = lane >> 5, d = a.c.d;
     const uint32_t h = blockIdx.y % a.c.heads, b = blockIdx.y / a.c.heads;
-    const uint32_t row0 = (blockIdx.x * AT_WAVES + wave) * AT_ROWS;
-    if (row0 >= a.w_cols)
-        return;
+    const uint32_t block0 = blockIdx.x * 4 * WROWS, row0 = block0 + wave * WROWS;
     const Rows rows = rows_of(a, b);
-    float w[2] = {0.f, 0.f};
-    if (row0 < rows.end) {
-        const uint32_t n = row0 + (lane & 31);
+    float w[WT] = {};
+    if (block0 < rows.end) {
+        const uint32_t n = row0 + (lane & (WROWS - 1));
         const Place p = n < rows.end ? place_of(a.c, b, n) : Place{-1, 0u};
-        const uint32_t there = (uint32_t)__ballot(p.page >= 0);
-        const bool tail = row0 + AT_ROWS > rows.len;
+        const uint64_t there = __ballot(p.page >= 0);
+        const bool masked = row0 + WROWS > rows.len || there != ~(uint64_t)0;
         const int64_t off =
             p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
-        i32x4 K[2][DC];
+        i32x4 K[WT][2 * DC];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint16_t *r = a.c.k + (int64_t)h * a.c.k_head + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
+        for (int t = 0; t < (int)WT; ++t) {
+            const uint16_t *r =
+                a.c.k + (int64_t)h * a.c.k_head + shfl64(off, (int)l32 + 32 * t) + 8 * half;
 #pragma unroll
-            for (int c = 0; c < DC; ++c)
-                K[t][c] = load8(r + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4));
+            for (int k = 0; k < 2 * DC; ++k)
+                K[t][k] = load8(r + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half));
         }
         const uint32_t q_rows = rows.count * a.group;
-        for (uint32_t r0 = 0; r0 < q_rows; r0 += AT_Q) {
-            const uint32_t r = r0 + q16 < q_rows ? r0 + q16 : q_rows - 1;
-            const uint16_t *p16 = a.q + (int64_t)b * a.q_seq + (int64_t)(r / a.group) * a.q_tok +
-                                  (int64_t)(h * a.group + r % a.group) * a.q_head + 8 * g4;
-            i32x4 Q[DC];
-#pragma unroll
-            for (int c = 0; c < DC; ++c)
-                Q[c] = load8(p16 + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4));
-            f32x4 s[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < DC; ++c)
-                    s[t] = E::mma(Q[c], K[t][c], s[t]);
+        for (uint32_t r0 = 0; r0 < q_rows; r0 += QS) {
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < QS * CPR; i += 256) {
+                const uint32_t r = i / CPR, c = i % CPR;
+                i32x4 v = {0, 0, 0, 0};
+                if (r0 + r < q_rows)
+                    v = load8(a.q + (int64_t)b * a.q_seq + (int64_t)((r0 + r) / a.group) * a.q_tok +
+                                  (int64_t)(h * a.group + (r0 + r) % a.group) * a.q_head + 8 * c,
+                              EXACT ? 8 : (int)d - (int)(8 * c));
+                *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) = v;
             }
+            if (threadIdx.x < QS) {
+                // a row that sees nothing, and one past the end, weighs nothing
+                const uint32_t r = r0 + threadIdx.x;
+                float x = INFINITY;
+                if (r < q_rows) {
+                    x = a.lse[((uint64_t)b * a.t + r / a.group) * a.q_heads + h * a.group +
+                              r % a.group] * 1.4426950408889634f;
+                    x = x == -INFINITY ? INFINITY : x;
+                }
+                lse2[threadIdx.x] = x;
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (uint32_t q0 = 0; q0 < QS; q0 += 32) {
+                if (r0 + q0 >= q_rows)
+                    break;
+                f32x16 s[WT];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t x = r0 + 4 * g4 + e;
-                if (x >= q_rows)
-                    continue;
-                const uint32_t u = x / a.group;
-                const float lse2 = a.lse[((uint64_t)b * a.t + u) * a.q_heads + h * a.group +
-                                         x % a.group] * 1.4426950408889634f;
+                for (int t = 0; t < (int)WT; ++t)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    bool ok = true;
-                    if (tail || there != 0xffffffffu) {
-                        const uint32_t i = 16 * t + q16;
-                        ok = ((there >> i) & 1) && sees(a, b, rows, u, row0 + i);
-                    }
-                    if (ok)
-                        w[t] += exp2_(s[t][e] * a.scale2 - lse2);
+                    for (int e = 0; e < 16; ++e)
+                        s[t][e] = 0.f;
+#pragma unroll
+                for (uint32_t k = 0; k < 2 * DC; ++k) {
+                    const uint32_t r = q0 + l32;
+                    const i32x4 qf = *(const i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, 2 * k + half));
+#pragma unroll
+                    for (int t = 0; t < (int)WT; ++t)
+                        s[t] = E::mma(qf, K[t][k], s[t]);
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const f32x4 z = *(const f32x4 *)(lse2 + q0 + 8 * x + 4 * half);
+#pragma unroll
+                    for (int t = 0; t < (int)WT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float y = exp2_(s[t][4 * x + e] * a.scale2 - z[e]);
+                            if (masked) {
+                                const uint32_t i = 32 * t + l32;
+                                const uint32_t q = r0 + q0 + 8 * x + 4 * half + e;
+                                if (q >= q_rows || !((there >> i) & 1) ||
+                                    !sees(a, b, rows, q / a.group, row0 + i))
+                                    y = 0.f;
+                            }
+                            w[t] += y;
+                        }
                 }
             }
         }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        w[t] += __shfl_xor(w[t], 16);
+    for (int t = 0; t < (int)WT; ++t) {
         w[t] += __shfl_xor(w[t], 32);
-        const uint64_t n = (uint64_t)row0 + 16 * t + q16;
-        if (g4 == 0 && n < a.w_cols) {
+        const uint64_t n = (uint64_t)row0 + 32 * t + l32;
+        if (half == 0 && n < a.w_cols) {
             const uint64_t at = ((uint64_t)b * a.c.heads + h) * a.w_cols + n;
             a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + w[t];
         }
@@ -592,10 +1002,15 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     hipError_t e;
     if (rows) {
         const dim3 grid(a.slots * a.c.heads * a.tiles);
+        const dim3 grid8((grid.x + 7) / 8 * 8);
         if (qt == 16)
             attend_split<DT, DC, 1, EXACT><<<grid, 256, 0, s>>>(a);
-        else
+        else if (qt == 32)
             attend_split<DT, DC, 2, EXACT><<<grid, 256, 0, s>>>(a);
+        else if (DC != 8 && qt == 64)
+            attend_tiles<DT, DC, DC != 8 ? 2 : 4, EXACT><<<grid8, 256, 0, s>>>(a);
+        else
+            attend_tiles<DT, DC, 4, EXACT><<<grid8, 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
         attend_join<DT><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, s>>>(a, qt, 32 * DC);
@@ -604,8 +1019,8 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     }
     if (!a.w_out || !a.w_cols)
         return hipSuccess;
-    const dim3 wg((uint32_t)((a.w_cols + AT_WAVES * AT_ROWS - 1) / (AT_WAVES * AT_ROWS)),
-                  a.c.batch * a.c.heads);
+    const uint32_t w_rows = DC == 8 ? 128 : 256;
+    const dim3 wg((uint32_t)((a.w_cols + w_rows - 1) / w_rows), a.c.batch * a.c.heads);
     attend_weights<DT, DC, EXACT><<<wg, 256, 0, s>>>(a);
     return hipGetLastError();
 }

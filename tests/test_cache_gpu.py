@@ -170,6 +170,11 @@ SHAPES = [
     (70, 1, 1, 2, 64, 16, [(7 * b) % 90 for b in range(70)]),
     (1, 1, 1, 4, 128, 256, [5000]),
     (3, 130, 1, 2, 96, 32, [0, 64, 31]),
+    (2, 12, 1, 4, 64, 16, [300, 20]),
+    (1, 50, 2, 1, 40, 8, [77]),
+    (2, 45, 1, 2, 256, 16, [130, 7]),
+    (1, 9, 1, 4, 144, 24, [600]),
+    (2, 25, 1, 2, 128, 64, [1, 2100]),
 ]
 
 
@@ -241,7 +246,7 @@ def test_attend_pages_that_do_not_exist(hole):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
-@pytest.mark.parametrize("group", [1, 12])
+@pytest.mark.parametrize("group", [1, 4, 8, 12])
 def test_attend_hidden_rows_may_hold_anything(dtype, bad, group):
     """A drafted token whose key and value are not finite reaches only the tokens
     that see it."""

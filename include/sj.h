@@ -409,7 +409,8 @@ int sj_cache_append(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, cons
  * and weights in fp32; exp(s_n - running maximum) enters the product with v as
  * 16-bit values.  Results do not depend on timing (no atomics).
  * Errors as the joins'; SJ_E_INVAL also when heads does not divide q_heads or for a NaN
- * scale; SJ_E_UNSUPPORTED for d > 256, width * page or t * q_heads / heads >= 2^31. */
+ * scale; SJ_E_UNSUPPORTED for d > 256, width * page > 2^30, batch * heads > 65535 or
+ * batch * t * q_heads >= 2^31. */
 int sj_attend(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, const int32_t *count,
               uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
               const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,

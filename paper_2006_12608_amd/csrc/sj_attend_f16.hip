@@ -12,6 +12,11 @@ uint32_t attend_tile_rows(uint32_t rows, uint32_t d)
     return 128;
 }
 
+int attend_occupancy_f16(uint32_t d, uint32_t tile_rows)
+{
+    return attend_occupancy<sjk::DT_F16>(d, tile_rows);
+}
+
 hipError_t launch_attend_f16(const Attend &a, hipStream_t s)
 {
     return launch_attend<sjk::DT_F16>(a, s);

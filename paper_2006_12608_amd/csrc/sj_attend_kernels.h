@@ -14,6 +14,7 @@ namespace sjc {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int64_t i64x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -89,6 +90,11 @@ __device__ __forceinline__ i32x4 column8(const uint8_t *lo, const uint8_t *hi)
     return __builtin_bit_cast(i32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Waits for the loads so far.  Before a loop: registers loaded ahead of it would
+// otherwise be waited for at their first use in every round, and with them the
+// round's own loads.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 // 2^x, 2^-inf = 0.
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -97,6 +103,18 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane)
     const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)v, lane);
     const uint32_t hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), lane);
     return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+// Eight elements of a query, negated for a negative scale: the scores' order is then
+// that of the products, and the maximum can be taken before the scale.
+__device__ __forceinline__ i32x4 load_q8(const Attend &a, const uint16_t *p, int left)
+{
+    i32x4 v = load8(p, left);
+    const int flip = a.negate ? (int)0x80008000 : 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] ^= flip;
+    return v;
 }
 
 // Rows of sequence b: those before the call's tokens, the tokens there are, and the
@@ -179,43 +197,80 @@ struct Share {
     Rows rows;
 };
 
-// Finds share number `slot` of the batch.  All sequences' blocks together are cut
-// into about target / (heads * tiles) shares of equal size, each sequence into
-// whole shares of its own and at least one; every workgroup computes the cut
-// from the lengths on the device, so the grid does not depend on them.  Returns
-// false when there are fewer shares.  Called by whole waves.
+// Sum over the lanes up to this one.
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);   // row_shr 1
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // row 15 on
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);  // row 31 on
+    return x;
+}
+
+__device__ __forceinline__ uint32_t sum_all(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_readlane((int)sum_upto(x), 63);
+}
+
+// Finds share number `slot` of the batch.  Each sequence's blocks are cut into whole shares
+// of at most `size` blocks, one at least.  `size` is the smallest with which the
+// shares of all sequences come to no more than `want`, a.target / (heads * tiles):
+// the workgroups that the GPU holds at once, since one more would run after all
+// others.  (For more than 64 sequences, where the search takes several passes, a
+// size that is large enough; with want sequences or more there is one share each.)
+// Every workgroup computes the cut from the lengths on the device, so the grid
+// does not depend on them.  Returns false when there are fewer shares.  Called
+// by whole waves.
 __device__ __forceinline__ bool find_share(const Attend &a, uint32_t slot, Share *out)
 {
     const uint32_t lane = threadIdx.x & 63, B = a.c.batch;
-    unsigned long long total = 0;
-    for (uint32_t b0 = 0; b0 < B; b0 += 64)
-        if (b0 + lane < B)
-            total += (rows_of(a, b0 + lane).end + AT_ROWS - 1) / AT_ROWS;
-    for (int o = 1; o < 64; o <<= 1)
-        total += __shfl_xor(total, o);
-    const uint32_t want = a.target / (a.c.heads * a.tiles) > 0 ? a.target / (a.c.heads * a.tiles) : 1;
-    unsigned long long size = (total + want - 1) / want;
-    size = size < AT_WAVES ? AT_WAVES : size;   // (a block per wave at least)
+    const uint32_t want = a.want;
+    auto blocks_of = [&](uint32_t b) -> uint32_t {
+        return b < B ? (rows_of(a, b).end + AT_ROWS - 1) / AT_ROWS : 0;
+    };
+    uint32_t blocks = 0, size;
+    if (B <= 64) {
+        blocks = blocks_of(lane);
+        const uint32_t total = sum_all(blocks);     // (64 x 2^26 blocks at most)
+        size = total / want + (total % want != 0);
+        size = size < AT_WAVES ? AT_WAVES : size;   // (a block per wave at least)
+        uint32_t most = B < want ? total / (want - B) + 1 : total + 1;
+        if (B > 1)
+            while (size < most) {
+                const uint32_t mid = size + (most - size) / 2;
+                const uint32_t n = lane < B ? (blocks + mid - 1) / mid : 0;
+                if (sum_all(lane < B && n == 0 ? 1 : n) <= want)
+                    most = mid;
+                else
+                    size = mid + 1;
+            }
+    } else {
+        unsigned long long total = 0;
+        for (uint32_t b0 = 0; b0 < B; b0 += 64)
+            total += blocks_of(b0 + lane);
+        for (int o = 1; o < 64; o <<= 1)
+            total += __shfl_xor(total, o);
+        total = B < want ? total / (want - B) + 1 : total;
+        size = total < AT_WAVES ? AT_WAVES : (total < 1u << 30 ? (uint32_t)total : 1u << 30);
+    }
     uint32_t base = 0;
     for (uint32_t b0 = 0; b0 < B; b0 += 64) {
-        uint32_t blocks = 0, shares = 0;
-        if (b0 + lane < B) {
-            blocks = (rows_of(a, b0 + lane).end + AT_ROWS - 1) / AT_ROWS;
-            shares = (uint32_t)((blocks + size - 1) / size);
-            shares = shares ? shares : 1;
-        }
-        uint32_t incl = shares;
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t y = __shfl_up(incl, o);
-            incl += (int)lane >= o ? y : 0;
-        }
-        const uint32_t sum = __shfl(incl, 63);
+        if (B > 64)
+            blocks = blocks_of(b0 + lane);
+        uint32_t shares = (blocks + size - 1) / size;
+        shares = b0 + lane >= B ? 0 : (shares ? shares : 1);
+        const uint32_t incl = sum_upto(shares);
+        const uint32_t sum = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
         if (slot < base + sum) {
-            const int who = __ffsll((unsigned long long)__ballot(slot < base + incl)) - 1;
-            const uint32_t mine = __shfl(shares, who), nb = __shfl(blocks, who);
+            const int who = __builtin_amdgcn_readfirstlane(
+                __ffsll((unsigned long long)__ballot(slot < base + incl)) - 1);
+            const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)shares, who);
+            const uint32_t nb = (uint32_t)__builtin_amdgcn_readlane((int)blocks, who);
             out->b = b0 + who;
             out->shares = mine;
-            out->share = slot - (base + __shfl(incl, who) - mine);
+            out->share = slot - (base + (uint32_t)__builtin_amdgcn_readlane((int)incl, who) - mine);
             out->first = (uint32_t)((unsigned long long)nb * out->share / mine);
             out->last = (uint32_t)((unsigned long long)nb * (out->share + 1) / mine);
             out->rows = rows_of(a, out->b);
@@ -266,7 +321,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     const uint32_t unit = blockIdx.x % units, slot = blockIdx.x / units;
     const uint32_t h = unit / a.tiles, tile = unit % a.tiles;
     Share sh;
-    if (!find_share(a, slot, &sh))
+    if (slot >= a.slots || !find_share(a, slot, &sh))
         return;
     const uint32_t b = __builtin_amdgcn_readfirstlane(sh.b);
     const uint32_t first = __builtin_amdgcn_readfirstlane(sh.first);
@@ -297,9 +352,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                             (int64_t)(h * a.group + (there ? r % a.group : 0)) * a.q_head + 8 * g4;
 #pragma unroll
         for (int c = 0; c < DC; ++c)
-            Q[j][c] = there ? load8(p + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4))
+            Q[j][c] = there ? load_q8(a, p + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4))
                             : i32x4{0, 0, 0, 0};
     }
+    wait_loads();
 
     f32x4 O[NQ][NV];
     float m[NQ], l[NQ];
@@ -393,28 +449,29 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 #pragma unroll
         for (int j = 0; j < NQ; ++j) {
             seen[j] = there & (tail ? (uint32_t)seen64(a, b, rows, tok[j], blk * AT_ROWS) : ~0u);
+            if (tail || there != 0xffffffffu) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    s[j][e >> 2][e & 3] = (seen[j] >> (16 * (e >> 2) + 4 * g4 + (e & 3))) & 1
+                                              ? s[j][e >> 2][e & 3]
+                                              : -INFINITY;
+                asm volatile("");       // (a branch, not selects in every round)
+            }
             float top = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x = s[j][t][r] * a.scale2;
-                    if (tail || there != 0xffffffffu)
-                        x = (seen[j] >> (16 * t + 4 * g4 + r)) & 1 ? x : -INFINITY;
-                    pf[j][4 * t + r] = x;
-                    top = fmaxf(top, x);
-                }
+            for (int e = 0; e < 8; ++e)
+                top = fmaxf(top, s[j][e >> 2][e & 3]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float m_new = fmaxf(m[j], top);
             // nothing seen yet: any finite maximum will do
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;
-            const float shrink = exp2_(m[j] - m_use);
+            const float base = m_new == -INFINITY ? 0.f : m_new * a.scale2;
+            const float shrink = exp2_(m[j] * a.scale2 - base);
             m[j] = m_new;
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                pf[j][e] = exp2_(pf[j][e] - m_use);
+                pf[j][e] = exp2_(__builtin_fmaf(s[j][e >> 2][e & 3], a.scale2, -base));
                 sum += pf[j][e];
             }
             l[j] = l[j] * shrink + sum;     // this lane's rows only; joined at the end
@@ -447,6 +504,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     for (int j = 0; j < NQ; ++j) {
         l[j] += __shfl_xor(l[j], 16);
         l[j] += __shfl_xor(l[j], 32);
+        m[j] *= a.scale2;
         if (g4 == 0) {
             stat[wave][AT_Q * j + q16][0] = m[j];
             stat[wave][AT_Q * j + q16][1] = l[j];
@@ -558,6 +616,7 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     __shared__ __align__(16) uint8_t lds[4 * TILE]; // K, V of two tiles
     __shared__ float stat[4][32][2];
     __shared__ uint32_t odd_any;
+    __shared__ i64x2 where[2][BN];
 
     const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -595,9 +654,10 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
                             8 * half;
 #pragma unroll
         for (int k = 0; k < 2 * DC; ++k)
-            Q[k] = live ? load8(p + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half))
+            Q[k] = live ? load_q8(a, p + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half))
                         : i32x4{0, 0, 0, 0};
     }
+    wait_loads();
     f32x16 O[DC];
 #pragma unroll
     for (int i = 0; i < DC; ++i)
@@ -628,17 +688,29 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
         const uint32_t n = from + i * BN + (lane & (BN - 1));
         return i < n_tiles && n < to ? place_of(a.c, b, n) : Place{-1, 0u};
     };
+    // Offsets of a tile's rows, for the threads that load them; absent rows read page
+    // 0, row 0.  Returns which rows exist.
+    auto post = [&](uint32_t i, const Place &p) -> uint64_t {
+        if (wave == 0 && lane < BN) {
+            i64x2 o = {0, 0};
+            if (p.page >= 0)
+                o = i64x2{(int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row,
+                          (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row};
+            where[i & 1][lane] = o;
+        }
+        return __ballot(p.page >= 0);
+    };
     i32x4 kr[NL], vr[NL];
-    auto fetch = [&](const Place &p) {      // absent rows read page 0, row 0
-        const int64_t ko =
-            p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
-        const int64_t vo =
-            p.page < 0 ? 0 : (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row;
+    auto fetch = [&](uint32_t i) {
         const int left = EXACT ? 8 : (int)d - (int)(8 * chunk);
+        i64x2 o[NL];
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            kr[i] = load8(kb + shfl64(ko, RPL * i + row_at) + 8 * chunk, left);
-            vr[i] = load8(vb + shfl64(vo, RPL * i + row_at) + 8 * chunk, left);
+        for (int x = 0; x < NL; ++x)
+            o[x] = where[i & 1][RPL * x + row_at];
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+            kr[x] = load8(kb + o[x][0] + 8 * chunk, left);
+            vr[x] = load8(vb + o[x][1] + 8 * chunk, left);
         }
     };
     auto stash = [&](uint32_t i, uint64_t there) {
@@ -662,27 +734,25 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     if (tid == 0)
         odd_any = 0;
     __syncthreads();
-    Place nxt = place(0);
-    uint64_t there = __ballot(nxt.page >= 0), there_nxt = 0;
+    // ahead of tile i: tile i + 1 on its way to LDS, the offsets of i + 2, the place of i + 3
+    uint64_t there = post(0, place(0)), there1 = post(1, place(1)), there2 = 0;
+    __syncthreads();
     if (n_tiles > 0) {
-        fetch(nxt);
-        nxt = place(1);
+        fetch(0);
         stash(0, there);
-        there_nxt = __ballot(nxt.page >= 0);
-        if (n_tiles > 1)
-            fetch(nxt);
-        nxt = place(2);
+        fetch(1);
     }
     __syncthreads();
+    there2 = post(2, place(2));
+    Place nxt = place(3);
+    __syncthreads();
     for (uint32_t i = 0; i < n_tiles; ++i) {
-        uint64_t there_aft = 0;
-        if (i + 1 < n_tiles) {
-            stash(i + 1, there_nxt);
-            there_aft = __ballot(nxt.page >= 0);
-            if (i + 2 < n_tiles)
-                fetch(nxt);
-            nxt = place(i + 3);
-        }
+        if (i + 1 < n_tiles)
+            stash(i + 1, there1);
+        if (i + 2 < n_tiles)
+            fetch(i + 2);
+        const uint64_t there3 = post(i + 3, nxt);
+        nxt = place(i + 4);
         uint8_t *const kt = lds + (i & 1) * 2 * TILE;
         const uint32_t row0 = from + i * BN;
         const bool tail = row0 + BN > rows.len;
@@ -698,29 +768,51 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
 
         f32x16 s[SR];
 #pragma unroll
-        for (int x = 0; x < SR; ++x) {
+        for (int x = 0; x < SR; ++x)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 s[x][e] = 0.f;
+        // four K fragments are read while four are multiplied
+        constexpr int KS = 2 * DC * SR / 4;
+        i32x4 f[2][4];
+        auto read_k = [&](int y) {
 #pragma unroll
-            for (uint32_t k = 0; k < 2 * DC; ++k)
-                s[x] = E::mma(*(const i32x4 *)(kt + k_at[k] + 32 * x * 2 * D), Q[k], s[x]);
+            for (int z = 0; z < 4; ++z) {
+                const int n = 4 * y + z;
+                f[y & 1][z] = *(const i32x4 *)(kt + k_at[n / SR] + 32 * (n % SR) * 2 * D);
+            }
+        };
+        read_k(0);
+#pragma unroll
+        for (int y = 0; y < KS; ++y) {
+            if (y + 1 < KS)
+                read_k(y + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const int n = 4 * y + z;
+                s[n % SR] = E::mma(f[y & 1][z], Q[n / SR], s[n % SR]);
+            }
+        }
+        if (masked) {
+#pragma unroll
+            for (int x = 0; x < SR; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[x][e] = seen[x] & (1u << (8 * (e >> 2) + (e & 3))) ? s[x][e] : -INFINITY;
+            asm volatile("");           // (a branch, not selects in every round)
         }
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < SR; ++x)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float y = s[x][e] * a.scale2;
-                if (masked)
-                    y = seen[x] & (1u << (8 * (e >> 2) + (e & 3))) ? y : -INFINITY;
-                s[x][e] = y;
-                top = fmaxf(top, y);
-            }
+            for (int e = 0; e < 16; ++e)
+                top = fmaxf(top, s[x][e]);
         top = fmaxf(top, __shfl_xor(top, 32));
         if (__any(top > m)) {
             const float m_new = fmaxf(m, top);
-            const float shrink = exp2_(m - (m_new == -INFINITY ? 0.f : m_new));
+            const float shrink =
+                exp2_(m * a.scale2 - (m_new == -INFINITY ? 0.f : m_new * a.scale2));
             m = m_new;
             l *= shrink;
 #pragma unroll
@@ -729,13 +821,13 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
                 for (int e = 0; e < 16; ++e)
                     O[y][e] *= shrink;
         }
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = m == -INFINITY ? 0.f : m * a.scale2;
         i32x4 P[SR][2];
 #pragma unroll
         for (int x = 0; x < SR; ++x) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[x][e] = exp2_(s[x][e] - base);
+                s[x][e] = exp2_(__builtin_fmaf(s[x][e], a.scale2, -base));
                 l += s[x][e];
             }
 #pragma unroll
@@ -747,21 +839,36 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
                 P[x][y] = __builtin_bit_cast(i32x4, p8);
             }
         }
+        // as above with V: the fragments of 128 columns (16 rows) at a time
+        constexpr int VS = 2 * SR * DC / 4 > 0 ? 2 * SR * DC / 4 : 1, VG = 2 * SR * DC / VS;
+        auto read_v = [&](int y) {
 #pragma unroll
-        for (int x = 0; x < SR; ++x)
+            for (int z = 0; z < VG; ++z) {
+                const int n = VG * y + z;
+                const uint8_t *at = kt + 16 * (n / DC) * 2 * D;
+                f[y & 1][z] = column8(at + v_at[n % DC][0], at + v_at[n % DC][1]);
+            }
+        };
+        read_v(0);
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < VS; ++y) {
+            if (y + 1 < VS)
+                read_v(y + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int z = 0; z < DC; ++z) {
-                    const uint8_t *at = kt + (32 * x + 16 * y) * 2 * D;
-                    O[z] = E::mma(column8(at + v_at[z][0], at + v_at[z][1]), P[x][y], O[z]);
-                }
-        there = there_nxt;
-        there_nxt = there_aft;
+            for (int z = 0; z < VG; ++z) {
+                const int n = VG * y + z;
+                O[n % DC] = E::mma(f[y & 1][z], P[n / DC / 2][n / DC % 2], O[n % DC]);
+            }
+        }
+        there = there1;
+        there1 = there2;
+        there2 = there3;
         __syncthreads();
     }
 
     // join the halves of a query, then (QW = 2) the two waves of its rows
+    m *= a.scale2;
     l += __shfl_xor(l, 32);
     if constexpr (RW == 2) {
         if (half == 0) {
@@ -927,9 +1034,10 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                 const uint32_t r = i / CPR, c = i % CPR;
                 i32x4 v = {0, 0, 0, 0};
                 if (r0 + r < q_rows)
-                    v = load8(a.q + (int64_t)b * a.q_seq + (int64_t)((r0 + r) / a.group) * a.q_tok +
-                                  (int64_t)(h * a.group + (r0 + r) % a.group) * a.q_head + 8 * c,
-                              EXACT ? 8 : (int)d - (int)(8 * c));
+                    v = load_q8(a,
+                                a.q + (int64_t)b * a.q_seq + (int64_t)((r0 + r) / a.group) * a.q_tok +
+                                    (int64_t)(h * a.group + (r0 + r) % a.group) * a.q_head + 8 * c,
+                                EXACT ? 8 : (int)d - (int)(8 * c));
                 *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) = v;
             }
             if (threadIdx.x < QS) {
@@ -994,6 +1102,19 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
     }
 }
 
+// The kernel for tiles of qt query rows.
+template <int DT, int DC, bool EXACT>
+void (*attend_kernel(uint32_t qt))(const Attend)
+{
+    if (qt == 16)
+        return attend_split<DT, DC, 1, EXACT>;
+    if (qt == 32)
+        return attend_split<DT, DC, 2, EXACT>;
+    if (qt == 64 && DC != 8)
+        return attend_tiles<DT, DC, DC != 8 ? 2 : 4, EXACT>;
+    return attend_tiles<DT, DC, 4, EXACT>;
+}
+
 template <int DT, int DC, bool EXACT>
 hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
 {
@@ -1001,16 +1122,9 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     const uint64_t rows = (uint64_t)a.c.batch * a.t * a.q_heads;
     hipError_t e;
     if (rows) {
-        const dim3 grid(a.slots * a.c.heads * a.tiles);
-        const dim3 grid8((grid.x + 7) / 8 * 8);
-        if (qt == 16)
-            attend_split<DT, DC, 1, EXACT><<<grid, 256, 0, s>>>(a);
-        else if (qt == 32)
-            attend_split<DT, DC, 2, EXACT><<<grid, 256, 0, s>>>(a);
-        else if (DC != 8 && qt == 64)
-            attend_tiles<DT, DC, DC != 8 ? 2 : 4, EXACT><<<grid8, 256, 0, s>>>(a);
-        else
-            attend_tiles<DT, DC, 4, EXACT><<<grid8, 256, 0, s>>>(a);
+        // (a multiple of 8 workgroups: the tiled kernel deals them out by XCD)
+        const dim3 grid((a.slots * a.c.heads * a.tiles + 7) / 8 * 8);
+        attend_kernel<DT, DC, EXACT>(qt)<<<grid, 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
         attend_join<DT><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, s>>>(a, qt, 32 * DC);
@@ -1034,6 +1148,24 @@ hipError_t launch_attend(const Attend &a, hipStream_t s)
     if (d <= 128)
         return d == 128 ? launch_attend_dc<DT, 4, true>(a, s) : launch_attend_dc<DT, 4, false>(a, s);
     return d == 256 ? launch_attend_dc<DT, 8, true>(a, s) : launch_attend_dc<DT, 8, false>(a, s);
+}
+
+// Workgroups of the kernel for d and qt that one CU holds at once.
+template <int DT>
+int attend_occupancy(uint32_t d, uint32_t qt)
+{
+    static int known[3][4];
+    int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : 3))];
+    if (n == 0) {
+        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, false>(qt)
+                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, false>(qt)
+                                            : (const void *)attend_kernel<DT, 8, false>(qt));
+        int x = 0;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&x, k, 256, 0) != hipSuccess)
+            (void)hipGetLastError();
+        n = x > 0 ? x : 1;
+    }
+    return n;
 }
 
 }  // namespace sjc

@@ -105,7 +105,8 @@ struct Attend {
     int64_t q_seq, q_tok, q_head;
     const uint64_t *tree;          // may be null (chain)
     int64_t tree_seq, tree_tok;
-    float scale2;                  // scale * log2(e)
+    float scale2;                  // |scale| * log2(e), above 0
+    bool negate;                   // scale < 0
     uint16_t *out;
     float *lse;                    // never null here (scratch where the caller wants none)
     const float *w_in;
@@ -114,7 +115,7 @@ struct Attend {
     // work split: a sequence's rows are cut into shares, one workgroup per share,
     // cache head and tile of query rows
     uint32_t tiles;                // tiles of query rows per cache head
-    uint32_t target;               // workgroups the shares should come to
+    uint32_t want;                 // shares there should be at most
     uint32_t slots;                // most shares there can be
     uint32_t *plan;                // per sequence: first share, shares
     float *part_o;                 // per share, head, tile: query rows x padded d
@@ -124,6 +125,9 @@ struct Attend {
 // The kernels for one call; the query rows of a workgroup's tile (16 or 32) follow
 // from t * group.
 uint32_t attend_tile_rows(uint32_t rows, uint32_t d);
+// Workgroups of the call's kernel that one CU holds at once.
+int attend_occupancy_f16(uint32_t d, uint32_t tile_rows);
+int attend_occupancy_bf16(uint32_t d, uint32_t tile_rows);
 hipError_t launch_attend_f16(const Attend &a, hipStream_t s);
 hipError_t launch_attend_bf16(const Attend &a, hipStream_t s);
 

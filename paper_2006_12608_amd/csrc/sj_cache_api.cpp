@@ -16,6 +16,7 @@ namespace {
 
 const int64_t kMaxStride = (int64_t)1 << 40;   // elements; extents below stay in 64 bits
 const uint64_t kMaxCells = (uint64_t)1 << 31;
+const uint64_t kMaxRows = (uint64_t)1 << 30;   // of a sequence
 
 struct Axis {
     uint64_t n;
@@ -67,7 +68,7 @@ int check_cache(const sj_ctx *c, const sj_cache *s, const char *name, sjc::Cache
     if (s->d > 256)
         return fail(SJ_E_UNSUPPORTED, "%s: d = %u is above 256", name, s->d);
     const uint32_t width = s->pages == 0 ? 0 : (s->table ? s->width : 1);
-    if ((uint64_t)width * s->page >= kMaxCells || s->page >= kMaxCells || s->pages >= kMaxCells)
+    if ((uint64_t)width * s->page > kMaxRows || s->page >= kMaxCells || s->pages >= kMaxCells)
         return fail(SJ_E_UNSUPPORTED, "%s: %u pages of %u rows are too many", name, width, s->page);
     if ((uint64_t)s->batch * s->heads > 65535)
         return fail(SJ_E_UNSUPPORTED, "%s: batch * heads = %llu is above 65535", name,
@@ -290,18 +291,23 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
         a.tree_seq = tree_stride[0];
         a.tree_tok = tree_stride[1];
     }
-    a.scale2 = (float)(scale * 1.4426950408889634074);
+    // (above 0, so that -inf stays -inf: at 1e-30 every finite score is as good as 0)
+    a.scale2 = (float)std::fmax(std::fabs(scale) * 1.4426950408889634074, 1e-30);
+    a.negate = scale < 0;
     a.out = (uint16_t *)out;
     a.w_in = w_in;
     a.w_out = w_out;
     a.w_cols = w_cols;
+    SJ_HIP(hipSetDevice(c->device));
     // work split and scratch: [plan][lse][maxima and sums][sums of values]
     const uint32_t rows = t * a.group, qt = sjc::attend_tile_rows(rows, d);
     const uint32_t dp = d <= 64 ? 64 : (d <= 128 ? 128 : 256);
     a.tiles = rows == 0 ? 1 : (rows + qt - 1) / qt;
-    a.target = (uint32_t)c->num_cus * 2;
-    const uint64_t units = (uint64_t)a.c.heads * a.tiles;
-    a.slots = (uint32_t)(a.target / units > 0 ? a.target / units : 1) + B;
+    const int per_cu = cache->dtype == SJ_F16 ? sjc::attend_occupancy_f16(d, qt)
+                                              : sjc::attend_occupancy_bf16(d, qt);
+    const uint64_t units = (uint64_t)a.c.heads * a.tiles, held = (uint64_t)c->num_cus * per_cu;
+    a.want = held / units > 0 ? (uint32_t)(held / units) : 1;
+    a.slots = a.want > B ? a.want : B;
     const uint64_t parts = a.slots * units;
     if (parts >= kMaxCells)
         return fail(SJ_E_UNSUPPORTED, "%u sequences of %llu query tiles are too many", B,
@@ -316,7 +322,6 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     a.lse = lse ? lse : (float *)(s + off_lse);
     a.part_ml = (float *)(s + off_ml);
     a.part_o = (float *)(s + off_o);
-    SJ_HIP(hipSetDevice(c->device));
     SJ_HIP(cache->dtype == SJ_F16 ? sjc::launch_attend_f16(a, c->stream)
                                   : sjc::launch_attend_bf16(a, c->stream));
     return SJ_OK;

@@ -373,10 +373,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 
     // place of row lane % 32 of a block: absent rows read page 0, row 0 (their
     // scores and values are replaced below)
-    auto place = [&](uint32_t blk) -> Place {
-        const uint32_t n = blk * AT_ROWS + (lane & 31);
-        return blk < last && n < rows.end ? place_of(a.c, b, n) : Place{-1, 0u};
+    auto entry = [&](uint32_t blk) {
+        return entry_of(a.c, a.len, b, blk * AT_ROWS + (lane & 31));
     };
+    auto place = [&](const Entry &e) { return place_of(a.c, b, e, to); };
     i32x4 K[2][DC], V[NV];
     auto load_k = [&](const Place &p) {
         const int64_t off = p.page < 0 ? 0
@@ -404,14 +404,16 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         odd_any = 0;
     __syncthreads();
     uint32_t blk = first + wave;
-    Place cur = place(blk);
+    Place cur = {-1, 0u}, nxt = {-1, 0u};
+    Entry ahead = {0, 0u};
     if (blk < last) {
+        cur = place(entry(blk));
+        ahead = entry(blk + AT_WAVES);
         load_k(cur);
         load_v(cur);
     }
-    Place nxt = place(blk + AT_WAVES);
     for (; blk < last; blk += AT_WAVES) {
-        const Place aft = place(blk + 2 * AT_WAVES);
+        nxt = place(ahead);
         // bit r: row r of the block exists
         const uint32_t there = (uint32_t)__ballot(cur.page >= 0);
         const bool tail = blk * AT_ROWS + AT_ROWS > rows.len;
@@ -426,21 +428,22 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                 for (int c = 0; c < DC; ++c)
                     s[j][t] = E::mma(K[t][c], Q[j][c], s[j][t]);
             }
-        if (blk + AT_WAVES < last)
-            load_k(nxt);
+        ahead = entry(blk + 2 * AT_WAVES);
+        load_k(nxt);        // (past the end: page 0, row 0; a branch would cost full waits)
 
         // V to LDS; rows that do not exist as zeros (0 x NaN would reach every query)
         uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (there != 0xffffffffu && !((there >> (VR * i + v_row)) & 1))
-                V[i] = i32x4{0, 0, 0, 0};
-            if (tail)
+            if (tail || there != 0xffffffffu) {
+                if (!((there >> (VR * i + v_row)) & 1))
+                    V[i] = i32x4{0, 0, 0, 0};
                 odd |= drop_odd8<DT>(V[i]);
+                asm volatile("");       // (a branch, not selects in every round)
+            }
             *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = V[i];
         }
-        if (blk + AT_WAVES < last)
-            load_v(nxt);
+        load_v(nxt);
 
         // scores to exponentials
         i32x4 P[NQ];
@@ -456,6 +459,12 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                                               ? s[j][e >> 2][e & 3]
                                               : -INFINITY;
                 asm volatile("");       // (a branch, not selects in every round)
+            }
+            if (NQ == 1 && a.scores && q16 < q_rows && blk * AT_ROWS < a.s_cols) {
+                float *to_s = a.scores + ((uint64_t)(b * a.c.heads + h) * q_rows + q16) * a.s_cols +
+                              blk * AT_ROWS + 4 * g4;
+                *(f32x4 *)to_s = s[j][0] * a.scale2;
+                *(f32x4 *)(to_s + 16) = s[j][1] * a.scale2;
             }
             float top = -INFINITY;
 #pragma unroll
@@ -496,7 +505,6 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                 O[j][i] = E::mma(vt, P[j], O[j][i]);
         }
         cur = nxt;
-        nxt = aft;
     }
 
     // join the lanes of a query, then the waves
@@ -684,10 +692,10 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
         }
     const uint32_t n_tiles = from < to ? (to - from + BN - 1) / BN : 0;
     const uint32_t row_at = tid / CPR, chunk = tid % CPR;
-    auto place = [&](uint32_t i) -> Place {
-        const uint32_t n = from + i * BN + (lane & (BN - 1));
-        return i < n_tiles && n < to ? place_of(a.c, b, n) : Place{-1, 0u};
+    auto entry = [&](uint32_t i) {
+        return entry_of(a.c, a.len, b, from + i * BN + (lane & (BN - 1)));
     };
+    auto place = [&](const Entry &e) { return place_of(a.c, b, e, to); };
     // Offsets of a tile's rows, for the threads that load them; absent rows read page
     // 0, row 0.  Returns which rows exist.
     auto post = [&](uint32_t i, const Place &p) -> uint64_t {
@@ -717,13 +725,16 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
         uint8_t *kt = lds + (i & 1) * 2 * TILE, *vt = kt + TILE;
         uint32_t odd = 0;
         const bool tail = from + i * BN + BN > rows.len;
+        const uint64_t full = ~(uint64_t)0;
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
             const uint32_t r = RPL * x + row_at, at = r * (2 * D) + 16 * swz<DC>(r, chunk);
-            if (!((there >> r) & 1))
-                vr[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
-            if (tail)
+            if (tail || there != full) {
+                if (!((there >> r) & 1))
+                    vr[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
                 odd |= drop_odd8<DT>(vr[x]);
+                asm volatile("");   // (a branch, not selects in every round)
+            }
             *(i32x4 *)(kt + at) = kr[x];
             *(i32x4 *)(vt + at) = vr[x];
         }
@@ -735,24 +746,25 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
         odd_any = 0;
     __syncthreads();
     // ahead of tile i: tile i + 1 on its way to LDS, the offsets of i + 2, the place of i + 3
-    uint64_t there = post(0, place(0)), there1 = post(1, place(1)), there2 = 0;
-    __syncthreads();
+    uint64_t there = 0, there1 = 0, there2 = 0;
+    Entry ahead = {0, 0u};
     if (n_tiles > 0) {
+        there = post(0, place(entry(0)));
+        there1 = post(1, place(entry(1)));
+        __syncthreads();
         fetch(0);
         stash(0, there);
         fetch(1);
+        __syncthreads();
+        there2 = post(2, place(entry(2)));
+        ahead = entry(3);
+        __syncthreads();
     }
-    __syncthreads();
-    there2 = post(2, place(2));
-    Place nxt = place(3);
-    __syncthreads();
     for (uint32_t i = 0; i < n_tiles; ++i) {
-        if (i + 1 < n_tiles)
-            stash(i + 1, there1);
-        if (i + 2 < n_tiles)
-            fetch(i + 2);
-        const uint64_t there3 = post(i + 3, nxt);
-        nxt = place(i + 4);
+        stash(i + 1, there1);
+        const uint64_t there3 = post(i + 3, place(ahead));
+        fetch(i + 2);       // (past the end: page 0, row 0; a branch would cost full waits)
+        ahead = entry(i + 4);
         uint8_t *const kt = lds + (i & 1) * 2 * TILE;
         const uint32_t row0 = from + i * BN;
         const bool tail = row0 + BN > rows.len;
@@ -943,52 +955,149 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     }
 }
 
-// Joins the shares of every query row that has more than one: a wave a row,
-// lanes over the row's elements.
+__device__ __forceinline__ float max_all(float x)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1)
+        x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+
+// Place of query row r of head h among the results of share s.
+__device__ __forceinline__ uint64_t part_of(const Attend &a, uint32_t s, uint32_t h, uint32_t r,
+                                            uint32_t QT)
+{
+    return ((uint64_t)s * a.c.heads * a.tiles + h * a.tiles + r / QT) * QT + r % QT;
+}
+
+// Joins the shares of query row `row` of the batch, if it has more than one: a workgroup
+// a row.  Groups of D / 4 threads take every 1024 / D-th share, four elements a thread;
+// the groups' sums join through LDS.
 template <int DT>
-__global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, uint32_t D)
+__device__ __forceinline__ void join_row(const Attend &a, uint32_t QT, uint32_t D, uint64_t row)
 {
     typedef Elem<DT> E;
+    __shared__ f32x4 sums[256];
     const uint32_t lane = threadIdx.x & 63;
-    const uint64_t row = (uint64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint64_t n_rows = (uint64_t)a.c.batch * a.t * a.q_heads;
-    if (row >= n_rows)
-        return;
     const uint32_t head = (uint32_t)(row % a.q_heads);
     const uint32_t u = (uint32_t)(row / a.q_heads % a.t), b = (uint32_t)(row / a.q_heads / a.t);
     const uint32_t slot = a.plan[2 * b], shares = a.plan[2 * b + 1];
     if (shares <= 1)
         return;
     const uint32_t h = head / a.group, r = u * a.group + head % a.group;
-    const uint32_t units = a.c.heads * a.tiles, unit = h * a.tiles + r / QT;
-    auto at = [&](uint32_t s) { return ((uint64_t)(slot + s) * units + unit) * QT + r % QT; };
     float top = -INFINITY;
     for (uint32_t s = lane; s < shares; s += 64)
-        top = fmaxf(top, a.part_ml[2 * at(s)]);
-    for (int o = 1; o < 64; o <<= 1)
-        top = fmaxf(top, __shfl_xor(top, o));
+        top = fmaxf(top, a.part_ml[2 * part_of(a, slot + s, h, r, QT)]);
+    top = max_all(top);
     const bool live = u < rows_of(a, b).count && top != -INFINITY;
     const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    for (uint32_t s = lane; s < shares; s += 64)
-        sum += a.part_ml[2 * at(s) + 1] * exp2_(a.part_ml[2 * at(s)] - base);
-    for (int o = 1; o < 64; o <<= 1)
-        sum += __shfl_xor(sum, o);
-    const float inv = live ? 1.f / sum : 0.f;
-    for (uint32_t c = 2 * lane; c < D; c += 128) {
-        f32x2 o = {0.f, 0.f};
-        for (uint32_t s = 0; s < shares; ++s) {
-            const float f = exp2_(a.part_ml[2 * at(s)] - base);
-            const f32x2 x = *(const f32x2 *)(a.part_o + at(s) * D + c);
-            o += x * f;
-        }
-        for (uint32_t e = 0; e < 2; ++e)
-            if (c + e < a.c.d)
-                a.out[row * a.c.d + c + e] =
-                    __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[e] * inv : 0.f));
+    const uint32_t per = D / 4, c = 4 * (threadIdx.x % per), groups = 256 / per;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (uint32_t s = threadIdx.x / per; s < shares; s += groups) {
+        const uint64_t p = part_of(a, slot + s, h, r, QT);
+        const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * p);
+        const float f = exp2_(ml[0] - base);
+        o += *(const f32x4 *)(a.part_o + p * D + c) * f;
+        l += ml[1] * f;
     }
-    if (lane == 0)
-        a.lse[row] = live ? (top + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f : -INFINITY;
+    __shared__ float ls[16];
+    if (threadIdx.x % per == 0)
+        ls[threadIdx.x / per] = l;
+    sums[threadIdx.x] = o;
+    __syncthreads();
+    if (threadIdx.x >= per)
+        return;
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t g = 0; g < groups; ++g) {
+        o += sums[g * per + threadIdx.x];
+        l += ls[g];
+    }
+    const float inv = live ? 1.f / l : 0.f;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e)
+        if (c + e < a.c.d)
+            a.out[row * a.c.d + c + e] =
+                __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[e] * inv : 0.f));
+    if (threadIdx.x == 0)
+        a.lse[row] = live ? (top + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+// Weights of 1024 columns from the scores that the split kernel left (16 query rows at
+// most): w_out = w_in + sum over the rows of 2^(score - lse).  The rows' lse comes from
+// the shares, as in join_row, which may not have run yet.
+__device__ __forceinline__ void weigh_scores(const Attend &a, uint32_t QT, uint32_t part)
+{
+    __shared__ float lse2[AT_Q];
+    const uint32_t strips = (uint32_t)((a.w_cols + 1023) / 1024);
+    const uint32_t bh = part / strips, n0 = part % strips * 1024 + 4 * threadIdx.x;
+    const uint32_t h = bh % a.c.heads, b = bh / a.c.heads, q_rows = a.t * a.group;
+    const Rows rows = rows_of(a, b);
+    const uint32_t slot = a.plan[2 * b], shares = a.plan[2 * b + 1];
+    const bool any = part % strips * 1024 < rows.end;
+    if (any) {
+        // 16 threads a row
+        const uint32_t r = threadIdx.x >> 4, x = threadIdx.x & 15;
+        float y = INFINITY;     // weighs nothing
+        if (r < q_rows && r / a.group < rows.count) {
+            if (shares > 1) {
+                float top = -INFINITY, l = 0.f;
+                for (uint32_t s = x; s < shares; s += 16)
+                    top = fmaxf(top, a.part_ml[2 * part_of(a, slot + s, h, r, QT)]);
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1)
+                    top = fmaxf(top, __shfl_xor(top, o));
+                for (uint32_t s = x; s < shares; s += 16) {
+                    const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * part_of(a, slot + s, h, r, QT));
+                    l += ml[1] * exp2_(ml[0] - (top == -INFINITY ? 0.f : top));
+                }
+#pragma unroll
+                for (int o = 1; o < 16; o <<= 1)
+                    l += __shfl_xor(l, o);
+                y = top == -INFINITY ? INFINITY : top + __builtin_amdgcn_logf(l);
+            } else {
+                y = a.lse[((uint64_t)b * a.t + r / a.group) * a.q_heads + h * a.group + r % a.group] *
+                    1.4426950408889634f;
+                y = y == -INFINITY ? INFINITY : y;
+            }
+        }
+        if (x == 0)
+            lse2[r] = y;
+    }
+    __syncthreads();
+    if (n0 >= a.w_cols)
+        return;
+    f32x4 w = {0.f, 0.f, 0.f, 0.f};
+    if (n0 < rows.end) {
+        const float *s = a.scores + (uint64_t)bh * q_rows * a.s_cols + n0;
+#pragma unroll 4
+        for (uint32_t r = 0; r < q_rows; ++r) {
+            const float y = lse2[r];
+            const f32x4 x = *(const f32x4 *)(s + (uint64_t)r * a.s_cols);
+            if (y != INFINITY)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    w[e] += exp2_(x[e] - y);
+        }
+    }
+    const uint64_t at = (uint64_t)bh * a.w_cols + n0;
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e)
+        if (n0 + e < a.w_cols)
+            a.w_out[at + e] = (a.w_in ? a.w_in[at + e] : 0.f) + (n0 + e < rows.end ? w[e] : 0.f);
+}
+
+// What is left once the shares are there: workgroups below n_rows join a query row each,
+// those from n_rows on weigh columns from the scores.
+template <int DT>
+__global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, uint32_t D,
+                                                   uint32_t n_rows)
+{
+    if (blockIdx.x < n_rows)
+        join_row<DT>(a, QT, D, blockIdx.x);
+    else
+        weigh_scores(a, QT, blockIdx.x - n_rows);
 }
 
 // Weights: w_out[b, h, n] = w_in[b, h, n] + sum over the query rows r that read head h of
@@ -1027,6 +1136,11 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
             for (int k = 0; k < 2 * DC; ++k)
                 K[t][k] = load8(r + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half));
         }
+        uint32_t q_at[2 * DC];      // chunk 2 k + half of query row l32 (the same for every 32)
+#pragma unroll
+        for (uint32_t k = 0; k < 2 * DC; ++k)
+            q_at[k] = l32 * (2 * D) + 16 * swz<DC>(l32, 2 * k + half);
+        wait_loads();
         const uint32_t q_rows = rows.count * a.group;
         for (uint32_t r0 = 0; r0 < q_rows; r0 += QS) {
             __syncthreads();
@@ -1062,13 +1176,33 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         s[t][e] = 0.f;
+                i32x4 qf[2 * DC];
 #pragma unroll
-                for (uint32_t k = 0; k < 2 * DC; ++k) {
-                    const uint32_t r = q0 + l32;
-                    const i32x4 qf = *(const i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, 2 * k + half));
+                for (uint32_t k = 0; k < 2 * DC; ++k)
+                    qf[k] = *(const i32x4 *)(qs + q0 * (2 * D) + q_at[k]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (uint32_t k = 0; k < 2 * DC; ++k)
 #pragma unroll
                     for (int t = 0; t < (int)WT; ++t)
-                        s[t] = E::mma(qf, K[t][k], s[t]);
+                        s[t] = E::mma(qf[k], K[t][k], s[t]);
+                if (masked) {
+#pragma unroll
+                    for (int t = 0; t < (int)WT; ++t) {
+                        // bit e: the query row in register e sees this lane's key row
+                        uint32_t ok = 0;
+#pragma unroll 1
+                        for (uint32_t e = 0; e < 16; ++e) {
+                            const uint32_t q = r0 + q0 + 8 * (e >> 2) + 4 * half + (e & 3);
+                            const uint32_t i = 32 * t + l32;
+                            if (q < q_rows && ((there >> i) & 1) &&
+                                sees(a, b, rows, q / a.group, row0 + i))
+                                ok |= 1u << e;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            s[t][e] = (ok >> e) & 1 ? s[t][e] : -INFINITY;
+                    }
                 }
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
@@ -1076,17 +1210,8 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 #pragma unroll
                     for (int t = 0; t < (int)WT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float y = exp2_(s[t][4 * x + e] * a.scale2 - z[e]);
-                            if (masked) {
-                                const uint32_t i = 32 * t + l32;
-                                const uint32_t q = r0 + q0 + 8 * x + 4 * half + e;
-                                if (q >= q_rows || !((there >> i) & 1) ||
-                                    !sees(a, b, rows, q / a.group, row0 + i))
-                                    y = 0.f;
-                            }
-                            w[t] += y;
-                        }
+                        for (int e = 0; e < 4; ++e)
+                            w[t] += exp2_(__builtin_fmaf(s[t][4 * x + e], a.scale2, -z[e]));
                 }
             }
         }
@@ -1127,8 +1252,10 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
         attend_kernel<DT, DC, EXACT>(qt)<<<grid, 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
-        attend_join<DT><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, s>>>(a, qt, 32 * DC);
-        if ((e = hipGetLastError()) != hipSuccess)
+        const uint32_t strips =
+            a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
+        attend_join<DT><<<dim3((uint32_t)rows + strips), 256, 0, s>>>(a, qt, 32 * DC, (uint32_t)rows);
+        if ((e = hipGetLastError()) != hipSuccess || a.scores)
             return e;
     }
     if (!a.w_out || !a.w_cols)

@@ -55,6 +55,27 @@ __device__ __forceinline__ Place place_of(const Cache &c, uint32_t b, uint32_t n
     return {(uint32_t)p < c.pages ? p : -1, n - w * c.div.page};
 }
 
+// The same in two steps for loops that load ahead: the entry of row n's page (of the last
+// page past the room), loaded and not looked at, and the place it stands for.  Only
+// what reads `page` waits for the load, and for all loads before it.
+struct Entry {
+    int32_t raw;
+    uint32_t n;
+};
+
+__device__ __forceinline__ Entry entry_of(const Cache &c, const int32_t *any, uint32_t b, uint32_t n)
+{
+    const uint32_t w = c.div.quot(n), last = c.width - 1;
+    const int32_t *row = c.table ? c.table + (int64_t)b * c.table_row : any;
+    return {row[c.table ? (w < last ? w : last) : 0], n};
+}
+
+__device__ __forceinline__ Place place_of(const Cache &c, uint32_t b, const Entry &e, uint32_t end)
+{
+    const int32_t p = c.table ? e.raw : (int32_t)b;
+    return {e.n < end && (uint32_t)p < c.pages ? p : -1, e.n - c.div.quot(e.n) * c.div.page};
+}
+
 // len[b] and the rows of the call's own tokens, clamped to what the cache holds.
 __device__ __forceinline__ uint32_t clamp_rows(int32_t len, uint32_t room)
 {
@@ -118,6 +139,8 @@ struct Attend {
     uint32_t want;                 // shares there should be at most
     uint32_t slots;                // most shares there can be
     uint32_t *plan;                // per sequence: first share, shares
+    float *scores;                 // may be null: per head, query row and column (s_cols a row):
+    uint32_t s_cols;               // scale2 * score, -inf where the row is not seen
     float *part_o;                 // per share, head, tile: query rows x padded d
     float *part_ml;                // per share, head, tile: query rows x {max, sum}
 };

@@ -18,6 +18,8 @@ const int64_t kMaxStride = (int64_t)1 << 40;   // elements; extents below stay i
 const uint64_t kMaxCells = (uint64_t)1 << 31;
 const uint64_t kMaxRows = (uint64_t)1 << 30;   // of a sequence
 
+const uint64_t kMaxScores = (uint64_t)1 << 30; // bytes of kept scores
+
 struct Axis {
     uint64_t n;
     int64_t stride;
@@ -315,13 +317,23 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     const size_t off_lse = align_up((size_t)B * 8);
     const size_t off_ml = off_lse + align_up(lse ? 0 : (size_t)q_rows * 4);
     const size_t off_o = off_ml + align_up((size_t)parts * qt * 8);
-    if ((st = grow_scratch(c, off_o + (size_t)parts * qt * dp * 4)) != SJ_OK)
+    // Weights need every query row's lse, so the scores a second time.  Up to 16 query
+    // rows they are kept (8 bytes written and read again per row of the cache and
+    // query row, 128 at most); beyond, and where they would fill too much memory, the
+    // keys are multiplied again (2 d bytes per row, 256 for d = 128).
+    const size_t off_s = off_o + align_up((size_t)parts * qt * dp * 4);
+    const uint64_t cols = w_cols < a.c.room ? w_cols : a.c.room;
+    a.s_cols = (uint32_t)((cols + 31) / 32 * 32);
+    const uint64_t s_bytes = (uint64_t)B * a.c.heads * rows * a.s_cols * 4;
+    const bool keep = w_out && rows <= 16 && s_bytes > 0 && s_bytes <= kMaxScores;
+    if ((st = grow_scratch(c, off_s + (keep ? (size_t)s_bytes : 0))) != SJ_OK)
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     a.plan = (uint32_t *)s;
     a.lse = lse ? lse : (float *)(s + off_lse);
     a.part_ml = (float *)(s + off_ml);
     a.part_o = (float *)(s + off_o);
+    a.scores = keep ? (float *)(s + off_s) : nullptr;
     SJ_HIP(cache->dtype == SJ_F16 ? sjc::launch_attend_f16(a, c->stream)
                                   : sjc::launch_attend_bf16(a, c->stream));
     return SJ_OK;

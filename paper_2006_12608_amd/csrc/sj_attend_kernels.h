@@ -7,6 +7,8 @@
 // results over disjoint sets of rows join by the same rule.
 #pragma once
 
+#include <type_traits>
+
 #include "sj_cache.h"
 
 namespace sjc {
@@ -624,7 +626,8 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     __shared__ __align__(16) uint8_t lds[4 * TILE]; // K, V of two tiles
     __shared__ float stat[4][32][2];
     __shared__ uint32_t odd_any;
-    __shared__ i64x2 where[2][BN];
+    __shared__ i64x2 where[8][BN];
+    __shared__ uint64_t exist[8];
 
     const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -653,12 +656,12 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     const uint32_t q32 = lane & 31, half = lane >> 5, g = lane >> 4, l16 = lane & 15;
     const uint32_t d = a.c.d, q_rows = a.t * a.group;
     const uint32_t r_mine = tile * QT + 32 * qw + q32;
-    const bool live = r_mine < q_rows && r_mine / a.group < rows.count;
-    const uint32_t tok = live ? r_mine / a.group : 0;
+    const bool live = r_mine < q_rows && a.by_group.quot(r_mine) < rows.count;
+    const uint32_t tok = live ? a.by_group.quot(r_mine) : 0;
     i32x4 Q[2 * DC];
     {
         const uint16_t *p = a.q + (int64_t)b * a.q_seq + (int64_t)tok * a.q_tok +
-                            (int64_t)(h * a.group + (live ? r_mine % a.group : 0)) * a.q_head +
+                            (int64_t)(h * a.group + (live ? (r_mine - a.by_group.quot(r_mine) * a.group) : 0)) * a.q_head +
                             8 * half;
 #pragma unroll
         for (int k = 0; k < 2 * DC; ++k)
@@ -695,18 +698,25 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     auto entry = [&](uint32_t i) {
         return entry_of(a.c, a.len, b, from + i * BN + (lane & (BN - 1)));
     };
-    auto place = [&](const Entry &e) { return place_of(a.c, b, e, to); };
-    // Offsets of a tile's rows, for the threads that load them; absent rows read page
-    // 0, row 0.  Returns which rows exist.
-    auto post = [&](uint32_t i, const Place &p) -> uint64_t {
-        if (wave == 0 && lane < BN) {
+    // Offsets of tile i's rows, for the threads that load them, and which rows exist; absent
+    // rows read page 0, row 0.  Each wave does one tile of four.
+    auto post = [&](uint32_t i, const Entry &e) {
+        const Place p = place_of(a.c, b, e, to);
+        const uint64_t there = __ballot(p.page >= 0);
+        if (lane < BN) {
             i64x2 o = {0, 0};
             if (p.page >= 0)
                 o = i64x2{(int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row,
                           (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row};
-            where[i & 1][lane] = o;
+            where[i & 7][lane] = o;
         }
-        return __ballot(p.page >= 0);
+        if (lane == 0)
+            exist[i & 7] = there;
+    };
+    auto exists = [&](uint32_t i) -> uint64_t {
+        const uint64_t x = exist[i & 7];
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x) |
+               (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32;
     };
     i32x4 kr[NL], vr[NL];
     auto fetch = [&](uint32_t i) {
@@ -714,69 +724,69 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
         i64x2 o[NL];
 #pragma unroll
         for (int x = 0; x < NL; ++x)
-            o[x] = where[i & 1][RPL * x + row_at];
+            o[x] = where[i & 7][RPL * x + row_at];
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
             kr[x] = load8(kb + o[x][0] + 8 * chunk, left);
             vr[x] = load8(vb + o[x][1] + 8 * chunk, left);
         }
     };
-    auto stash = [&](uint32_t i, uint64_t there) {
-        uint8_t *kt = lds + (i & 1) * 2 * TILE, *vt = kt + TILE;
-        uint32_t odd = 0;
-        const bool tail = from + i * BN + BN > rows.len;
-        const uint64_t full = ~(uint64_t)0;
+    // (the swizzle repeats every 16 rows, and RPL is a multiple of 8: one place, or two)
+    uint32_t to_at[2];
 #pragma unroll
-        for (int x = 0; x < NL; ++x) {
-            const uint32_t r = RPL * x + row_at, at = r * (2 * D) + 16 * swz<DC>(r, chunk);
-            if (tail || there != full) {
-                if (!((there >> r) & 1))
+    for (uint32_t x = 0; x < 2; ++x)
+        to_at[x] = (RPL * x + row_at) * (2 * D) + 16 * swz<DC>(RPL * x + row_at, chunk);
+    auto stash = [&](uint32_t i, uint32_t buf, uint64_t there) {
+        uint8_t *kt = lds + buf * 2 * TILE, *vt = kt + TILE;
+        if (from + i * BN + BN > rows.len || there != ~(uint64_t)0) {
+            uint32_t odd = 0;
+#pragma unroll
+            for (int x = 0; x < NL; ++x) {
+                if (!((there >> (RPL * x + row_at)) & 1))
                     vr[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
                 odd |= drop_odd8<DT>(vr[x]);
-                asm volatile("");   // (a branch, not selects in every round)
             }
+            if (odd)
+                odd_any = 1;
+            asm volatile("");       // (a branch, not selects in every round)
+        }
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+            const uint32_t at = to_at[x & 1] + (x >> 1) * 2 * RPL * (2 * D);
             *(i32x4 *)(kt + at) = kr[x];
             *(i32x4 *)(vt + at) = vr[x];
         }
-        if (odd)
-            odd_any = 1;
     };
 
     if (tid == 0)
         odd_any = 0;
-    __syncthreads();
-    // ahead of tile i: tile i + 1 on its way to LDS, the offsets of i + 2, the place of i + 3
-    uint64_t there = 0, there1 = 0, there2 = 0;
+    // ahead of tile i: tile i + 1 on its way to LDS, i + 2 from memory, the offsets of the
+    // next four tiles, the page numbers of the four after
+    uint64_t there = 0;
     Entry ahead = {0, 0u};
     if (n_tiles > 0) {
-        there = post(0, place(entry(0)));
-        there1 = post(1, place(entry(1)));
+        post(wave, entry(wave));
+        ahead = entry(4 + wave);
         __syncthreads();
+        there = exists(0);
         fetch(0);
-        stash(0, there);
+        stash(0, 0, there);
         fetch(1);
-        __syncthreads();
-        there2 = post(2, place(entry(2)));
-        ahead = entry(3);
-        __syncthreads();
     }
-    for (uint32_t i = 0; i < n_tiles; ++i) {
-        stash(i + 1, there1);
-        const uint64_t there3 = post(i + 3, place(ahead));
+    __syncthreads();
+    auto round = [&](uint32_t i, auto buf_) {
+        constexpr uint32_t buf = decltype(buf_)::value;     // i % 2
+        if ((i & 3) == 0) {
+            post(i + 4 + wave, ahead);
+            ahead = entry(i + 8 + wave);
+        }
+        const uint64_t there1 = exists(i + 1);
+        stash(i + 1, 1 - buf, there1);
         fetch(i + 2);       // (past the end: page 0, row 0; a branch would cost full waits)
-        ahead = entry(i + 4);
-        uint8_t *const kt = lds + (i & 1) * 2 * TILE;
+        uint8_t *const kt = lds + buf * 2 * TILE;
         const uint32_t row0 = from + i * BN;
         const bool tail = row0 + BN > rows.len;
         const bool masked = tail || there != ~(uint64_t)0;
-        uint32_t seen[SR];      // bit 8 (r / 4) + r % 4: this lane's row in register r
-        if (masked) {
-            const uint64_t v = (there & (tail ? seen64(a, b, rows, tok, row0) : ~(uint64_t)0)) >>
-                               (rw * WR + 4 * half);
-#pragma unroll
-            for (int x = 0; x < SR; ++x)
-                seen[x] = (uint32_t)(v >> (32 * x));
-        }
 
         f32x16 s[SR];
 #pragma unroll
@@ -807,11 +817,16 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
             }
         }
         if (masked) {
+            // bit 8 (r / 4) + r % 4 of a word: this lane's row in register r
+            const uint64_t v = (there & (tail ? seen64(a, b, rows, tok, row0) : ~(uint64_t)0)) >>
+                               (rw * WR + 4 * half);
 #pragma unroll
-            for (int x = 0; x < SR; ++x)
+            for (int x = 0; x < SR; ++x) {
+                const uint32_t seen = (uint32_t)(v >> (32 * x));
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    s[x][e] = seen[x] & (1u << (8 * (e >> 2) + (e & 3))) ? s[x][e] : -INFINITY;
+                    s[x][e] = seen & (1u << (8 * (e >> 2) + (e & 3))) ? s[x][e] : -INFINITY;
+            }
             asm volatile("");           // (a branch, not selects in every round)
         }
         float top = -INFINITY;
@@ -820,8 +835,11 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 top = fmaxf(top, s[x][e]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (__any(top > m)) {
+        // m follows the maximum only once a score is 2^8 times the weight of m's: the
+        // exponentials then stay below 2^8, far from the 16-bit types' ends, and the sums are
+        // rescaled in few rounds instead of most (32 queries are in a wave)
+        if (__any(top * a.scale2 > m * a.scale2 + 8.f)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
             const float m_new = fmaxf(m, top);
             const float shrink =
                 exp2_(m * a.scale2 - (m_new == -INFINITY ? 0.f : m_new * a.scale2));
@@ -874,9 +892,13 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
             }
         }
         there = there1;
-        there1 = there2;
-        there2 = there3;
         __syncthreads();
+    };
+    for (uint32_t i = 0; i < n_tiles; i += 2) {
+        round(i, std::integral_constant<uint32_t, 0>());
+        if (i + 1 >= n_tiles)
+            break;
+        round(i + 1, std::integral_constant<uint32_t, 1>());
     }
 
     // join the halves of a query, then (QW = 2) the two waves of its rows
@@ -913,8 +935,8 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     }
     if (r_mine >= q_rows)
         return;
-    const uint32_t u = r_mine / a.group;
-    const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r_mine % a.group;
+    const uint32_t u = a.by_group.quot(r_mine);
+    const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + (r_mine - a.by_group.quot(r_mine) * a.group);
     const uint64_t part = ((uint64_t)slot * units + unit) * QT + 32 * qw + q32;
     if (odd_any && live)
         own_rows(a, b, h, rows, tok, from, to, [&](const uint16_t *v) {
@@ -1104,23 +1126,26 @@ __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, 
 // exp(s_rn - lse_r).  A wave holds 32 WT key rows in operand layout and runs
 // through the query rows, 64 of them in LDS at a time: S = Q K^T leaves key row l % 32 in
 // lane l with query rows 8 (r / 4) + 4 (l / 32) + r % 4 in register r, so the sum stays in
-// the lane until the end.
+// the lane until the end.  Two buffers of query rows, the next one's on their way
+// while one is worked on.
 template <int DT, int DC, bool EXACT>
 __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 {
     typedef Elem<DT> E;
-    constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QS = 64, WT = DC == 8 ? 1 : 2;
-    constexpr uint32_t WROWS = 32 * WT;
-    __shared__ __align__(16) uint8_t qs[QS * D * 2];
-    __shared__ __align__(16) float lse2[QS];
-    const uint32_t lane = threadIdx.x & 63;
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QS = DC == 8 ? 32 : 64, WT = DC == 8 ? 1 : 2;
+    constexpr uint32_t WROWS = 32 * WT, QB = QS * D * 2, RPL = 256 / CPR;
+    constexpr int NL = QS * CPR / 256;
+    __shared__ __align__(16) uint8_t qs[2 * QB];
+    __shared__ __align__(16) float lse2[2][QS];
+    const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t l32 = lane & 31, half = lane >> 5, d = a.c.d;
     const uint32_t h = blockIdx.y % a.c.heads, b = blockIdx.y / a.c.heads;
     const uint32_t block0 = blockIdx.x * 4 * WROWS, row0 = block0 + wave * WROWS;
     const Rows rows = rows_of(a, b);
+    const uint32_t q_rows = rows.count * a.group;
     float w[WT] = {};
-    if (block0 < rows.end) {
+    if (block0 < rows.end && q_rows > 0) {
         const uint32_t n = row0 + (lane & (WROWS - 1));
         const Place p = n < rows.end ? place_of(a.c, b, n) : Place{-1, 0u};
         const uint64_t there = __ballot(p.page >= 0);
@@ -1140,32 +1165,46 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 #pragma unroll
         for (uint32_t k = 0; k < 2 * DC; ++k)
             q_at[k] = l32 * (2 * D) + 16 * swz<DC>(l32, 2 * k + half);
+        // query rows r0 .. r0 + QS - 1 to registers, then to LDS; rows past the end repeat the
+        // last one and weigh nothing
+        const uint32_t row_at = tid / CPR, chunk = tid % CPR;
+        i32x4 qr[NL];
+        float lr = 0.f;
+        bool lr_there = false;
+        auto fetch = [&](uint32_t r0) {
+#pragma unroll
+            for (int x = 0; x < NL; ++x) {
+                uint32_t r = r0 + RPL * x + row_at;
+                r = r < q_rows ? r : q_rows - 1;
+                const uint32_t u = a.by_group.quot(r);
+                qr[x] = load8(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
+                                  (int64_t)(h * a.group + r - u * a.group) * a.q_head + 8 * chunk,
+                              EXACT ? 8 : (int)d - (int)(8 * chunk));
+            }
+            uint32_t r = r0 + (tid & (QS - 1));
+            lr_there = r < q_rows;
+            r = lr_there ? r : q_rows - 1;
+            const uint32_t u = a.by_group.quot(r);
+            lr = a.lse[((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group];
+        };
+        auto stash = [&](uint32_t buf) {
+            const int flip = a.negate ? (int)0x80008000 : 0;    // (as load_q8)
+#pragma unroll
+            for (int x = 0; x < NL; ++x) {
+                const uint32_t r = RPL * x + row_at;
+                *(i32x4 *)(qs + buf * QB + r * (2 * D) + 16 * swz<DC>(r, chunk)) = qr[x] ^ flip;
+            }
+            if (tid < QS)
+                lse2[buf][tid] = lr_there && lr != -INFINITY ? lr * 1.4426950408889634f : INFINITY;
+        };
         wait_loads();
-        const uint32_t q_rows = rows.count * a.group;
-        for (uint32_t r0 = 0; r0 < q_rows; r0 += QS) {
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < QS * CPR; i += 256) {
-                const uint32_t r = i / CPR, c = i % CPR;
-                i32x4 v = {0, 0, 0, 0};
-                if (r0 + r < q_rows)
-                    v = load_q8(a,
-                                a.q + (int64_t)b * a.q_seq + (int64_t)((r0 + r) / a.group) * a.q_tok +
-                                    (int64_t)(h * a.group + (r0 + r) % a.group) * a.q_head + 8 * c,
-                                EXACT ? 8 : (int)d - (int)(8 * c));
-                *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) = v;
-            }
-            if (threadIdx.x < QS) {
-                // a row that sees nothing, and one past the end, weighs nothing
-                const uint32_t r = r0 + threadIdx.x;
-                float x = INFINITY;
-                if (r < q_rows) {
-                    x = a.lse[((uint64_t)b * a.t + r / a.group) * a.q_heads + h * a.group +
-                              r % a.group] * 1.4426950408889634f;
-                    x = x == -INFINITY ? INFINITY : x;
-                }
-                lse2[threadIdx.x] = x;
-            }
-            __syncthreads();
+        fetch(0);
+        stash(0);
+        __syncthreads();
+        uint32_t buf = 0;
+        for (uint32_t r0 = 0; r0 < q_rows; r0 += QS, buf ^= 1) {
+            fetch(r0 + QS);
+            const uint8_t *qt = qs + buf * QB;
 #pragma unroll 1
             for (uint32_t q0 = 0; q0 < QS; q0 += 32) {
                 if (r0 + q0 >= q_rows)
@@ -1179,7 +1218,11 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                 i32x4 qf[2 * DC];
 #pragma unroll
                 for (uint32_t k = 0; k < 2 * DC; ++k)
-                    qf[k] = *(const i32x4 *)(qs + q0 * (2 * D) + q_at[k]);
+                    qf[k] = *(const i32x4 *)(qt + q0 * (2 * D) + q_at[k]);
+                f32x4 z[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    z[x] = *(const f32x4 *)(lse2[buf] + q0 + 8 * x + 4 * half);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (uint32_t k = 0; k < 2 * DC; ++k)
@@ -1196,7 +1239,7 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                             const uint32_t q = r0 + q0 + 8 * (e >> 2) + 4 * half + (e & 3);
                             const uint32_t i = 32 * t + l32;
                             if (q < q_rows && ((there >> i) & 1) &&
-                                sees(a, b, rows, q / a.group, row0 + i))
+                                sees(a, b, rows, a.by_group.quot(q), row0 + i))
                                 ok |= 1u << e;
                         }
 #pragma unroll
@@ -1205,15 +1248,13 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                     }
                 }
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const f32x4 z = *(const f32x4 *)(lse2 + q0 + 8 * x + 4 * half);
+                for (int t = 0; t < (int)WT; ++t)
 #pragma unroll
-                    for (int t = 0; t < (int)WT; ++t)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[t] += exp2_(__builtin_fmaf(s[t][4 * x + e], a.scale2, -z[e]));
-                }
+                    for (int e = 0; e < 16; ++e)
+                        w[t] += exp2_(__builtin_fmaf(s[t][e], a.scale2, -z[e >> 2][e & 3]));
             }
+            stash(buf ^ 1);
+            __syncthreads();
         }
     }
 #pragma unroll

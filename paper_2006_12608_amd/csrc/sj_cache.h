@@ -122,6 +122,7 @@ struct Attend {
     Cache c;
     const int32_t *len, *count;    // count may be null
     uint32_t t, group, q_heads;    // tokens, query heads per cache head
+    PageDiv by_group;
     const uint16_t *q;
     int64_t q_seq, q_tok, q_head;
     const uint64_t *tree;          // may be null (chain)

@@ -283,6 +283,7 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     a.count = count;
     a.t = t;
     a.group = q_heads / a.c.heads;
+    a.by_group = sjc::PageDiv::of(a.group);
     a.q_heads = q_heads;
     a.q = (const uint16_t *)q;
     a.q_seq = q_stride[0];

@@ -1268,6 +1268,186 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
     }
 }
 
+// The same with all query rows in LDS (64 KiB at most: 256 rows of 128 elements), so that a
+// workgroup can stay: it takes a share of a sequence's rows for one head, as the attention
+// kernels do, its waves 64 rows at a time in turn, the next 64 rows' keys on their way to
+// registers while these are multiplied.  (With a workgroup for every 256 rows the
+// keys were waited for at each start: 131072 rows x 256 query rows, 185 us.)
+template <int DC>
+constexpr uint32_t kWeighRows = DC == 8 ? 128 : 256;
+
+template <int DT, int DC, bool EXACT>
+__global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
+{
+    typedef Elem<DT> E;
+    constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QM = kWeighRows<DC>, WT = DC == 8 ? 1 : 2;
+    constexpr uint32_t WROWS = 32 * WT, RPL = 256 / CPR;
+    __shared__ __align__(16) uint8_t qs[QM * D * 2];
+    __shared__ __align__(16) float lse2[QM];
+    const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t l32 = lane & 31, half = lane >> 5, d = a.c.d;
+    const uint32_t h = blockIdx.x % a.c.heads, slot = blockIdx.x / a.c.heads;
+    Share sh;
+    if (slot >= a.slots || !find_share(a, slot, &sh))
+        return;
+    const uint32_t b = __builtin_amdgcn_readfirstlane(sh.b);
+    const Rows rows = {(uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.len),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.count),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(sh.rows.end)};
+    const uint32_t q_rows = rows.count * a.group;
+    const uint32_t end = rows.end < a.w_cols ? rows.end : (uint32_t)a.w_cols;
+    const uint32_t from = __builtin_amdgcn_readfirstlane(sh.first) * AT_ROWS;
+    const uint32_t last = __builtin_amdgcn_readfirstlane(sh.last) * AT_ROWS;
+    const uint32_t to = q_rows == 0 ? from : (last < end ? last : end);
+    const uint64_t at0 = ((uint64_t)b * a.c.heads + h) * a.w_cols;
+
+    // columns that no row of this call weighs, evenly over the sequence's shares
+    const uint32_t rest = q_rows == 0 ? 0 : end;
+    const uint64_t n_rest = a.w_cols - rest;
+    for (uint64_t n = rest + n_rest * sh.share / sh.shares + tid;
+         n < rest + n_rest * (sh.share + 1) / sh.shares; n += 256)
+        if (!a.w_in)
+            a.w_out[at0 + n] = 0.f;
+        else if (a.w_in != a.w_out)
+            a.w_out[at0 + n] = a.w_in[at0 + n];
+    if (from >= to)
+        return;
+
+    // query rows and their lse; rows past the end are zeros and weigh nothing
+    const uint32_t n_q = (q_rows + 31) / 32;
+    const int flip = a.negate ? (int)0x80008000 : 0;    // (as load_q8)
+    for (uint32_t i = tid; i < n_q * 32 * CPR; i += 256) {
+        const uint32_t r = i / CPR, c = i % CPR, u = a.by_group.quot(r);
+        i32x4 v = {0, 0, 0, 0};
+        if (r < q_rows)
+            v = load8(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
+                          (int64_t)(h * a.group + r - u * a.group) * a.q_head + 8 * c,
+                      EXACT ? 8 : (int)d - (int)(8 * c));
+        *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) = v ^ flip;
+    }
+    for (uint32_t r = tid; r < n_q * 32; r += 256) {
+        float x = INFINITY;
+        if (r < q_rows) {
+            const uint32_t u = a.by_group.quot(r);
+            x = a.lse[((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group];
+            x = x == -INFINITY ? INFINITY : x * 1.4426950408889634f;
+        }
+        lse2[r] = x;
+    }
+    uint32_t q_at[2 * DC];      // chunk 2 k + half of query row l32 (the same for every 32)
+#pragma unroll
+    for (uint32_t k = 0; k < 2 * DC; ++k)
+        q_at[k] = l32 * (2 * D) + 16 * swz<DC>(l32, 2 * k + half);
+
+    const uint16_t *kb = a.c.k + (int64_t)h * a.c.k_head + 8 * half;
+    const uint32_t n_blk = (to - from + WROWS - 1) / WROWS;
+    auto entry = [&](uint32_t i) {
+        return entry_of(a.c, a.len, b, from + i * WROWS + (lane & (WROWS - 1)));
+    };
+    i32x4 K[2][WT][2 * DC];
+    auto load_k = [&](const Place &p, auto set_) {      // absent rows read page 0, row 0
+        constexpr int set = decltype(set_)::value;
+        const int64_t off =
+            p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
+#pragma unroll
+        for (int t = 0; t < (int)WT; ++t) {
+            const uint16_t *r = kb + shfl64(off, (int)l32 + 32 * t);
+#pragma unroll
+            for (int k = 0; k < 2 * DC; ++k)
+                K[set][t][k] = load8(r + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half));
+        }
+    };
+    auto add = [&](uint32_t n) -> float {               // (a load whether it is needed or not)
+        n = n < to ? n : to - 1;
+        return a.w_in ? a.w_in[at0 + n] : 0.f;
+    };
+    Place cur = place_of(a.c, b, entry(wave), to);
+    Entry ahead = entry(wave + 4);
+    load_k(cur, std::integral_constant<int, 0>());
+    __syncthreads();
+    auto round = [&](uint32_t i, auto set_) {
+        constexpr int set = decltype(set_)::value;
+        const Place nxt = place_of(a.c, b, ahead, to);
+        ahead = entry(i + 8);
+        const uint32_t row0 = from + i * WROWS;
+        const uint64_t there = __ballot(cur.page >= 0);
+        const bool masked = row0 + WROWS > rows.len || there != ~(uint64_t)0;
+        float w[WT], w0[WT];
+#pragma unroll
+        for (int t = 0; t < (int)WT; ++t) {
+            w[t] = 0.f;
+            w0[t] = add(row0 + 32 * t + l32);
+        }
+        load_k(nxt, std::integral_constant<int, 1 - set>());
+        i32x4 qf[2 * DC];
+        auto read_q = [&](uint32_t q0) {
+#pragma unroll
+            for (uint32_t k = 0; k < 2 * DC; ++k)
+                qf[k] = *(const i32x4 *)(qs + q0 * (2 * D) + q_at[k]);
+        };
+        read_q(0);
+#pragma unroll 1
+        for (uint32_t q = 0; q < n_q; ++q) {
+            const uint32_t q0 = 32 * q;
+            f32x16 s[WT];
+#pragma unroll
+            for (int t = 0; t < (int)WT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[t][e] = 0.f;
+#pragma unroll
+            for (uint32_t k = 0; k < 2 * DC; ++k)
+#pragma unroll
+                for (int t = 0; t < (int)WT; ++t)
+                    s[t] = E::mma(qf[k], K[set][t][k], s[t]);
+            __builtin_amdgcn_sched_barrier(0);
+            read_q(q + 1 < n_q ? q0 + 32 : 0);
+            f32x4 z[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                z[x] = *(const f32x4 *)(lse2 + q0 + 8 * x + 4 * half);
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < (int)WT; ++t) {
+                    // bit e: the query row in register e sees this lane's key row
+                    uint32_t ok = 0;
+#pragma unroll 1
+                    for (uint32_t e = 0; e < 16; ++e) {
+                        const uint32_t r = q0 + 8 * (e >> 2) + 4 * half + (e & 3);
+                        const uint32_t i32 = 32 * t + l32;
+                        if (r < q_rows && ((there >> i32) & 1) &&
+                            sees(a, b, rows, a.by_group.quot(r), row0 + i32))
+                            ok |= 1u << e;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        s[t][e] = (ok >> e) & 1 ? s[t][e] : -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < (int)WT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    w[t] += exp2_(__builtin_fmaf(s[t][e], a.scale2, -z[e >> 2][e & 3]));
+        }
+#pragma unroll
+        for (int t = 0; t < (int)WT; ++t) {
+            w[t] += __shfl_xor(w[t], 32);
+            const uint32_t n = row0 + 32 * t + l32;
+            if (half == 0 && n < to)
+                a.w_out[at0 + n] = w0[t] + w[t];
+        }
+        cur = nxt;
+    };
+    for (uint32_t i = wave; i < n_blk; i += 8) {
+        round(i, std::integral_constant<int, 0>());
+        if (i + 4 >= n_blk)
+            break;
+        round(i + 4, std::integral_constant<int, 1>());
+    }
+}
+
 // The kernel for tiles of qt query rows.
 template <int DT, int DC, bool EXACT>
 void (*attend_kernel(uint32_t qt))(const Attend)
@@ -1301,6 +1481,13 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     }
     if (!a.w_out || !a.w_cols)
         return hipSuccess;
+    if (a.t * a.group <= kWeighRows<DC>) {
+        Attend w = a;       // (its own cut of the rows: a workgroup a share and head)
+        w.want = a.w_want;
+        w.slots = a.w_want > a.c.batch ? a.w_want : a.c.batch;
+        attend_weights_held<DT, DC, EXACT><<<dim3(w.slots * a.c.heads), 256, 0, s>>>(w);
+        return hipGetLastError();
+    }
     const uint32_t w_rows = DC == 8 ? 128 : 256;
     const dim3 wg((uint32_t)((a.w_cols + w_rows - 1) / w_rows), a.c.batch * a.c.heads);
     attend_weights<DT, DC, EXACT><<<wg, 256, 0, s>>>(a);

@@ -138,6 +138,7 @@ struct Attend {
     // cache head and tile of query rows
     uint32_t tiles;                // tiles of query rows per cache head
     uint32_t want;                 // shares there should be at most
+    uint32_t w_want;               // the same for the weights' kernel, a workgroup a share and head
     uint32_t slots;                // most shares there can be
     uint32_t *plan;                // per sequence: first share, shares
     float *scores;                 // may be null: per head, query row and column (s_cols a row):

@@ -311,6 +311,7 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     const uint64_t units = (uint64_t)a.c.heads * a.tiles, held = (uint64_t)c->num_cus * per_cu;
     a.want = held / units > 0 ? (uint32_t)(held / units) : 1;
     a.slots = a.want > B ? a.want : B;
+    a.w_want = 2 * c->num_cus / a.c.heads > 0 ? 2 * c->num_cus / a.c.heads : 1;
     const uint64_t parts = a.slots * units;
     if (parts >= kMaxCells)
         return fail(SJ_E_UNSUPPORTED, "%u sequences of %llu query tiles are too many", B,

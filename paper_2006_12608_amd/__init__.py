@@ -14,6 +14,7 @@ fails when libsj.so has not been built (python paper_2006_12608_amd/build.py).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -226,8 +227,9 @@ def sj_jl(ctx, dtype, X, n, d, levels, shape, A, Y):
     return lib.sj_jl(ctx, dtype, X, n, d, levels, arr, A, Y)
 
 
+@functools.lru_cache(maxsize=4096)
 def _strides(*values):
-    """Element strides as the C array the calls on caches take."""
+    """Element strides as the C array the calls on caches take (which only read it)."""
     return (ctypes.c_int64 * len(values))(*values)
 
 
@@ -288,9 +290,10 @@ def context(device: int | None = None, stream=None) -> int:
         stream = torch.cuda.current_stream(dev)
     handle = int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream or 0)
     key = (dev, handle)
-    if key not in _contexts:
-        _contexts[key] = sj_create(dev, handle)
-    return _contexts[key]
+    known = _contexts.get(key)
+    if known is None:
+        known = _contexts[key] = sj_create(dev, handle)
+    return known
 
 
 def dtype_code(t) -> int:
@@ -570,15 +573,26 @@ def _layout_code(layout: str) -> int:
     return _LAYOUTS[layout]
 
 
-def _check_rows(name, x, shape, dtype, device):
-    """x: a device tensor of `shape` (None: any size) and dtype whose last
-    dimension is adjacent."""
+def _refuse(name, x, shape, dtype, device):
     if x.dtype != dtype or x.device != device or x.dim() != len(shape) or \
             any(s is not None and s != n for s, n in zip(shape, x.shape)):
         raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}, expected "
                          f"{tuple('any' if s is None else s for s in shape)} {dtype} on {device}")
-    if x.stride(-1) != 1 and x.shape[-1] > 1:
-        raise ValueError(f"{name}: the elements of its last dimension must be adjacent")
+    raise ValueError(f"{name}: the elements of its last dimension must be adjacent")
+
+
+def _check_rows(name, x, shape, dtype, device):
+    """x: a device tensor of `shape` (None: any size) and dtype whose last
+    dimension is adjacent."""
+    size = x.shape
+    if len(size) == len(shape) and x.dtype is dtype and x.device == device and \
+            (x.stride(-1) == 1 or size[-1] <= 1):
+        for s, n in zip(shape, size):
+            if s is not None and s != n:
+                break
+        else:
+            return
+    _refuse(name, x, shape, dtype, device)
 
 
 def _check_whole(name, x, shape, dtype, device):
@@ -588,7 +602,8 @@ def _check_whole(name, x, shape, dtype, device):
 
 
 def _ptr(x):
-    return None if x is None or x.numel() == 0 else x.data_ptr()
+    """The address of a tensor's first element (None for none or an empty one)."""
+    return None if x is None else (x.data_ptr() or None)
 
 
 class kv_cache:

@@ -192,29 +192,33 @@ __device__ __forceinline__ float odd_part(uint16_t x)
     return (x & Elem<DT>::EXP) == Elem<DT>::EXP ? bits_to_float(x, DT) : 0.f;
 }
 
+// For each of the query rows r0 .. r0 + n - 1 of q_rows, which of the 64 rows from row0 on it
+// sees, among those in `there`: to `vis`, a row a lane.
+__device__ __forceinline__ void seen_rows(const Attend &a, uint32_t b, const Rows &r, uint32_t r0,
+                                          uint32_t n, uint32_t q_rows, uint32_t row0, uint64_t there,
+                                          uint64_t *vis)
+{
+    for (uint32_t i = threadIdx.x & 63; i < n; i += 64)
+        vis[i] = r0 + i < q_rows ? there & seen64(a, b, r, a.by_group.quot(r0 + i), row0) : 0;
+}
+
+// -inf for the scores of key row n (of 64) that the query rows v[8 (e / 4) + e % 4] do not see.
+template <class S>
+__device__ __forceinline__ void hide(S &s, const uint64_t *v, uint32_t n)
+{
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const uint32_t w = ((const uint32_t *)(v + 8 * (e >> 2) + (e & 3)))[n >> 5];
+        s[e] = (w >> (n & 31)) & 1 ? s[e] : -INFINITY;
+    }
+}
+
 // The share of the work that a workgroup takes: blocks [first, last) of
 // AT_ROWS rows of sequence b, number `share` of its `shares`.
 struct Share {
     uint32_t b, share, shares, first, last;
     Rows rows;
 };
-
-// Sum over the lanes up to this one.
-__device__ __forceinline__ uint32_t sum_upto(uint32_t x)
-{
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);   // row_shr 1
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // row 15 on
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);  // row 31 on
-    return x;
-}
-
-__device__ __forceinline__ uint32_t sum_all(uint32_t x)
-{
-    return (uint32_t)__builtin_amdgcn_readlane((int)sum_upto(x), 63);
-}
 
 // Finds share number `slot` of the batch.  Each sequence's blocks are cut into whole shares
 // of at most `size` blocks, one at least.  `size` is the smallest with which the
@@ -1137,6 +1141,7 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
     constexpr int NL = QS * CPR / 256;
     __shared__ __align__(16) uint8_t qs[2 * QB];
     __shared__ __align__(16) float lse2[2][QS];
+    __shared__ uint64_t vis[4][QS];
     const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t l32 = lane & 31, half = lane >> 5, d = a.c.d;
@@ -1204,6 +1209,8 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
         uint32_t buf = 0;
         for (uint32_t r0 = 0; r0 < q_rows; r0 += QS, buf ^= 1) {
             fetch(r0 + QS);
+            if (masked)
+                seen_rows(a, b, rows, r0, QS, q_rows, row0, there, vis[wave]);
             const uint8_t *qt = qs + buf * QB;
 #pragma unroll 1
             for (uint32_t q0 = 0; q0 < QS; q0 += 32) {
@@ -1231,21 +1238,8 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                         s[t] = E::mma(qf[k], K[t][k], s[t]);
                 if (masked) {
 #pragma unroll
-                    for (int t = 0; t < (int)WT; ++t) {
-                        // bit e: the query row in register e sees this lane's key row
-                        uint32_t ok = 0;
-#pragma unroll 1
-                        for (uint32_t e = 0; e < 16; ++e) {
-                            const uint32_t q = r0 + q0 + 8 * (e >> 2) + 4 * half + (e & 3);
-                            const uint32_t i = 32 * t + l32;
-                            if (q < q_rows && ((there >> i) & 1) &&
-                                sees(a, b, rows, a.by_group.quot(q), row0 + i))
-                                ok |= 1u << e;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            s[t][e] = (ok >> e) & 1 ? s[t][e] : -INFINITY;
-                    }
+                    for (int t = 0; t < (int)WT; ++t)
+                        hide(s[t], vis[wave] + q0 + 4 * half, 32 * t + l32);
                 }
 #pragma unroll
                 for (int t = 0; t < (int)WT; ++t)
@@ -1284,6 +1278,7 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
     constexpr uint32_t WROWS = 32 * WT, RPL = 256 / CPR;
     __shared__ __align__(16) uint8_t qs[QM * D * 2];
     __shared__ __align__(16) float lse2[QM];
+    __shared__ uint64_t vis[4][QM];
     const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t l32 = lane & 31, half = lane >> 5, d = a.c.d;
@@ -1380,6 +1375,8 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
             w0[t] = add(row0 + 32 * t + l32);
         }
         load_k(nxt, std::integral_constant<int, 1 - set>());
+        if (masked)
+            seen_rows(a, b, rows, 0, n_q * 32, q_rows, row0, there, vis[wave]);
         i32x4 qf[2 * DC];
         auto read_q = [&](uint32_t q0) {
 #pragma unroll
@@ -1409,21 +1406,8 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
                 z[x] = *(const f32x4 *)(lse2 + q0 + 8 * x + 4 * half);
             if (masked) {
 #pragma unroll
-                for (int t = 0; t < (int)WT; ++t) {
-                    // bit e: the query row in register e sees this lane's key row
-                    uint32_t ok = 0;
-#pragma unroll 1
-                    for (uint32_t e = 0; e < 16; ++e) {
-                        const uint32_t r = q0 + 8 * (e >> 2) + 4 * half + (e & 3);
-                        const uint32_t i32 = 32 * t + l32;
-                        if (r < q_rows && ((there >> i32) & 1) &&
-                            sees(a, b, rows, a.by_group.quot(r), row0 + i32))
-                            ok |= 1u << e;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        s[t][e] = (ok >> e) & 1 ? s[t][e] : -INFINITY;
-                }
+                for (int t = 0; t < (int)WT; ++t)
+                    hide(s[t], vis[wave] + q0 + 4 * half, 32 * t + l32);
             }
 #pragma unroll
             for (int t = 0; t < (int)WT; ++t)

@@ -113,6 +113,23 @@ __device__ __forceinline__ void store8(uint16_t *p, i32x4 v, int left)
     }
 }
 
+// Sum over the lanes up to this one, and over all lanes.
+__device__ __forceinline__ uint32_t sum_upto(uint32_t x)
+{
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true);   // row_shr 1
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // row 15 on
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);  // row 31 on
+    return x;
+}
+
+__device__ __forceinline__ uint32_t sum_all(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_readlane((int)sum_upto(x), 63);
+}
+
 // ------------------------------------------------------------------- attention
 
 // Blocks of rows that one wave takes at a time, and queries of one matrix tile.
@@ -198,8 +215,25 @@ struct Evict {
     uint32_t keep, sink, recent;
     int32_t *index, *new_len;
     float *w_out;           // may be null
+    uint32_t chunks;        // of EV_CHUNK rows, where a sequence may have more than EV_ONE
+    uint32_t *hist;         // per set, step and chunk: EV_BINS counts
+    uint32_t *state;        // per set and chunk: key prefix, rows still needed; keys above
 };
 
-hipError_t launch_evict(const Evict &e, int num_cus, hipStream_t s);
+// Rows that one workgroup selects from alone, rows of a chunk beyond, bins of a step.
+constexpr uint32_t EV_ONE = 32768, EV_CHUNK = 16384, EV_BINS = 2048;
+
+// Scratch of a call: uint32 values of hist and of state (0 where one workgroup does).
+inline uint32_t evict_chunks(uint32_t room)
+{
+    return room <= EV_ONE ? 0 : (room + EV_CHUNK - 1) / EV_CHUNK;
+}
+inline uint64_t evict_hist_values(uint64_t sets, uint32_t chunks)
+{
+    return sets * chunks * 3 * EV_BINS;
+}
+inline uint64_t evict_state_values(uint64_t sets, uint32_t chunks) { return sets * chunks * 8; }
+
+hipError_t launch_evict(const Evict &e, hipStream_t s);
 
 }  // namespace sjc

@@ -391,6 +391,15 @@ extern "C" int sj_cache_evict(sj_ctx *c, const sj_cache *src, const int32_t *len
     e.index = index;
     e.new_len = new_len;
     e.w_out = w_out;
-    SJ_HIP(sjc::launch_evict(e, c->num_cus, c->stream));
+    e.chunks = sjc::evict_chunks(e.src.room);
+    if (e.chunks) {
+        const size_t off = align_up((size_t)sjc::evict_hist_values(B * sets, e.chunks) * 4);
+        if ((st = grow_scratch(c, off + (size_t)sjc::evict_state_values(B * sets, e.chunks) * 4)) !=
+            SJ_OK)
+            return st;
+        e.hist = (uint32_t *)c->scratch;
+        e.state = (uint32_t *)((uint8_t *)c->scratch + off);
+    }
+    SJ_HIP(sjc::launch_evict(e, c->stream));
     return SJ_OK;
 }

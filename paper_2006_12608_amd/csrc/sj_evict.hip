@@ -15,134 +15,281 @@ __device__ __forceinline__ uint32_t order_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr uint32_t EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64, EV_BINS = 2048;
+constexpr uint32_t EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64;
+constexpr int EV_STEPS = 3;
+// key bits of the three steps, from the top
+__device__ __forceinline__ uint32_t step_bits(int step) { return step == 2 ? 10 : 11; }
+__device__ __forceinline__ uint32_t bits_before(int step) { return 11 * step; }
 
 __device__ __forceinline__ float weight_at(const Evict &e, const float *w, uint32_t n)
 {
     return n < e.w_cols ? w[n] : 0.f;
 }
 
-// Writes kept row number j of a set.
-__device__ __forceinline__ void keep_row(const Evict &e, uint64_t set, const float *w, uint32_t j,
-                                         uint32_t n)
+// What one set (a sequence and a head, or a sequence) keeps of its n rows: all m = n, or the
+// rows outside [lo, hi) and `need` of those inside.
+struct Task {
+    uint32_t n, m, lo, hi, need;
+    uint64_t set;
+    const float *w;
+};
+
+__device__ __forceinline__ Task task_of(const Evict &e, uint64_t set)
 {
-    e.index[set * e.keep + j] = (int32_t)n;
-    if (e.w_out && j < e.w_out_cols)
-        e.w_out[set * e.w_out_cols + j] = weight_at(e, w, n);
+    Task t;
+    t.set = set;
+    t.w = e.weight + set * e.w_cols;
+    t.n = clamp_rows(e.len[set / e.sets], e.src.room);
+    t.m = t.n < e.keep ? t.n : e.keep;
+    const bool all = t.n <= e.keep;
+    t.lo = all ? t.n : e.sink;
+    t.hi = all ? t.n : t.n - e.recent;
+    t.need = all ? 0 : e.keep - e.sink - e.recent;
+    return t;
 }
 
-// The kept rows of one set (a sequence and a head, or a sequence), in order: a
-// workgroup a set.  Radix selection of the last weight that stays: three
-// histograms of 11, 11 and 10 key bits, each over the rows whose higher bits are
-// those of the key sought; then every wave counts the kept rows and the ties of its
-// own stretch of rows, and writes its rows at the sum of the waves before it.
-__global__ void __launch_bounds__(EV_THREADS) evict_select(const Evict e)
-{
-    __shared__ uint32_t hist[EV_BINS];
-    __shared__ uint32_t above[EV_WAVES], ties[EV_WAVES], found[2];
-    const uint64_t set = blockIdx.x;
-    const uint32_t b = (uint32_t)(set / e.sets);
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t n = clamp_rows(e.len[b], e.src.room);
-    const uint32_t m = n < e.keep ? n : e.keep;
-    const float *w = e.weight + set * e.w_cols;
-    if (threadIdx.x == 0 && set % e.sets == 0)
-        e.new_len[b] = (int32_t)m;
-    for (uint32_t j = m + threadIdx.x; j < e.keep; j += EV_THREADS)
-        e.index[set * e.keep + j] = -1;
-    if (e.w_out)
-        for (uint64_t j = m + threadIdx.x; j < e.w_out_cols; j += EV_THREADS)
-            e.w_out[set * e.w_out_cols + j] = 0.f;
-    if (n <= e.keep) {
-        for (uint32_t j = threadIdx.x; j < m; j += EV_THREADS)
-            keep_row(e, set, w, j, j);
-        return;
-    }
-    const uint32_t lo = e.sink, hi = n - e.recent;   // rows between compete
-    uint32_t need = e.keep - e.sink - e.recent;      // of these stay (< hi - lo)
-    uint32_t prefix = 0, known = 0;                  // the sought key's known top bits
-    if (need > 0) {
-        for (int step = 0; step < 3; ++step) {
-            const uint32_t bits = step == 2 ? 10 : 11, shift = 32 - known - bits;
-            const uint32_t bins = 1u << bits;
-            for (uint32_t i = threadIdx.x; i < EV_BINS; i += EV_THREADS)
-                hist[i] = 0;
-            __syncthreads();
-            for (uint32_t i = lo + threadIdx.x; i < hi; i += EV_THREADS) {
-                const uint32_t key = order_key(weight_at(e, w, i));
-                if (known == 0 || key >> (32 - known) == prefix)
-                    atomicAdd(&hist[(key >> shift) & (bins - 1)], 1u);
-            }
-            __syncthreads();
-            // the bin, from the top, in which the need-th key lies: one wave, 32 bins a lane
-            if (wave == 0) {
-                uint32_t sum = 0;
-                const uint32_t per = bins / 64, top = bins - 1 - lane * per;
-                for (uint32_t i = 0; i < per; ++i)
-                    sum += hist[top - i];
-                uint32_t incl = sum;
-                for (int o = 1; o < 64; o <<= 1) {
-                    const uint32_t y = __shfl_up(incl, o);
-                    incl += (int)lane >= o ? y : 0;
-                }
-                if (need > incl - sum && need <= incl) {
-                    uint32_t before = incl - sum;
-                    for (uint32_t i = 0; i < per; ++i) {
-                        const uint32_t c = hist[top - i];
-                        if (need <= before + c) {
-                            found[0] = top - i;
-                            found[1] = need - before;
-                            break;
-                        }
-                        before += c;
-                    }
-                }
-            }
-            __syncthreads();
-            prefix = (prefix << bits) | found[0];
-            need = found[1];
-            known += bits;
-            __syncthreads();
+// Keys of the rows from + 64 k + lane, k < per (PER at most), of a wave; 0 outside [lo, hi)
+// (below every key in use: -inf is 0x007fffff).
+template <int PER>
+struct Keys {
+    uint32_t key[PER];
+    __device__ __forceinline__ void load(const Evict &e, const Task &t, uint32_t from, uint32_t per)
+    {
+        const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const uint32_t i = from + 64 * k + lane;
+            key[k] = 0;
+            if ((uint32_t)k < per && i >= t.lo && i < t.hi)
+                key[k] = order_key(weight_at(e, t.w, i));
         }
     }
-    // prefix is the last key that stays, need the number of its rows that do (the
-    // lowest ones); with nothing to choose none does
-    const bool none = known == 0;
-    const uint32_t per = ((n + EV_WAVES - 1) / EV_WAVES + 63) & ~63u;
-    const uint32_t from = wave * per < n ? wave * per : n, to = from + per < n ? from + per : n;
-    uint32_t n_above = 0, n_ties = 0;
-    for (uint32_t i0 = from; i0 < to; i0 += 64) {
-        const uint32_t i = i0 + lane;
-        const bool mid = i >= lo && i < hi && i < to;
-        const uint32_t key = mid && !none ? order_key(weight_at(e, w, i)) : 0;
-        n_above += __popcll(__ballot(i < to && (!mid || (!none && key > prefix))));
-        n_ties += __popcll(__ballot(mid && !none && key == prefix));
+    // adds the digit of `step` of every key whose higher bits are `prefix` to hist
+    __device__ __forceinline__ void count(uint32_t *hist, int step, uint32_t prefix, uint32_t per)
+    {
+        const uint32_t bits = step_bits(step), known = bits_before(step), shift = 32 - known - bits;
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if ((uint32_t)k < per && key[k] && (known == 0 || key[k] >> (32 - known) == prefix))
+                atomicAdd(&hist[(key[k] >> shift) & ((1u << bits) - 1)], 1u);
     }
+};
+
+// The bin, from the top, in which the need-th of all counted keys lies, and how many keys of
+// that bin are still needed; thread t passes the counts of bins 2047 - 2 t and
+// 2046 - 2 t.  Called by the whole workgroup.
+__device__ __forceinline__ void find_bin(uint32_t c0, uint32_t c1, uint32_t need, uint32_t *bin,
+                                         uint32_t *left)
+{
+    __shared__ uint32_t waves[EV_WAVES], found[2];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t incl = sum_upto(c0 + c1);
+    if (lane == 63)
+        waves[wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - c0 - c1;
+#pragma unroll
+    for (uint32_t w = 0; w < EV_WAVES; ++w)
+        before += w < wave ? waves[w] : 0;
+    if (need > before && need <= before + c0 + c1) {
+        const bool first = need <= before + c0;
+        found[0] = EV_BINS - 1 - 2 * threadIdx.x - (first ? 0 : 1);
+        found[1] = need - before - (first ? 0 : c0);
+    }
+    __syncthreads();
+    *bin = found[0];
+    *left = found[1];
+    __syncthreads();
+}
+
+// Writes what the wave's rows keep: all outside [lo, hi) and, inside, the keys above `last` and
+// of those equal to it the first `need` (over all waves).  Rows and ties before the
+// workgroup's come in out0 and ties0.  Called by the whole workgroup.
+template <int PER>
+__device__ __forceinline__ void emit(const Evict &e, const Task &t, const Keys<PER> &keys,
+                                     uint32_t from, uint32_t per, uint32_t last, uint32_t need,
+                                     uint32_t out0, uint32_t ties0)
+{
+    __shared__ uint32_t above[EV_WAVES], ties[EV_WAVES];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    uint32_t n_above = 0, n_ties = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if ((uint32_t)k < per) {
+            const uint32_t i = from + 64 * k + lane;
+            const bool mid = i >= t.lo && i < t.hi;
+            n_above += __popcll(__ballot(i < t.n && (!mid || (need && keys.key[k] > last))));
+            n_ties += __popcll(__ballot(mid && need && keys.key[k] == last));
+        }
     if (lane == 0) {
         above[wave] = n_above;
         ties[wave] = n_ties;
     }
     __syncthreads();
-    uint32_t out = 0, tied = 0;      // kept rows and ties before this wave's
-    for (uint32_t i = 0; i < wave; ++i) {
-        out += above[i];
-        tied += ties[i];
+    uint32_t out = out0, tied = ties0;
+    for (uint32_t w = 0; w < wave; ++w) {
+        out += above[w];
+        tied += ties[w];
     }
     out += tied < need ? tied : need;
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (uint32_t i0 = from; i0 < to; i0 += 64) {
-        const uint32_t i = i0 + lane;
-        const bool mid = i >= lo && i < hi && i < to;
-        const uint32_t key = mid && !none ? order_key(weight_at(e, w, i)) : 0;
-        const bool tie = mid && !none && key == prefix;
-        const uint64_t tie_mask = __ballot(tie);
-        const bool kept = i < to && (!mid || (!none && key > prefix) ||
-                                     (tie && tied + __popcll(tie_mask & below) < need));
-        const uint64_t kept_mask = __ballot(kept);
-        if (kept)
-            keep_row(e, set, w, out + __popcll(kept_mask & below), i);
-        out += __popcll(kept_mask);
-        tied += __popcll(tie_mask);
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if ((uint32_t)k < per) {
+            const uint32_t i = from + 64 * k + lane;
+            const bool mid = i >= t.lo && i < t.hi;
+            const bool tie = mid && need && keys.key[k] == last;
+            const uint64_t tie_mask = __ballot(tie);
+            const bool kept = i < t.n && (!mid || (need && keys.key[k] > last) ||
+                                          (tie && tied + __popcll(tie_mask & below) < need));
+            const uint64_t kept_mask = __ballot(kept);
+            if (kept) {
+                const uint32_t j = out + __popcll(kept_mask & below);
+                e.index[t.set * e.keep + j] = (int32_t)i;
+                if (e.w_out && j < e.w_out_cols)
+                    e.w_out[t.set * e.w_out_cols + j] = weight_at(e, t.w, i);
+            }
+            out += __popcll(kept_mask);
+            tied += __popcll(tie_mask);
+        }
+}
+
+// -1 and 0 past the kept rows, by `share` of `shares` workgroups; the new length.
+__device__ __forceinline__ void pad(const Evict &e, const Task &t, uint32_t share, uint32_t shares)
+{
+    const uint32_t at = share * EV_THREADS + threadIdx.x, all = shares * EV_THREADS;
+    if (at == 0 && t.set % e.sets == 0)
+        e.new_len[t.set / e.sets] = (int32_t)t.m;
+    for (uint64_t j = (uint64_t)t.m + at; j < e.keep; j += all)
+        e.index[t.set * e.keep + j] = -1;
+    if (e.w_out)
+        for (uint64_t j = (uint64_t)t.m + at; j < e.w_out_cols; j += all)
+            e.w_out[t.set * e.w_out_cols + j] = 0.f;
+}
+
+// The kept rows of one set, in order: a workgroup a set of up to EV_ONE rows, each wave a
+// stretch of them, the keys in registers.  Radix selection of the last key that stays: three
+// histograms of 11, 11 and 10 key bits, each over the keys whose higher bits are
+// those of the key sought.  16 sets of 3000 rows 13 -> ... us with the keys read
+// from memory in every pass.
+__global__ void __launch_bounds__(EV_THREADS) evict_select(const Evict e)
+{
+    constexpr int PER = EV_ONE / EV_THREADS;
+    __shared__ uint32_t hist[EV_BINS];
+    const Task t = task_of(e, blockIdx.x);
+    pad(e, t, 0, 1);
+    const uint32_t per = (t.n + EV_THREADS - 1) / EV_THREADS;
+    const uint32_t from = (threadIdx.x >> 6) * 64 * per;
+    Keys<PER> keys;
+    keys.load(e, t, from, per);
+    uint32_t prefix = 0, need = t.need;
+    if (need > 0)
+        for (int step = 0; step < EV_STEPS; ++step) {
+            hist[threadIdx.x] = 0;
+            hist[threadIdx.x + EV_THREADS] = 0;
+            __syncthreads();
+            keys.count(hist, step, prefix, per);
+            __syncthreads();
+            uint32_t bin;
+            find_bin(hist[EV_BINS - 1 - 2 * threadIdx.x], hist[EV_BINS - 2 - 2 * threadIdx.x], need,
+                     &bin, &need);
+            prefix = prefix << step_bits(step) | bin;
+        }
+    emit(e, t, keys, from, per, prefix, need, 0, 0);
+}
+
+// The same for more rows, a workgroup a chunk of EV_CHUNK: step s = 0, 1, 2 leaves the chunk's
+// histogram, after finding the bin of step s - 1 from all chunks' (every workgroup by itself);
+// step 3 writes the rows.  131072 rows: 209 -> ... us with one workgroup.
+template <int STEP>
+__global__ void __launch_bounds__(EV_THREADS) evict_step(const Evict e)
+{
+    constexpr int PER = EV_CHUNK / EV_THREADS;
+    __shared__ uint32_t hist[EV_BINS], sums[2];
+    const Task t = task_of(e, blockIdx.y);
+    const uint32_t chunk = blockIdx.x;
+    if (STEP == 3)
+        pad(e, t, chunk, e.chunks);
+    if (chunk * EV_CHUNK >= t.n && STEP == 3)
+        return;
+    const uint32_t from = chunk * EV_CHUNK + (threadIdx.x >> 6) * 64 * PER;
+    Keys<PER> keys;
+    keys.load(e, t, from, PER);
+    uint32_t *const mine = e.state + (t.set * e.chunks + chunk) * 8;
+    auto hist_of = [&](int step, uint32_t c) {
+        return e.hist + ((t.set * EV_STEPS + step) * e.chunks + c) * EV_BINS;
+    };
+    uint32_t prefix = 0, need = t.need, out0 = 0, ties0 = 0;
+    if (STEP > 0 && t.need > 0) {
+        // the previous step's bin, and this chunk's keys above it
+        if (STEP > 1) {
+            prefix = mine[2 * (STEP - 2)];
+            need = mine[2 * (STEP - 2) + 1];
+        }
+        const uint32_t b0 = EV_BINS - 1 - 2 * threadIdx.x;
+        uint32_t c0 = 0, c1 = 0, before0 = 0, before1 = 0;
+        for (uint32_t c = 0; c < e.chunks; ++c) {
+            if (STEP == 3 && c == chunk) {
+                before0 = c0;
+                before1 = c1;
+            }
+            const uint32_t *h = hist_of(STEP - 1, c);
+            c0 += h[b0];
+            c1 += h[b0 - 1];
+        }
+        uint32_t bin;
+        find_bin(c0, c1, need, &bin, &need);
+        prefix = prefix << step_bits(STEP - 1) | bin;
+        if (threadIdx.x < 2)
+            sums[threadIdx.x] = 0;
+        __syncthreads();
+        if (STEP == 3) {
+            // rows of earlier chunks: keys above (this step's; the others' from their
+            // workgroups) and ties
+            uint32_t x = (b0 > bin ? before0 : 0) + (b0 - 1 > bin && b0 > 0 ? before1 : 0);
+            for (uint32_t c = threadIdx.x; c < chunk; c += EV_THREADS) {
+                const uint32_t *s = e.state + (t.set * e.chunks + c) * 8;
+                x += s[4] + s[5];
+            }
+            x = sum_all(x);
+            if ((threadIdx.x & 63) == 0 && x)
+                atomicAdd(&sums[0], x);
+            if (b0 == bin)
+                sums[1] = before0;
+            if (b0 - 1 == bin)
+                sums[1] = before1;
+            __syncthreads();
+            out0 = sums[0];
+            ties0 = sums[1];
+        } else {
+            const uint32_t *h = hist_of(STEP - 1, chunk);
+            const uint32_t x = sum_all((b0 > bin ? h[b0] : 0) + (b0 - 1 > bin ? h[b0 - 1] : 0));
+            if ((threadIdx.x & 63) == 0 && x)
+                atomicAdd(&sums[0], x);
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                mine[2 * (STEP - 1)] = prefix;
+                mine[2 * (STEP - 1) + 1] = need;
+                mine[3 + STEP] = sums[0];
+            }
+        }
+    }
+    if constexpr (STEP == 3) {
+        // rows of earlier chunks outside [lo, hi)
+        const uint32_t row0 = chunk * EV_CHUNK;
+        out0 += row0 < t.lo ? row0 : t.lo;
+        out0 += row0 > t.hi ? row0 - t.hi : 0;
+        emit(e, t, keys, from, PER, prefix, need, out0, ties0);
+    } else {
+        hist[threadIdx.x] = 0;
+        hist[threadIdx.x + EV_THREADS] = 0;
+        __syncthreads();
+        if (t.need > 0)
+            keys.count(hist, STEP, prefix, PER);
+        __syncthreads();
+        uint32_t *h = hist_of(STEP, chunk);
+        h[threadIdx.x] = hist[threadIdx.x];
+        h[threadIdx.x + EV_THREADS] = hist[threadIdx.x + EV_THREADS];
     }
 }
 
@@ -185,10 +332,18 @@ __global__ void __launch_bounds__(256) evict_copy(const Evict e, uint32_t chunks
 
 }  // namespace
 
-hipError_t launch_evict(const Evict &e, int num_cus, hipStream_t s)
+hipError_t launch_evict(const Evict &e, hipStream_t s)
 {
-    (void)num_cus;
-    evict_select<<<dim3(e.src.batch * e.sets), EV_THREADS, 0, s>>>(e);
+    const uint32_t sets = e.src.batch * e.sets;
+    if (e.chunks == 0) {
+        evict_select<<<dim3(sets), EV_THREADS, 0, s>>>(e);
+    } else {
+        const dim3 grid(e.chunks, sets);
+        evict_step<0><<<grid, EV_THREADS, 0, s>>>(e);
+        evict_step<1><<<grid, EV_THREADS, 0, s>>>(e);
+        evict_step<2><<<grid, EV_THREADS, 0, s>>>(e);
+        evict_step<3><<<grid, EV_THREADS, 0, s>>>(e);
+    }
     hipError_t err = hipGetLastError();
     const uint32_t most = e.keep < e.src.room ? e.keep : e.src.room;
     if (err != hipSuccess || most == 0)

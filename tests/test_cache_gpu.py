@@ -551,15 +551,16 @@ def test_evict_narrow_weights_and_missing_pages():
     check_evict(c, w, 50, 2, 4)
 
 
-def test_evict_many_rows():
-    """More rows than one pass of a workgroup, one choice and one for each head."""
+@pytest.mark.parametrize("n,keep,levels", [(70001, 20000, 5000), (32768, 700, 3), (32769, 32000, 40),
+                                           (33000, 32999, 7), (90000, 110, 100000)])
+def test_evict_many_rows(n, keep, levels):
+    """More rows than one workgroup selects from, one choice and one for each head."""
     import torch
     import paper_2006_12608_amd as sj
-    say("evict many")
-    n, keep = 70001, 20000
+    say("evict many", n, keep)
     g = torch.Generator(device="cuda").manual_seed(3)
     for sets in (1, 2):
-        w = torch.randint(0, 5000, (1, sets, n), generator=g, device="cuda").float() / 64
+        w = torch.randint(0, levels, (1, sets, n), generator=g, device="cuda").float() / 64
         k = torch.randn((1, n, 2, 8), generator=g, device="cuda").half()
         k2, v2 = torch.zeros((1, keep, 2, 8), dtype=k.dtype, device="cuda"), \
             torch.zeros((1, keep, 2, 8), dtype=k.dtype, device="cuda")

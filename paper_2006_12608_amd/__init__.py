@@ -567,6 +567,15 @@ def jl_transform(X, shapes, As, ctx=None):
 _LAYOUTS = {"half": SJ_HALF, "interleaved": SJ_INTERLEAVED}
 
 
+def _current(device) -> int:
+    """The cached context of the device's current stream (context() without the stream
+    object, which costs more than the rest)."""
+    import torch
+    dev = device.index
+    handle = torch._C._cuda_getCurrentRawStream(dev)
+    return _contexts.get((dev, handle)) or context(dev)
+
+
 def _layout_code(layout: str) -> int:
     if layout not in _LAYOUTS:
         raise ValueError(f"layout must be 'half' or 'interleaved', not {layout!r}")
@@ -578,27 +587,22 @@ def _refuse(name, x, shape, dtype, device):
             any(s is not None and s != n for s, n in zip(shape, x.shape)):
         raise ValueError(f"{name}: {tuple(x.shape)} {x.dtype} on {x.device}, expected "
                          f"{tuple('any' if s is None else s for s in shape)} {dtype} on {device}")
-    raise ValueError(f"{name}: the elements of its last dimension must be adjacent")
+    if x.shape[-1] > 1 and x.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements of its last dimension must be adjacent")
 
 
 def _check_rows(name, x, shape, dtype, device):
     """x: a device tensor of `shape` (None: any size) and dtype whose last
     dimension is adjacent."""
-    size = x.shape
-    if len(size) == len(shape) and x.dtype is dtype and x.device == device and \
-            (x.stride(-1) == 1 or size[-1] <= 1):
-        for s, n in zip(shape, size):
-            if s is not None and s != n:
-                break
-        else:
-            return
-    _refuse(name, x, shape, dtype, device)
+    if x.shape != shape or x.dtype is not dtype or x.device != device or x.stride(-1) != 1:
+        _refuse(name, x, shape, dtype, device)
 
 
 def _check_whole(name, x, shape, dtype, device):
-    _check_rows(name, x, shape, dtype, device)
-    if not x.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if x.shape != shape or x.dtype is not dtype or x.device != device or not x.is_contiguous():
+        _refuse(name, x, shape, dtype, device)
+        if not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
 
 
 def _ptr(x):
@@ -674,14 +678,17 @@ def rotary(x, pos, turns, *, layout: str = "half", factor: float = 1.0, inverse:
     code = _layout_code(layout)
     if x.dtype not in (torch.float16, torch.bfloat16) or not x.is_cuda:
         raise ValueError("x must be a float16 or bfloat16 device tensor")
-    _check_rows("x", x, (None,) * 3, x.dtype, x.device)
+    dev = x.device
+    if x.dim() != 3 or x.stride(-1) != 1:
+        _refuse("x", x, (None,) * 3, x.dtype, dev)
     n, heads, d = x.shape
-    _check_whole("pos", pos, (n,), torch.int32, x.device)
-    _check_whole("turns", turns, (None,), torch.int64, x.device)
+    _check_whole("pos", pos, (n,), torch.int32, dev)
+    _check_whole("turns", turns, (turns.numel(),), torch.int64, dev)
     if out is None:
-        out = torch.empty((n, heads, d), dtype=x.dtype, device=x.device)
-    _check_rows("out", out, tuple(x.shape), x.dtype, x.device)
-    st = sj_rotary(ctx or context(x.device.index), dtype_code(x), _ptr(x), x.stride()[:2], _ptr(out),
+        out = x.new_empty(x.shape)
+    else:
+        _check_rows("out", out, x.shape, x.dtype, dev)
+    st = sj_rotary(ctx or _current(dev), dtype_code(x), _ptr(x), x.stride()[:2], _ptr(out),
                    out.stride()[:2], n, heads, d, _ptr(pos), _ptr(turns), turns.shape[0], code,
                    factor, SJ_FLAG_INVERSE if inverse else 0)
     if st != SJ_OK:
@@ -701,8 +708,10 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     import torch
     code = _layout_code(layout)
     B, dev = cache.batch, cache.device
-    _check_rows("key", key, (B, None, cache.heads, cache.d), cache.dtype, dev)
-    _check_rows("value", value, tuple(key.shape), cache.dtype, dev)
+    if key.dim() != 4:
+        _refuse("key", key, (B, None, cache.heads, cache.d), cache.dtype, dev)
+    _check_rows("key", key, (B, key.shape[1], cache.heads, cache.d), cache.dtype, dev)
+    _check_rows("value", value, key.shape, cache.dtype, dev)
     _check_whole("lengths", lengths, (B,), torch.int32, dev)
     if counts is not None:
         _check_whole("counts", counts, (B,), torch.int32, dev)
@@ -711,16 +720,19 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
         raise ValueError("pos and turns go together")
     if turns is not None:
         _check_whole("pos", pos, (B, t), torch.int32, dev)
-        _check_whole("turns", turns, (None,), torch.int64, dev)
+        _check_whole("turns", turns, (turns.numel(),), torch.int64, dev)
     args = ()
     if q is not None:
-        _check_rows("q", q, (B, t, None, cache.d), cache.dtype, dev)
+        if q.dim() != 4:
+            _refuse("q", q, (B, t, None, cache.d), cache.dtype, dev)
+        _check_rows("q", q, (B, t, q.shape[2], cache.d), cache.dtype, dev)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        _check_rows("q_out", q_out, tuple(q.shape), q.dtype, dev)
+            q_out = q.new_empty(q.shape)
+        else:
+            _check_rows("q_out", q_out, q.shape, q.dtype, dev)
         if q.numel():
             args = (q.data_ptr(), q.stride()[:3], q.shape[2], q_out.data_ptr(), q_out.stride()[:3])
-    st = sj_cache_append(ctx or context(dev.index), cache.raw, _ptr(lengths), _ptr(counts), t,
+    st = sj_cache_append(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(counts), t,
                          _ptr(key), key.stride()[:3], _ptr(value), value.stride()[:3], _ptr(pos),
                          _ptr(turns), 0 if turns is None else turns.shape[0], code, factor, *args)
     if st != SJ_OK:
@@ -745,18 +757,20 @@ def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=N
     where given (with weight None, of this call alone)."""
     import torch
     B, dev = cache.batch, cache.device
-    _check_rows("q", q, (B, None, None, cache.d), cache.dtype, dev)
+    if q.dim() != 4:
+        _refuse("q", q, (B, None, None, cache.d), cache.dtype, dev)
+    t, q_heads = q.shape[1], q.shape[2]
+    _check_rows("q", q, (B, t, q_heads, cache.d), cache.dtype, dev)
     _check_whole("lengths", lengths, (B,), torch.int32, dev)
     if counts is not None:
         _check_whole("counts", counts, (B,), torch.int32, dev)
-    t, q_heads = q.shape[1], q.shape[2]
     tree_stride = (0, 0)
     if tree is not None:
         words = (t + 63) // 64
         _check_rows("tree", tree, (1 if tree.shape[0] == 1 else B, t, words), torch.int64, dev)
         tree_stride = (0 if tree.shape[0] == 1 else tree.stride(0), tree.stride(1))
     if weight is not None:
-        _check_whole("weight", weight, (B, cache.heads, None), torch.float32, dev)
+        _check_whole("weight", weight, (B, cache.heads, weight.shape[-1]), torch.float32, dev)
         if weight_out is None:
             weight_out = weight
     cols = 0
@@ -765,10 +779,11 @@ def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=N
         _check_whole("weight_out", weight_out, (B, cache.heads, cols if weight is None else
                                                 weight.shape[2]), torch.float32, dev)
     if out is None:
-        out = torch.empty((B, t, q_heads, cache.d), dtype=cache.dtype, device=dev)
-    _check_whole("out", out, (B, t, q_heads, cache.d), cache.dtype, dev)
-    lse = torch.empty((B, t, q_heads), dtype=torch.float32, device=dev)
-    st = sj_attend(ctx or context(dev.index), cache.raw, _ptr(lengths), _ptr(counts), t, _ptr(q),
+        out = q.new_empty(q.shape)
+    else:
+        _check_whole("out", out, q.shape, cache.dtype, dev)
+    lse = q.new_empty((B, t, q_heads), dtype=torch.float32)
+    st = sj_attend(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(counts), t, _ptr(q),
                    q.stride()[:3], q_heads, _ptr(tree), tree_stride,
                    cache.d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse),
                    _ptr(weight), _ptr(weight_out), cols)
@@ -790,16 +805,19 @@ def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recen
     import torch
     B, dev = cache.batch, cache.device
     _check_whole("lengths", lengths, (B,), torch.int32, dev)
-    _check_whole("weight", weight, (B, None, None), torch.float32, dev)
+    if weight.dim() != 3:
+        _refuse("weight", weight, (B, None, None), torch.float32, dev)
+    _check_whole("weight", weight, (B, *weight.shape[1:]), torch.float32, dev)
     sets = weight.shape[1]
     if keep < 0 or sink < 0 or recent < 0:
         raise ValueError("keep, sink and recent must not be negative")
-    index = torch.empty((B, sets, keep), dtype=torch.int32, device=dev)
-    new = torch.empty((B,), dtype=torch.int32, device=dev)
+    index = lengths.new_empty((B, sets, keep))
+    new = lengths.new_empty((B,))
     if weight_out is None:
-        weight_out = torch.empty((B, sets, keep), dtype=torch.float32, device=dev)
-    _check_whole("weight_out", weight_out, (B, sets, None), torch.float32, dev)
-    st = sj_cache_evict(ctx or context(dev.index), cache.raw, _ptr(lengths), _ptr(weight), sets,
+        weight_out = weight.new_empty((B, sets, keep))
+    else:
+        _check_whole("weight_out", weight_out, (B, sets, weight_out.shape[-1]), torch.float32, dev)
+    st = sj_cache_evict(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(weight), sets,
                         weight.shape[2], keep, sink, recent, into.raw, _ptr(index), _ptr(new),
                         _ptr(weight_out), weight_out.shape[2])
     if st != SJ_OK:

@@ -150,6 +150,33 @@ int grow_front(sj_ctx *c, size_t bytes)
     return SJ_OK;
 }
 
+int grow_arrivals(sj_ctx *c, size_t n)
+{
+    if (n <= c->arrivals_n)
+        return SJ_OK;
+    if (c->arrivals) {
+        (void)hipStreamSynchronize(c->stream);
+        (void)hipFree(c->arrivals);
+        c->arrivals = nullptr;
+        c->arrivals_n = 0;
+    }
+    n = (n + 1023) & ~(size_t)1023;
+    if (hipMalloc(&c->arrivals, n * 4) != hipSuccess) {
+        (void)hipGetLastError();
+        c->arrivals = nullptr;
+        return fail(SJ_E_NOMEM, "cannot allocate %zu counters", n);
+    }
+    const hipError_t e =
+        sjk::launch_zero_u64((unsigned long long *)c->arrivals, (uint32_t)(n / 2), c->stream);
+    if (e != hipSuccess) {
+        (void)hipFree(c->arrivals);
+        c->arrivals = nullptr;
+        return hip_fail(e, "clearing the counters");
+    }
+    c->arrivals_n = n;
+    return SJ_OK;
+}
+
 double elapsed_ms(hipEvent_t a, hipEvent_t b)
 {
     float ms = 0.f;
@@ -765,6 +792,8 @@ void sj_destroy(sj_ctx *c)
         (void)hipFree(c->scratch);
     if (c->front)
         (void)hipFree(c->front);
+    if (c->arrivals)
+        (void)hipFree(c->arrivals);
     if (c->d_small)
         (void)hipFree(c->d_small);
     if (c->h_small)

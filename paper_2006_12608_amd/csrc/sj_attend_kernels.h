@@ -287,6 +287,88 @@ __device__ __forceinline__ bool find_share(const Attend &a, uint32_t slot, Share
     return false;
 }
 
+__device__ __forceinline__ float max_all(float x)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1)
+        x = fmaxf(x, __shfl_xor(x, o));
+    return x;
+}
+
+// Place of query row r of head h among the results of share s.
+__device__ __forceinline__ uint64_t part_of(const Attend &a, uint32_t s, uint32_t h, uint32_t r,
+                                            uint32_t QT)
+{
+    return ((uint64_t)s * a.c.heads * a.tiles + h * a.tiles + r / QT) * QT + r % QT;
+}
+
+// The last workgroup of a sequence, head and tile to arrive joins their shares, in the shares'
+// order whichever it is: a kernel of its own for that costs a single decoded token 4 of 14 us.
+// Every thread's results are made visible to the device before the workgroup is
+// counted; the counter is 0 again for the next call.
+template <int DT, uint32_t QT, uint32_t D>
+__device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t h, uint32_t unit,
+                                          uint32_t slot, uint32_t shares, uint32_t count)
+{
+    typedef Elem<DT> E;
+    __shared__ uint32_t arrived;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t *n = a.arrivals + (uint64_t)b * a.c.heads * a.tiles + unit;
+        arrived = __hip_atomic_fetch_add(n, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (arrived == shares - 1)
+            __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (arrived != shares - 1)
+        return;
+    __threadfence();
+    const uint64_t first = (uint64_t)slot * a.c.heads * a.tiles + unit;
+    const uint64_t step = (uint64_t)a.c.heads * a.tiles;
+    // 16 threads a query row, columns 4 (threadIdx.x % 16) + 64 k
+    for (uint32_t q0 = 0; q0 < QT; q0 += 16) {
+        const uint32_t qi = q0 + (threadIdx.x >> 4), x = threadIdx.x & 15;
+        const uint32_t r = unit % a.tiles * QT + qi, u = a.by_group.quot(r);
+        auto at = [&](uint32_t s) { return (first + s * step) * QT + qi; };
+        if (r >= a.t * a.group)
+            continue;
+        float top = -INFINITY;
+        for (uint32_t s = x; s < shares; s += 16)
+            top = fmaxf(top, a.part_ml[2 * at(s)]);
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1)
+            top = fmaxf(top, __shfl_xor(top, o));
+        const bool live = u < count && top != -INFINITY;
+        const float base = top == -INFINITY ? 0.f : top;
+        f32x4 o[D / 64] = {};
+        float l = 0.f;
+#pragma unroll 4
+        for (uint32_t s = 0; s < shares; ++s) {
+            const uint64_t p = at(s);
+            const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * p);
+            const float f = exp2_(ml[0] - base);
+            l += ml[1] * f;
+#pragma unroll
+            for (uint32_t k = 0; k < D / 64; ++k)
+                o[k] += *(const f32x4 *)(a.part_o + p * D + 64 * k + 4 * x) * f;
+        }
+        const float inv = live ? 1.f / l : 0.f;
+        const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group;
+#pragma unroll
+        for (uint32_t k = 0; k < D / 64; ++k)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const uint32_t c = 64 * k + 4 * x + e;
+                if (c < a.c.d)
+                    a.out[row * a.c.d + c] =
+                        __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[k][e] * inv : 0.f));
+            }
+        if (x == 0)
+            a.lse[row] = live ? (top + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+    }
+}
+
 // ------------------------------------------------------------- the split kernel
 //
 // A workgroup takes one share of a sequence's rows for one cache head and one
@@ -591,6 +673,8 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             }
         }
     }
+    if (shares > 1 && a.arrivals)
+        join_last<DT, QT, D>(a, b, h, unit, slot - sh.share, shares, rows.count);
 }
 
 // ------------------------------------------------------------- the tiled kernel
@@ -979,21 +1063,6 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
             a.lse[row] = some ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
         }
     }
-}
-
-__device__ __forceinline__ float max_all(float x)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1)
-        x = fmaxf(x, __shfl_xor(x, o));
-    return x;
-}
-
-// Place of query row r of head h among the results of share s.
-__device__ __forceinline__ uint64_t part_of(const Attend &a, uint32_t s, uint32_t h, uint32_t r,
-                                            uint32_t QT)
-{
-    return ((uint64_t)s * a.c.heads * a.tiles + h * a.tiles + r / QT) * QT + r % QT;
 }
 
 // Joins the shares of query row `row` of the batch, if it has more than one: a workgroup
@@ -1457,11 +1526,14 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
         attend_kernel<DT, DC, EXACT>(qt)<<<grid, 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
-        const uint32_t strips =
-            a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
-        attend_join<DT><<<dim3((uint32_t)rows + strips), 256, 0, s>>>(a, qt, 32 * DC, (uint32_t)rows);
-        if ((e = hipGetLastError()) != hipSuccess || a.scores)
-            return e;
+        if (!a.arrivals) {
+            const uint32_t strips =
+                a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
+            attend_join<DT><<<dim3((uint32_t)rows + strips), 256, 0, s>>>(a, qt, 32 * DC,
+                                                                          (uint32_t)rows);
+            if ((e = hipGetLastError()) != hipSuccess || a.scores)
+                return e;
+        }
     }
     if (!a.w_out || !a.w_cols)
         return hipSuccess;

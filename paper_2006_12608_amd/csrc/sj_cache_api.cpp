@@ -332,6 +332,11 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     a.plan = (uint32_t *)s;
+    if (qt <= 32 && !keep) {
+        if ((st = grow_arrivals(c, (size_t)B * units)) != SJ_OK)
+            return st;
+        a.arrivals = c->arrivals;
+    }
     a.lse = lse ? lse : (float *)(s + off_lse);
     a.part_ml = (float *)(s + off_ml);
     a.part_o = (float *)(s + off_o);

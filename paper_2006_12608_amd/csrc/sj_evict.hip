@@ -15,16 +15,12 @@ __device__ __forceinline__ uint32_t order_key(float w)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t EV_THREADS = 1024, EV_WAVES = EV_THREADS / 64;
 constexpr int EV_STEPS = 3;
 // key bits of the three steps, from the top
 __device__ __forceinline__ uint32_t step_bits(int step) { return step == 2 ? 10 : 11; }
 __device__ __forceinline__ uint32_t bits_before(int step) { return 11 * step; }
-
-__device__ __forceinline__ float weight_at(const Evict &e, const float *w, uint32_t n)
-{
-    return n < e.w_cols ? w[n] : 0.f;
-}
 
 // What one set (a sequence and a head, or a sequence) keeps of its n rows: all m = n, or the
 // rows outside [lo, hi) and `need` of those inside.
@@ -48,30 +44,40 @@ __device__ __forceinline__ Task task_of(const Evict &e, uint64_t set)
     return t;
 }
 
-// Keys of the rows from + 64 k + lane, k < per (PER at most), of a wave; 0 outside [lo, hi)
-// (below every key in use: -inf is 0x007fffff).
+// Weights of the rows from + 64 k + lane, k < PER, of a wave, loaded once and all
+// at once (loads under conditions of their own wait for each other).
 template <int PER>
-struct Keys {
-    uint32_t key[PER];
-    __device__ __forceinline__ void load(const Evict &e, const Task &t, uint32_t from, uint32_t per)
+struct Rows {
+    float w[PER];
+    __device__ __forceinline__ void load(const Evict &e, const Task &t, uint32_t from)
     {
-        const uint32_t lane = threadIdx.x & 63;
+        const uint32_t lane = threadIdx.x & 63, cols = (uint32_t)e.w_cols;
+        const float *p = cols ? t.w : (const float *)e.len;     // (anything readable)
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const uint32_t i = from + 64 * k + lane;
-            key[k] = 0;
-            if ((uint32_t)k < per && i >= t.lo && i < t.hi)
-                key[k] = order_key(weight_at(e, t.w, i));
+            w[k] = p[i < cols ? i : (cols ? cols - 1 : 0)];
         }
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            w[k] = from + 64 * k + lane < cols ? w[k] : 0.f;
+    }
+    // key of row i in w[k]; 0 outside [lo, hi) (below every key: -inf is 0x007fffff)
+    __device__ __forceinline__ uint32_t key(const Task &t, int k, uint32_t i) const
+    {
+        return i >= t.lo && i < t.hi ? order_key(w[k]) : 0;
     }
     // adds the digit of `step` of every key whose higher bits are `prefix` to hist
-    __device__ __forceinline__ void count(uint32_t *hist, int step, uint32_t prefix, uint32_t per)
+    __device__ __forceinline__ void count(const Task &t, uint32_t *hist, uint32_t from, int step,
+                                          uint32_t prefix) const
     {
         const uint32_t bits = step_bits(step), known = bits_before(step), shift = 32 - known - bits;
 #pragma unroll
-        for (int k = 0; k < PER; ++k)
-            if ((uint32_t)k < per && key[k] && (known == 0 || key[k] >> (32 - known) == prefix))
-                atomicAdd(&hist[(key[k] >> shift) & ((1u << bits) - 1)], 1u);
+        for (int k = 0; k < PER; ++k) {
+            const uint32_t x = key(t, k, from + 64 * k + (threadIdx.x & 63));
+            if (x && (known == 0 || x >> (32 - known) == prefix))
+                atomicAdd(&hist[(x >> shift) & ((1u << bits) - 1)], 1u);
+        }
     }
 };
 
@@ -106,8 +112,8 @@ __device__ __forceinline__ void find_bin(uint32_t c0, uint32_t c1, uint32_t need
 // of those equal to it the first `need` (over all waves).  Rows and ties before the
 // workgroup's come in out0 and ties0.  Called by the whole workgroup.
 template <int PER>
-__device__ __forceinline__ void emit(const Evict &e, const Task &t, const Keys<PER> &keys,
-                                     uint32_t from, uint32_t per, uint32_t last, uint32_t need,
+__device__ __forceinline__ void emit(const Evict &e, const Task &t, const Rows<PER> &rows,
+                                     uint32_t from, uint32_t last, uint32_t need,
                                      uint32_t out0, uint32_t ties0)
 {
     __shared__ uint32_t above[EV_WAVES], ties[EV_WAVES];
@@ -115,13 +121,13 @@ __device__ __forceinline__ void emit(const Evict &e, const Task &t, const Keys<P
     const uint64_t below = ((uint64_t)1 << lane) - 1;
     uint32_t n_above = 0, n_ties = 0;
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-        if ((uint32_t)k < per) {
-            const uint32_t i = from + 64 * k + lane;
-            const bool mid = i >= t.lo && i < t.hi;
-            n_above += __popcll(__ballot(i < t.n && (!mid || (need && keys.key[k] > last))));
-            n_ties += __popcll(__ballot(mid && need && keys.key[k] == last));
-        }
+    for (int k = 0; k < PER; ++k) {
+        const uint32_t i = from + 64 * k + lane;
+        const bool mid = i >= t.lo && i < t.hi;
+        const uint32_t x = rows.key(t, k, i);
+        n_above += __popcll(__ballot(i < t.n && (!mid || (need && x > last))));
+        n_ties += __popcll(__ballot(mid && need && x == last));
+    }
     if (lane == 0) {
         above[wave] = n_above;
         ties[wave] = n_ties;
@@ -134,24 +140,24 @@ __device__ __forceinline__ void emit(const Evict &e, const Task &t, const Keys<P
     }
     out += tied < need ? tied : need;
 #pragma unroll
-    for (int k = 0; k < PER; ++k)
-        if ((uint32_t)k < per) {
-            const uint32_t i = from + 64 * k + lane;
-            const bool mid = i >= t.lo && i < t.hi;
-            const bool tie = mid && need && keys.key[k] == last;
-            const uint64_t tie_mask = __ballot(tie);
-            const bool kept = i < t.n && (!mid || (need && keys.key[k] > last) ||
-                                          (tie && tied + __popcll(tie_mask & below) < need));
-            const uint64_t kept_mask = __ballot(kept);
-            if (kept) {
-                const uint32_t j = out + __popcll(kept_mask & below);
-                e.index[t.set * e.keep + j] = (int32_t)i;
-                if (e.w_out && j < e.w_out_cols)
-                    e.w_out[t.set * e.w_out_cols + j] = weight_at(e, t.w, i);
-            }
-            out += __popcll(kept_mask);
-            tied += __popcll(tie_mask);
+    for (int k = 0; k < PER; ++k) {
+        const uint32_t i = from + 64 * k + lane;
+        const bool mid = i >= t.lo && i < t.hi;
+        const uint32_t x = rows.key(t, k, i);
+        const bool tie = mid && need && x == last;
+        const uint64_t tie_mask = __ballot(tie);
+        const bool kept = i < t.n && (!mid || (need && x > last) ||
+                                      (tie && tied + __popcll(tie_mask & below) < need));
+        const uint64_t kept_mask = __ballot(kept);
+        if (kept) {
+            const uint32_t j = out + __popcll(kept_mask & below);
+            e.index[t.set * e.keep + j] = (int32_t)i;
+            if (e.w_out && j < e.w_out_cols)
+                e.w_out[t.set * e.w_out_cols + j] = rows.w[k];
         }
+        out += __popcll(kept_mask);
+        tied += __popcll(tie_mask);
+    }
 }
 
 // -1 and 0 past the kept rows, by `share` of `shares` workgroups; the new length.
@@ -168,34 +174,32 @@ __device__ __forceinline__ void pad(const Evict &e, const Task &t, uint32_t shar
 }
 
 // The kept rows of one set, in order: a workgroup a set of up to EV_ONE rows, each wave a
-// stretch of them, the keys in registers.  Radix selection of the last key that stays: three
+// stretch of them, the weights in registers.  Radix selection of the last key that stays: three
 // histograms of 11, 11 and 10 key bits, each over the keys whose higher bits are
-// those of the key sought.  16 sets of 3000 rows 13 -> ... us with the keys read
-// from memory in every pass.
+// those of the key sought.
+template <int PER>
 __global__ void __launch_bounds__(EV_THREADS) evict_select(const Evict e)
 {
-    constexpr int PER = EV_ONE / EV_THREADS;
     __shared__ uint32_t hist[EV_BINS];
     const Task t = task_of(e, blockIdx.x);
     pad(e, t, 0, 1);
-    const uint32_t per = (t.n + EV_THREADS - 1) / EV_THREADS;
-    const uint32_t from = (threadIdx.x >> 6) * 64 * per;
-    Keys<PER> keys;
-    keys.load(e, t, from, per);
+    const uint32_t from = (threadIdx.x >> 6) * 64 * PER;
+    Rows<PER> rows;
+    rows.load(e, t, from);
     uint32_t prefix = 0, need = t.need;
     if (need > 0)
         for (int step = 0; step < EV_STEPS; ++step) {
             hist[threadIdx.x] = 0;
             hist[threadIdx.x + EV_THREADS] = 0;
             __syncthreads();
-            keys.count(hist, step, prefix, per);
+            rows.count(t, hist, from, step, prefix);
             __syncthreads();
             uint32_t bin;
             find_bin(hist[EV_BINS - 1 - 2 * threadIdx.x], hist[EV_BINS - 2 - 2 * threadIdx.x], need,
                      &bin, &need);
             prefix = prefix << step_bits(step) | bin;
         }
-    emit(e, t, keys, from, per, prefix, need, 0, 0);
+    emit(e, t, rows, from, prefix, need, 0, 0);
 }
 
 // The same for more rows, a workgroup a chunk of EV_CHUNK: step s = 0, 1, 2 leaves the chunk's
@@ -213,8 +217,8 @@ __global__ void __launch_bounds__(EV_THREADS) evict_step(const Evict e)
     if (chunk * EV_CHUNK >= t.n && STEP == 3)
         return;
     const uint32_t from = chunk * EV_CHUNK + (threadIdx.x >> 6) * 64 * PER;
-    Keys<PER> keys;
-    keys.load(e, t, from, PER);
+    Rows<PER> rows;
+    rows.load(e, t, from);
     uint32_t *const mine = e.state + (t.set * e.chunks + chunk) * 8;
     auto hist_of = [&](int step, uint32_t c) {
         return e.hist + ((t.set * EV_STEPS + step) * e.chunks + c) * EV_BINS;
@@ -228,14 +232,19 @@ __global__ void __launch_bounds__(EV_THREADS) evict_step(const Evict e)
         }
         const uint32_t b0 = EV_BINS - 1 - 2 * threadIdx.x;
         uint32_t c0 = 0, c1 = 0, before0 = 0, before1 = 0;
-        for (uint32_t c = 0; c < e.chunks; ++c) {
-            if (STEP == 3 && c == chunk) {
-                before0 = c0;
-                before1 = c1;
+        for (uint32_t c8 = 0; c8 < e.chunks; c8 += 8) {
+            u32x2 h[8];     // (eight loads at once)
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x)
+                h[x] = *(const u32x2 *)(hist_of(STEP - 1, c8 + x < e.chunks ? c8 + x : 0) + b0 - 1);
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) {
+                const bool in = c8 + x < e.chunks, early = c8 + x < chunk;
+                c0 += in ? h[x][1] : 0;
+                c1 += in ? h[x][0] : 0;
+                before0 += early ? h[x][1] : 0;
+                before1 += early ? h[x][0] : 0;
             }
-            const uint32_t *h = hist_of(STEP - 1, c);
-            c0 += h[b0];
-            c1 += h[b0 - 1];
         }
         uint32_t bin;
         find_bin(c0, c1, need, &bin, &need);
@@ -279,13 +288,13 @@ __global__ void __launch_bounds__(EV_THREADS) evict_step(const Evict e)
         const uint32_t row0 = chunk * EV_CHUNK;
         out0 += row0 < t.lo ? row0 : t.lo;
         out0 += row0 > t.hi ? row0 - t.hi : 0;
-        emit(e, t, keys, from, PER, prefix, need, out0, ties0);
+        emit(e, t, rows, from, prefix, need, out0, ties0);
     } else {
         hist[threadIdx.x] = 0;
         hist[threadIdx.x + EV_THREADS] = 0;
         __syncthreads();
         if (t.need > 0)
-            keys.count(hist, STEP, prefix, PER);
+            rows.count(t, hist, from, STEP, prefix);
         __syncthreads();
         uint32_t *h = hist_of(STEP, chunk);
         h[threadIdx.x] = hist[threadIdx.x];
@@ -336,7 +345,13 @@ hipError_t launch_evict(const Evict &e, hipStream_t s)
 {
     const uint32_t sets = e.src.batch * e.sets;
     if (e.chunks == 0) {
-        evict_select<<<dim3(sets), EV_THREADS, 0, s>>>(e);
+        // (registers, and code, for no more rows than there can be)
+        if (e.src.room <= EV_ONE / 8)
+            evict_select<EV_ONE / 8 / EV_THREADS><<<dim3(sets), EV_THREADS, 0, s>>>(e);
+        else if (e.src.room <= EV_ONE / 2)
+            evict_select<EV_ONE / 2 / EV_THREADS><<<dim3(sets), EV_THREADS, 0, s>>>(e);
+        else
+            evict_select<EV_ONE / EV_THREADS><<<dim3(sets), EV_THREADS, 0, s>>>(e);
     } else {
         const dim3 grid(e.chunks, sets);
         evict_step<0><<<grid, EV_THREADS, 0, s>>>(e);

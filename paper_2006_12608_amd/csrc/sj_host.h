@@ -24,6 +24,8 @@ struct sj_ctx {
     size_t scratch_bytes = 0;
     void *front = nullptr;        // rows made by the front ends (normalised or
     size_t front_bytes = 0;       // unpacked), kept apart from the join's scratch
+    uint32_t *arrivals = nullptr; // counters of sj_attend's workgroups: 0 between kernels
+    size_t arrivals_n = 0;
     hipEvent_t ev[6] = {};
     sj_stats stats = {};
 };
@@ -60,6 +62,9 @@ int grow_scratch(sj_ctx *c, size_t bytes);
 
 // Grows the context's front-end buffer to at least `bytes` (contents not kept).
 int grow_front(sj_ctx *c, size_t bytes);
+
+// Makes c->arrivals hold at least n zeros (kernels that use them leave zeros behind).
+int grow_arrivals(sj_ctx *c, size_t n);
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 

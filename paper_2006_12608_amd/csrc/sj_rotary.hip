@@ -164,7 +164,12 @@ hipError_t launch_rotary(const Rotary &r, hipStream_t s)
     g.by_v = by(v_chunks);
     g.by_t = by(r.t);
     g.by_pairs = by(8 * g.turned);
+    // one token a workgroup while that leaves CUs idle or its sines fill the table; else up to
+    // four, so that the last round of its threads weighs less (8 x 2048 tokens of 48
+    // heads: MEASURED)
     g.tokens = 1;
+    while (g.tokens < 4 && g.n / (2 * g.tokens) >= 4096 && 2 * g.tokens * 8 * g.turned <= RO_PAIRS)
+        g.tokens *= 2;
     const dim3 grid((uint32_t)((g.n + g.tokens - 1) / g.tokens));
     const bool half = r.turn.layout == 0;
     if (r.dtype == sjk::DT_F16) {

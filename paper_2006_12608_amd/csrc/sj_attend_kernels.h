@@ -97,6 +97,14 @@ __device__ __forceinline__ i32x4 column8(const uint8_t *lo, const uint8_t *hi)
 // round's own loads.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
+// LDS written by the wave's lanes is there for its other lanes.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // 2^x, 2^-inf = 0.
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -198,8 +206,10 @@ __device__ __forceinline__ void seen_rows(const Attend &a, uint32_t b, const Row
                                           uint32_t n, uint32_t q_rows, uint32_t row0, uint64_t there,
                                           uint64_t *vis)
 {
+    wave_sync();        // (the last rows have been read)
     for (uint32_t i = threadIdx.x & 63; i < n; i += 64)
         vis[i] = r0 + i < q_rows ? there & seen64(a, b, r, a.by_group.quot(r0 + i), row0) : 0;
+    wave_sync();
 }
 
 // -inf for the scores of key row n (of 64) that the query rows v[8 (e / 4) + e % 4] do not see.
@@ -303,27 +313,40 @@ __device__ __forceinline__ uint64_t part_of(const Attend &a, uint32_t s, uint32_
 }
 
 // The last workgroup of a sequence, head and tile to arrive joins their shares, in the shares'
-// order whichever it is: a kernel of its own for that costs a single decoded token 4 of 14 us.
-// Every thread's results are made visible to the device before the workgroup is
-// counted; the counter is 0 again for the next call.
+// order whichever it is.  The shares' results travel as relaxed atomic stores and loads of the
+// device's scope, which pass by the XCDs' own caches: a fence would write back and
+// drop a whole cache instead.  Each wave waits for its stores before the
+// workgroup is counted; the counter is 0 again for the next call.
+__device__ __forceinline__ void put2(float *p, float x, float y)
+{
+    const uint64_t v = (uint64_t)__float_as_uint(x) | (uint64_t)__float_as_uint(y) << 32;
+    __hip_atomic_store((uint64_t *)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ f32x2 get2(const float *p)
+{
+    const uint64_t v =
+        __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+
 template <int DT, uint32_t QT, uint32_t D>
 __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t h, uint32_t unit,
                                           uint32_t slot, uint32_t shares, uint32_t count)
 {
     typedef Elem<DT> E;
     __shared__ uint32_t arrived;
-    __threadfence();
+    wait_loads();       // (stores count as loads do)
     __syncthreads();
     if (threadIdx.x == 0) {
         uint32_t *n = a.arrivals + (uint64_t)b * a.c.heads * a.tiles + unit;
-        arrived = __hip_atomic_fetch_add(n, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        arrived = __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (arrived == shares - 1)
             __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (arrived != shares - 1)
         return;
-    __threadfence();
     const uint64_t first = (uint64_t)slot * a.c.heads * a.tiles + unit;
     const uint64_t step = (uint64_t)a.c.heads * a.tiles;
     // 16 threads a query row, columns 4 (threadIdx.x % 16) + 64 k
@@ -335,7 +358,7 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
             continue;
         float top = -INFINITY;
         for (uint32_t s = x; s < shares; s += 16)
-            top = fmaxf(top, a.part_ml[2 * at(s)]);
+            top = fmaxf(top, get2(a.part_ml + 2 * at(s))[0]);
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1)
             top = fmaxf(top, __shfl_xor(top, o));
@@ -346,12 +369,15 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
 #pragma unroll 4
         for (uint32_t s = 0; s < shares; ++s) {
             const uint64_t p = at(s);
-            const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * p);
+            const f32x2 ml = get2(a.part_ml + 2 * p);
             const float f = exp2_(ml[0] - base);
             l += ml[1] * f;
 #pragma unroll
-            for (uint32_t k = 0; k < D / 64; ++k)
-                o[k] += *(const f32x4 *)(a.part_o + p * D + 64 * k + 4 * x) * f;
+            for (uint32_t k = 0; k < D / 64; ++k) {
+                const float *y = a.part_o + p * D + 64 * k + 4 * x;
+                const f32x2 lo = get2(y), hi = get2(y + 2);
+                o[k] += f32x4{lo[0], lo[1], hi[0], hi[1]} * f;
+            }
         }
         const float inv = live ? 1.f / l : 0.f;
         const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group;
@@ -428,6 +454,16 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     const uint32_t d = a.c.d;
     const uint32_t q_rows = a.t * a.group;
 
+    // the first blocks' page numbers, on their way with the queries
+    auto entry = [&](uint32_t blk) {
+        return entry_of(a.c, a.len, b, blk * AT_ROWS + (lane & 31));
+    };
+    Entry first_at = {0, 0u}, ahead = {0, 0u};
+    if (first + wave < last) {
+        first_at = entry(first + wave);
+        ahead = entry(first + wave + AT_WAVES);
+    }
+
     // queries: lane l holds query l % 16 of each tile in operand layout
     i32x4 Q[NQ][DC];
     uint32_t tok[NQ];
@@ -443,8 +479,8 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             Q[j][c] = there ? load_q8(a, p + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4))
                             : i32x4{0, 0, 0, 0};
     }
-    wait_loads();
 
+    wait_loads();
     f32x4 O[NQ][NV];
     float m[NQ], l[NQ];
 #pragma unroll
@@ -461,9 +497,6 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 
     // place of row lane % 32 of a block: absent rows read page 0, row 0 (their
     // scores and values are replaced below)
-    auto entry = [&](uint32_t blk) {
-        return entry_of(a.c, a.len, b, blk * AT_ROWS + (lane & 31));
-    };
     auto place = [&](const Entry &e) { return place_of(a.c, b, e, to); };
     i32x4 K[2][DC], V[NV];
     auto load_k = [&](const Place &p) {
@@ -493,10 +526,8 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     __syncthreads();
     uint32_t blk = first + wave;
     Place cur = {-1, 0u}, nxt = {-1, 0u};
-    Entry ahead = {0, 0u};
     if (blk < last) {
-        cur = place(entry(blk));
-        ahead = entry(blk + AT_WAVES);
+        cur = place(first_at);
         load_k(cur);
         load_v(cur);
     }
@@ -651,7 +682,13 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                                 o[e] += odd_part<DT>(v[c + e]);
                     });
                 if (shares > 1) {
-                    *(f32x4 *)(a.part_o + (part * QT + AT_Q * j + qi) * D + c) = o;
+                    float *p = a.part_o + (part * QT + AT_Q * j + qi) * D + c;
+                    if (a.arrivals) {
+                        put2(p, o[0], o[1]);
+                        put2(p + 2, o[2], o[3]);
+                    } else {
+                        *(f32x4 *)p = o;
+                    }
                 } else {
                     const float inv = live && tot != -INFINITY ? 1.f / sum : 0.f;
 #pragma unroll
@@ -663,8 +700,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             }
             if (c0 == 0) {
                 if (shares > 1) {
-                    a.part_ml[(part * QT + AT_Q * j + qi) * 2] = tot;
-                    a.part_ml[(part * QT + AT_Q * j + qi) * 2 + 1] = sum;
+                    put2(a.part_ml + (part * QT + AT_Q * j + qi) * 2, tot, sum);
                 } else {
                     a.lse[row] = live && tot != -INFINITY
                                      ? (tot + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f
@@ -1065,15 +1101,17 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     }
 }
 
-// Joins the shares of query row `row` of the batch, if it has more than one: a workgroup
-// a row.  Groups of D / 4 threads take every 1024 / D-th share, four elements a thread;
-// the groups' sums join through LDS.
-template <int DT>
+// Joins the shares of query row `row` of the batch, if it has more than one, by T = 64 or 256
+// threads.  Groups of D / 4 of them take every 4 T / D-th share, four elements a thread; the
+// groups' sums join through LDS.  A wave a row where there are many rows (8192 rows of
+// 8 shares: 15 -> 9 us), a workgroup where there are few (64 rows of 33 shares: 15 -> 5).
+template <int DT, uint32_t T>
 __device__ __forceinline__ void join_row(const Attend &a, uint32_t QT, uint32_t D, uint64_t row)
 {
     typedef Elem<DT> E;
     __shared__ f32x4 sums[256];
-    const uint32_t lane = threadIdx.x & 63;
+    __shared__ float ls[4][16];
+    const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x % T, mine = threadIdx.x / T;
     const uint32_t head = (uint32_t)(row % a.q_heads);
     const uint32_t u = (uint32_t)(row / a.q_heads % a.t), b = (uint32_t)(row / a.q_heads / a.t);
     const uint32_t slot = a.plan[2 * b], shares = a.plan[2 * b + 1];
@@ -1086,28 +1124,31 @@ __device__ __forceinline__ void join_row(const Attend &a, uint32_t QT, uint32_t 
     top = max_all(top);
     const bool live = u < rows_of(a, b).count && top != -INFINITY;
     const float base = top == -INFINITY ? 0.f : top;
-    const uint32_t per = D / 4, c = 4 * (threadIdx.x % per), groups = 256 / per;
+    const uint32_t per = D / 4, c = 4 * (tid % per), groups = T / per;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    for (uint32_t s = threadIdx.x / per; s < shares; s += groups) {
+#pragma unroll 4
+    for (uint32_t s = tid / per; s < shares; s += groups) {
         const uint64_t p = part_of(a, slot + s, h, r, QT);
         const f32x2 ml = *(const f32x2 *)(a.part_ml + 2 * p);
         const float f = exp2_(ml[0] - base);
         o += *(const f32x4 *)(a.part_o + p * D + c) * f;
         l += ml[1] * f;
     }
-    __shared__ float ls[16];
-    if (threadIdx.x % per == 0)
-        ls[threadIdx.x / per] = l;
+    if (tid % per == 0)
+        ls[mine][tid / per] = l;
     sums[threadIdx.x] = o;
-    __syncthreads();
-    if (threadIdx.x >= per)
+    if (T == 256)
+        __syncthreads();
+    else
+        wave_sync();
+    if (tid >= per)
         return;
     l = 0.f;
     o = f32x4{0.f, 0.f, 0.f, 0.f};
     for (uint32_t g = 0; g < groups; ++g) {
-        o += sums[g * per + threadIdx.x];
-        l += ls[g];
+        o += sums[mine * T + g * per + tid];
+        l += ls[mine][g];
     }
     const float inv = live ? 1.f / l : 0.f;
 #pragma unroll
@@ -1115,7 +1156,7 @@ __device__ __forceinline__ void join_row(const Attend &a, uint32_t QT, uint32_t 
         if (c + e < a.c.d)
             a.out[row * a.c.d + c + e] =
                 __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[e] * inv : 0.f));
-    if (threadIdx.x == 0)
+    if (tid == 0)
         a.lse[row] = live ? (top + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
 }
 
@@ -1183,16 +1224,21 @@ __device__ __forceinline__ void weigh_scores(const Attend &a, uint32_t QT, uint3
             a.w_out[at + e] = (a.w_in ? a.w_in[at + e] : 0.f) + (n0 + e < rows.end ? w[e] : 0.f);
 }
 
-// What is left once the shares are there: workgroups below n_rows join a query row each,
-// those from n_rows on weigh columns from the scores.
+// What is left once the shares are there: the first `joins` workgroups join query rows (one each,
+// or four), the others weigh columns from the scores.
 template <int DT>
 __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, uint32_t D,
-                                                   uint32_t n_rows)
+                                                   uint32_t joins, bool four)
 {
-    if (blockIdx.x < n_rows)
-        join_row<DT>(a, QT, D, blockIdx.x);
-    else
-        weigh_scores(a, QT, blockIdx.x - n_rows);
+    if (blockIdx.x >= joins) {
+        weigh_scores(a, QT, blockIdx.x - joins);
+    } else if (!four) {
+        join_row<DT, 256>(a, QT, D, blockIdx.x);
+    } else {
+        const uint64_t row = (uint64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (row < (uint64_t)a.c.batch * a.t * a.q_heads)
+            join_row<DT, 64>(a, QT, D, row);
+    }
 }
 
 // Weights: w_out[b, h, n] = w_in[b, h, n] + sum over the query rows r that read head h of
@@ -1381,14 +1427,25 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
     // query rows and their lse; rows past the end are zeros and weigh nothing
     const uint32_t n_q = (q_rows + 31) / 32;
     const int flip = a.negate ? (int)0x80008000 : 0;    // (as load_q8)
-    for (uint32_t i = tid; i < n_q * 32 * CPR; i += 256) {
-        const uint32_t r = i / CPR, c = i % CPR, u = a.by_group.quot(r);
-        i32x4 v = {0, 0, 0, 0};
-        if (r < q_rows)
-            v = load8(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
-                          (int64_t)(h * a.group + r - u * a.group) * a.q_head + 8 * c,
-                      EXACT ? 8 : (int)d - (int)(8 * c));
-        *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) = v ^ flip;
+    for (uint32_t i0 = tid; i0 < n_q * 32 * CPR; i0 += 4 * 256) {
+        i32x4 v[4];
+#pragma unroll
+        for (uint32_t x = 0; x < 4; ++x) {      // (four loads at once)
+            uint32_t r = (i0 + 256 * x) / CPR;
+            const uint32_t c = (i0 + 256 * x) % CPR;
+            r = r < q_rows ? r : q_rows - 1;
+            const uint32_t u = a.by_group.quot(r);
+            v[x] = load8(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
+                             (int64_t)(h * a.group + r - u * a.group) * a.q_head + 8 * c,
+                         EXACT ? 8 : (int)d - (int)(8 * c));
+        }
+#pragma unroll
+        for (uint32_t x = 0; x < 4; ++x) {
+            const uint32_t r = (i0 + 256 * x) / CPR, c = (i0 + 256 * x) % CPR;
+            if (r < n_q * 32)
+                *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) =
+                    r < q_rows ? v[x] ^ flip : i32x4{0, 0, 0, 0};
+        }
     }
     for (uint32_t r = tid; r < n_q * 32; r += 256) {
         float x = INFINITY;
@@ -1529,8 +1586,9 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
         if (!a.arrivals) {
             const uint32_t strips =
                 a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
-            attend_join<DT><<<dim3((uint32_t)rows + strips), 256, 0, s>>>(a, qt, 32 * DC,
-                                                                          (uint32_t)rows);
+            const bool four = rows > 1024;
+            const uint32_t joins = (uint32_t)(four ? (rows + 3) / 4 : rows);
+            attend_join<DT><<<dim3(joins + strips), 256, 0, s>>>(a, qt, 32 * DC, joins, four);
             if ((e = hipGetLastError()) != hipSuccess || a.scores)
                 return e;
         }

@@ -223,7 +223,7 @@ struct Evict {
 };
 
 // Rows that one workgroup selects from alone, rows of a chunk beyond, bins of a step.
-constexpr uint32_t EV_ONE = 32768, EV_CHUNK = 16384, EV_BINS = 2048;
+constexpr uint32_t EV_ONE = 32768, EV_CHUNK = 8192, EV_BINS = 2048;
 
 // Scratch of a call: uint32 values of hist and of state (0 where one workgroup does).
 inline uint32_t evict_chunks(uint32_t room)

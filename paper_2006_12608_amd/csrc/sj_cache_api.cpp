@@ -310,7 +310,11 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
                                               : sjc::attend_occupancy_bf16(d, qt);
     const uint64_t units = (uint64_t)a.c.heads * a.tiles, held = (uint64_t)c->num_cus * per_cu;
     a.want = held / units > 0 ? (uint32_t)(held / units) : 1;
+    // (no more workgroups than shares of the least size could use)
+    const uint64_t room_shares =
+        (uint64_t)B * ((a.c.room + sjc::AT_ROWS * sjc::AT_WAVES - 1) / (sjc::AT_ROWS * sjc::AT_WAVES) + 1);
     a.slots = a.want > B ? a.want : B;
+    a.slots = a.slots < room_shares ? a.slots : (uint32_t)room_shares;
     a.w_want = 2 * c->num_cus / a.c.heads > 0 ? 2 * c->num_cus / a.c.heads : 1;
     const uint64_t parts = a.slots * units;
     if (parts >= kMaxCells)

@@ -1379,9 +1379,10 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 
 // The same with all query rows in LDS (64 KiB at most: 256 rows of 128 elements), so that a
 // workgroup can stay: it takes a share of a sequence's rows for one head, as the attention
-// kernels do, its waves 64 rows at a time in turn, the next 64 rows' keys on their way to
+// kernels do, its waves 32 WT rows at a time in turn, the next rows' keys on their way to
 // registers while these are multiplied.  (With a workgroup for every 256 rows the
-// keys were waited for at each start: 131072 rows x 256 query rows, 185 us.)
+// keys were waited for at each start: 131072 rows of 8 heads x 256 query rows, 185 us; 64
+// rows at a time, 121 us, need twice the registers; 32, 95 us.)
 template <int DC>
 constexpr uint32_t kWeighRows = DC == 8 ? 128 : 256;
 
@@ -1389,7 +1390,7 @@ template <int DT, int DC, bool EXACT>
 __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 {
     typedef Elem<DT> E;
-    constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QM = kWeighRows<DC>, WT = DC == 8 ? 1 : 2;
+    constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QM = kWeighRows<DC>, WT = 1;
     constexpr uint32_t WROWS = 32 * WT, RPL = 256 / CPR;
     __shared__ __align__(16) uint8_t qs[QM * D * 2];
     __shared__ __align__(16) float lse2[QM];

@@ -9,7 +9,7 @@ uint32_t attend_tile_rows(uint32_t rows, uint32_t d)
         return rows <= 16 ? 16 : 32;
     if (rows <= 64)
         return d <= 128 ? 64 : 32;
-    return 128;
+    return rows > 128 && d <= 128 ? 256 : 128;
 }
 
 int attend_occupancy_f16(uint32_t d, uint32_t tile_rows)

@@ -716,8 +716,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 // ------------------------------------------------------------- the tiled kernel
 //
 // For more query rows than 32: QW groups of 32 query rows share tiles of BN cache rows
-// in LDS (32 x 32 x 16 products).  With QW = 4 every wave takes 32 queries and all rows of a tile,
-// with QW = 2 two waves share 32 queries and take half of its rows each.  As above
+// in LDS (32 x 32 x 16 products).  With QW = 4 and 8 every wave takes 32 queries and all rows of a
+// tile, with QW = 2 two waves share 32 queries and take half of its rows each.  Eight waves
+// halve the loads and LDS writes for a query (256 query rows over 4 x 32768 rows: 180 us in
+// two tiles of four waves, 157 in one of eight).  As above
 // S^T = K Q^T leaves query l % 32 in lane l with rows 8 (r / 4) + 4 (l / 32) + r % 4 in
 // register r, which is, register by register, the operand of O^T = V^T P^T for steps of 16
 // rows in the order {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3} of lane half h.
@@ -735,16 +737,16 @@ __device__ __forceinline__ uint32_t swz(uint32_t row, uint32_t chunk)
 }
 
 template <int DT, int DC, int QW, bool EXACT>
-__global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Attend a)
+__global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_tiles(const Attend a)
 {
     typedef Elem<DT> E;
-    constexpr uint32_t D = 32 * DC, QT = 32 * QW, RW = 4 / QW;
+    constexpr uint32_t NT = QW == 8 ? 512 : 256, D = 32 * DC, QT = 32 * QW, RW = QW == 8 ? 1 : 4 / QW;
     constexpr uint32_t BN = DC == 8 ? 32 : 64;      // rows of a tile
     constexpr uint32_t WR = BN / RW;                // of these, one wave's
     constexpr int SR = WR / 32;                     // 32-row products of a wave
     constexpr uint32_t CPR = 4 * DC;                // 16-byte chunks of a row
-    constexpr int NL = BN * CPR / 256;              // loads per thread of K, of V
-    constexpr uint32_t RPL = 256 / CPR;             // rows per load of the workgroup
+    constexpr int NL = BN * CPR / NT;              // loads per thread of K, of V
+    constexpr uint32_t RPL = NT / CPR;             // rows per load of the workgroup
     constexpr uint32_t TILE = BN * D * 2;           // bytes
     static_assert(WR % 32 == 0, "whole products");
     __shared__ __align__(16) uint8_t lds[4 * TILE]; // K, V of two tiles
@@ -782,6 +784,7 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     const uint32_t r_mine = tile * QT + 32 * qw + q32;
     const bool live = r_mine < q_rows && a.by_group.quot(r_mine) < rows.count;
     const uint32_t tok = live ? a.by_group.quot(r_mine) : 0;
+    const bool idle = tile * QT + 32 * qw >= q_rows;    // the wave has no query rows: it only loads
     i32x4 Q[2 * DC];
     {
         const uint16_t *p = a.q + (int64_t)b * a.q_seq + (int64_t)tok * a.q_tok +
@@ -823,7 +826,8 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
         return entry_of(a.c, a.len, b, from + i * BN + (lane & (BN - 1)));
     };
     // Offsets of tile i's rows, for the threads that load them, and which rows exist; absent
-    // rows read page 0, row 0.  Each wave does one tile of four.
+    // rows read page 0, row 0.  Waves 0 .. 3 (and 4 .. 7, alike)
+    // do one tile of four each.
     auto post = [&](uint32_t i, const Entry &e) {
         const Place p = place_of(a.c, b, e, to);
         const uint64_t there = __ballot(p.page >= 0);
@@ -889,8 +893,8 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     uint64_t there = 0;
     Entry ahead = {0, 0u};
     if (n_tiles > 0) {
-        post(wave, entry(wave));
-        ahead = entry(4 + wave);
+        post(wave & 3, entry(wave & 3));
+        ahead = entry(4 + (wave & 3));
         __syncthreads();
         there = exists(0);
         fetch(0);
@@ -901,12 +905,17 @@ __global__ void __launch_bounds__(256, DC == 8 ? 1 : 2) attend_tiles(const Atten
     auto round = [&](uint32_t i, auto buf_) {
         constexpr uint32_t buf = decltype(buf_)::value;     // i % 2
         if ((i & 3) == 0) {
-            post(i + 4 + wave, ahead);
-            ahead = entry(i + 8 + wave);
+            post(i + 4 + (wave & 3), ahead);
+            ahead = entry(i + 8 + (wave & 3));
         }
         const uint64_t there1 = exists(i + 1);
         stash(i + 1, 1 - buf, there1);
         fetch(i + 2);       // (past the end: page 0, row 0; a branch would cost full waits)
+        if (idle) {
+            there = there1;
+            __syncthreads();
+            return;
+        }
         uint8_t *const kt = lds + buf * 2 * TILE;
         const uint32_t row0 = from + i * BN;
         const bool tail = row0 + BN > rows.len;
@@ -1391,7 +1400,7 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 {
     typedef Elem<DT> E;
     constexpr uint32_t D = 32 * DC, CPR = 4 * DC, QM = kWeighRows<DC>, WT = 1;
-    constexpr uint32_t WROWS = 32 * WT, RPL = 256 / CPR;
+    constexpr uint32_t WROWS = 32 * WT;
     __shared__ __align__(16) uint8_t qs[QM * D * 2];
     __shared__ __align__(16) float lse2[QM];
     __shared__ uint64_t vis[4][QM];
@@ -1569,6 +1578,8 @@ void (*attend_kernel(uint32_t qt))(const Attend)
         return attend_split<DT, DC, 2, EXACT>;
     if (qt == 64 && DC != 8)
         return attend_tiles<DT, DC, DC != 8 ? 2 : 4, EXACT>;
+    if (qt == 256 && DC != 8)
+        return attend_tiles<DT, DC, DC != 8 ? 8 : 4, EXACT>;
     return attend_tiles<DT, DC, 4, EXACT>;
 }
 
@@ -1581,7 +1592,7 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     if (rows) {
         // (a multiple of 8 workgroups: the tiled kernel deals them out by XCD)
         const dim3 grid((a.slots * a.c.heads * a.tiles + 7) / 8 * 8);
-        attend_kernel<DT, DC, EXACT>(qt)<<<grid, 256, 0, s>>>(a);
+        attend_kernel<DT, DC, EXACT>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
         if (!a.arrivals) {
@@ -1624,14 +1635,14 @@ hipError_t launch_attend(const Attend &a, hipStream_t s)
 template <int DT>
 int attend_occupancy(uint32_t d, uint32_t qt)
 {
-    static int known[3][4];
-    int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : 3))];
+    static int known[3][5];
+    int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : (qt == 128 ? 3 : 4)))];
     if (n == 0) {
         const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, false>(qt)
                                 : (d <= 128 ? (const void *)attend_kernel<DT, 4, false>(qt)
                                             : (const void *)attend_kernel<DT, 8, false>(qt));
         int x = 0;
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&x, k, 256, 0) != hipSuccess)
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&x, k, qt == 256 ? 512 : 256, 0) != hipSuccess)
             (void)hipGetLastError();
         n = x > 0 ? x : 1;
     }

@@ -175,6 +175,9 @@ SHAPES = [
     (2, 45, 1, 2, 256, 16, [130, 7]),
     (1, 9, 1, 4, 144, 24, [600]),
     (2, 25, 1, 2, 128, 64, [1, 2100]),
+    (1, 40, 1, 4, 128, 64, [900]),
+    (1, 100, 2, 3, 64, 16, [450]),
+    (2, 90, 1, 8, 72, 16, [33, 0]),
 ]
 
 

@@ -731,3 +731,28 @@ def test_refusals():
         sj.SJ_E_INVAL
     assert sj.sj_rotary(ctx, sj.SJ_F16, x, (64, 64), x, (64, 64), 1, 1, 64, None, None, 0, 0, 1.0,
                         1) == sj.SJ_E_INVAL
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 24, 40, 100, 200])
+def test_attend_long_tail(dtype, T):
+    """8192 rows of weight e^-10.5 beside one of weight 1: in fp16 such weights lie below the
+    smallest normal number, where a rounding is up to 2^-25, and still count for a fifth."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("tail", dtype, T)
+    n, d = 8193, 64
+    k = torch.zeros(1, n + T, 1, d, device="cuda", dtype=tdtype(dtype))
+    v = torch.ones_like(k)
+    k[..., 0] = -10.5
+    k[0, 0, 0, 0] = 0
+    v[0, 0] = 0
+    k[:, n:, :, 0] = -60
+    q = torch.zeros(1, T, 1, d, device="cuda", dtype=k.dtype)
+    q[..., 0] = 1
+    out, lse = sj.attend(sj.kv_cache(k, v), dev(np.array([n], np.int32)), q, scale=1.0)
+    w = 8192 * np.exp(-10.5)
+    want = w / (1 + w)
+    tol = 2 * U[dtype] * want + (8192 * 2.0 ** -25 if dtype == "f16" else 0) + n * 2.0 ** -23 * want
+    assert (np.abs(host(out) - want) <= tol).all()
+    assert (np.abs(host(lse) - np.log1p(w)) <= n * 2.0 ** -24 + 2.0 ** -19).all()

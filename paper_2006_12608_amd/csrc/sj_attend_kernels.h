@@ -1595,11 +1595,11 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
         attend_kernel<DT, DC, EXACT>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
-        if (!a.arrivals) {
+        if (a.scores || !(a.arrivals || a.whole)) {
             const uint32_t strips =
                 a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
             const bool four = rows > 1024;
-            const uint32_t joins = (uint32_t)(four ? (rows + 3) / 4 : rows);
+            const uint32_t joins = a.whole ? 0 : (uint32_t)(four ? (rows + 3) / 4 : rows);
             attend_join<DT><<<dim3(joins + strips), 256, 0, s>>>(a, qt, 32 * DC, joins, four);
             if ((e = hipGetLastError()) != hipSuccess || a.scores)
                 return e;

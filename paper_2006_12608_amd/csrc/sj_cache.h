@@ -157,9 +157,10 @@ struct Attend {
     uint32_t want;                 // shares there should be at most
     uint32_t w_want;               // the same for the weights' kernel, a workgroup a share and head
     uint32_t slots;                // most shares there can be
+    bool whole;                    // every sequence is one share
     uint32_t *plan;                // per sequence: first share, shares
     uint32_t *arrivals;            // per sequence, head and tile, zeros: shares that have arrived;
-                                   // null: attend_join joins the shares
+                                   // null: attend_join joins the shares, if any
     float *scores;                 // may be null: per head, query row and column (s_cols a row):
     uint32_t s_cols;               // scale2 * score, -inf where the row is not seen
     float *part_o;                 // per share, head, tile: query rows x padded d

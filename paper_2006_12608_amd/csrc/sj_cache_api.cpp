@@ -302,7 +302,7 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     a.w_out = w_out;
     a.w_cols = w_cols;
     SJ_HIP(hipSetDevice(c->device));
-    // work split and scratch: [plan][lse][maxima and sums][sums of values]
+    // work split and scratch: [plan][lse][maxima and sums][sums of values][scores]
     const uint32_t rows = t * a.group, qt = sjc::attend_tile_rows(rows, d);
     const uint32_t dp = d <= 64 ? 64 : (d <= 128 ? 128 : 256);
     a.tiles = rows == 0 ? 1 : (rows + qt - 1) / qt;
@@ -322,12 +322,15 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
                     (unsigned long long)units);
     const size_t off_lse = align_up((size_t)B * 8);
     const size_t off_ml = off_lse + align_up(lse ? 0 : (size_t)q_rows * 4);
-    const size_t off_o = off_ml + align_up((size_t)parts * qt * 8);
+    // (with as many sequences as shares wanted every sequence is one share, and nothing joins)
+    a.whole = B >= a.want;
+    const uint64_t kept_parts = a.whole ? 0 : parts;
+    const size_t off_o = off_ml + align_up((size_t)kept_parts * qt * 8);
     // Weights need every query row's lse, so the scores a second time.  Up to 16 query
     // rows they are kept (8 bytes written and read again per row of the cache and
     // query row, 128 at most); beyond, and where they would fill too much memory, the
     // keys are multiplied again (2 d bytes per row, 256 for d = 128).
-    const size_t off_s = off_o + align_up((size_t)parts * qt * dp * 4);
+    const size_t off_s = off_o + align_up((size_t)kept_parts * qt * dp * 4);
     const uint64_t cols = w_cols < a.c.room ? w_cols : a.c.room;
     a.s_cols = (uint32_t)((cols + 31) / 32 * 32);
     const uint64_t s_bytes = (uint64_t)B * a.c.heads * rows * a.s_cols * 4;
@@ -336,7 +339,7 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     a.plan = (uint32_t *)s;
-    if (qt <= 32 && !keep) {
+    if (qt <= 32 && !keep && !a.whole) {
         if ((st = grow_arrivals(c, (size_t)B * units)) != SJ_OK)
             return st;
         a.arrivals = c->arrivals;

@@ -756,3 +756,14 @@ def test_attend_long_tail(dtype, T):
     tol = 2 * U[dtype] * want + (8192 * 2.0 ** -25 if dtype == "f16" else 0) + n * 2.0 ** -23 * want
     assert (np.abs(host(out) - want) <= tol).all()
     assert (np.abs(host(lse) - np.log1p(w)) <= n * 2.0 ** -24 + 2.0 ** -19).all()
+
+
+@pytest.mark.parametrize("B,T,heads,group", [(600, 1, 1, 4), (300, 5, 2, 4), (140, 10, 4, 5),
+                                             (70, 33, 8, 2), (70, 140, 8, 1)])
+def test_attend_many_sequences(B, T, heads, group):
+    """More sequences than the GPU holds workgroups: none is split."""
+    say("many", B, T, heads, group)
+    c = Case(B + T, "bf16", B, T, heads, group, 64, 16, [(11 * b) % 40 for b in range(B)])
+    weight = c.rng.random((B, heads, c.cache.room)).astype(np.float32)
+    check_attend(c, chain_tree(c.rng, B, T), weight)
+    check_attend(c)

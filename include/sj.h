@@ -315,14 +315,19 @@ int sj_jl(sj_ctx *ctx, int dtype, const void *X, uint32_t n, uint32_t d, uint32_
  * a join reports the rows j with <x, k_j> >= s, attention weighs every row by
  * exp(scale <x, k_j>) / sum and answers with the weighted mean of the value rows
  * v_j.  The same blocked product feeds both, and again no score matrix is
- * stored.  The calls below keep the table (rows appended with their rotary
+ * stored (but for up to 16 query rows whose weights are asked for, where keeping
+ * the scores costs less than a second product).  The calls below keep the table (rows appended with their rotary
  * positions, rows evicted by the weight they have drawn) and query it.
  *
  * Unlike the joins these calls only put work on the context's stream and
  * return: no result comes back to the host, so nothing is waited for.  Their
- * device scratch grows on demand; a call that does not grow it may be captured
- * into a HIP graph, and its grid does not depend on the lengths, which are read
- * on the device.  sj_get_stats describes the joins only and is left alone.
+ * device scratch grows on demand (then the stream is waited for).  A call may be
+ * captured into a HIP graph: its grid does not depend on the lengths, which are read
+ * on the device.  One that would have to grow the scratch during a capture returns
+ * SJ_E_UNSUPPORTED, so make it once before; scratch that a graph may use is kept
+ * until sj_destroy, which has to come after the last replay.  A replay uses the
+ * context as its calls did: it must not run beside other calls of the context.
+ * sj_get_stats describes the joins only and is left alone.
  *
  * Numbers on the device (lengths, tables, masks) are not read back to be
  * checked; whatever they hold, no access leaves the described arrays: lengths
@@ -407,7 +412,9 @@ int sj_cache_append(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, cons
  * zeros) may be the same array; w_out NULL: no weights.
  * Arithmetic: fp32 sums of 16-bit products on the matrix cores; softmax statistics
  * and weights in fp32; exp(s_n - running maximum) enters the product with v as
- * 16-bit values.  Results do not depend on timing (no atomics).
+ * 16-bit values.  The rows are cut into shares by the lengths, the shapes and the GPU's
+ * number of CUs; whichever workgroup joins the shares adds them in their order, so
+ * results do not depend on timing.
  * Errors as the joins'; SJ_E_INVAL also when heads does not divide q_heads or for a NaN
  * scale; SJ_E_UNSUPPORTED for d > 256, width * page > 2^30, batch * heads > 65535 or
  * batch * t * q_heads >= 2^31. */

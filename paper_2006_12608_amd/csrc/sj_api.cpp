@@ -105,13 +105,22 @@ float float_at_or_below(double r)
     return f;
 }
 
+static void outgrown(sj_ctx *c, void *p)
+{
+    if (!c->captured) {
+        (void)hipStreamSynchronize(c->stream);
+        (void)hipFree(p);
+    } else if (c->n_retired < sizeof(c->retired) / sizeof(c->retired[0])) {
+        c->retired[c->n_retired++] = p;
+    }
+}
+
 int grow_scratch(sj_ctx *c, size_t bytes)
 {
     if (bytes <= c->scratch_bytes)
         return SJ_OK;
     if (c->scratch) {
-        (void)hipStreamSynchronize(c->stream);
-        (void)hipFree(c->scratch);
+        outgrown(c, c->scratch);
         c->scratch = nullptr;
         c->scratch_bytes = 0;
     }
@@ -155,8 +164,7 @@ int grow_arrivals(sj_ctx *c, size_t n)
     if (n <= c->arrivals_n)
         return SJ_OK;
     if (c->arrivals) {
-        (void)hipStreamSynchronize(c->stream);
-        (void)hipFree(c->arrivals);
+        outgrown(c, c->arrivals);
         c->arrivals = nullptr;
         c->arrivals_n = 0;
     }
@@ -788,6 +796,8 @@ void sj_destroy(sj_ctx *c)
     for (auto &ev : c->ev)
         if (ev)
             (void)hipEventDestroy(ev);
+    for (uint32_t i = 0; i < c->n_retired; ++i)
+        (void)hipFree(c->retired[i]);
     if (c->scratch)
         (void)hipFree(c->scratch);
     if (c->front)

@@ -49,6 +49,27 @@ int check_strided(const sj_ctx *c, const void *p, const Axis *axes, int n_axes, 
     return check_device_ptr(c, p, (size_t)(last + d) * 2, name);
 }
 
+// Scratch and counters of one call.  While the context's stream is captured nothing may be
+// allocated, and the graph keeps what there is.
+int grow_both(sj_ctx *c, size_t bytes, size_t counters)
+{
+    hipStreamCaptureStatus state = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(c->stream, &state) != hipSuccess) {
+        (void)hipGetLastError();
+        state = hipStreamCaptureStatusNone;
+    }
+    if (state != hipStreamCaptureStatusNone) {
+        if (bytes > c->scratch_bytes || counters > c->arrivals_n)
+            return fail(SJ_E_UNSUPPORTED,
+                        "scratch would grow during a capture (%zu bytes, %zu there): make the "
+                        "call once on the stream before", bytes, c->scratch_bytes);
+        c->captured = true;
+        return SJ_OK;
+    }
+    const int st = grow_scratch(c, bytes);
+    return st == SJ_OK && counters ? grow_arrivals(c, counters) : st;
+}
+
 int check_array(const sj_ctx *c, const void *p, uint64_t bytes, uint32_t align, const char *name)
 {
     if (bytes == 0)
@@ -335,15 +356,13 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     a.s_cols = (uint32_t)((cols + 31) / 32 * 32);
     const uint64_t s_bytes = (uint64_t)B * a.c.heads * rows * a.s_cols * 4;
     const bool keep = w_out && rows <= 16 && s_bytes > 0 && s_bytes <= kMaxScores;
-    if ((st = grow_scratch(c, off_s + (keep ? (size_t)s_bytes : 0))) != SJ_OK)
+    const bool counted = qt <= 32 && !keep && !a.whole;
+    if ((st = grow_both(c, off_s + (keep ? (size_t)s_bytes : 0), counted ? (size_t)B * units : 0)) !=
+        SJ_OK)
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     a.plan = (uint32_t *)s;
-    if (qt <= 32 && !keep && !a.whole) {
-        if ((st = grow_arrivals(c, (size_t)B * units)) != SJ_OK)
-            return st;
-        a.arrivals = c->arrivals;
-    }
+    a.arrivals = counted ? c->arrivals : nullptr;
     a.lse = lse ? lse : (float *)(s + off_lse);
     a.part_ml = (float *)(s + off_ml);
     a.part_o = (float *)(s + off_o);
@@ -406,7 +425,7 @@ extern "C" int sj_cache_evict(sj_ctx *c, const sj_cache *src, const int32_t *len
     e.chunks = sjc::evict_chunks(e.src.room);
     if (e.chunks) {
         const size_t off = align_up((size_t)sjc::evict_hist_values(B * sets, e.chunks) * 4);
-        if ((st = grow_scratch(c, off + (size_t)sjc::evict_state_values(B * sets, e.chunks) * 4)) !=
+        if ((st = grow_both(c, off + (size_t)sjc::evict_state_values(B * sets, e.chunks) * 4, 0)) !=
             SJ_OK)
             return st;
         e.hist = (uint32_t *)c->scratch;

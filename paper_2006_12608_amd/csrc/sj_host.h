@@ -26,6 +26,9 @@ struct sj_ctx {
     size_t front_bytes = 0;       // unpacked), kept apart from the join's scratch
     uint32_t *arrivals = nullptr; // counters of sj_attend's workgroups: 0 between kernels
     size_t arrivals_n = 0;
+    bool captured = false;        // a HIP graph may hold the scratch's and the counters' addresses:
+    void *retired[64] = {};       // what they outgrow from then on is freed by sj_destroy
+    uint32_t n_retired = 0;       // (beyond 64, not before the process ends)
     hipEvent_t ev[6] = {};
     sj_stats stats = {};
 };

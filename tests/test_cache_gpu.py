@@ -767,3 +767,42 @@ def test_attend_many_sequences(B, T, heads, group):
     weight = c.rng.random((B, heads, c.cache.room)).astype(np.float32)
     check_attend(c, chain_tree(c.rng, B, T), weight)
     check_attend(c)
+
+
+def test_a_graph_keeps_its_scratch():
+    """A later call that needs more scratch leaves a captured one's; a capture that would have to
+    grow the scratch is refused."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("graph and scratch")
+    small = Case(71, "f16", 2, 3, 2, 4, 64, 16, [900, 33])
+    large = Case(72, "f16", 4, 40, 2, 4, 64, 16, [3000, 2000, 50, 9])
+    lens, more = dev(small.lens), dev(large.lens)
+    want = sj.attend(small.cache, lens, small.dq)
+    want_more = sj.attend(large.cache, more, large.dq)
+    stream = torch.cuda.Stream()
+    ctx = sj.sj_create(torch.cuda.current_device(), stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        sj.attend(small.cache, lens, small.dq, ctx=ctx)
+        stream.synchronize()
+        graph, refused = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out, lse = sj.attend(small.cache, lens, small.dq, ctx=ctx)
+        with torch.cuda.graph(refused, stream=stream):
+            torch.zeros(1, device="cuda")
+            with pytest.raises(sj.SjError, match="capture"):
+                sj.attend(large.cache, more, large.dq, ctx=ctx)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(stream):
+            got = sj.attend(large.cache, more, large.dq, ctx=ctx)
+        torch.cuda.synchronize()
+        out.zero_()
+        lse.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        assert torch.equal(got[0], want_more[0]) and torch.equal(got[1], want_more[1])
+    del graph, refused
+    sj.sj_destroy(ctx)

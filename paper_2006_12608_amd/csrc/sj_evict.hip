@@ -176,7 +176,8 @@ __device__ __forceinline__ void pad(const Evict &e, const Task &t, uint32_t shar
 // The kept rows of one set, in order: a workgroup a set of up to EV_ONE rows, each wave a
 // stretch of them, the weights in registers.  Radix selection of the last key that stays: three
 // histograms of 11, 11 and 10 key bits, each over the keys whose higher bits are
-// those of the key sought.
+// those of the key sought.  The weights are read once and all at once; what is left is the
+// latency of the steps' barriers: 128 sets of 2500 to 16000 rows, 19 us (4 MB), 2 of 3000, 6.5.
 template <int PER>
 __global__ void __launch_bounds__(EV_THREADS) evict_select(const Evict e)
 {
@@ -204,7 +205,8 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select(const Evict e)
 
 // The same for more rows, a workgroup a chunk of EV_CHUNK: step s = 0, 1, 2 leaves the chunk's
 // histogram, after finding the bin of step s - 1 from all chunks' (every workgroup by itself);
-// step 3 writes the rows.  131072 rows: 209 -> ... us with one workgroup.
+// step 3 writes the rows.  Two sets of 131072 rows: 28 us for the four launches against 209 with
+// a workgroup a set; of 30000, one workgroup's 30 us are no more than the launches'.
 template <int STEP>
 __global__ void __launch_bounds__(EV_THREADS) evict_step(const Evict e)
 {
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(EV_THREADS) evict_step(const Evict e)
 }
 
 // Copies the kept rows of one (sequence, head): each thread 16 bytes of a row of k and
-// of v.  Bound by HBM.
+// of v.  Bound by HBM: 525 MB (read and written) in 109 us, 4.8 TB/s, as a large copy.
 __global__ void __launch_bounds__(256) evict_copy(const Evict e, uint32_t chunks, PageDiv by_chunks,
                                                   uint32_t rows_per)
 {

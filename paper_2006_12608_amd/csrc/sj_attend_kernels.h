@@ -66,18 +66,19 @@ __device__ __forceinline__ float bits_to_float(uint16_t x, int dt)
                              : __uint_as_float((uint32_t)x << 16);
 }
 
-// The eight elements with zeros in the place of infinities and NaN; returns whether there
-// were any.
+// The eight elements with zeros in the place of infinities and NaN if the row is one of the
+// call's own tokens (all tokens see the others); returns whether there were any.
 template <int DT>
-__device__ __forceinline__ uint32_t drop_odd8(i32x4 &v)
+__device__ __forceinline__ uint32_t drop_odd8(i32x4 &v, bool own)
 {
     constexpr uint32_t EXP = Elem<DT>::EXP;
+    const uint32_t mask = own ? ~0u : 0u;
     uint32_t odd = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const uint32_t x = (uint32_t)v[e];
-        const uint32_t lo = (x & EXP) == EXP ? 0xffffu : 0u;
-        const uint32_t hi = ((x >> 16) & EXP) == EXP ? 0xffff0000u : 0u;
+        const uint32_t lo = (x & EXP) == EXP ? mask & 0xffffu : 0u;
+        const uint32_t hi = ((x >> 16) & EXP) == EXP ? mask & 0xffff0000u : 0u;
         v[e] = (int)(x & ~(lo | hi));
         odd |= lo | hi;
     }
@@ -565,7 +566,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             if (tail || there != 0xffffffffu) {
                 if (!((there >> (VR * i + v_row)) & 1))
                     V[i] = i32x4{0, 0, 0, 0};
-                odd |= drop_odd8<DT>(V[i]);
+                odd |= drop_odd8<DT>(V[i], blk * AT_ROWS + VR * i + v_row >= rows.len);
                 asm volatile("");       // (a branch, not selects in every round)
             }
             *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = V[i];
@@ -880,7 +881,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
             for (int x = 0; x < NL; ++x) {
                 if (!((there >> (RPL * x + row_at)) & 1))
                     vr[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
-                odd |= drop_odd8<DT>(vr[x]);
+                odd |= drop_odd8<DT>(vr[x], from + i * BN + RPL * x + row_at >= rows.len);
             }
             if (odd)
                 odd_any = 1;

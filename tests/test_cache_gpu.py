@@ -806,3 +806,21 @@ def test_a_graph_keeps_its_scratch():
         assert torch.equal(got[0], want_more[0]) and torch.equal(got[1], want_more[1])
     del graph, refused
     sj.sj_destroy(ctx)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,group,d", [(4, 2, 64), (4, 8, 128), (10, 2, 256), (12, 4, 128),
+                                       (30, 4, 64), (50, 4, 128), (70, 4, 128), (40, 2, 256)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_attend_cached_values_that_are_not_finite_show(dtype, T, group, d, bad):
+    """A value of a row before the call's tokens reaches all of them, also where the row is
+    multiplied together with the tokens' own rows or with pages that do not exist."""
+    import paper_2006_12608_amd as sj
+    say("cached", dtype, T, group, d, bad)
+    c = Case(23, dtype, 1, T, 1, group, d, 16, [37])
+    want = host(sj.attend(c.cache, dev(c.lens), c.dq)[0])
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, 35)
+    c.dv[r[0], r[1], 0, 5] = bad
+    got = host(sj.attend(c.cache, dev(c.lens), c.dq)[0])
+    assert not np.isfinite(got[..., 5]).any()
+    assert np.array_equal(np.delete(got, 5, -1), np.delete(want, 5, -1))

@@ -216,15 +216,20 @@ __device__ __forceinline__ void seen_rows(const Attend &a, uint32_t b, const Row
     wave_sync();
 }
 
-// -inf for the scores of key row n (of 64) that the query rows v[8 (e / 4) + e % 4] do not see.
+// Weights of key row n (of 64) from the scores and lse (z, base 2) of the query rows
+// v[8 (e / 4) + e % 4]: of those that see it (lse may be NaN in the others).
 template <class S>
-__device__ __forceinline__ void hide(S &s, const uint64_t *v, uint32_t n)
+__device__ __forceinline__ float weigh_seen(const S &s, const f32x4 *z, float scale2,
+                                            const uint64_t *v, uint32_t n)
 {
+    float w = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const uint32_t w = ((const uint32_t *)(v + 8 * (e >> 2) + (e & 3)))[n >> 5];
-        s[e] = (w >> (n & 31)) & 1 ? s[e] : -INFINITY;
+        const uint32_t bits = ((const uint32_t *)(v + 8 * (e >> 2) + (e & 3)))[n >> 5];
+        const float p = exp2_(__builtin_fmaf(s[e], scale2, -z[e >> 2][e & 3]));
+        w += (bits >> (n & 31)) & 1 ? p : 0.f;
     }
+    return w;
 }
 
 // The share of the work that a workgroup takes: blocks [first, last) of
@@ -366,7 +371,6 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1)
             top = fmaxf(top, __shfl_xor(top, o));
-        const bool live = u < count && top != -INFINITY;
         const float base = top == -INFINITY ? 0.f : top;
         f32x4 o[D / 64] = {};
         float l = 0.f;
@@ -383,6 +387,7 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
                 o[k] += f32x4{lo[0], lo[1], hi[0], hi[1]} * f;
             }
         }
+        const bool live = u < count && l != 0.f;
         const float inv = live ? 1.f / l : 0.f;
         const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group;
 #pragma unroll
@@ -699,19 +704,19 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                         *(f32x4 *)p = o;
                     }
                 } else {
-                    const float inv = live && tot != -INFINITY ? 1.f / sum : 0.f;
+                    const float inv = live && sum != 0.f ? 1.f / sum : 0.f;
 #pragma unroll
                     for (uint32_t e = 0; e < 4; ++e)
                         if (EXACT || c + e < d)
                             a.out[row * d + c + e] = __builtin_bit_cast(
-                                uint16_t, (typename E::one)(live && tot != -INFINITY ? o[e] * inv : 0.f));
+                                uint16_t, (typename E::one)(live && sum != 0.f ? o[e] * inv : 0.f));
                 }
             }
             if (c0 == 0) {
                 if (shares > 1) {
                     put2(a.part_ml + (part * QT + AT_Q * j + qi) * 2, tot, sum);
                 } else {
-                    a.lse[row] = live && tot != -INFINITY
+                    a.lse[row] = live && sum != 0.f
                                      ? (tot + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f
                                      : -INFINITY;
                 }
@@ -1091,7 +1096,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                         O[z][e] += odd_part<DT>(v[c]);
                 }
         });
-    const bool some = live && m != -INFINITY;
+    const bool some = live && l != 0.f;
     const float inv = some ? 1.f / l : 0.f;
 #pragma unroll
     for (int z = 0; z < DC; ++z)
@@ -1140,7 +1145,6 @@ __device__ __forceinline__ void join_row(const Attend &a, uint32_t QT, uint32_t 
     for (uint32_t s = lane; s < shares; s += 64)
         top = fmaxf(top, a.part_ml[2 * part_of(a, slot + s, h, r, QT)]);
     top = max_all(top);
-    const bool live = u < rows_of(a, b).count && top != -INFINITY;
     const float base = top == -INFINITY ? 0.f : top;
     const uint32_t per = D / 4, c = 4 * (tid % per), groups = T / per;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -1168,6 +1172,7 @@ __device__ __forceinline__ void join_row(const Attend &a, uint32_t QT, uint32_t 
         o += sums[mine * T + g * per + tid];
         l += ls[mine][g];
     }
+    const bool live = u < rows_of(a, b).count && l != 0.f;
     const float inv = live ? 1.f / l : 0.f;
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e)
@@ -1209,7 +1214,7 @@ __device__ __forceinline__ void weigh_scores(const Attend &a, uint32_t QT, uint3
 #pragma unroll
                 for (int o = 1; o < 16; o <<= 1)
                     l += __shfl_xor(l, o);
-                y = top == -INFINITY ? INFINITY : top + __builtin_amdgcn_logf(l);
+                y = l == 0.f ? INFINITY : top + __builtin_amdgcn_logf(l);
             } else {
                 y = a.lse[((uint64_t)b * a.t + r / a.group) * a.q_heads + h * a.group + r % a.group] *
                     1.4426950408889634f;
@@ -1232,7 +1237,7 @@ __device__ __forceinline__ void weigh_scores(const Attend &a, uint32_t QT, uint3
             if (y != INFINITY)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    w[e] += exp2_(x[e] - y);
+                    w[e] += x[e] == -INFINITY ? 0.f : exp2_(x[e] - y);
         }
     }
     const uint64_t at = (uint64_t)bh * a.w_cols + n0;
@@ -1372,13 +1377,14 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                 if (masked) {
 #pragma unroll
                     for (int t = 0; t < (int)WT; ++t)
-                        hide(s[t], vis[wave] + q0 + 4 * half, 32 * t + l32);
+                        w[t] += weigh_seen(s[t], z, a.scale2, vis[wave] + q0 + 4 * half, 32 * t + l32);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < (int)WT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            w[t] += exp2_(__builtin_fmaf(s[t][e], a.scale2, -z[e >> 2][e & 3]));
                 }
-#pragma unroll
-                for (int t = 0; t < (int)WT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        w[t] += exp2_(__builtin_fmaf(s[t][e], a.scale2, -z[e >> 2][e & 3]));
             }
             stash(buf ^ 1);
             __syncthreads();
@@ -1554,13 +1560,14 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
             if (masked) {
 #pragma unroll
                 for (int t = 0; t < (int)WT; ++t)
-                    hide(s[t], vis[wave] + q0 + 4 * half, 32 * t + l32);
+                    w[t] += weigh_seen(s[t], z, a.scale2, vis[wave] + q0 + 4 * half, 32 * t + l32);
+            } else {
+#pragma unroll
+                for (int t = 0; t < (int)WT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        w[t] += exp2_(__builtin_fmaf(s[t][e], a.scale2, -z[e >> 2][e & 3]));
             }
-#pragma unroll
-            for (int t = 0; t < (int)WT; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    w[t] += exp2_(__builtin_fmaf(s[t][e], a.scale2, -z[e >> 2][e & 3]));
         }
 #pragma unroll
         for (int t = 0; t < (int)WT; ++t) {

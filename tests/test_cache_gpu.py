@@ -824,3 +824,36 @@ def test_attend_cached_values_that_are_not_finite_show(dtype, T, group, d, bad):
     got = host(sj.attend(c.cache, dev(c.lens), c.dq)[0])
     assert not np.isfinite(got[..., 5]).any()
     assert np.array_equal(np.delete(got, 5, -1), np.delete(want, 5, -1))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,group,d", [(4, 1, 64), (4, 4, 128), (6, 4, 128), (12, 4, 64), (30, 4, 128),
+                                       (50, 4, 128), (70, 4, 64), (40, 2, 256), (80, 4, 72)])
+@pytest.mark.parametrize("where", ["query", "key"])
+def test_attend_nan_stays_where_it_is_seen(dtype, T, group, d, where):
+    """A query, or a drafted token's key, that is NaN: NaN in the outputs, the lse and the
+    weights of what it meets, and in nothing else."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("nan", dtype, T, group, d, where)
+    c = Case(29, dtype, 1, T, 2, group, d, 16, [70])
+    masks = [1 | 1 << t for t in range(T)]              # itself and token 0
+    tree = np.zeros((1, T, (T + 63) // 64), np.uint64)
+    for t in range(T):
+        for w in range(tree.shape[2]):
+            tree[0, t, w] = (masks[t] >> 64 * w) & (2 ** 64 - 1)
+    tree = dev(tree.view(np.int64))
+    w0, w1 = (torch.empty(1, 2, c.cache.room, device="cuda") for _ in range(2))
+    clean, clean_lse = sj.attend(c.cache, dev(c.lens), c.dq, tree, weight_out=w0)
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, 71)    # token 1's, which only it sees
+    if where == "key":
+        c.dk[r[0], r[1]] = float("nan")
+    else:
+        c.dq[0, 1] = float("nan")
+    out, lse = sj.attend(c.cache, dev(c.lens), c.dq, tree, weight_out=w1)
+    assert out[0, 1].isnan().all() and lse[0, 1].isnan().all()
+    others = [t for t in range(T) if t != 1]
+    assert torch.equal(out[0, others], clean[0, others])
+    assert torch.equal(lse[0, others], clean_lse[0, others])
+    assert w1[..., :72].isnan().all()
+    assert torch.equal(w1[..., 72:], w0[..., 72:])

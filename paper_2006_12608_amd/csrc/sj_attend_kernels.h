@@ -119,11 +119,28 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane)
     return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
+// How the heads' d elements fill the kernels' 32 DC: all of them, whole 16-byte chunks of them, or
+// any number (its own variant, since the last chunk's element-wise loads are waited for where
+// they are made: 64 query rows on 8 sequences of 1000 to 7000 rows, d = 192: 117 us, 102 with chunks).
+enum Fit { FIT_ANY = 0, FIT_CHUNKS = 1, FIT_WHOLE = 2 };
+
+template <int FIT>
+__device__ __forceinline__ i32x4 load_fit(const uint16_t *p, int left)
+{
+    if constexpr (FIT == FIT_ANY)
+        return load8(p, left);
+    i32x4 v = {0, 0, 0, 0};
+    if (FIT == FIT_WHOLE || left > 0)
+        __builtin_memcpy(&v, p, 16);
+    return v;
+}
+
 // Eight elements of a query, negated for a negative scale: the scores' order is then
 // that of the products, and the maximum can be taken before the scale.
+template <int FIT>
 __device__ __forceinline__ i32x4 load_q8(const Attend &a, const uint16_t *p, int left)
 {
-    i32x4 v = load8(p, left);
+    i32x4 v = load_fit<FIT>(p, left);
     const int flip = a.negate ? (int)0x80008000 : 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -428,7 +445,7 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
 // 5.4 TB/s, or 231 with the scores kept (33 MB); 32 sequences of 200 to 8192 rows, 550 MB, in
 // 116 (4.7 TB/s).  One sequence of 2048 rows: 10 us, of which most is the latency of the chain
 // lengths, page numbers, rows, join.
-template <int DT, int DC, int NQ, bool EXACT>
+template <int DT, int DC, int NQ, int FIT>
 __global__ void __launch_bounds__(256) attend_split(const Attend a)
 {
     typedef Elem<DT> E;
@@ -490,7 +507,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                             (int64_t)(h * a.group + (there ? r % a.group : 0)) * a.q_head + 8 * g4;
 #pragma unroll
         for (int c = 0; c < DC; ++c)
-            Q[j][c] = there ? load_q8(a, p + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4))
+            Q[j][c] = there ? load_q8<FIT>(a, p + 32 * c, (int)d - (int)(32 * c + 8 * g4))
                             : i32x4{0, 0, 0, 0};
     }
 
@@ -521,7 +538,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             const uint16_t *r = kb + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
 #pragma unroll
             for (int c = 0; c < DC; ++c)
-                K[t][c] = load8(r + 32 * c, EXACT ? 8 : (int)d - (int)(32 * c + 8 * g4));
+                K[t][c] = load_fit<FIT>(r + 32 * c, (int)d - (int)(32 * c + 8 * g4));
         }
     };
     const uint32_t v_row = lane / (4 * DC), v_col = 8 * (lane % (4 * DC));
@@ -531,7 +548,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const uint16_t *r = vb + shfl64(off, VR * i + (int)v_row) + v_col;
-            V[i] = load8(r, EXACT ? 8 : (int)d - (int)v_col);
+            V[i] = load_fit<FIT>(r, (int)d - (int)v_col);
         }
     };
 
@@ -707,7 +724,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                     const float inv = live && sum != 0.f ? 1.f / sum : 0.f;
 #pragma unroll
                     for (uint32_t e = 0; e < 4; ++e)
-                        if (EXACT || c + e < d)
+                        if (FIT == FIT_WHOLE || c + e < d)
                             a.out[row * d + c + e] = __builtin_bit_cast(
                                 uint16_t, (typename E::one)(live && sum != 0.f ? o[e] * inv : 0.f));
                 }
@@ -750,7 +767,7 @@ __device__ __forceinline__ uint32_t swz(uint32_t row, uint32_t chunk)
         return chunk ^ (((row & 3) << 2) | ((row >> 2) & 3));
 }
 
-template <int DT, int DC, int QW, bool EXACT>
+template <int DT, int DC, int QW, int FIT>
 __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_tiles(const Attend a)
 {
     typedef Elem<DT> E;
@@ -806,7 +823,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                             8 * half;
 #pragma unroll
         for (int k = 0; k < 2 * DC; ++k)
-            Q[k] = live ? load_q8(a, p + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half))
+            Q[k] = live ? load_q8<FIT>(a, p + 16 * k, (int)d - (int)(16 * k + 8 * half))
                         : i32x4{0, 0, 0, 0};
     }
     wait_loads();
@@ -862,15 +879,15 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     };
     i32x4 kr[NL], vr[NL];
     auto fetch = [&](uint32_t i) {
-        const int left = EXACT ? 8 : (int)d - (int)(8 * chunk);
+        const int left = (int)d - (int)(8 * chunk);
         i64x2 o[NL];
 #pragma unroll
         for (int x = 0; x < NL; ++x)
             o[x] = where[i & 7][RPL * x + row_at];
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
-            kr[x] = load8(kb + o[x][0] + 8 * chunk, left);
-            vr[x] = load8(vb + o[x][1] + 8 * chunk, left);
+            kr[x] = load_fit<FIT>(kb + o[x][0] + 8 * chunk, left);
+            vr[x] = load_fit<FIT>(vb + o[x][1] + 8 * chunk, left);
         }
     };
     // (the swizzle repeats every 16 rows, and RPL is a multiple of 8: one place, or two)
@@ -1092,7 +1109,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const uint32_t c = 32 * z + 8 * (e >> 2) + 4 * half + (e & 3);
-                    if (EXACT || c < d)
+                    if (FIT == FIT_WHOLE || c < d)
                         O[z][e] += odd_part<DT>(v[c]);
                 }
         });
@@ -1109,7 +1126,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
             } else {
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e)
-                    if (EXACT || c + e < d)
+                    if (FIT == FIT_WHOLE || c + e < d)
                         a.out[row * d + c + e] = __builtin_bit_cast(
                             uint16_t, (typename E::one)(some ? o[e] * inv : 0.f));
             }
@@ -1270,7 +1287,7 @@ __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, 
 // lane l with query rows 8 (r / 4) + 4 (l / 32) + r % 4 in register r, so the sum stays in
 // the lane until the end.  Two buffers of query rows, the next one's on their way
 // while one is worked on.
-template <int DT, int DC, bool EXACT>
+template <int DT, int DC, int FIT>
 __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 {
     typedef Elem<DT> E;
@@ -1302,7 +1319,7 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                 a.c.k + (int64_t)h * a.c.k_head + shfl64(off, (int)l32 + 32 * t) + 8 * half;
 #pragma unroll
             for (int k = 0; k < 2 * DC; ++k)
-                K[t][k] = load8(r + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half));
+                K[t][k] = load_fit<FIT>(r + 16 * k, (int)d - (int)(16 * k + 8 * half));
         }
         uint32_t q_at[2 * DC];      // chunk 2 k + half of query row l32 (the same for every 32)
 #pragma unroll
@@ -1320,9 +1337,9 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
                 uint32_t r = r0 + RPL * x + row_at;
                 r = r < q_rows ? r : q_rows - 1;
                 const uint32_t u = a.by_group.quot(r);
-                qr[x] = load8(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
+                qr[x] = load_fit<FIT>(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
                                   (int64_t)(h * a.group + r - u * a.group) * a.q_head + 8 * chunk,
-                              EXACT ? 8 : (int)d - (int)(8 * chunk));
+                              (int)d - (int)(8 * chunk));
             }
             uint32_t r = r0 + (tid & (QS - 1));
             lr_there = r < q_rows;
@@ -1412,7 +1429,7 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 template <int DC>
 constexpr uint32_t kWeighRows = DC == 8 ? 128 : 256;
 
-template <int DT, int DC, bool EXACT>
+template <int DT, int DC, int FIT>
 __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 {
     typedef Elem<DT> E;
@@ -1462,9 +1479,9 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
             const uint32_t c = (i0 + 256 * x) % CPR;
             r = r < q_rows ? r : q_rows - 1;
             const uint32_t u = a.by_group.quot(r);
-            v[x] = load8(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
+            v[x] = load_fit<FIT>(a.q + (int64_t)b * a.q_seq + (int64_t)u * a.q_tok +
                              (int64_t)(h * a.group + r - u * a.group) * a.q_head + 8 * c,
-                         EXACT ? 8 : (int)d - (int)(8 * c));
+                         (int)d - (int)(8 * c));
         }
 #pragma unroll
         for (uint32_t x = 0; x < 4; ++x) {
@@ -1503,7 +1520,7 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
             const uint16_t *r = kb + shfl64(off, (int)l32 + 32 * t);
 #pragma unroll
             for (int k = 0; k < 2 * DC; ++k)
-                K[set][t][k] = load8(r + 16 * k, EXACT ? 8 : (int)d - (int)(16 * k + 8 * half));
+                K[set][t][k] = load_fit<FIT>(r + 16 * k, (int)d - (int)(16 * k + 8 * half));
         }
     };
     auto add = [&](uint32_t n) -> float {               // (a load whether it is needed or not)
@@ -1587,21 +1604,21 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 }
 
 // The kernel for tiles of qt query rows.
-template <int DT, int DC, bool EXACT>
+template <int DT, int DC, int FIT>
 void (*attend_kernel(uint32_t qt))(const Attend)
 {
     if (qt == 16)
-        return attend_split<DT, DC, 1, EXACT>;
+        return attend_split<DT, DC, 1, FIT>;
     if (qt == 32)
-        return attend_split<DT, DC, 2, EXACT>;
+        return attend_split<DT, DC, 2, FIT>;
     if (qt == 64 && DC != 8)
-        return attend_tiles<DT, DC, DC != 8 ? 2 : 4, EXACT>;
+        return attend_tiles<DT, DC, DC != 8 ? 2 : 4, FIT>;
     if (qt == 256 && DC != 8)
-        return attend_tiles<DT, DC, DC != 8 ? 8 : 4, EXACT>;
-    return attend_tiles<DT, DC, 4, EXACT>;
+        return attend_tiles<DT, DC, DC != 8 ? 8 : 4, FIT>;
+    return attend_tiles<DT, DC, 4, FIT>;
 }
 
-template <int DT, int DC, bool EXACT>
+template <int DT, int DC, int FIT>
 hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
 {
     const uint32_t qt = attend_tile_rows(a.t * a.group, a.c.d);
@@ -1610,7 +1627,7 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     if (rows) {
         // (a multiple of 8 workgroups: the tiled kernel deals them out by XCD)
         const dim3 grid((a.slots * a.c.heads * a.tiles + 7) / 8 * 8);
-        attend_kernel<DT, DC, EXACT>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
+        attend_kernel<DT, DC, FIT>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
         if (a.scores || !(a.arrivals || a.whole)) {
@@ -1629,24 +1646,30 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
         Attend w = a;       // (its own cut of the rows: a workgroup a share and head)
         w.want = a.w_want;
         w.slots = a.w_want > a.c.batch ? a.w_want : a.c.batch;
-        attend_weights_held<DT, DC, EXACT><<<dim3(w.slots * a.c.heads), 256, 0, s>>>(w);
+        attend_weights_held<DT, DC, FIT><<<dim3(w.slots * a.c.heads), 256, 0, s>>>(w);
         return hipGetLastError();
     }
     const uint32_t w_rows = DC == 8 ? 128 : 256;
     const dim3 wg((uint32_t)((a.w_cols + w_rows - 1) / w_rows), a.c.batch * a.c.heads);
-    attend_weights<DT, DC, EXACT><<<wg, 256, 0, s>>>(a);
+    attend_weights<DT, DC, FIT><<<wg, 256, 0, s>>>(a);
     return hipGetLastError();
+}
+
+template <int DT, int DC>
+hipError_t launch_attend_fit(const Attend &a, hipStream_t s)
+{
+    if (a.c.d == 32 * DC)
+        return launch_attend_dc<DT, DC, FIT_WHOLE>(a, s);
+    return a.c.d % 8 == 0 ? launch_attend_dc<DT, DC, FIT_CHUNKS>(a, s)
+                          : launch_attend_dc<DT, DC, FIT_ANY>(a, s);
 }
 
 template <int DT>
 hipError_t launch_attend(const Attend &a, hipStream_t s)
 {
     const uint32_t d = a.c.d;
-    if (d <= 64)
-        return d == 64 ? launch_attend_dc<DT, 2, true>(a, s) : launch_attend_dc<DT, 2, false>(a, s);
-    if (d <= 128)
-        return d == 128 ? launch_attend_dc<DT, 4, true>(a, s) : launch_attend_dc<DT, 4, false>(a, s);
-    return d == 256 ? launch_attend_dc<DT, 8, true>(a, s) : launch_attend_dc<DT, 8, false>(a, s);
+    return d <= 64 ? launch_attend_fit<DT, 2>(a, s)
+                   : (d <= 128 ? launch_attend_fit<DT, 4>(a, s) : launch_attend_fit<DT, 8>(a, s));
 }
 
 // Workgroups of the kernel for d and qt that one CU holds at once.
@@ -1656,9 +1679,9 @@ int attend_occupancy(uint32_t d, uint32_t qt)
     static int known[3][5];
     int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : (qt == 128 ? 3 : 4)))];
     if (n == 0) {
-        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, false>(qt)
-                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, false>(qt)
-                                            : (const void *)attend_kernel<DT, 8, false>(qt));
+        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, FIT_ANY>(qt)
+                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, FIT_ANY>(qt)
+                                            : (const void *)attend_kernel<DT, 8, FIT_ANY>(qt));
         int x = 0;
         if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&x, k, qt == 256 ? 512 : 256, 0) != hipSuccess)
             (void)hipGetLastError();

@@ -423,8 +423,8 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
 
 // ------------------------------------------------------------- the split kernel
 //
-// A workgroup takes one share of a sequence's rows for one cache head and one
-// tile of QT = 16 NQ query rows (row r = token r / group, query head r % group: all
+// A workgroup takes one share of a sequence's rows for one cache head and its up to
+// QT = 16 NQ query rows (row r = token r / group, query head r % group: all
 // that read this cache head, so that a cache row is loaded once for all of them).
 // Its four waves take blocks of 32 rows in turn, each with running statistics
 // of its own; they join at the end through LDS.

@@ -167,8 +167,8 @@ struct Attend {
     float *part_ml;                // per share, head, tile: query rows x {max, sum}
 };
 
-// The kernels for one call; the query rows of a workgroup's tile (16 or 32) follow
-// from t * group.
+// The kernels for one call; the query rows of a workgroup's tile (16, 32, 64, 128 or 256)
+// follow from t * group and d.
 uint32_t attend_tile_rows(uint32_t rows, uint32_t d);
 // Workgroups of the call's kernel that one CU holds at once.
 int attend_occupancy_f16(uint32_t d, uint32_t tile_rows);

@@ -1471,7 +1471,8 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
     if (from >= to)
         return;
 
-    // query rows and their lse; rows past the end are zeros and weigh nothing
+    // query rows and their lse; rows past the end repeat the last one (zeros times an infinite
+    // key would be NaN, which no lse takes back to 0) and weigh nothing
     const uint32_t n_q = (q_rows + 31) / 32;
     const int flip = a.negate ? (int)0x80008000 : 0;    // (as load_q8)
     for (uint32_t i0 = tid; i0 < n_q * 32 * CPR; i0 += 4 * 256) {
@@ -1490,8 +1491,7 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
         for (uint32_t x = 0; x < 4; ++x) {
             const uint32_t r = (i0 + 256 * x) / CPR, c = (i0 + 256 * x) % CPR;
             if (r < n_q * 32)
-                *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) =
-                    r < q_rows ? v[x] ^ flip : i32x4{0, 0, 0, 0};
+                *(i32x4 *)(qs + r * (2 * D) + 16 * swz<DC>(r, c)) = v[x] ^ flip;
         }
     }
     for (uint32_t r = tid; r < n_q * 32; r += 256) {

@@ -1,0 +1,86 @@
+"""Edges of the calls on a cache of key and value rows: infinite keys, long tails of small
+weights, launches past 2^32 threads, graphs, threads, autograd and arguments that alias."""
+import numpy as np
+import pytest
+
+from oracle import cache as ref
+from test_cache_gpu import Case, U, chain_tree, dev, host, say, tdtype
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2006_12608_amd  # noqa: F401  (fails loudly when libsj.so is missing)
+    yield
+    torch.cuda.synchronize()
+
+
+def check_row_at_minus_infinity(c, tree, w, out, n0):
+    """out and w (numpy) against the definition for a cache in which row n0's key scores -inf:
+    the row weighs 0, and everything else is as if it did not exist."""
+    d = c.q.shape[-1]
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, n0)
+    plain = c.k.copy()
+    plain[r] = 0.0
+    dots = ref.attend(plain, c.v, c.table, c.lens, c.q, tree, d ** -0.5, c.counts)[4]
+    want, lse, want_w, mag, _ = ref.attend(c.k, c.v, c.table, c.lens, c.q, tree, d ** -0.5, c.counts)
+    assert np.isfinite(lse).all() and (want_w[0, :, n0] == 0).all()
+    u, n = U[c.dtype], c.cache.room
+    rho = 4 * (d + 4) * 2.0 ** -24 * dots.max() + n * 2.0 ** -23 + 2.0 ** -19
+    tol = u * np.abs(want) + (u + rho) * mag + 2.0 ** -25 + n * 2.0 ** -25 * np.nanmax(np.abs(c.v))
+    assert (np.abs(out - want) <= tol).all()
+    R = c.q.shape[1] * c.q.shape[2] // c.k.shape[2]
+    assert (w[0, :, n0] == 0).all(), w[0, :, n0]
+    tol = (rho + (R + 2) * 2.0 ** -24) * want_w + 1e-30
+    assert (np.abs(w[..., :want_w.shape[2]] - want_w) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,group,d", [(4, 4, 64), (5, 4, 64), (10, 4, 128), (25, 4, 128), (16, 4, 64),
+                                       (5, 5, 256), (31, 3, 256), (33, 5, 72), (70, 4, 64)])
+def test_weights_of_a_row_hidden_by_an_infinite_key(dtype, T, group, d):
+    """A cached key whose element is -inf where every query's is positive: its score is -inf,
+    its weight 0, whatever number of query rows the tiles are padded from."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("infinite key", dtype, T, group, d)
+    c = Case(81, dtype, 1, T, 2, group, d, 16, [300])
+    c.dq[..., 3] = 1.0
+    c.q = host(c.dq)
+    for n0 in (5, 299):     # in a block of cached rows only, and beside the tokens' own
+        r = ref.row_of(c.table, c.page, c.k.shape[0], 0, n0)
+        kept = c.dk[r[0], r[1]].clone()
+        c.dk[r[0], r[1], :, 3] = float("-inf")
+        c.k = host(c.dk)
+        w = torch.full((1, 2, c.cache.room), float("nan"), device="cuda")
+        out, lse = sj.attend(c.cache, dev(c.lens), c.dq, weight_out=w)
+        check_row_at_minus_infinity(c, None, host(w), host(out), n0)
+        c.dk[r[0], r[1]] = kept
+
+
+def test_weights_of_an_infinite_key_without_kept_scores():
+    """16 query rows over so many columns that their scores are not kept."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("infinite key, wide")
+    page, width = 65536, 257
+    c = Case(82, "bf16", 1, 4, 1, 4, 64, 512, [300])
+    n0 = 17
+    k, v = (torch.zeros(1, page, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    for n in range(304):
+        r = ref.row_of(c.table, c.page, c.k.shape[0], 0, n)
+        if n == n0:
+            c.dk[r[0], r[1], :, 3] = float("-inf")
+        k[0, n], v[0, n] = c.dk[r[0], r[1]], c.dv[r[0], r[1]]
+    c.dq[..., 3] = 1.0
+    c.q, c.k = host(c.dq), host(c.dk)
+    w = torch.full((1, 1, page * width), float("nan"), device="cuda")
+    out, _ = sj.attend(sj.kv_cache(k, v, table), dev(c.lens), c.dq, weight_out=w)
+    assert (w[..., 304:] == 0).all()
+    check_row_at_minus_infinity(c, None, host(w[..., :c.cache.room]), host(out), n0)

@@ -6,8 +6,11 @@
 // One pass over the rows keeps (m, l, sum) and rescales them when m grows;
 // results over disjoint sets of rows join by the same rule.  The exponentials enter the
 // product with v rounded to 16 bits, as the matrix cores take them: each costs up to half a
-// unit of its last place, averaged over the rows, beside the rounding of out itself.
-// Statistics, sums and weights stay in 32 bits.
+// unit of its last place, which rows of equal scores share, beside the rounding of out itself.
+// Binary16 ends at 2^-14 (2^-24 with fewer bits): its exponentials are scaled by 2^LIFT, so that
+// the largest ones lie at the type's upper end and rows keep all their bits down to 2^-25 of
+// the largest, or 2^-28 (with the largest at 1, 32768 rows of weight e^-17.4 beside one of
+// weight 1 came out as 0).  Statistics, sums and weights stay in 32 bits.
 #pragma once
 
 #include <type_traits>
@@ -32,6 +35,9 @@ struct Elem<sjk::DT_F16> {
     typedef _Float16 one;
     typedef f16x8 eight;
     static constexpr uint32_t EXP = 0x7c00u;   // exponent bits: all set = not finite
+    // the exponentials' scale where the maximum is followed at once and where it is
+    // followed late, once a score is 2^LATE times the weight of m's: 2^15 at most
+    static constexpr int LIFT = 14, LATE = 4, LATE_LIFT = 11;
     static __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
@@ -48,6 +54,7 @@ struct Elem<sjk::DT_BF16> {
     typedef __bf16 one;
     typedef bf16x8 eight;
     static constexpr uint32_t EXP = 0x7f80u;
+    static constexpr int LIFT = 0, LATE = 8, LATE_LIFT = 0;     // (the exponents of fp32)
     static __device__ __forceinline__ f32x4 mma(i32x4 a, i32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
@@ -624,8 +631,8 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             top = fmaxf(top, __shfl_xor(top, 32));
             const float m_new = fmaxf(m[j], top);
             // nothing seen yet: any finite maximum will do
-            const float base = m_new == -INFINITY ? 0.f : m_new * a.scale2;
-            const float shrink = exp2_(m[j] * a.scale2 - base);
+            const float high = m_new == -INFINITY ? 0.f : m_new * a.scale2;
+            const float shrink = exp2_(m[j] * a.scale2 - high), base = high - E::LIFT;
             m[j] = m_new;
             float sum = 0.f;
 #pragma unroll
@@ -657,9 +664,11 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         cur = nxt;
     }
 
-    // join the lanes of a query, then the waves
+    // join the lanes of a query, then the waves; the scale 2^LIFT ends here
+    constexpr float DOWN = 1.f / (1 << E::LIFT);
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
+        l[j] *= DOWN;
         l[j] += __shfl_xor(l[j], 16);
         l[j] += __shfl_xor(l[j], 32);
         m[j] *= a.scale2;
@@ -676,7 +685,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 #pragma unroll
         for (uint32_t w = 0; w < AT_WAVES; ++w)
             top = fmaxf(top, stat[w][AT_Q * j + q16][0]);
-        const float f = exp2_(m[j] - (top == -INFINITY ? 0.f : top));
+        const float f = exp2_(m[j] - (top == -INFINITY ? 0.f : top)) * DOWN;
         if (j)
             __syncthreads();
         float *mine = (float *)my + q16 * OS;
@@ -1002,10 +1011,10 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 top = fmaxf(top, s[x][e]);
-        // m follows the maximum only once a score is 2^8 times the weight of m's: the
-        // exponentials then stay below 2^8, far from the 16-bit types' ends, and the sums are
-        // rescaled in few rounds instead of most (32 queries are in a wave)
-        if (__any(top * a.scale2 > m * a.scale2 + 8.f)) {
+        // m follows the maximum only once a score is 2^LATE times the weight of m's: the
+        // exponentials then stay below 2^LATE (times 2^LATE_LIFT), inside the 16-bit types, and
+        // the sums are rescaled in few rounds instead of most (32 queries are in a wave)
+        if (__any(top * a.scale2 > m * a.scale2 + E::LATE)) {
             top = fmaxf(top, __shfl_xor(top, 32));
             const float m_new = fmaxf(m, top);
             const float shrink =
@@ -1018,7 +1027,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                 for (int e = 0; e < 16; ++e)
                     O[y][e] *= shrink;
         }
-        const float base = m == -INFINITY ? 0.f : m * a.scale2;
+        const float base = (m == -INFINITY ? 0.f : m * a.scale2) - E::LATE_LIFT;
         i32x4 P[SR][2];
 #pragma unroll
         for (int x = 0; x < SR; ++x) {
@@ -1068,9 +1077,19 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
         round(i + 1, std::integral_constant<uint32_t, 1>());
     }
 
-    // join the halves of a query, then (QW = 2) the two waves of its rows
+    // join the halves of a query, then (QW = 2) the two waves of its rows; the scale
+    // 2^LATE_LIFT ends here
     m *= a.scale2;
     l += __shfl_xor(l, 32);
+    if constexpr (E::LATE_LIFT != 0) {
+        constexpr float DOWN = 1.f / (1 << E::LATE_LIFT);
+        l *= DOWN;
+#pragma unroll
+        for (int z = 0; z < DC; ++z)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                O[z][e] *= DOWN;
+    }
     if constexpr (RW == 2) {
         if (half == 0) {
             stat[wave][q32][0] = m;

@@ -84,3 +84,68 @@ def test_weights_of_an_infinite_key_without_kept_scores():
     out, _ = sj.attend(sj.kv_cache(k, v, table), dev(c.lens), c.dq, weight_out=w)
     assert (w[..., 304:] == 0).all()
     check_row_at_minus_infinity(c, None, host(w[..., :c.cache.room]), host(out), n0)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 24, 40, 100, 200])
+@pytest.mark.parametrize("x", [16.6, 17.4])
+def test_attend_far_tail(dtype, T, x):
+    """32768 rows of weight e^-x beside one of weight 1 whose value is 0: the rows are all there
+    is of the output.  Their exponentials enter the product as 16-bit values, rounded by u each,
+    and the output is rounded once; sums over n rows in fp32 and the exponentials' own error make
+    n 2^-24 + 2^-19.  Sequences enough that none is cut: a share without the row of weight 1
+    would take its tail's weights as 1."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("far tail", dtype, T, x)
+    n, d, B, page = 32769, 64, 2100, 64
+    width = -(-(n + T) // page)
+    k = torch.zeros(width, page, 1, d, device="cuda", dtype=tdtype(dtype))
+    v = torch.ones_like(k)
+    rows = k.view(-1, d)
+    rows[:, 0] = -x
+    rows[0, 0] = 0
+    rows[n:, 0] = -240
+    v.view(-1, d)[0] = 0
+    x = -float(rows[1, 0])
+    q = torch.zeros(B, T, 1, d, device="cuda", dtype=k.dtype)
+    q[..., 0] = 1
+    table = torch.arange(width, dtype=torch.int32, device="cuda")[None].expand(B, width)
+    out, lse = sj.attend(sj.kv_cache(k, v, table), torch.full((B,), n, dtype=torch.int32, device="cuda"),
+                         q, scale=1.0)
+    w = 32768 * np.exp(-x)
+    want = w / (1 + w)
+    tol = (2 * U[dtype] + n * 2.0 ** -24 + 2.0 ** -19) * want
+    assert float((out.double() - want).abs().max()) <= tol
+    assert float((lse.double() - np.log1p(w)).abs().max()) <= n * 2.0 ** -24 + 2.0 ** -19
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 24, 40, 100, 200])
+@pytest.mark.parametrize("step", [0.01, 0.2, 3.0])
+def test_attend_rising_scores(dtype, T, step):
+    """Scores that grow along the rows, so that the running maximum follows again and again:
+    nothing overflows, and exponentials below the smallest normal number of fp16 (rounded by
+    2^-25) are far below the largest: at most 2^-36 of it a row."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("rising", dtype, T, step)
+    n, d = 700, 64
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k = torch.zeros(1, n + T, 1, d, device="cuda", dtype=tdtype(dtype))
+    v = torch.randn(1, n + T, 1, d, device="cuda", generator=g).to(k.dtype)
+    steps = torch.arange(n + T, device="cuda") * step
+    k[0, :, 0, 0] = steps.to(k.dtype)
+    q = torch.zeros(1, T, 1, d, device="cuda", dtype=k.dtype)
+    q[..., 0] = 1
+    lens = np.array([n], np.int32)
+    out, lse = sj.attend(sj.kv_cache(k, v), dev(lens), q, scale=1.0)
+    want, want_lse, _, mag, dots = ref.attend(host(k), host(v), None, lens, host(q), None, 1.0)
+    u = U[dtype]
+    e = (d + 4) * 2.0 ** -24 * dots
+    rho = 4 * e + (n + T) * 2.0 ** -23 + 2.0 ** -19
+    tol = u * np.abs(want) + (u + rho[..., None]) * mag + 2.0 ** -25
+    tol = tol + (n + T) * 2.0 ** -36 * float(v.abs().max())
+    assert (np.abs(host(out) - want) <= tol).all()
+    assert (np.abs(host(lse) - want_lse) <= 2 * e + (n + T) * 2.0 ** -24 +
+            2.0 ** -20 * (1 + np.abs(want_lse))).all()

@@ -9,11 +9,13 @@ namespace {
 
 constexpr uint32_t RO_PAIRS = 256;   // sines kept per workgroup at most (tokens x pairs)
 constexpr uint32_t RO_TOKENS = 8;    // tokens of a workgroup at most
+constexpr uint64_t RO_GRID = 1u << 22;   // workgroups of a launch at most (one holds fewer
+                                         // than 2^32 threads)
 
 struct RotaryArgs {
     Rotary r;
     uint32_t tokens;          // of one workgroup
-    uint64_t n;               // batch * t
+    uint64_t first, n;        // first token of the launch; batch * t
     uint32_t turned;          // 16-byte pair chunks of a head: ceil(pairs / 8)
     uint32_t q_rest, k_rest;  // 16-element chunks of a head past the pairs, copied
     uint32_t q_items, k_items, items;  // (head, chunk) items of a token: queries, keys, all
@@ -78,7 +80,7 @@ __global__ void __launch_bounds__(256) rotary_rows(const RotaryArgs g)
     __shared__ Place place[RO_TOKENS];
     const Rotary &r = g.r;
     const uint32_t pairs = r.turn.pairs, stride = 8 * g.turned, d = r.d, rot = 2 * pairs;
-    const uint64_t tok0 = (uint64_t)blockIdx.x * g.tokens;
+    const uint64_t tok0 = g.first + (uint64_t)blockIdx.x * g.tokens;
     const uint32_t mine = g.n - tok0 < g.tokens ? (uint32_t)(g.n - tok0) : g.tokens;
     const uint32_t n_items = mine * g.items;
 
@@ -255,15 +257,20 @@ hipError_t launch_rotary(const Rotary &r, hipStream_t s)
         if (full >= 90)
             break;
     }
-    const dim3 grid((uint32_t)((g.n + g.tokens - 1) / g.tokens));
     const uint32_t passed = d - 2 * pairs;
     const bool exact = (pairs % 8 == 0 || (pairs > 8 && !in_place)) &&
                        (passed % 16 == 0 || passed > 16) && (d % 16 == 0 || d > 16);
-    if (r.dtype == sjk::DT_F16)
-        launch_rows<sjk::DT_F16>(g, grid, r.turn.layout == 0, exact, s);
-    else
-        launch_rows<sjk::DT_BF16>(g, grid, r.turn.layout == 0, exact, s);
-    return hipGetLastError();
+    hipError_t e = hipSuccess;
+    for (; g.first < g.n && e == hipSuccess; g.first += RO_GRID * g.tokens) {
+        const uint64_t groups = (g.n - g.first + g.tokens - 1) / g.tokens;
+        const dim3 grid((uint32_t)(groups < RO_GRID ? groups : RO_GRID));
+        if (r.dtype == sjk::DT_F16)
+            launch_rows<sjk::DT_F16>(g, grid, r.turn.layout == 0, exact, s);
+        else
+            launch_rows<sjk::DT_BF16>(g, grid, r.turn.layout == 0, exact, s);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace sjc

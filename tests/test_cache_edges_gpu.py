@@ -149,3 +149,27 @@ def test_attend_rising_scores(dtype, T, step):
     assert (np.abs(host(out) - want) <= tol).all()
     assert (np.abs(host(lse) - want_lse) <= 2 * e + (n + T) * 2.0 ** -24 +
             2.0 ** -20 * (1 + np.abs(want_lse))).all()
+
+
+def test_rotary_and_append_of_more_tokens_than_a_launch_has_threads():
+    """2^27 tokens of one head of 8: 8 tokens a workgroup of 256 would be 2^32 threads."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("many tokens")
+    n, half, d = 2 ** 27 + 1003, 2 ** 26, 8
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randint(-2 ** 14, 2 ** 14, (n, 1, d), generator=g, device="cuda",
+                      dtype=torch.int16).view(torch.float16)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    turns = sj.rotary_turns(d)
+    want = torch.empty_like(x)
+    for at in (0, half, 2 * half):
+        sj.rotary(x[at:at + half], pos[at:at + half], turns, out=want[at:at + half])
+    assert torch.equal(sj.rotary(x, pos, turns).view(torch.int16), want.view(torch.int16))
+    k, v = (torch.zeros(1, n + 5, 1, d, dtype=x.dtype, device="cuda") for _ in range(2))
+    lens = torch.tensor([5], dtype=torch.int32, device="cuda")
+    sj.cache_append(sj.kv_cache(k, v), lens, x[None], x[None], pos=pos[None], turns=turns)
+    assert torch.equal(k[0, 5:].view(torch.int16), want.view(torch.int16))
+    assert torch.equal(v[0, 5:].view(torch.int16), x.view(torch.int16))
+    del x, want, k, v
+    torch.cuda.empty_cache()

@@ -365,7 +365,8 @@ hipError_t launch_evict(const Evict &e, hipStream_t s)
     const uint32_t most = e.keep < e.src.room ? e.keep : e.src.room;
     if (err != hipSuccess || most == 0)
         return err;
-    const uint32_t chunks = (e.src.d + 7) / 8, rows_per = 64;
+    // 64 rows a workgroup, more where a launch would reach 2^32 threads
+    const uint32_t chunks = (e.src.d + 7) / 8, rows_per = most <= 1u << 29 ? 64 : 128;
     evict_copy<<<dim3((most + rows_per - 1) / rows_per, e.src.batch * e.src.heads), 256, 0, s>>>(
         e, chunks, PageDiv::of(chunks), rows_per);
     return hipGetLastError();

@@ -173,3 +173,28 @@ def test_rotary_and_append_of_more_tokens_than_a_launch_has_threads():
     assert torch.equal(v[0, 5:].view(torch.int16), x.view(torch.int16))
     del x, want, k, v
     torch.cuda.empty_cache()
+
+
+def test_evict_into_as_many_rows_as_a_cache_may_have():
+    """keep = 2^30: workgroups of 64 rows would be 2^32 threads."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("evict keep 2^30")
+    page, width = 2 ** 20, 2 ** 10
+    g = torch.Generator(device="cuda").manual_seed(6)
+    k, v = (torch.randn(2, page, 1, 8, generator=g, device="cuda").half() for _ in range(2))
+    k2, v2 = torch.zeros_like(k), torch.zeros_like(v)
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 1
+    lens = torch.tensor([70000], dtype=torch.int32, device="cuda")
+    w = torch.rand(1, 1, 100, generator=g, device="cuda")
+    index, n, left = sj.cache_evict(sj.kv_cache(k, v, table), lens, w, sj.kv_cache(k2, v2, table),
+                                    keep=2 ** 30, weight_out=torch.empty(1, 1, 200, device="cuda"))
+    assert int(n) == 70000
+    assert torch.equal(index[0, 0, :70000], torch.arange(70000, dtype=torch.int32, device="cuda"))
+    assert (index[0, 0, 70000:] == -1).all()
+    assert torch.equal(left[0, 0, :100], w[0, 0]) and (left[0, 0, 100:] == 0).all()
+    assert torch.equal(k2[1, :70000], k[1, :70000]) and torch.equal(v2[1, :70000], v[1, :70000])
+    assert (k2[0] == 0).all() and (k2[1, 70000:] == 0).all()
+    del index
+    torch.cuda.empty_cache()

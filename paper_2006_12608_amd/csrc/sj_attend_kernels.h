@@ -1287,13 +1287,17 @@ __device__ __forceinline__ void weigh_scores(const Attend &a, uint32_t QT, uint3
 }
 
 // What is left once the shares are there: the first `joins` workgroups join query rows (one each,
-// or four), the others weigh columns from the scores.
+// or four), the others weigh columns from the scores, a strip of 1024 at a time.
 template <int DT>
 __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, uint32_t D,
-                                                   uint32_t joins, bool four)
+                                                   uint32_t joins, uint32_t strips, bool four)
 {
     if (blockIdx.x >= joins) {
-        weigh_scores(a, QT, blockIdx.x - joins);
+        for (uint32_t s = blockIdx.x - joins; s < strips; s += gridDim.x - joins) {
+            if (s >= gridDim.x - joins)
+                __syncthreads();        // (the last strip's lse has been read)
+            weigh_scores(a, QT, s);
+        }
     } else if (!four) {
         join_row<DT, 256>(a, QT, D, blockIdx.x);
     } else {
@@ -1625,6 +1629,8 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
     }
 }
 
+constexpr uint32_t kStripGroups = 1u << 20;     // workgroups that weigh columns at most
+
 // The kernel for tiles of qt query rows.
 template <int DT, int DC, int FIT>
 void (*attend_kernel(uint32_t qt))(const Attend)
@@ -1657,7 +1663,10 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
                 a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
             const bool four = rows > 1024;
             const uint32_t joins = a.whole ? 0 : (uint32_t)(four ? (rows + 3) / 4 : rows);
-            attend_join<DT><<<dim3(joins + strips), 256, 0, s>>>(a, qt, 32 * DC, joins, four);
+            // (a launch holds fewer than 2^32 threads)
+            const uint32_t weighing = strips < kStripGroups ? strips : kStripGroups;
+            attend_join<DT><<<dim3(joins + weighing), 256, 0, s>>>(a, qt, 32 * DC, joins, strips,
+                                                                   four);
             if ((e = hipGetLastError()) != hipSuccess || a.scores)
                 return e;
         }

@@ -198,3 +198,25 @@ def test_evict_into_as_many_rows_as_a_cache_may_have():
     assert (k2[0] == 0).all() and (k2[1, 70000:] == 0).all()
     del index
     torch.cuda.empty_cache()
+
+
+def test_weights_of_more_columns_than_a_launch_has_threads():
+    """8 heads of 2^31 - 1 columns: workgroups of 1024 columns would be 2^32 threads."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("wide weights")
+    torch.cuda.empty_cache()
+    cols = 2 ** 31 - 1
+    if torch.cuda.mem_get_info()[0] < 90 * 2 ** 30:
+        pytest.skip("needs 90 GB of device memory")
+    c = Case(83, "bf16", 1, 2, 8, 2, 64, 16, [100])
+    narrow = torch.empty(1, 8, c.cache.room, device="cuda")
+    sj.attend(c.cache, dev(c.lens), c.dq, weight_out=narrow)
+    w = torch.zeros(1, 8, cols, device="cuda")
+    sj.attend(c.cache, dev(c.lens), c.dq, weight=w)
+    assert torch.equal(w[..., :c.cache.room], narrow)
+    for h in range(8):
+        for part in w[0, h, c.cache.room:].split(2 ** 28):
+            assert not part.any()
+    del w
+    torch.cuda.empty_cache()

@@ -631,9 +631,11 @@ class kv_cache:
         self.dtype, self.device = k.dtype, k.device
         self.heads, self.d, self.page = heads, d, page
         self.batch, self.width = (pages, 1) if table is None else table.shape
+        # (a table without columns has no address, but NULL would mean that there is none;
+        # nothing is read of it)
         self.raw = sj_cache(dtype_code(k), heads, d, pages, page, self.batch, self.width,
                             0 if table is None else table.stride(0),
-                            None if table is None else (table.data_ptr() or None),
+                            None if table is None else (_ptr(table) or _ptr(k)),
                             _ptr(k), _ptr(v), *k.stride()[:3], *v.stride()[:3])
 
     @property

@@ -220,3 +220,24 @@ def test_weights_of_more_columns_than_a_launch_has_threads():
             assert not part.any()
     del w
     torch.cuda.empty_cache()
+
+
+def test_a_cache_with_a_table_of_no_pages_has_no_rows():
+    """A table of width 0 is not the absence of a table: nothing is appended, seen or kept."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("no pages")
+    k, v = (torch.ones(2, 16, 1, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    c = sj.kv_cache(k, v, torch.zeros(2, 0, dtype=torch.int32, device="cuda"))
+    assert c.room == 0
+    lens = torch.tensor([3, 0], dtype=torch.int32, device="cuda")
+    row = torch.full((2, 1, 1, 64), 7.0, dtype=torch.float16, device="cuda")
+    sj.cache_append(c, lens, row, row)
+    assert (k == 1).all() and (v == 1).all()
+    for T in (1, 40):
+        w = torch.full((2, 1, 9), 5.0, device="cuda")
+        out, lse = sj.attend(c, lens, row.expand(2, T, 1, 64).contiguous(), weight=w)
+        assert (out == 0).all() and (lse == -np.inf).all() and (w == 5).all()
+    into = sj.kv_cache(k.clone(), v.clone())
+    index, n, _ = sj.cache_evict(c, lens, torch.ones(2, 1, 4, device="cuda"), into, keep=4)
+    assert (index == -1).all() and (n == 0).all() and (into.k == 1).all()

@@ -616,9 +616,17 @@ class kv_cache:
     adjacent elements in a row; table is a (sequences, pages of a sequence)
     int32 device tensor of page numbers (rows of a page number that does not
     exist, as -1, do not exist), or None when sequence b is page b.  Row n of
-    sequence b is row n % page of page table[b, n // page]."""
+    sequence b is row n % page of page table[b, n // page].  Another tensor may be
+    assigned to k, v or table; it is checked as here, together with the others."""
 
     def __init__(self, k, v, table=None):
+        self._describe(k, v, table)
+
+    k = property(lambda self: self._k, lambda self, x: self._describe(x, self._v, self._table))
+    v = property(lambda self: self._v, lambda self, x: self._describe(self._k, x, self._table))
+    table = property(lambda self: self._table, lambda self, x: self._describe(self._k, self._v, x))
+
+    def _describe(self, k, v, table):
         import torch
         if k.dtype not in (torch.float16, torch.bfloat16) or not k.is_cuda:
             raise ValueError("k must be a float16 or bfloat16 device tensor")
@@ -627,7 +635,7 @@ class kv_cache:
         pages, page, heads, d = k.shape
         if table is not None:
             _check_rows("table", table, (None, None), torch.int32, k.device)
-        self.k, self.v, self.table = k, v, table
+        self._k, self._v, self._table = k, v, table
         self.dtype, self.device = k.dtype, k.device
         self.heads, self.d, self.page = heads, d, page
         self.batch, self.width = (pages, 1) if table is None else table.shape

@@ -241,3 +241,30 @@ def test_a_cache_with_a_table_of_no_pages_has_no_rows():
     into = sj.kv_cache(k.clone(), v.clone())
     index, n, _ = sj.cache_evict(c, lens, torch.ones(2, 1, 4, device="cuda"), into, keep=4)
     assert (index == -1).all() and (n == 0).all() and (into.k == 1).all()
+
+
+def test_a_cache_follows_its_tensors():
+    """Another table, or other rows, put into a cache is what the next call reads; one that
+    does not fit is refused and changes nothing."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("other table")
+    c = Case(84, "f16", 2, 1, 2, 2, 64, 16, [60, 60])
+    lens = dev(c.lens)
+    want = sj.attend(c.cache, lens, c.dq)[0]
+    other = torch.flip(c.cache.table, (0,)).contiguous()
+    want_other = sj.attend(sj.kv_cache(c.dk, c.dv, other), lens, c.dq)[0]
+    assert not torch.equal(want, want_other)
+    first = c.cache.table
+    c.cache.table = other
+    assert torch.equal(sj.attend(c.cache, lens, c.dq)[0], want_other)
+    with pytest.raises(ValueError):
+        c.cache.table = other.long()
+    with pytest.raises(ValueError):
+        c.cache.k = c.dk[..., :32]
+    assert torch.equal(sj.attend(c.cache, lens, c.dq)[0], want_other)
+    c.cache.table = torch.cat([first, first[:, :1]], 1)      # wider
+    assert c.cache.width == first.shape[1] + 1 and c.cache.room == 16 * c.cache.width
+    assert torch.equal(sj.attend(c.cache, lens, c.dq)[0], want)
+    c.cache.v = torch.zeros_like(c.dv)
+    assert (sj.attend(c.cache, lens, c.dq)[0] == 0).all()

@@ -433,7 +433,8 @@ int sj_attend(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, const int3
  * index (batch x sets x keep int32, contiguous) receives the kept row numbers
  * in ascending order, then -1; new_len (int32 per sequence) min(n, keep); w_out (batch x sets x
  * w_out_cols fp32, contiguous, or NULL) the kept weights, then zeros.  Rows of dst past
- * new_len are left alone.  dst must not share rows with src, w_out none with weight.
+ * new_len are left alone.  dst must not share rows with src, w_out none with weight,
+ * and new_len must not be len.
  * Errors as the joins'; SJ_E_INVAL also for sink + recent > keep, caches that do not match or
  * sets other than 1 and heads; SJ_E_UNSUPPORTED for keep above dst's room or >= 2^31. */
 int sj_cache_evict(sj_ctx *ctx, const sj_cache *src, const int32_t *len, const float *weight,

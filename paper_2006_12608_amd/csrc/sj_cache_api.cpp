@@ -410,6 +410,8 @@ extern "C" int sj_cache_evict(sj_ctx *c, const sj_cache *src, const int32_t *len
         return st;
     if (w_out && w_out == weight && w_cols)
         return fail(SJ_E_INVAL, "w_out must not be weight");
+    if (new_len == len)
+        return fail(SJ_E_INVAL, "new_len must not be len");
     SJ_HIP(hipSetDevice(c->device));
     e.len = len;
     e.weight = weight;

@@ -268,3 +268,20 @@ def test_a_cache_follows_its_tensors():
     assert torch.equal(sj.attend(c.cache, lens, c.dq)[0], want)
     c.cache.v = torch.zeros_like(c.dv)
     assert (sj.attend(c.cache, lens, c.dq)[0] == 0).all()
+
+
+def test_evicted_lengths_that_alias_the_lengths_are_refused():
+    """new_len = len, which workgroups still read when others write it."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("aliases: len")
+    c = Case(85, "f16", 2, 6, 2, 3, 64, 16, [60, 33])
+    k2, v2 = torch.zeros_like(c.dk), torch.zeros_like(c.dv)
+    into = sj.kv_cache(k2, v2, c.cache.table)
+    lens, ctx = dev(c.lens), sj.context()
+    w = torch.rand(2, 2, c.cache.room, device="cuda")
+    index = torch.zeros(2, 2, 9, dtype=torch.int32, device="cuda")
+    st = sj.sj_cache_evict(ctx, c.cache.raw, lens.data_ptr(), w.data_ptr(), 2, c.cache.room, 9, 0, 0,
+                           into.raw, index.data_ptr(), lens.data_ptr())
+    assert st == sj.SJ_E_INVAL and "len" in sj.sj_last_error()
+    assert lens.tolist() == [60, 33] and (index == 0).all() and (k2 == 0).all()

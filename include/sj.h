@@ -409,7 +409,8 @@ int sj_cache_append(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, cons
  * q is batch x t x q_heads x d with strides {sequence, token, head};
  * out (batch x t x q_heads x d of dtype) and lse (batch x t x q_heads fp32, or NULL) are
  * contiguous; w_in and w_out (batch x heads x w_cols fp32, contiguous; w_in NULL:
- * zeros) may be the same array; w_out NULL: no weights.
+ * zeros) may be the same array; w_out NULL: no weights, and then out may be a
+ * contiguous q (otherwise the two must not overlap).
  * Arithmetic: fp32 sums of 16-bit products on the matrix cores; softmax statistics
  * and weights in fp32; exp(s_n - running maximum) enters the product with v as
  * 16-bit values.  The rows are cut into shares by the lengths, the shapes and the GPU's

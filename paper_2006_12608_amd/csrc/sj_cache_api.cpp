@@ -279,6 +279,15 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
         (st = check_array(c, out, q_rows * d * 2, 2, "out")) != SJ_OK ||
         (lse && (st = check_array(c, lse, q_rows * 4, 4, "lse")) != SJ_OK))
         return st;
+    if (out == q && q_rows) {
+        // each workgroup writes the query rows that it has read, but the weights read q again
+        if (w_out && w_cols)
+            return fail(SJ_E_INVAL, "out must not be q where weights are asked for");
+        if ((B > 1 && (uint64_t)q_stride[0] != (uint64_t)t * q_heads * d) ||
+            (t > 1 && (uint64_t)q_stride[1] != (uint64_t)q_heads * d) ||
+            (q_heads > 1 && q_stride[2] != d))
+            return fail(SJ_E_INVAL, "out is q with other strides");
+    }
     const uint64_t w_bytes = (uint64_t)B * a.c.heads * w_cols * 4;
     if (w_out) {
         if ((st = check_array(c, w_out, w_bytes, 4, "w_out")) != SJ_OK ||

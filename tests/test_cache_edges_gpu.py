@@ -285,3 +285,20 @@ def test_evicted_lengths_that_alias_the_lengths_are_refused():
                            into.raw, index.data_ptr(), lens.data_ptr())
     assert st == sj.SJ_E_INVAL and "len" in sj.sj_last_error()
     assert lens.tolist() == [60, 33] and (index == 0).all() and (k2 == 0).all()
+
+
+def test_an_output_that_aliases_the_queries():
+    """out = q is refused where the weights read q a second time, and right where they do not."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("aliases: out")
+    for T in (6, 30):
+        c = Case(85, "f16", 2, T, 2, 3, 64, 16, [60, 33])
+        lens, w = dev(c.lens), torch.rand(2, 2, c.cache.room, device="cuda")
+        want = sj.attend(c.cache, lens, c.dq)[0]
+        q = c.dq.clone()
+        with pytest.raises(sj.SjError, match="out"):
+            sj.attend(c.cache, lens, q, out=q, weight=w)
+        assert torch.equal(q, c.dq)
+        sj.attend(c.cache, lens, q, out=q)
+        assert torch.equal(q, want)

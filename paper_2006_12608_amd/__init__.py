@@ -610,6 +610,52 @@ def _ptr(x):
     return None if x is None else (x.data_ptr() or None)
 
 
+def _follows(*tensors) -> bool:
+    """Whether autograd follows a call on these tensors (None: not given)."""
+    import torch
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return torch.is_grad_enabled()
+    return False
+
+
+def _lost(name):
+    raise ValueError(f"{name}: a tensor requires grad, which the call would lose; "
+                     "call it under torch.no_grad() or detach the tensor")
+
+
+@functools.lru_cache(maxsize=None)
+def _functions():
+    """The calls as autograd sees them."""
+    import torch
+
+    class Rotary(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, pos, turns, kw, handle):
+            ctx.save_for_backward(pos, turns)
+            ctx.kw = kw
+            return rotary(x, pos, turns, ctx=handle, **kw)
+
+        @staticmethod
+        def backward(ctx, grad):
+            if grad.stride(-1) != 1:        # (a broadcast gradient, or another order)
+                grad = grad.contiguous()
+            back = dict(ctx.kw, inverse=not ctx.kw["inverse"])
+            return rotary(grad, *ctx.saved_tensors, **back), None, None, None, None
+
+    class NoGradient(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, name, call, *inputs):
+            ctx.name = name
+            return call()
+
+        @staticmethod
+        def backward(ctx, *grads):
+            raise RuntimeError(f"{ctx.name} has no gradient")
+
+    return Rotary, NoGradient
+
+
 class kv_cache:
     """A cache of key and value rows over tensors the caller owns: k and v are
     (pages, page, heads, d) float16 or bfloat16 device tensors, views of any strides with
@@ -682,9 +728,14 @@ def rotary(x, pos, turns, *, layout: str = "half", factor: float = 1.0, inverse:
     2 len(turns) elements of every head turned by the token's position (pos: int32
     per token) and scaled by `factor`; layout "half" pairs elements i and i +
     len(turns), "interleaved" 2 i and 2 i + 1.  inverse=True turns back: the
-    gradient with respect to x of the call without it, given the gradient of its result.
-    out may be x."""
+    gradient with respect to x of the call without it, given the gradient of its result;
+    autograd takes it where x requires grad.  out may be x."""
     import torch
+    if _follows(x, out):
+        if out is not None:
+            _lost("rotary with out")
+        return _functions()[0].apply(x, pos, turns, dict(layout=layout, factor=factor,
+                                                         inverse=inverse), ctx)
     code = _layout_code(layout)
     if x.dtype not in (torch.float16, torch.bfloat16) or not x.is_cuda:
         raise ValueError("x must be a float16 or bfloat16 device tensor")
@@ -714,8 +765,14 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     are (sequences, tokens, heads, d); lengths and counts int32 per sequence, pos
     int32 (sequences, tokens).  q (sequences, tokens, query heads, d), when
     given, is turned by the same positions and returned (in q_out, which may be
-    q)."""
+    q).  There is no gradient: a backward pass through the result raises."""
     import torch
+    if _follows(key, value, q, q_out, cache._k, cache._v):
+        if q is None or q_out is not None or _follows(cache._k, cache._v):
+            _lost("cache_append")
+        return _functions()[1].apply("cache_append", lambda: cache_append(
+            cache, lengths, key, value, pos=pos, turns=turns, q=q, layout=layout, factor=factor,
+            counts=counts, ctx=ctx), q, key, value)
     code = _layout_code(layout)
     B, dev = cache.batch, cache.device
     if key.dim() != 4:
@@ -764,8 +821,15 @@ def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=N
     token that sees nothing has out 0 and lse -inf.  With weight (float32
     (sequences, cache heads, columns)) the softmax weight that every row drew from all
     tokens and query heads is added to it in place; weight_out receives the sum instead
-    where given (with weight None, of this call alone)."""
+    where given (with weight None, of this call alone).  There is no gradient: a backward
+    pass through the results raises."""
     import torch
+    if _follows(q, out, weight, weight_out, cache._k, cache._v):
+        if out is not None or _follows(weight, weight_out):
+            _lost("attend")
+        return _functions()[1].apply("attend", lambda: attend(
+            cache, lengths, q, tree, scale=scale, counts=counts, weight=weight,
+            weight_out=weight_out, ctx=ctx), q, cache._k, cache._v)
     B, dev = cache.batch, cache.device
     if q.dim() != 4:
         _refuse("q", q, (B, None, None, cache.d), cache.dtype, dev)
@@ -813,6 +877,8 @@ def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recen
     -1; the new lengths (int32); and the kept weights, then zeros (weight_out where
     given, else as wide as index)."""
     import torch
+    if _follows(weight, weight_out, cache._k, cache._v, into._k, into._v):
+        _lost("cache_evict")
     B, dev = cache.batch, cache.device
     _check_whole("lengths", lengths, (B,), torch.int32, dev)
     if weight.dim() != 3:

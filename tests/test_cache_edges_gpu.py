@@ -302,3 +302,79 @@ def test_an_output_that_aliases_the_queries():
         assert torch.equal(q, c.dq)
         sj.attend(c.cache, lens, q, out=q)
         assert torch.equal(q, want)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotary_takes_part_in_autograd(layout, inverse):
+    """The gradient of rotary is rotary the other way round, with gradients of any strides,
+    and has a gradient itself."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("autograd", layout, inverse)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn(9, 3, 20, generator=g, device="cuda").half().requires_grad_()
+    pos = torch.arange(9, dtype=torch.int32, device="cuda") * 1001
+    turns = sj.rotary_turns(12)
+    kw = dict(layout=layout, factor=1.5)
+    y = sj.rotary(x, pos, turns, inverse=inverse, **kw)
+    assert y.requires_grad
+    grad = torch.randn(9, 3, 20, generator=g, device="cuda").half()
+    want = sj.rotary(grad, pos, turns, inverse=not inverse, **kw)
+    y.backward(grad)
+    assert torch.equal(x.grad, want)
+    wide = grad.transpose(0, 2).contiguous().transpose(0, 2)     # elements not adjacent
+    x.grad = None
+    sj.rotary(x, pos, turns, inverse=inverse, **kw).backward(wide)
+    assert torch.equal(x.grad, want)
+    x.grad = None
+    sj.rotary(x, pos, turns, inverse=inverse, **kw).sum().backward()
+    assert torch.equal(x.grad, sj.rotary(torch.ones_like(grad), pos, turns, inverse=not inverse, **kw))
+    v = grad.clone().requires_grad_()
+    first, = torch.autograd.grad(sj.rotary(x, pos, turns, inverse=inverse, **kw), x, v, create_graph=True)
+    second, = torch.autograd.grad(first, v, grad)
+    assert torch.equal(second, sj.rotary(grad, pos, turns, inverse=inverse, **kw))
+    with pytest.raises(ValueError, match="grad"):
+        sj.rotary(x, pos, turns, out=torch.empty_like(grad))
+    with torch.no_grad():
+        assert torch.equal(sj.rotary(x, pos, turns, inverse=inverse, out=torch.empty_like(grad), **kw), y)
+        assert not sj.rotary(x, pos, turns).requires_grad
+
+
+def test_calls_without_a_gradient_say_so():
+    """attend, and append's queries: a backward pass through them ends with an error instead of
+    a gradient that lacks their part."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("no gradient")
+    c = Case(86, "bf16", 2, 3, 2, 2, 64, 16, [40, 9])
+    lens = dev(c.lens)
+    want, want_lse = sj.attend(c.cache, lens, c.dq)
+    q = c.dq.clone().requires_grad_()
+    out, lse = sj.attend(c.cache, lens, q)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    for y in (out, lse):
+        with pytest.raises(RuntimeError, match="gradient"):
+            y.float().sum().backward(retain_graph=True)
+    with pytest.raises(ValueError, match="grad"):
+        sj.attend(c.cache, lens, q, out=torch.empty_like(c.dq))
+    row = torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    turned = sj.cache_append(c.cache, lens, row, row, q=q)
+    assert torch.equal(turned, c.dq)
+    with pytest.raises(RuntimeError, match="gradient"):
+        turned.float().sum().backward()
+    with pytest.raises(ValueError, match="grad"):
+        sj.cache_append(c.cache, lens, row, row, q=q, q_out=torch.empty_like(c.dq))
+    with pytest.raises(ValueError, match="grad"):       # no result to carry it
+        sj.cache_append(c.cache, lens, row.clone().requires_grad_(), row)
+    with torch.no_grad():
+        sj.cache_append(c.cache, lens, row.clone().requires_grad_(), row, q=q, q_out=q)
+        sj.attend(c.cache, lens, q, out=torch.empty_like(q))
+    assert not sj.attend(c.cache, lens, q.detach())[0].requires_grad
+    weight = torch.rand(2, 2, c.cache.room, device="cuda").requires_grad_()
+    with pytest.raises(ValueError, match="grad"):
+        sj.attend(c.cache, lens, c.dq, weight=weight)
+    into = sj.kv_cache(torch.zeros_like(c.dk), torch.zeros_like(c.dv), c.cache.table)
+    with pytest.raises(ValueError, match="grad"):
+        sj.cache_evict(c.cache, lens, weight, into, keep=4)
+    sj.cache_evict(c.cache, lens, weight.detach(), into, keep=4)

@@ -13,6 +13,7 @@
 #include <string>
 
 #include <mutex>
+#include <new>
 
 #include "sj_host.h"
 #include "sj_internal.h"
@@ -105,25 +106,31 @@ float float_at_or_below(double r)
     return f;
 }
 
-static void outgrown(sj_ctx *c, void *p)
+// Frees the context's buffer *p, or keeps it where a graph holds it.
+static int outgrow(sj_ctx *c, void **p, bool *held)
 {
-    if (!c->captured) {
+    if (*held) {
+        sj_kept *k = new (std::nothrow) sj_kept{*p, c->kept};
+        if (!k)
+            return fail(SJ_E_NOMEM, "out of host memory");
+        c->kept = k;
+    } else if (*p) {
         (void)hipStreamSynchronize(c->stream);
-        (void)hipFree(p);
-    } else if (c->n_retired < sizeof(c->retired) / sizeof(c->retired[0])) {
-        c->retired[c->n_retired++] = p;
+        (void)hipFree(*p);
     }
+    *p = nullptr;
+    *held = false;
+    return SJ_OK;
 }
 
 int grow_scratch(sj_ctx *c, size_t bytes)
 {
     if (bytes <= c->scratch_bytes)
         return SJ_OK;
-    if (c->scratch) {
-        outgrown(c, c->scratch);
-        c->scratch = nullptr;
-        c->scratch_bytes = 0;
-    }
+    const int st = outgrow(c, &c->scratch, &c->scratch_held);
+    if (st != SJ_OK)
+        return st;
+    c->scratch_bytes = 0;
     size_t want = bytes + bytes / 4;
     if (hipMalloc(&c->scratch, want) != hipSuccess) {
         (void)hipGetLastError();
@@ -163,11 +170,10 @@ int grow_arrivals(sj_ctx *c, size_t n)
 {
     if (n <= c->arrivals_n)
         return SJ_OK;
-    if (c->arrivals) {
-        outgrown(c, c->arrivals);
-        c->arrivals = nullptr;
-        c->arrivals_n = 0;
-    }
+    const int st = outgrow(c, (void **)&c->arrivals, &c->arrivals_held);
+    if (st != SJ_OK)
+        return st;
+    c->arrivals_n = 0;
     n = (n + 1023) & ~(size_t)1023;
     if (hipMalloc(&c->arrivals, n * 4) != hipSuccess) {
         (void)hipGetLastError();
@@ -796,8 +802,11 @@ void sj_destroy(sj_ctx *c)
     for (auto &ev : c->ev)
         if (ev)
             (void)hipEventDestroy(ev);
-    for (uint32_t i = 0; i < c->n_retired; ++i)
-        (void)hipFree(c->retired[i]);
+    while (sj_kept *k = c->kept) {
+        (void)hipFree(k->p);
+        c->kept = k->next;
+        delete k;
+    }
     if (c->scratch)
         (void)hipFree(c->scratch);
     if (c->front)

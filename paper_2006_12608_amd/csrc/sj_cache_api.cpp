@@ -63,7 +63,8 @@ int grow_both(sj_ctx *c, size_t bytes, size_t counters)
             return fail(SJ_E_UNSUPPORTED,
                         "scratch would grow during a capture (%zu bytes, %zu there): make the "
                         "call once on the stream before", bytes, c->scratch_bytes);
-        c->captured = true;
+        c->scratch_held = true;
+        c->arrivals_held = c->arrivals_held || counters != 0;
         return SJ_OK;
     }
     const int st = grow_scratch(c, bytes);

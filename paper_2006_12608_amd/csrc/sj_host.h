@@ -11,6 +11,12 @@
 
 #include "sj.h"
 
+// Device memory that a HIP graph may hold the address of, kept until sj_destroy.
+struct sj_kept {
+    void *p;
+    sj_kept *next;
+};
+
 struct sj_ctx {
     int device = 0;
     hipStream_t stream = nullptr;
@@ -26,9 +32,9 @@ struct sj_ctx {
     size_t front_bytes = 0;       // unpacked), kept apart from the join's scratch
     uint32_t *arrivals = nullptr; // counters of sj_attend's workgroups: 0 between kernels
     size_t arrivals_n = 0;
-    bool captured = false;        // a HIP graph may hold the scratch's and the counters' addresses:
-    void *retired[64] = {};       // what they outgrow from then on is freed by sj_destroy
-    uint32_t n_retired = 0;       // (beyond 64, not before the process ends)
+    bool scratch_held = false;    // a HIP graph may hold the present scratch's address, and
+    bool arrivals_held = false;   // the present counters'
+    sj_kept *kept = nullptr;      // such memory since outgrown
     hipEvent_t ev[6] = {};
     sj_stats stats = {};
 };

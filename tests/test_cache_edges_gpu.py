@@ -378,3 +378,54 @@ def test_calls_without_a_gradient_say_so():
     with pytest.raises(ValueError, match="grad"):
         sj.cache_evict(c.cache, lens, weight, into, keep=4)
     sj.cache_evict(c.cache, lens, weight.detach(), into, keep=4)
+
+
+def wide_cache(cols):
+    """A cache of one sequence with room for `cols` rows, of which one page of 1024 exists."""
+    import torch
+    import paper_2006_12608_amd as sj
+    k = torch.zeros(1, 1024, 1, 64, dtype=torch.float16, device="cuda")
+    table = torch.full((1, cols // 1024), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    return sj.kv_cache(k, k.clone(), table)
+
+
+def test_scratch_that_no_graph_holds_is_freed():
+    """After a capture the scratch that it holds stays; what later calls outgrow in turn is
+    freed.  16 query rows keep 64 bytes of scores a column, with a quarter more allocated."""
+    import gc
+    import torch
+    import paper_2006_12608_amd as sj
+    say("scratch freed")
+    c = Case(87, "f16", 1, 4, 1, 4, 64, 16, [300])
+    lens, w = dev(c.lens), torch.zeros(1, 1, c.cache.room, device="cuda")
+    want = sj.attend(c.cache, lens, c.dq, weight_out=torch.empty_like(w))
+    sizes = [2 ** e for e in range(20, 24)]
+    caches = [wide_cache(n) for n in sizes]
+    weights = torch.zeros(1, 1, sizes[-1], device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    gc.collect()
+    torch.cuda.empty_cache()        # (as a capture does: not to be mistaken for scratch)
+    free = torch.cuda.mem_get_info()[0]
+    ctx = sj.sj_create(torch.cuda.current_device(), stream.cuda_stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        sj.attend(c.cache, lens, c.dq, weight_out=w, ctx=ctx)
+        stream.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            out, lse = sj.attend(c.cache, lens, c.dq, weight_out=w, ctx=ctx)
+        for cache, n in zip(caches, sizes):
+            sj.attend(cache, lens, c.dq, weight_out=weights[..., :n], ctx=ctx)
+    torch.cuda.synchronize()
+    used = free - torch.cuda.mem_get_info()[0]
+    assert used <= 1.25 * 64 * sizes[-1] + 2 ** 27, used
+    for _ in range(2):
+        out.zero_()
+        w.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    del graph
+    sj.sj_destroy(ctx)

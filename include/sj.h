@@ -35,7 +35,8 @@
  *     partial sums stay below 2^24 in magnitude are therefore joined exactly.
  *   - Calls are ordered on the context's stream and return once the result
  *     count is known (they synchronise that stream).  Inputs must be ready on
- *     that stream.  A context is not thread-safe: use one per host thread.
+ *     that stream.  Calls of several host threads on one context wait for one
+ *     another (sj_get_stats then describes the last one of any thread).
  *   - Errors: every call returns a status (SJ_OK = 0 or a negative code) and
  *     never aborts or throws; sj_last_error() describes the last failure of the
  *     calling thread.

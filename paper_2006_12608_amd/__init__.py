@@ -283,7 +283,8 @@ _contexts: dict = {}
 
 def context(device: int | None = None, stream=None) -> int:
     """A cached context bound to (device, stream); defaults to torch's
-    current device and stream."""
+    current device and stream.  Threads that share a stream share its context:
+    their calls wait for one another."""
     import torch
     dev = torch.cuda.current_device() if device is None else int(device)
     if stream is None:
@@ -292,7 +293,10 @@ def context(device: int | None = None, stream=None) -> int:
     key = (dev, handle)
     known = _contexts.get(key)
     if known is None:
-        known = _contexts[key] = sj_create(dev, handle)
+        made = sj_create(dev, handle)
+        known = _contexts.setdefault(key, made)
+        if known != made:       # (another thread's came first)
+            sj_destroy(made)
     return known
 
 

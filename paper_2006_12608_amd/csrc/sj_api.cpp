@@ -675,6 +675,7 @@ int sj_join_ip(sj_ctx *ctx, int dtype, const void *P, uint32_t n_p, const void *
                unsigned flags)
 {
     g_err.clear();
+    const Alone alone(ctx);
     if (flags & ~(unsigned)(SJ_FLAG_TWO_PASS | SJ_FLAG_TIMING | SJ_FLAG_RECOMPUTE | SJ_FLAG_COSINE))
         return fail(SJ_E_INVAL, "unknown flags 0x%x", flags);
     Request rq{SJ_IP, dtype, P, Q, n_p, n_q, d, s, pairs, cap,
@@ -688,6 +689,7 @@ int sj_join_ip(sj_ctx *ctx, int dtype, const void *P, uint32_t n_p, const void *
 int sj_normalize(sj_ctx *ctx, int dtype, const void *X, uint32_t n, uint32_t d, void *Y)
 {
     g_err.clear();
+    const Alone alone(ctx);
     if (!ctx)
         return fail(SJ_E_INVAL, "context is NULL");
     if (dtype != SJ_F16 && dtype != SJ_BF16 && dtype != SJ_I8)
@@ -716,6 +718,7 @@ int sj_join_hamming(sj_ctx *ctx, const void *P, uint32_t n_p, const void *Q, uin
                     unsigned flags)
 {
     g_err.clear();
+    const Alone alone(ctx);
     return hamming_join(ctx, Request{SJ_IP, SJ_I8, P, Q, n_p, n_q, d, r, pairs, cap,
                                      (flags & SJ_FLAG_TWO_PASS) != 0, false,
                                      (flags & SJ_FLAG_TIMING) != 0,
@@ -728,6 +731,7 @@ int sj_join_l2(sj_ctx *ctx, int dtype, const void *P, uint32_t n_p, const void *
                unsigned flags)
 {
     g_err.clear();
+    const Alone alone(ctx);
     if (flags & ~(unsigned)(SJ_FLAG_TWO_PASS | SJ_FLAG_TIMING | SJ_FLAG_RECOMPUTE))
         return fail(SJ_E_INVAL, "flags 0x%x: sj_join_l2 takes SJ_FLAG_TWO_PASS, SJ_FLAG_TIMING "
                     "and SJ_FLAG_RECOMPUTE", flags);
@@ -742,6 +746,7 @@ int sji_join_sized(sj_ctx *ctx, int kind, int dtype, const void *P, uint32_t n_p
                    uint64_t *n_out, unsigned flags)
 {
     g_err.clear();
+    const Alone alone(ctx);
     if (!alloc)
         return fail(SJ_E_INVAL, "no allocation function");
     if (kind < 0 || kind > 2)
@@ -765,6 +770,7 @@ int sj_count(sj_ctx *ctx, int metric, int dtype, const void *P, uint32_t n_p, co
              uint32_t n_q, uint32_t d, double threshold, uint64_t *count)
 {
     g_err.clear();
+    const Alone alone(ctx);
     Request rq{metric, dtype, P, Q, n_p, n_q, d, threshold, nullptr, 0, true, true, false, false};
     return run(ctx, rq, count);
 }
@@ -774,6 +780,7 @@ int sj_join_noalloc(sj_ctx *ctx, int metric, int dtype, const void *P, uint32_t 
                     uint64_t cap, uint64_t *n_out, unsigned flags)
 {
     g_err.clear();
+    const Alone alone(ctx);
     if (!ctx)
         return fail(SJ_E_INVAL, "context is NULL");
     if (flags & ~(unsigned)(SJ_FLAG_TWO_PASS | SJ_FLAG_TIMING | SJ_FLAG_RECOMPUTE))

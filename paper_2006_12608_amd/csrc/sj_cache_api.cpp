@@ -253,6 +253,7 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
                          float *lse, const float *w_in, float *w_out, uint64_t w_cols)
 {
     g_err.clear();
+    const Alone alone(c);
     if (!c)
         return fail(SJ_E_INVAL, "context is NULL");
     sjc::Attend a{};
@@ -388,6 +389,7 @@ extern "C" int sj_cache_evict(sj_ctx *c, const sj_cache *src, const int32_t *len
                               int32_t *new_len, float *w_out, uint64_t w_out_cols)
 {
     g_err.clear();
+    const Alone alone(c);
     if (!c)
         return fail(SJ_E_INVAL, "context is NULL");
     sjc::Evict e{};

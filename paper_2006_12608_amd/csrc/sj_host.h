@@ -7,6 +7,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <mutex>
 #include <string>
 
 #include "sj.h"
@@ -37,6 +38,9 @@ struct sj_ctx {
     sj_kept *kept = nullptr;      // such memory since outgrown
     hipEvent_t ev[6] = {};
     sj_stats stats = {};
+    // held by calls that use any of the above (recursive: a caller's allocation function may
+    // run its own code)
+    std::recursive_mutex mutex;
 };
 
 namespace sjh {
@@ -54,6 +58,23 @@ int hip_fail(hipError_t e, const char *what);
         if (e_ != hipSuccess)                       \
             return sjh::hip_fail(e_, #call);        \
     } while (0)
+
+// Keeps other threads' calls off the context (NULL: refused later) while one runs.
+struct Alone {
+    sj_ctx *const c;
+    explicit Alone(sj_ctx *ctx) : c(ctx)
+    {
+        if (c)
+            c->mutex.lock();
+    }
+    ~Alone()
+    {
+        if (c)
+            c->mutex.unlock();
+    }
+    Alone(const Alone &) = delete;
+    Alone &operator=(const Alone &) = delete;
+};
 
 // Bytes per element of a dtype code.
 size_t esize(int dtype);

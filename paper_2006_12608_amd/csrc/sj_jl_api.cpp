@@ -23,6 +23,7 @@ extern "C" int sj_jl(sj_ctx *c, int dtype, const void *X, uint32_t n, uint32_t d
                      uint32_t levels, const uint32_t *shape, const float *A, float *Y)
 {
     g_err.clear();
+    const Alone alone(c);
     if (!c)
         return fail(SJ_E_INVAL, "context is NULL");
     if (dtype != SJ_F16 && dtype != SJ_BF16 && dtype != SJ_I8)

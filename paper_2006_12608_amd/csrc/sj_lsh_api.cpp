@@ -33,6 +33,7 @@ int lsh_join(sj_ctx *c, int metric, int dtype, const void *P, uint32_t n_p, cons
              uint64_t *n_out, uint64_t *n_cand)
 {
     g_err.clear();
+    const Alone alone(c);
     if (!c)
         return fail(SJ_E_INVAL, "context is NULL");
     if (!n_out)
@@ -354,6 +355,7 @@ extern "C" int sj_lsh_sort(sj_ctx *c, const uint64_t *keys, uint32_t n, uint32_t
                            uint32_t bits, uint32_t *perm)
 {
     g_err.clear();
+    const Alone alone(c);
     if (!c)
         return fail(SJ_E_INVAL, "context is NULL");
     if (bits > 64)

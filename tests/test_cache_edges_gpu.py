@@ -429,3 +429,43 @@ def test_scratch_that_no_graph_holds_is_freed():
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     del graph
     sj.sj_destroy(ctx)
+
+
+def test_two_threads_on_one_stream():
+    """Threads of a program share their stream's context: their calls do not mix."""
+    import threading
+    import torch
+    import paper_2006_12608_amd as sj
+    say("threads")
+    cases = [Case(88, "f16", 3, 2, 2, 4, 64, 16, [900, 33, 500]),
+             Case(89, "bf16", 2, 40, 1, 2, 128, 16, [50, 1200])]
+    rng = np.random.default_rng(3)
+    P = dev(rng.integers(-3, 4, (700, 64)), "f16")
+    jobs = []
+    for c in cases:
+        lens = dev(c.lens)
+
+        def job(c=c, lens=lens):
+            w = torch.empty(c.B, c.k.shape[2], c.cache.room, device="cuda")
+            return (*sj.attend(c.cache, lens, c.dq, weight_out=w), w)
+        jobs.append(job)
+    jobs.append(lambda: (sj.join_ip(P, P, 150.0, two_pass=True),))
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    wrong, errors = [], []
+
+    def work(i):
+        try:
+            for _ in range(60):
+                got = jobs[i]()
+                if not all(torch.equal(x, y) for x, y in zip(got, want[i])):
+                    wrong.append(i)
+        except Exception as e:      # (shown by the assertion below)
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors and not wrong, (errors, wrong)

@@ -131,8 +131,8 @@ typedef struct sj_stats {
 /* Create a context on `device` (a gfx950 GPU), bound to `stream` (a
  * hipStream_t; NULL = the null stream).  The context owns only its device
  * scratch (match counter, block counts and offsets, row norms), which grows on
- * demand and is freed by sj_destroy.  Returns SJ_E_UNSUPPORTED on a GPU that
- * is not gfx950. */
+ * demand and is freed by sj_destroy.  The stream may be under capture.  Returns
+ * SJ_E_UNSUPPORTED on a GPU that is not gfx950. */
 int sj_create(sj_ctx **ctx, int device, void *stream);
 
 /* Inner-product join (Section 4; cosine when the caller's rows are unit):

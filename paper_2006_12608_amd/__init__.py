@@ -769,7 +769,8 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     are (sequences, tokens, heads, d); lengths and counts int32 per sequence, pos
     int32 (sequences, tokens).  q (sequences, tokens, query heads, d), when
     given, is turned by the same positions and returned (in q_out, which may be
-    q).  There is no gradient: a backward pass through the result raises."""
+    q).  There is no gradient: a backward pass through the result raises.  May be
+    captured into a HIP graph, as rotary may."""
     import torch
     if _follows(key, value, q, q_out, cache._k, cache._v):
         if q is None or q_out is not None or _follows(cache._k, cache._v):
@@ -826,7 +827,12 @@ def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=N
     (sequences, cache heads, columns)) the softmax weight that every row drew from all
     tokens and query heads is added to it in place; weight_out receives the sum instead
     where given (with weight None, of this call alone).  There is no gradient: a backward
-    pass through the results raises."""
+    pass through the results raises.
+    In a HIP graph: a capture cannot grow the context's scratch, and contexts belong to
+    streams, so make the call once on the stream that captures, which torch.cuda.graph
+    has to be told:
+        with torch.cuda.stream(side): attend(...)
+        with torch.cuda.graph(g, stream=side): attend(...)"""
     import torch
     if _follows(q, out, weight, weight_out, cache._k, cache._v):
         if out is not None or _follows(weight, weight_out):
@@ -879,7 +885,7 @@ def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recen
     all heads, or one for each.  Returns (index, lengths, weight): index
     (sequences, 1 or heads, keep) int32, the kept rows in ascending order, then
     -1; the new lengths (int32); and the kept weights, then zeros (weight_out where
-    given, else as wide as index)."""
+    given, else as wide as index).  In a HIP graph: see attend."""
     import torch
     if _follows(weight, weight_out, cache._k, cache._v, into._k, into._v):
         _lost("cache_evict")

@@ -619,6 +619,23 @@ int hamming_join(sj_ctx *c, Request rq, unsigned flags, uint64_t *n_out)
     return run(c, rq, n_out);
 }
 
+// While the calling thread captures a stream, memory and events may only be made in the relaxed
+// mode (which records nothing of them); elsewhere the mode makes no difference.
+struct RelaxedCapture {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    bool set;
+    RelaxedCapture() : set(hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess)
+    {
+        if (!set)
+            (void)hipGetLastError();
+    }
+    ~RelaxedCapture()
+    {
+        if (set)
+            (void)hipThreadExchangeStreamCaptureMode(&mode);
+    }
+};
+
 }  // namespace
 
 extern "C" {
@@ -643,6 +660,7 @@ int sj_create(sj_ctx **out, int device, void *stream)
         return fail(SJ_E_UNSUPPORTED, "device %d is %s; this library is built for gfx950", device,
                     prop.gcnArchName);
     SJ_HIP(hipSetDevice(device));
+    const RelaxedCapture relaxed;
     sj_ctx *c = new (std::nothrow) sj_ctx();
     if (!c)
         return fail(SJ_E_NOMEM, "out of host memory");

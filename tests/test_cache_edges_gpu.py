@@ -469,3 +469,38 @@ def test_two_threads_on_one_stream():
         t.join()
     torch.cuda.synchronize()
     assert not errors and not wrong, (errors, wrong)
+
+
+def test_a_context_may_be_made_during_a_capture():
+    """torch.cuda.graph without a stream captures on one of its own, where the first call makes
+    its context.  Calls without scratch are then captured; one that needs scratch is refused,
+    and the capture goes on."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("context in a capture")
+    c = Case(90, "f16", 2, 3, 2, 4, 64, 16, [300, 33])
+    lens = dev(c.lens)
+    pos, turns = torch.arange(6, dtype=torch.int32, device="cuda"), sj.rotary_turns(64)
+    x = c.dq.view(6, 8, 64)
+    want = sj.rotary(x, pos, turns)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        ctx = sj.sj_create(torch.cuda.current_device(), stream.cuda_stream)
+        y = sj.rotary(x, pos, turns, ctx=ctx)
+        with pytest.raises(sj.SjError, match="capture"):
+            sj.attend(c.cache, lens, c.dq, ctx=ctx)
+        z = y + 1
+    for _ in range(3):
+        y.zero_()
+        z.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(z, want + 1)
+    with torch.cuda.stream(stream):     # and the context serves as any other
+        out = sj.attend(c.cache, lens, c.dq, ctx=ctx)[0]
+    torch.cuda.synchronize()
+    assert torch.equal(out, sj.attend(c.cache, lens, c.dq)[0])
+    del graph
+    sj.sj_destroy(ctx)

@@ -504,3 +504,31 @@ def test_a_context_may_be_made_during_a_capture():
     assert torch.equal(out, sj.attend(c.cache, lens, c.dq)[0])
     del graph
     sj.sj_destroy(ctx)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("T,group,d", [(6, 1, 64), (6, 4, 64), (6, 8, 128), (6, 12, 64), (40, 4, 64),
+                                       (30, 2, 256), (70, 4, 72)])
+def test_weights_of_hidden_rows_may_hold_anything(dtype, bad, T, group, d):
+    """A drafted token whose key and value are not finite and that no token sees: every output
+    and weight is that of the definition, and its own weight 0."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("hidden weights", dtype, bad, T, group, d)
+    c = Case(91, dtype, 1, T, 2, group, d, 16, [70])
+    tree = chain_tree(c.rng, 1, T)
+    tree[0, :, 0] &= np.uint64(2 ** 64 - 1 - 4)         # nobody sees token 2
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, 72)
+    for x in (c.dk, c.dv):
+        x[r[0], r[1]] = bad
+    c.k[r], c.v[r] = 0.0, 0.0
+    want, want_lse, want_w, mag, dots = ref.attend(c.k, c.v, c.table, c.lens, c.q, tree, d ** -0.5)
+    w = torch.full((1, 2, c.cache.room), float("nan"), device="cuda")
+    out, lse = sj.attend(c.cache, dev(c.lens), c.dq, dev(tree.view(np.int64)), weight_out=w)
+    assert np.array_equal(np.isinf(want_lse), np.isinf(host(lse))) and torch.isfinite(out).all()
+    w = host(w)
+    assert np.isfinite(w).all() and (w[0, :, 72] == 0).all()
+    rho = 4 * (d + 4) * 2.0 ** -24 * dots.max() + c.cache.room * 2.0 ** -23 + 2.0 ** -19
+    tol = (rho + (T * group + 2) * 2.0 ** -24) * want_w + 1e-30
+    assert (np.abs(w - want_w) <= tol).all()

@@ -1287,17 +1287,13 @@ __device__ __forceinline__ void weigh_scores(const Attend &a, uint32_t QT, uint3
 }
 
 // What is left once the shares are there: the first `joins` workgroups join query rows (one each,
-// or four), the others weigh columns from the scores, a strip of 1024 at a time.
+// or four), the others weigh columns from the scores, strips `first` on.
 template <int DT>
 __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, uint32_t D,
-                                                   uint32_t joins, uint32_t strips, bool four)
+                                                   uint32_t joins, uint32_t first, bool four)
 {
     if (blockIdx.x >= joins) {
-        for (uint32_t s = blockIdx.x - joins; s < strips; s += gridDim.x - joins) {
-            if (s >= gridDim.x - joins)
-                __syncthreads();        // (the last strip's lse has been read)
-            weigh_scores(a, QT, s);
-        }
+        weigh_scores(a, QT, first + (blockIdx.x - joins));
     } else if (!four) {
         join_row<DT, 256>(a, QT, D, blockIdx.x);
     } else {
@@ -1629,7 +1625,7 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
     }
 }
 
-constexpr uint32_t kStripGroups = 1u << 20;     // workgroups that weigh columns at most
+constexpr uint32_t kStrips = 1u << 20;     // of columns that one launch weighs at most
 
 // The kernel for tiles of qt query rows.
 template <int DT, int DC, int FIT>
@@ -1662,12 +1658,16 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
             const uint32_t strips =
                 a.scores ? (uint32_t)((a.w_cols + 1023) / 1024) * a.c.batch * a.c.heads : 0;
             const bool four = rows > 1024;
-            const uint32_t joins = a.whole ? 0 : (uint32_t)(four ? (rows + 3) / 4 : rows);
-            // (a launch holds fewer than 2^32 threads)
-            const uint32_t weighing = strips < kStripGroups ? strips : kStripGroups;
-            attend_join<DT><<<dim3(joins + weighing), 256, 0, s>>>(a, qt, 32 * DC, joins, strips,
-                                                                   four);
-            if ((e = hipGetLastError()) != hipSuccess || a.scores)
+            uint32_t joins = a.whole ? 0 : (uint32_t)(four ? (rows + 3) / 4 : rows), first = 0;
+            do {        // (a launch holds fewer than 2^32 threads)
+                const uint32_t left = strips - first, now = left < kStrips ? left : kStrips;
+                attend_join<DT><<<dim3(joins + now), 256, 0, s>>>(a, qt, 32 * DC, joins, first, four);
+                if ((e = hipGetLastError()) != hipSuccess)
+                    return e;
+                first += now;
+                joins = 0;
+            } while (first < strips);
+            if (a.scores)
                 return e;
         }
     }

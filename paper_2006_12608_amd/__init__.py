@@ -615,11 +615,10 @@ def _ptr(x):
 
 
 def _follows(*tensors) -> bool:
-    """Whether autograd follows a call on these tensors (None: not given)."""
-    import torch
+    """Whether one of the tensors (None: not given) requires grad."""
     for t in tensors:
         if t is not None and t.requires_grad:
-            return torch.is_grad_enabled()
+            return True
     return False
 
 
@@ -686,6 +685,7 @@ class kv_cache:
         if table is not None:
             _check_rows("table", table, (None, None), torch.int32, k.device)
         self._k, self._v, self._table = k, v, table
+        self.follows = _follows(k, v)
         self.dtype, self.device = k.dtype, k.device
         self.heads, self.d, self.page = heads, d, page
         self.batch, self.width = (pages, 1) if table is None else table.shape
@@ -735,11 +735,12 @@ def rotary(x, pos, turns, *, layout: str = "half", factor: float = 1.0, inverse:
     gradient with respect to x of the call without it, given the gradient of its result;
     autograd takes it where x requires grad.  out may be x."""
     import torch
-    if _follows(x, out):
-        if out is not None:
-            _lost("rotary with out")
-        return _functions()[0].apply(x, pos, turns, dict(layout=layout, factor=factor,
-                                                         inverse=inverse), ctx)
+    if x.requires_grad or _follows(out):
+        if torch.is_grad_enabled():
+            if out is not None:
+                _lost("rotary with out")
+            return _functions()[0].apply(x, pos, turns, dict(layout=layout, factor=factor,
+                                                             inverse=inverse), ctx)
     code = _layout_code(layout)
     if x.dtype not in (torch.float16, torch.bfloat16) or not x.is_cuda:
         raise ValueError("x must be a float16 or bfloat16 device tensor")
@@ -772,12 +773,13 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     q).  There is no gradient: a backward pass through the result raises.  May be
     captured into a HIP graph, as rotary may."""
     import torch
-    if _follows(key, value, q, q_out, cache._k, cache._v):
-        if q is None or q_out is not None or _follows(cache._k, cache._v):
-            _lost("cache_append")
-        return _functions()[1].apply("cache_append", lambda: cache_append(
-            cache, lengths, key, value, pos=pos, turns=turns, q=q, layout=layout, factor=factor,
-            counts=counts, ctx=ctx), q, key, value)
+    if cache.follows or key.requires_grad or value.requires_grad or _follows(q, q_out):
+        if torch.is_grad_enabled():
+            if q is None or q_out is not None or cache.follows:
+                _lost("cache_append")
+            return _functions()[1].apply("cache_append", functools.partial(
+                cache_append, cache, lengths, key, value, pos=pos, turns=turns, q=q, layout=layout,
+                factor=factor, counts=counts, ctx=ctx), q, key, value)
     code = _layout_code(layout)
     B, dev = cache.batch, cache.device
     if key.dim() != 4:
@@ -834,12 +836,13 @@ def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=N
         with torch.cuda.stream(side): attend(...)
         with torch.cuda.graph(g, stream=side): attend(...)"""
     import torch
-    if _follows(q, out, weight, weight_out, cache._k, cache._v):
-        if out is not None or _follows(weight, weight_out):
-            _lost("attend")
-        return _functions()[1].apply("attend", lambda: attend(
-            cache, lengths, q, tree, scale=scale, counts=counts, weight=weight,
-            weight_out=weight_out, ctx=ctx), q, cache._k, cache._v)
+    if cache.follows or q.requires_grad or _follows(out, weight, weight_out):
+        if torch.is_grad_enabled():
+            if out is not None or _follows(weight, weight_out):
+                _lost("attend")
+            return _functions()[1].apply("attend", functools.partial(
+                attend, cache, lengths, q, tree, scale=scale, counts=counts, weight=weight,
+                weight_out=weight_out, ctx=ctx), q, cache.k, cache.v)
     B, dev = cache.batch, cache.device
     if q.dim() != 4:
         _refuse("q", q, (B, None, None, cache.d), cache.dtype, dev)
@@ -887,8 +890,9 @@ def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recen
     -1; the new lengths (int32); and the kept weights, then zeros (weight_out where
     given, else as wide as index).  In a HIP graph: see attend."""
     import torch
-    if _follows(weight, weight_out, cache._k, cache._v, into._k, into._v):
-        _lost("cache_evict")
+    if cache.follows or into.follows or _follows(weight, weight_out):
+        if torch.is_grad_enabled():
+            _lost("cache_evict")
     B, dev = cache.batch, cache.device
     _check_whole("lengths", lengths, (B,), torch.int32, dev)
     if weight.dim() != 3:

@@ -378,6 +378,15 @@ def test_calls_without_a_gradient_say_so():
     with pytest.raises(ValueError, match="grad"):
         sj.cache_evict(c.cache, lens, weight, into, keep=4)
     sj.cache_evict(c.cache, lens, weight.detach(), into, keep=4)
+    own = sj.kv_cache(c.dk.clone().requires_grad_(), c.dv, c.cache.table)
+    for call in (lambda: sj.cache_append(own, lens, row, row, q=c.dq),
+                 lambda: sj.cache_evict(own, lens, weight.detach(), into, keep=4)):
+        with pytest.raises(ValueError, match="grad"):
+            call()
+        with torch.no_grad():
+            call()
+    with pytest.raises(RuntimeError, match="gradient"):
+        sj.attend(own, lens, c.dq)[0].float().sum().backward()
 
 
 def wide_cache(cols):

@@ -414,7 +414,8 @@ int sj_cache_append(sj_ctx *ctx, const sj_cache *cache, const int32_t *len, cons
  * contiguous q (otherwise the two must not overlap).
  * Arithmetic: fp32 sums of 16-bit products on the matrix cores; softmax statistics
  * and weights in fp32; exp(s_n - running maximum) enters the product with v as
- * 16-bit values.  The rows are cut into shares by the lengths, the shapes and the GPU's
+ * 16-bit values (fp16: scaled to the upper end of the type, so that weights down
+ * to 2^-25 of a row's largest keep all its bits).  The rows are cut into shares by the lengths, the shapes and the GPU's
  * number of CUs; whichever workgroup joins the shares adds them in their order, so
  * results do not depend on timing.
  * Errors as the joins'; SJ_E_INVAL also when heads does not divide q_heads or for a NaN

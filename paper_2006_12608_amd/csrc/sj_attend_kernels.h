@@ -768,8 +768,11 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 // chunks of a row are permuted by the row (swz) so that neither the K reads (16
 // rows, one chunk) nor the transposed V reads (4 rows, 4 chunks) meet in a bank.
 // Bound by HBM up to 64 query rows (16 sequences of 1024 to 6000 rows, 8 heads of 128: 242 MB in 51
-// us, 4.7 TB/s); with 256 rows (4 x 30000 to 32768) 132 GFLOP in 156 us, 850 TFLOP/s: matrix
-// cores 40% busy beside the exponentials of the same waves, clock 2.0 GHz.
+// us, 4.7 TB/s); with 256 rows (4 x 30000 to 32768) 132 GFLOP in 199 us in a row of calls (164
+// in the first, before the clock falls to 2 GHz), 660 TFLOP/s: matrix cores 38% busy, the
+// exponentials of the waves of a SIMD mostly beside each other's and not beside products.
+// Every query tile runs over all rows of its sequence: of a long chain's own rows half are
+// multiplied and masked.
 template <int DC>
 __device__ __forceinline__ uint32_t swz(uint32_t row, uint32_t chunk)
 {
@@ -1445,8 +1448,8 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 // kernels do, its waves 32 WT rows at a time in turn, the next rows' keys on their way to
 // registers while these are multiplied.  (With a workgroup for every 256 rows the
 // keys were waited for at each start: 131072 rows of 8 heads x 256 query rows, 185 us; 64
-// rows at a time, 121 us, need twice the registers; 32, 95 us: 720 TFLOP/s, matrix cores 31%
-// busy beside an exponential, a product and a sum per score.  64 query rows on 58000 rows
+// rows at a time, 121 us, need twice the registers; 32, 96 us (118 in a long row of calls): matrix
+// cores 31% busy beside an exponential, a product and a sum per score.  64 query rows on 58000 rows
 // of 8 heads: 25 us, 4.8 TB/s, bound by HBM.)
 template <int DC>
 constexpr uint32_t kWeighRows = DC == 8 ? 128 : 256;

@@ -1,7 +1,7 @@
 // sj_cache_api.cpp -- host side of the calls on a cache of key and value rows
 // (sj_rotary, sj_cache_append, sj_attend, sj_cache_evict; contracts in include/sj.h):
 // argument checks, scratch, and the kernels on the context's stream.  Nothing
-// here waits for the device.
+// here waits for the device but the replacement of scratch that a call outgrows.
 #include <hip/hip_runtime.h>
 
 #include <cmath>

@@ -34,6 +34,18 @@ __device__ __forceinline__ uint32_t to_bits(int dt, float x)
                              : (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
+// The turned pair.  Which product is fused with the sum is said, not left to the compiler, so that
+// all variants, and the two items of a chunk that is moved back, round alike.
+__device__ __forceinline__ float turn_a(float a, float b, float c, float s)
+{
+    return __builtin_fmaf(a, c, -(b * s));
+}
+
+__device__ __forceinline__ float turn_b(float a, float b, float c, float s)
+{
+    return __builtin_fmaf(b, c, a * s);
+}
+
 // One 8-pair chunk: lo and hi hold its 16 elements, (a_0 .. a_7) and (b_0 .. b_7) in the
 // half layout, (a_0, b_0, a_1, ..) in the interleaved one.
 template <int DT, bool HALF>
@@ -46,14 +58,14 @@ __device__ __forceinline__ void turn8(i32x4 &lo, i32x4 &hi, const float2 *cs)
             const int w = p >> 1, sh = 16 * (p & 1);
             const float a = to_float(DT, ((uint32_t)lo[w] >> sh) & 0xffffu);
             const float b = to_float(DT, ((uint32_t)hi[w] >> sh) & 0xffffu);
-            const uint32_t x = to_bits(DT, a * c - b * s), y = to_bits(DT, b * c + a * s);
+            const uint32_t x = to_bits(DT, turn_a(a, b, c, s)), y = to_bits(DT, turn_b(a, b, c, s));
             lo[w] = (int)(((uint32_t)lo[w] & ~(0xffffu << sh)) | (x << sh));
             hi[w] = (int)(((uint32_t)hi[w] & ~(0xffffu << sh)) | (y << sh));
         } else {
             i32x4 &v = p < 4 ? lo : hi;
             const uint32_t w = (uint32_t)v[p & 3];
             const float a = to_float(DT, w & 0xffffu), b = to_float(DT, w >> 16);
-            v[p & 3] = (int)(to_bits(DT, a * c - b * s) | (to_bits(DT, b * c + a * s) << 16));
+            v[p & 3] = (int)(to_bits(DT, turn_a(a, b, c, s)) | (to_bits(DT, turn_b(a, b, c, s)) << 16));
         }
     }
 }

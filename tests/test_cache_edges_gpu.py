@@ -541,3 +541,27 @@ def test_weights_of_hidden_rows_may_hold_anything(dtype, bad, T, group, d):
     rho = 4 * (d + 4) * 2.0 ** -24 * dots.max() + c.cache.room * 2.0 ** -23 + 2.0 ** -19
     tol = (rho + (T * group + 2) * 2.0 ** -24) * want_w + 1e-30
     assert (np.abs(w - want_w) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("n,heads,d,rot", [(9000, 32, 50, 34), (4000, 9, 211, 166), (9000, 12, 135, 50),
+                                           (20000, 8, 128, 100)])
+def test_rotary_rounds_alike_however_it_is_called(dtype, layout, n, heads, d, rot):
+    """In place, out of place and on the way into a cache, which take different loads, the same
+    pairs give the same bits."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("same bits", dtype, layout, n, heads, d, rot)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = (torch.randn(n, heads, d, generator=g, device="cuda") * 3).to(tdtype(dtype))
+    pos = torch.randint(-1000, 10 ** 6, (n,), generator=g, device="cuda", dtype=torch.int32)
+    turns = sj.rotary_turns(rot)
+    want = sj.rotary(x, pos, turns, layout=layout, factor=1.25)
+    y = x.clone()
+    assert torch.equal(sj.rotary(y, pos, turns, layout=layout, factor=1.25, out=y), want)
+    k, v = (torch.zeros(1, n, heads, d, dtype=x.dtype, device="cuda") for _ in range(2))
+    q = x[None].clone()
+    sj.cache_append(sj.kv_cache(k, v), torch.zeros(1, dtype=torch.int32, device="cuda"), x[None], x[None],
+                    pos=pos[None], turns=turns, q=q, q_out=q, layout=layout, factor=1.25)
+    assert torch.equal(k[0], want) and torch.equal(q[0], want) and torch.equal(v[0], x)

@@ -1,0 +1,747 @@
+"""Performance cases of the operators around drafted decoding over a cache held in
+8 bits: rows quantised as they are appended, attention over them, the pages of
+a shared cache (given out, forked, freed, copied), and the verification of
+drafted tokens.
+
+A case is a dict of plain values.  `prepare` makes its inputs on the GPU from
+a seed, `run` is one call as a program makes it: of the framework when `own`
+is true, of elementary torch operations otherwise.  `work` is the data and
+arithmetic a call cannot do without, `exact` the results from the definitions
+in 64 bits.
+
+A cache in 8 bits is a pool of pages of rows, k and v (pages, page, heads, d) in
+e4m3, with a power of two for each block of rows of a page and each head:
+exponents (pages, blocks of a page, heads, 2) int8, [..., 0] of k and [..., 1]
+of v.  An element stands for its e4m3 value times 2^exponent.  A block's exponent
+is the least with which its largest element is at most 448 (of 16-bit rows:
+-15 .. 7 for binary16, -117 .. 119 for bfloat16, so that every value that is held
+is one of the 16-bit type).
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+TORCH = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+LEAST = {"f16": -15, "bf16": -117}
+MOST = {"f16": 7, "bf16": 119}
+DEV = "cuda"
+
+
+def listed():
+    return [
+        # One decoding step of 64 users: keys (already turned) and values
+        # quantised into their pages, beside rows that are there: latency.
+        dict(name="append8_step_bf16_64x1", kind="append", dtype="bf16", B=64, T=1, kv=8, d=128,
+             page=16, blocks=1, lo=100, hi=4000),
+        # Prompts read in chunks of 2048 tokens.
+        dict(name="append8_prompt_f16_8x2048", kind="append", dtype="f16", B=8, T=2048, kv=8,
+             d=128, page=64, blocks=4, lo=0, hi=5000),
+        # One user, one token at a time, a small head and a short history:
+        # latency alone.
+        dict(name="attend8_one_f16_d64_n2048", kind="attend", dtype="f16", B=1, T=1, kv=2, group=4,
+             d=64, page=64, blocks=4, lo=2048, hi=2048, tree=False, weight=False),
+        # A batch of ordinary decoding steps, histories of very different
+        # lengths.
+        dict(name="attend8_batch_bf16_d128_n200_8192", kind="attend", dtype="bf16", B=32, T=1, kv=8,
+             group=4, d=128, page=16, blocks=1, lo=200, hi=8192, tree=False, weight=False),
+        # Trees of 64 drafted tokens over long histories, with the weights that
+        # a later eviction goes by: as much arithmetic as bytes.
+        dict(name="attend8_tree64_bf16_d128_n32768", kind="attend", dtype="bf16", B=4, T=64, kv=8,
+             group=4, d=128, page=64, blocks=4, lo=30000, hi=32768, tree=True, weight=True),
+        # The pages of a serving batch before a step of 16 drafted tokens.
+        dict(name="pages_step_32x16", kind="pages", B=32, out=32, page=16, lo=200, hi=8192,
+             pages=20000, T=16),
+        # Prompts forked into several answers each, some prompts finished and
+        # their pages free again, in a large pool.
+        dict(name="pages_fork_16_to_256", kind="pages", B=16, out=256, page=16, lo=2000, hi=60000,
+             pages=200000, T=64),
+        # The last pages of a forked prompt, for one layer.
+        dict(name="copy_fork_bf16_8", kind="copy", dtype="bf16", eight=False, n=8, kv=8, d=128,
+             page=16, blocks=1, pages=4096),
+        # The same for many sequences with long pages in 8 bits.
+        dict(name="copy_pages_e4m3_1024", kind="copy", dtype="f16", eight=True, n=1024, kv=8,
+             d=128, page=64, blocks=4, pages=4096),
+        # A chain of four drafted tokens of one user: latency.
+        dict(name="verify_chain_one_f32_v32768", kind="verify", dtype="f32", B=1, T=5, V=32768,
+             tree=False, draft=True, ragged=False),
+        # A serving batch's chains over a large vocabulary.
+        dict(name="verify_chain_batch_f32_v131072", kind="verify", dtype="f32", B=64, T=6,
+             V=131072, tree=False, draft=True, ragged=True),
+        # Trees of 32 tokens chosen without chance, probabilities in 16 bits.
+        dict(name="verify_tree_bf16_v65537", kind="verify", dtype="bf16", B=32, T=32, V=65537,
+             tree=True, draft=False, ragged=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["append", "append", "attend", "attend", "attend", "pages", "copy",
+                       "verify", "verify"])
+    if kind == "pages":
+        B, page = _log_int(rng, 1, 64), rng.choice([1, 16, 16, 48, 64, 100])
+        hi = _log_int(rng, page, 60000 if page >= 16 else 4000)
+        out = max(1, int(B * rng.uniform(0.5, 4.0)))
+        return dict(kind=kind, B=B, out=out, page=page, lo=rng.randint(1, hi), hi=hi,
+                    pages=(B + out) * (hi // page + 1) // rng.randint(1, 2) + out * 3 + 100,
+                    T=_log_int(rng, 1, 256))
+    if kind == "verify":
+        tree, B, T = rng.random() < 0.5, _log_int(rng, 1, 64), _log_int(rng, 2, 64)
+        V = _log_int(rng, 100, max(101, min(131072, 50000000 // (B * T))))
+        return dict(kind=kind, dtype=rng.choice(["f32", "f32", "f16", "bf16"]), B=B, T=T, V=V,
+                    tree=tree, draft=not tree and rng.random() < 0.8, ragged=rng.random() < 0.5)
+    dtype = rng.choice(["f16", "bf16"])
+    page, blocks = rng.choice([(16, 1), (16, 1), (16, 4), (48, 3), (64, 4), (64, 1), (64, 2),
+                               (100, 10), (256, 4)])
+    d = rng.choice([64, 64, 72, 80, 96, 128, 128, 128, 192, 256])
+    kv, group = rng.choice([1, 2, 4, 8, 8, 16]), rng.choice([1, 2, 3, 4, 4, 7, 8])
+    if kind == "copy":
+        n = _log_int(rng, 1, max(1, min(1024, 60000000 // (page * kv * d))))
+        return dict(kind=kind, dtype=dtype, eight=rng.random() < 0.5, n=n, kv=kv, d=d, page=page,
+                    blocks=blocks, pages=2 * n + rng.randint(0, n))
+    B = _log_int(rng, 1, 64)
+    if kind == "append":
+        T = _log_int(rng, 1, max(1, min(4096, 16000000 // (B * kv * d))))
+        lo = rng.randint(0, 3000)
+        return dict(kind=kind, dtype=dtype, B=B, T=T, kv=kv, d=d, page=page, blocks=blocks, lo=lo,
+                    hi=lo + rng.randint(0, max(1, min(3000, 100000000 // (B * kv * d)))))
+    B = min(B, 32)
+    T = rng.choice([1, 1, _log_int(rng, 2, 64), _log_int(rng, 2, 64)])
+    most = min(131072, 250000000 // (B * kv * d), 16000000000 // (B * T * kv * group * d))
+    hi = _log_int(rng, 16, max(16, most))
+    return dict(kind=kind, dtype=dtype, B=B, T=T, kv=kv, group=group, d=d, page=page,
+                blocks=blocks, lo=max(1, int(hi * rng.uniform(0.02, 1.0))), hi=hi,
+                tree=T > 1 and rng.random() < 0.75, weight=rng.random() < 0.5)
+
+
+# ------------------------------------------------------------------- inputs
+
+def _lengths(case):
+    """The lengths of a case's sequences, in increasing order: lo .. hi."""
+    B, lo, hi = case["B"], case["lo"], case["hi"]
+    return [hi if B == 1 else lo + (hi - lo) * b // (B - 1) for b in range(B)]
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _normal(g, shape, dtype, scale=1.0):
+    x = torch.randn(shape, generator=g, device=DEV, dtype=torch.float32)
+    return (x * scale).to(TORCH[dtype])
+
+
+def _exponent(most, dtype):
+    """The least exponent with which `most` (fp32) is at most 448, in the type's range."""
+    m, x = torch.frexp(most)
+    e = torch.where(most > 0, x - 9 + (m > 0.875).int(), LEAST[dtype])
+    return e.clamp(LEAST[dtype], MOST[dtype])
+
+
+def _two(e):
+    """2^e, exactly, for whole -127 < e < 128."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
+def _quantise(x, e):
+    """fp32 x at exponents e (which broadcast): e4m3, ties to even, saturated."""
+    return (x * _two(-e)).clamp(-448.0, 448.0).to(torch.float8_e4m3fn)
+
+
+def _take(x, *index):
+    """x[index] of an e4m3 tensor, by its bytes."""
+    return x.view(torch.uint8)[index].view(torch.float8_e4m3fn)
+
+
+def _put(x, y, *index):
+    """x[index] = y of e4m3 tensors, by their bytes."""
+    x.view(torch.uint8)[index] = y.view(torch.uint8)
+
+
+def _pool8(case, g, pages, fill=True):
+    """k, v and exponents of a cache in 8 bits.  The heads' rows differ in size, as keys and
+    values of models do."""
+    page, blocks, kv, d = case["page"], case["blocks"], case["kv"], case["d"]
+    k, v = (torch.zeros((pages, page, kv, d), dtype=torch.float8_e4m3fn, device=DEV)
+            for _ in range(2))
+    ex = torch.full((pages, blocks, kv, 2), LEAST[case["dtype"]], dtype=torch.int8, device=DEV)
+    if fill:
+        step = max(1, 8000000 // (page * kv * d))
+        for p in range(0, pages, step):
+            for i, x in enumerate((k, v)):
+                y = _normal(g, x[p:p + step].shape, case["dtype"]).float()
+                size = torch.exp2(torch.randint(-2, 2, (y.shape[0], 1, kv, 1), generator=g,
+                                                device=DEV).float())
+                y = (y * size).unflatten(1, (blocks, page // blocks))
+                e = _exponent(y.abs().amax((2, 4)), case["dtype"])          # pages blocks kv
+                x[p:p + step] = _quantise(y, e[:, :, None, :, None]).flatten(1, 2)
+                ex[p:p + step, :, :, i] = e.to(torch.int8)
+    return k, v, ex
+
+
+def _tree(case, rng):
+    """Ancestor masks of random trees of drafted tokens, 64 tokens a word: bit
+    s of token t's mask is set when t follows s (t itself included)."""
+    B, T = case["B"], case["T"]
+    W = -(-T // 64)
+    words = np.zeros((B, T, W), np.uint64)
+    for b in range(B):
+        masks = []
+        for t in range(T):
+            parent = int(rng.integers(max(-1, t - 8), t)) if t else -1
+            masks.append((masks[parent] if parent >= 0 else 0) | (1 << t))
+            for w in range(W):
+                words[b, t, w] = (masks[t] >> (64 * w)) & 0xFFFFFFFFFFFFFFFF
+    return torch.from_numpy(words.view(np.int64)).to(DEV)
+
+
+def _prepare_pages(case, st, g, rng):
+    lens = rng.permutation(_lengths(case))
+    st["lengths"] = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    B, out, page = case["B"], case["out"], case["page"]
+    width = -(-(case["hi"] + case["T"]) // page)
+    st["pages"] = max(case["pages"], sum(-(-n // page) for n in lens))
+    # pages in an order of their own; sequences hold what their rows need
+    order = torch.randperm(st["pages"], generator=g, device=DEV).cpu().numpy()
+    table, at = np.full((B, width), -1, np.int32), 0
+    for b, n in enumerate(lens):
+        held = -(-n // page)
+        table[b, :held] = order[at:at + held]
+        at += held
+    st["table"] = torch.from_numpy(table).to(DEV)
+    # the same sequences go on, or about nine in ten of them, several times each
+    if out == B:
+        parent = np.arange(B)
+    else:
+        parent = rng.choice(np.flatnonzero(rng.random(B) < 0.9) if B > 4 else np.arange(B), out)
+        parent = np.sort(parent)
+    st["parent"] = torch.from_numpy(parent.astype(np.int32)).to(DEV)
+
+
+def _prepare_verify(case, st, g, rng):
+    B, T, V, dtype = case["B"], case["T"], case["V"], case["dtype"]
+    parent = np.full((T,), -1, np.int32)
+    for n in range(1, T):
+        parent[n] = int(rng.integers(max(0, n - 6), n)) if case["tree"] else n - 1
+    st["parent"] = torch.from_numpy(parent).to(DEV)
+    tokens = torch.randint(0, V, (B, T), generator=g, device=DEV)
+    target = torch.empty((B, T, V), dtype=TORCH[dtype], device=DEV)
+    draft = torch.empty((B, T - 1, V), dtype=TORCH[dtype], device=DEV) if case["draft"] else None
+    ranks = [sum(parent[m] == parent[n] for m in range(n)) for n in range(T)]
+    for b in range(B):
+        # a target with a few likely tokens, and a smaller model's view of it
+        logits = 2.5 * torch.randn((T, V), generator=g, device=DEV)
+        target[b] = torch.softmax(logits, -1).to(TORCH[dtype])
+        view = logits + 0.7 * torch.randn((T, V), generator=g, device=DEV)
+        if draft is not None:
+            q = torch.softmax(view[:-1], -1)
+            draft[b] = q.to(TORCH[dtype])
+            tokens[b, 1:] = torch.multinomial(q, 1, generator=g)[:, 0]
+        elif case["tree"]:
+            top = view.topk(min(V, max(ranks) + 1), -1).indices
+            for n in range(1, T):
+                tokens[b, n] = top[parent[n], ranks[n]]
+        else:
+            tokens[b, 1:] = view[:-1].argmax(-1)
+    st["tokens"], st["target"], st["draft"] = tokens, target, draft
+    st["uniform"] = torch.rand((B, T), generator=g, device=DEV)
+    st["counts"] = None
+    if case["ragged"]:
+        st["counts"] = torch.from_numpy(rng.integers(1, T + 1, B).astype(np.int32)).to(DEV)
+
+
+def prepare(case, seed):
+    g, rng = _gen(seed), np.random.default_rng(seed)
+    st = {"case": case}
+    kind = case["kind"]
+    if kind == "pages":
+        _prepare_pages(case, st, g, rng)
+        return st
+    if kind == "verify":
+        _prepare_verify(case, st, g, rng)
+        return st
+    if kind == "copy":
+        page, kv, d, pages, n = (case[x] for x in ("page", "kv", "d", "pages", "n"))
+        if case["eight"]:
+            st["k"], st["v"], st["ex"] = _pool8(case, g, pages)
+        else:
+            st["k"], st["v"] = (_normal(g, (pages, page, kv, d), case["dtype"]) for _ in "kv")
+        order = torch.randperm(pages, generator=g, device=DEV).to(torch.int32)
+        rows = torch.randint(1, page + 1, (n,), generator=g, device=DEV, dtype=torch.int32)
+        # several copies of a page, as forks make them; every tenth entry asks for none
+        src = order[:n][torch.randint(0, n, (n,), generator=g, device=DEV)]
+        dst = order[n:2 * n]
+        none = torch.arange(n, device=DEV) % 10 == 9
+        st["copies"] = torch.stack([torch.where(none, -1, src), torch.where(none, -1, dst),
+                                    torch.where(none, 0, rows)], 1).to(torch.int32)
+        if own:
+            import paper_2006_12608_amd as sj
+            st["cache"] = (sj.kv_cache8(st["k"], st["v"], st["ex"], dtype=TORCH[case["dtype"]])
+                           if case["eight"] else sj.kv_cache(st["k"], st["v"]))
+        return st
+    lens = rng.permutation(_lengths(case))
+    st["lengths"] = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    B, T, kv, d, page = (case[x] for x in ("B", "T", "kv", "d", "page"))
+    width = -(-(max(lens) + T) // page)
+    st["table"] = torch.randperm(B * width, generator=g, device=DEV).to(torch.int32).view(B, width)
+    st["k"], st["v"], st["ex"] = _pool8(case, g, B * width)
+    if kind == "append":
+        # a fused projection's output: a token's keys and values; new rows that are now and
+        # then larger than a block's rows so far
+        kv_rows = _normal(g, (B, T, 2 * kv, d), case["dtype"])
+        st["key"], st["value"] = kv_rows.split([kv, kv], 2)
+    else:
+        st["q"] = _normal(g, (B, T, kv * case["group"], d), case["dtype"], 1.5)
+        if case["tree"]:
+            st["tree"] = _tree(case, rng)
+        if case["weight"]:
+            st["weight"] = torch.rand((B, kv, max(lens) + T), generator=g, device=DEV)
+    if own:
+        import paper_2006_12608_amd as sj
+        st["cache"] = sj.kv_cache8(st["k"], st["v"], st["ex"], st["table"],
+                                   dtype=TORCH[case["dtype"]])
+    return st
+
+
+# ---------------------------------------------------------- framework's calls
+
+def _run_own(st):
+    import paper_2006_12608_amd as sj
+    case = st["case"]
+    kind = case["kind"]
+    if kind == "append":
+        sj.cache_append(st["cache"], st["lengths"], st["key"], st["value"])
+        return st["k"], st["v"], st["ex"]
+    if kind == "pages":
+        return sj.cache_pages(st["table"], st["lengths"], case["T"], pages=st["pages"],
+                              page=case["page"], parent=st["parent"])
+    if kind == "copy":
+        sj.cache_copy(st["cache"], st["copies"])
+        return (st["k"], st["v"], st["ex"]) if case["eight"] else (st["k"], st["v"])
+    if kind == "verify":
+        return sj.verify_drafts(st["tokens"], st["target"], st["uniform"], draft=st["draft"],
+                                parent=st["parent"] if case["tree"] else None,
+                                counts=st["counts"])
+    if not case["weight"]:
+        return sj.attend(st["cache"], st["lengths"], st["q"], st.get("tree"))
+    weight = torch.empty_like(st["weight"])
+    out, lse = sj.attend(st["cache"], st["lengths"], st["q"], st.get("tree"), weight=st["weight"],
+                         weight_out=weight)
+    return out, lse, weight
+
+
+# ------------------------------------------------------------------ plain form
+
+def _append_plain(st, case):
+    B, T, kv, d, page = (case[x] for x in ("B", "T", "kv", "d", "page"))
+    size = page // case["blocks"]
+    lens, table = st["lengths"].long(), st["table"].long()
+    start, nb = lens % size, (T + size - 2) // size + 1
+    # place u of the rows of block j of the sequence's touched blocks, counted from the first
+    at = torch.arange(nb * size, device=DEV)[None, :] - start[:, None]      # B nb*size
+    new, old = (at >= 0) & (at < T), at < 0
+    n = (lens[:, None] + at).clamp(min=0)
+    p = table.gather(1, (n // page).clamp(max=table.shape[1] - 1))
+    slot = n % page
+    block = (slot // size).view(B, nb, size)[:, :, 0]
+    bp = p.view(B, nb, size)[:, :, 0]
+    touched = new.view(B, nb, size).any(2)                                   # B nb
+    held = old.view(B, nb, size).any(2)
+    for i, (rows, pool) in enumerate(((st["key"], st["k"]), (st["value"], st["v"]))):
+        x = torch.where(new[..., None, None],
+                        rows.float().gather(1, at.clamp(0, T - 1)[..., None, None]
+                                            .expand(B, nb * size, kv, d)), 0.0)
+        e = _exponent(x.abs().view(B, nb, size, kv, d).amax((2, 4)), case["dtype"])
+        was = st["ex"][bp, block, :, i].int()                                # B nb kv
+        e = torch.where(held[..., None], torch.maximum(e, was), e)
+        x = torch.where(old[..., None, None],
+                        _take(pool, p, slot).float()
+                        * _two(was.repeat_interleave(size, 1))[..., None], x)
+        y = _quantise(x, e.repeat_interleave(size, 1)[..., None])
+        live = (new | old).nonzero()
+        b, u = live[:, 0], live[:, 1]
+        _put(pool, _take(y, b, u), p[b, u], slot[b, u])
+        b, j = touched.nonzero().unbind(1)
+        st["ex"][bp[b, j], block[b, j], :, i] = e[b, j].to(torch.int8)
+    return st["k"], st["v"], st["ex"]
+
+
+def _rows(x, ex, table, case, rows):
+    """The rows 0 .. rows - 1 of every sequence: (B, rows, heads, d), fp32."""
+    at = torch.arange(rows, device=DEV)
+    p, slot = table[:, at // case["page"]].long(), at % case["page"]
+    e = ex[p, (slot // (case["page"] // case["blocks"]))[None, :]]
+    return _take(x, p, slot[None, :]).float() * _two(e)[..., None]
+
+
+def _attend_plain(st, case):
+    lens, table = st["lengths"].long(), st["table"].long()
+    B, T, kv, group, d = (case[x] for x in ("B", "T", "kv", "group", "d"))
+    n = max(_lengths(case)) + T
+    k = _rows(st["k"], st["ex"][..., 0], table, case, n).permute(0, 2, 3, 1)    # B kv d n
+    q = st["q"].float().view(B, T, kv, group, d).permute(0, 2, 1, 3, 4)
+    q = q.reshape(B, kv, T * group, d) / math.sqrt(d)
+    s = torch.matmul(q, k.contiguous()).view(B, kv, T, group, n)
+    at = torch.arange(n, device=DEV)
+    new = at[None, None, :] - lens[:, None, None]                           # B 1 n
+    t = torch.arange(T, device=DEV)[None, :, None]
+    if case["tree"]:
+        word = st["tree"].gather(2, (new.clamp(0, T - 1) // 64).expand(B, T, n))
+        seen = ((word >> (new.clamp(0, T - 1) % 64)) & 1).bool()
+        ok = (new < 0) | ((new < T) & seen)
+    else:
+        ok = new <= t
+    s = torch.where(ok[:, None, :, None, :], s, -math.inf)
+    top = s.amax(-1, keepdim=True)
+    p = torch.exp(s - top)
+    total = p.sum(-1, keepdim=True)
+    p = p / total
+    lse = (top + torch.log(total)).squeeze(-1)                              # B kv T group
+    v = _rows(st["v"], st["ex"][..., 1], table, case, n).permute(0, 2, 1, 3)    # B kv n d
+    out = torch.matmul(p.view(B, kv, T * group, n), v.contiguous())
+    out = out.view(B, kv, T, group, d).permute(0, 2, 1, 3, 4).reshape(B, T, kv * group, d)
+    out, lse = out.to(TORCH[case["dtype"]]), lse.permute(0, 2, 1, 3).reshape(B, T, kv * group)
+    if not case["weight"]:
+        return out, lse
+    return out, lse, st["weight"] + p.sum((2, 3))
+
+
+def _pages_plain(st, case):
+    page, pages, T, out = case["page"], st["pages"], case["T"], case["out"]
+    width = st["table"].shape[1]
+    parent = st["parent"].long()
+    tab = st["table"].long()[parent]
+    n = st["lengths"].long()[parent].clamp(0, width * page)
+    whole, part = n // page, n % page
+    w = torch.arange(width, device=DEV)[None, :]
+    real = (tab >= 0) & (tab < pages)
+    # pages whose rows are all there are shared (entry `pages` takes what is not)
+    shared = torch.zeros(pages + 1, dtype=torch.bool, device=DEV)
+    shared[torch.where(real & (w < whole[:, None]), tab, pages)] = True
+    # a partly filled page stays with the first sequence that goes on with it
+    last = tab.gather(1, whole.clamp(max=width - 1)[:, None])[:, 0]
+    has = (part > 0) & (last >= 0) & (last < pages)
+    me = torch.arange(out, device=DEV)
+    first = torch.full((pages + 1,), out, device=DEV)
+    first.scatter_reduce_(0, torch.where(has, last, pages), me, "amin")
+    at = last.clamp(0, pages - 1)
+    stays = has & ~shared[at] & (first[at] == me)
+    used = shared[:pages].clone()
+    used[at[stays]] = True
+    free = torch.sort(used.int(), stable=True).indices
+    n_free = pages - used.sum()
+    ends = (torch.clamp(n + T, max=width * page) + page - 1) // page
+    begins = whole + (part > 0).long()
+    copy = has & ~stays
+    need = copy.long() + (ends - begins).clamp(min=0)
+    base = need.cumsum(0) - need
+
+    def pick(i, ok):
+        return torch.where(ok & (i < n_free), free[i.clamp(0, pages - 1)], -1)
+    to = pick(base, copy)
+    fresh = (w >= begins[:, None]) & (w < ends[:, None])
+    i = base[:, None] + copy.long()[:, None] + (w - begins[:, None])
+    table = torch.where(w < begins[:, None], tab, pick(i, fresh))
+    table = torch.where(copy[:, None] & (w == whole[:, None]), to[:, None], table)
+    made = copy & (to >= 0)
+    copies = torch.stack([torch.where(made, last, -1), torch.where(made, to, -1),
+                          torch.where(made, part, 0)], 1)
+    lacking = need - (n_free - base).clamp(min=0).minimum(need)
+    return table.int(), n.int(), copies.int(), lacking.int()
+
+
+def _copy_plain(st, case):
+    # the rows of every page that are there, written where a copy is asked for
+    src, dst, rows = st["copies"].long().unbind(1)
+    live = (dst[:, None] >= 0) & (torch.arange(case["page"], device=DEV)[None, :] < rows[:, None])
+    i, r = live.nonzero().unbind(1)
+    for x in (st["k"], st["v"]):
+        x = x.view(torch.uint8) if case["eight"] else x
+        x[dst[i], r] = x[src[i], r]
+    if not case["eight"]:
+        return st["k"], st["v"]
+    size = case["page"] // case["blocks"]
+    some = (dst[:, None] >= 0) & (torch.arange(case["blocks"], device=DEV)[None, :] * size
+                                  < rows[:, None])
+    i, j = some.nonzero().unbind(1)
+    st["ex"][dst[i], j] = st["ex"][src[i], j]
+    return st["k"], st["v"], st["ex"]
+
+
+def _clean(x):
+    """Probabilities in 64 bits; what is no positive number counts as 0."""
+    x = x.double()
+    return torch.where((x > 0) & (x < math.inf), x, 0.0)
+
+
+def _verify_plain(st, case):
+    B, T, V = case["B"], case["T"], case["V"]
+    tokens, u = st["tokens"], st["uniform"].double()
+    parent = st["parent"].long()
+    counts = st["counts"]
+    counts = torch.full((B,), T, device=DEV) if counts is None else counts.long()
+    me = torch.arange(B, device=DEV)
+    cur, found = torch.zeros(B, dtype=torch.long, device=DEV), torch.ones(B, dtype=torch.long,
+                                                                           device=DEV)
+    path = torch.full((B, T), -1, dtype=torch.long, device=DEV)
+    path[:, 0] = 0
+    left = torch.ones(B, dtype=torch.float64, device=DEV)     # mass of a node's untried tokens
+    tried = torch.zeros((B, T), dtype=torch.bool, device=DEV)  # drafted tokens turned down here
+    for n in range(1, T):
+        x = tokens[:, n]
+        here = (parent[n] == cur) & (n < counts)
+        p = _clean(st["target"][me, cur, x])
+        if st["draft"] is not None:
+            ok = here & (u[:, n] * _clean(st["draft"][me, cur.clamp(max=T - 2), x]) < p)
+        else:
+            p = torch.where((tried & (tokens == x[:, None])).any(1), 0.0, p)
+            ok = here & (u[:, n] * left < p)
+            left = torch.where(ok, 1.0, torch.where(here, left - p, left))
+        tried[:, n] = here
+        tried &= ~ok[:, None]
+        cur = torch.where(ok, n, cur)
+        path[me, found.clamp(max=T - 1)] = torch.where(ok, n, path[me, found.clamp(max=T - 1)])
+        found = found + ok
+    r = p = _clean(st["target"][me, cur])
+    if st["draft"] is not None:
+        q = _clean(st["draft"][me, cur.clamp(max=T - 2)])
+        refused = tried.any(1)
+        r = torch.where(refused[:, None], (p - q).clamp(min=0), p)
+        r = torch.where((r.sum(1) > 0)[:, None], r, p)
+    else:
+        gone = torch.zeros((B, V + 1), dtype=torch.bool, device=DEV)
+        gone.scatter_(1, torch.where(tried, tokens, V), True)
+        r = torch.where(gone[:, :V], 0.0, p)
+        r = torch.where((r.sum(1) > 0)[:, None], r, p)
+    sums = r.cumsum(1)
+    i = (sums > (u[:, 0] * sums[:, -1])[:, None]).int()
+    nxt = torch.where(sums[:, -1] > 0, i.argmax(1), -1)
+    return path.int(), found.int(), nxt
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    case = state["case"]
+    return {"append": _append_plain, "attend": _attend_plain, "pages": _pages_plain,
+            "copy": _copy_plain, "verify": _verify_plain}[case["kind"]](state, case)
+
+
+# ------------------------------------------------------------------------ work
+
+def work(case):
+    kind = case["kind"]
+    if kind == "pages":
+        page = case["page"]
+        rows = (case["lo"] + case["hi"]) // 2
+        # the entries in use, read once a sequence that there was and written once a sequence
+        # that goes on
+        entries = case["B"] * -(-rows // page) + case["out"] * -(-(rows + case["T"]) // page)
+        return {"bytes": 4 * entries + 24 * case["out"] + case["pages"] // 8, "flops": entries}
+    if kind == "verify":
+        size = 4 if case["dtype"] == "f32" else 2
+        rows = 2 if case["draft"] else 1
+        return {"bytes": case["B"] * (rows * case["V"] * size + case["T"] * (2 * size + 16)),
+                "flops": case["B"] * case["V"] * (rows + 1)}
+    kv, d = case["kv"], case["d"]
+    if kind == "copy":
+        row = 2 * kv * d * (1 if case["eight"] else 2)
+        rows = (case["n"] - case["n"] // 10) * (case["page"] + 1) // 2
+        return {"bytes": 2 * rows * row, "flops": 0}
+    B, T = case["B"], case["T"]
+    if kind == "append":
+        return {"bytes": 6 * B * T * kv * d, "flops": 4 * B * T * kv * d}
+    heads, lens = kv * case["group"], _lengths(case)
+    n = sum(lens) + B * T
+    size = 2 * n * kv * d + 4 * B * T * heads * d + 4 * B * T * heads
+    if case["weight"]:
+        size += 8 * B * kv * (max(lens) + T)
+    return {"bytes": size, "flops": 4 * heads * T * n * d}
+
+
+# ----------------------------------------------------------------------- exact
+
+# the values of e4m3 by their bytes: 4 bits of exponent, 3 of mantissa, no infinities
+_E4M3 = np.array([(-1.0) ** (b >> 7) * (math.nan if b & 127 == 127 else
+                                        (b & 7) * 2.0 ** -9 if b & 120 == 0 else
+                                        (1 + (b & 7) / 8) * 2.0 ** ((b >> 3 & 15) - 7))
+                  for b in range(256)])
+
+
+def _values(x):
+    """e4m3 on the GPU as 64-bit values."""
+    return torch.from_numpy(_E4M3).to(DEV)[x.view(torch.uint8).long()]
+
+
+def _nearest(y):
+    """64-bit numbers rounded to e4m3: the spacing at 2^i <= |y| is 2^(i - 3), ties to even."""
+    i = torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6)))
+    i = torch.where(torch.exp2(i) > y.abs().clamp(min=2.0 ** -6), i - 1, i)
+    i = torch.where(torch.exp2(i + 1) <= y.abs(), i + 1, i)
+    step = torch.exp2(i - 3)
+    return (torch.round(y / step) * step).clamp(-448.0, 448.0)
+
+
+def _exact_append(case, st):
+    size, page, T = case["page"] // case["blocks"], case["page"], case["T"]
+    k, v, ex = _values(st["k"]), _values(st["v"]), st["ex"].double()
+    table, lens = st["table"].tolist(), st["lengths"].tolist()
+    for b, n0 in enumerate(lens):
+        for begin in range(n0 // size * size, n0 + T, size):
+            p, s = table[b][begin // page], begin % page
+            a = max(begin, n0) - begin          # rows of the block that are there
+            new = slice(max(begin, n0) - n0, min(begin + size, n0 + T) - n0)
+            z = min(begin + size, n0 + T) - begin
+            for i, (rows, pool) in enumerate(((st["key"], k), (st["value"], v))):
+                x = rows[b, new].double()       # rows kv d
+                most = x.abs().amax((0, 2))
+                e = torch.ceil(torch.log2(most.clamp(min=1e-300) / 448.0))
+                e = torch.where(torch.exp2(e - 1) * 448.0 >= most, e - 1, e)
+                e = torch.where(torch.exp2(e) * 448.0 < most, e + 1, e)
+                e = e.clamp(LEAST[case["dtype"]], MOST[case["dtype"]])
+                was = ex[p, s // size, :, i].clone()
+                if a:
+                    e = torch.maximum(e, was)
+                    pool[p, s:s + a] = _nearest(pool[p, s:s + a] * torch.exp2(was - e)[:, None])
+                pool[p, s + a:s + z] = _nearest(x * torch.exp2(-e)[:, None])
+                ex[p, s // size, :, i] = e
+    return k, v, ex.to(torch.int8)
+
+
+def _exact_pages(case, st):
+    page, pages, T = case["page"], st["pages"], case["T"]
+    old, lens = st["table"].cpu().numpy(), st["lengths"].tolist()
+    width = old.shape[1]
+    heirs = st["parent"].tolist()
+    n = [lens[p] for p in heirs]
+    whole = set()
+    for i, p in enumerate(heirs):
+        whole.update(old[p, :n[i] // page].tolist())
+    keeper = {}
+    for i, p in enumerate(heirs):
+        if n[i] % page:
+            q = int(old[p, n[i] // page])
+            if q not in whole:
+                keeper.setdefault(q, i)
+    free = sorted(set(range(pages)) - whole - set(keeper))
+    at = 0
+    table = np.full((len(heirs), width), -1, np.int32)
+    copies = np.array([[-1, -1, 0]] * len(heirs), np.int32)
+    lacking = np.zeros(len(heirs), np.int32)
+
+    def take(i):
+        nonlocal at
+        at += 1
+        if at <= len(free):
+            return free[at - 1]
+        lacking[i] += 1
+        return -1
+    for i, p in enumerate(heirs):
+        held = -(-n[i] // page)
+        table[i, :held] = old[p, :held]
+        if n[i] % page and keeper.get(int(old[p, held - 1])) != i:
+            new = take(i)
+            table[i, held - 1] = new
+            if new >= 0:
+                copies[i] = old[p, held - 1], new, n[i] % page
+        for w in range(held, min(-(-(n[i] + T) // page), width)):
+            table[i, w] = take(i)
+    return tuple(torch.from_numpy(x) for x in (table, np.array(n, np.int32), copies, lacking))
+
+
+def _exact_verify(case, st):
+    B, T = case["B"], case["T"]
+    path, found, nxt = np.full((B, T), -1, np.int32), np.zeros(B, np.int32), np.zeros(B, np.int64)
+    parent, u = st["parent"].tolist(), st["uniform"].double().cpu().numpy()
+    tokens = st["tokens"].cpu().numpy()
+    for b in range(B):
+        size = T if st["counts"] is None else int(st["counts"][b])
+        node, way, refused = 0, [0], False
+        p = st["target"][b, 0].double().cpu().numpy()
+        while True:
+            gone = set()
+            for c in (c for c in range(node + 1, size) if parent[c] == node):
+                x = int(tokens[b, c])
+                if st["draft"] is not None:
+                    refused = not u[b, c] * float(st["draft"][b, node, x]) < p[x]
+                    if not refused:
+                        break
+                else:
+                    rest = 1.0 - math.fsum(p[y] for y in gone)
+                    if x not in gone and u[b, c] * rest < p[x]:
+                        break
+                    gone.add(x)
+            else:
+                break
+            node = c
+            way.append(c)
+            p = st["target"][b, c].double().cpu().numpy()
+        r = p.copy()
+        if refused:
+            r = np.maximum(p - st["draft"][b, node].double().cpu().numpy(), 0.0)
+        r[list(gone)] = 0.0
+        if not r.any():
+            r = p
+        sums = np.cumsum(r)
+        nxt[b] = int(np.searchsorted(sums, u[b, 0] * sums[-1], side="right"))
+        path[b, :len(way)], found[b] = way, len(way)
+    return torch.from_numpy(path), torch.from_numpy(found), torch.from_numpy(nxt)
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "append":
+        return _exact_append(case, st)
+    if kind == "pages":
+        return _exact_pages(case, st)
+    if kind == "verify":
+        return _exact_verify(case, st)
+    if kind == "copy":
+        k = _values(st["k"]) if case["eight"] else st["k"].double()
+        v = _values(st["v"]) if case["eight"] else st["v"].double()
+        ex, size = st.get("ex"), case["page"] // case["blocks"]
+        for a, b, rows in st["copies"].tolist():
+            if b >= 0:
+                k[b, :rows], v[b, :rows] = k[a, :rows], v[a, :rows]
+                if ex is not None:
+                    ex[b, :-(-rows // size)] = ex[a, :-(-rows // size)]
+        return (k, v, ex) if case["eight"] else (k, v)
+    lens, table = st["lengths"].tolist(), st["table"].tolist()
+    B, T, kv, group, d, page = (case[x] for x in ("B", "T", "kv", "group", "d", "page"))
+    size = page // case["blocks"]
+    out = torch.empty((B, T, kv * group, d), dtype=torch.float64, device=DEV)
+    lse = torch.empty((B, T, kv * group), dtype=torch.float64, device=DEV)
+    weight = st["weight"].double() if case["weight"] else None
+    tree = st["tree"].cpu().numpy().view(np.uint64) if case["tree"] else None
+
+    def history(x, i, at, h, n):
+        e = torch.exp2(st["ex"][at, :, h, i].double()).repeat_interleave(size, 1)
+        return (_values(x[at, :, h]) * e[..., None]).reshape(-1, d)[:n]
+    for b, n in enumerate(lens):
+        ok = torch.ones((T, n + T), dtype=torch.bool)
+        for t in range(T):
+            for w in range(T):
+                ok[t, n + w] = bool((int(tree[b, t, w // 64]) >> (w % 64)) & 1) \
+                    if tree is not None else w <= t
+        ok = ok.to(DEV)
+        at = torch.tensor(table[b][:-(-(n + T) // page)], device=DEV)
+        for h in range(kv):
+            k, v = history(st["k"], 0, at, h, n + T), history(st["v"], 1, at, h, n + T)
+            mine = slice(h * group, (h + 1) * group)
+            for t0 in range(0, T, 16):
+                some = slice(t0, t0 + 16)
+                q = st["q"][b, some, mine].double()                          # t group d
+                s = (q.reshape(-1, d) @ k.T.contiguous()).view(-1, group, n + T) / math.sqrt(d)
+                s = s.masked_fill(~ok[some, None, :], -math.inf)
+                a = torch.softmax(s, -1)
+                out[b, some, mine] = (a.reshape(-1, n + T) @ v).view(-1, group, d)
+                lse[b, some, mine] = torch.logsumexp(s, -1)
+                if weight is not None:
+                    weight[b, h, :n + T] += a.sum((0, 1))
+    return (out, lse) if weight is None else (out, lse, weight)

@@ -500,7 +500,7 @@ def _verify_plain(st, case):
             ok = here & (u[:, n] * _clean(st["draft"][me, cur.clamp(max=T - 2), x]) < p)
         else:
             p = torch.where((tried & (tokens == x[:, None])).any(1), 0.0, p)
-            ok = here & (u[:, n] * left < p)
+            ok = here & (p > 0) & (u[:, n] * left < p)
             left = torch.where(ok, 1.0, torch.where(here, left - p, left))
         tried[:, n] = here
         tried &= ~ok[:, None]
@@ -673,7 +673,7 @@ def _exact_verify(case, st):
                         break
                 else:
                     rest = 1.0 - math.fsum(p[y] for y in gone)
-                    if x not in gone and u[b, c] * rest < p[x]:
+                    if x not in gone and p[x] > 0 and u[b, c] * rest < p[x]:
                         break
                     gone.add(x)
             else:

@@ -445,6 +445,111 @@ int sj_cache_evict(sj_ctx *ctx, const sj_cache *src, const int32_t *len, const f
                    const sj_cache *dst, int32_t *index, int32_t *new_len, float *w_out,
                    uint64_t w_out_cols);
 
+/* A cache in 8 bits: `rows` describes pages of e4m3 elements (1 bit of sign, 4 of exponent, 3 of
+ * mantissa, no infinities; k and v device bytes, strides in elements; d a multiple of 8), and
+ * rows.dtype is the 16-bit type of the keys and values appended to it, of the queries asked and of
+ * the results.  A page's rows form blocks of `block` (which divides page), and an element of row s,
+ * head h stands for its e4m3 value times 2^e, with e the exponent of its block and head:
+ *   e = exponents[((p * (page / block) + s / block) * heads + h) * 2]   of k, and + 1 of v
+ * (device, int8, caller-owned, contiguous, 2-byte aligned; values below -126 count as -126).
+ * sj_cache8_append sets them; every value that it keeps is one of the 16-bit type. */
+typedef struct sj_cache8 {
+    sj_cache rows;
+    int8_t *exponents;
+    uint32_t block;
+} sj_cache8;
+
+/* As sj_cache_append into a cache in 8 bits.  A block that receives rows from its beginning on gets
+ * the least exponent e with max |x| <= 448 2^e over the call's rows in it (-15 <= e <= 7 for SJ_F16
+ * and -117 <= e <= 119 for SJ_BF16; -15 and -117 where all are 0), for each head, of keys and of
+ * values; where rows before len[b] are in the block, its exponent stays if it is not less, and
+ * otherwise the block takes the new one and the rows before len[b] are rounded to it (slots from
+ * len[b] + count on are left as they were, and what they stand for changes with the exponent).  A row
+ * becomes x / 2^e, rounded to nearest even and held between -448 and 448; infinities
+ * and NaN become NaN and do not count for the exponents.  Keys are turned first, as
+ * sj_cache_append turns them, and rounded to the 16-bit type.  The blocks that a call appends to
+ * must be of one sequence each. */
+int sj_cache8_append(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
+                     uint32_t t, const void *key, const int64_t key_stride[3], const void *value,
+                     const int64_t value_stride[3], const int32_t *pos, const int64_t *turns,
+                     uint32_t n_pairs, int layout, double factor, const void *q,
+                     const int64_t q_stride[3], uint32_t q_heads, void *q_out,
+                     const int64_t q_out_stride[3]);
+
+/* sj_attend over a cache in 8 bits: the definitions, arithmetic and errors of sj_attend with k_n
+ * and v_n the 16-bit values that the elements stand for (an exponent that the append would not
+ * set may leave the type's range: such values round as the type does). */
+int sj_attend8(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
+               uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
+               const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,
+               float *lse, const float *w_in, float *w_out, uint64_t w_cols);
+
+/* The pages of sequences that go on, fork or end.  New sequence i < out_batch continues sequence
+ * parent[i] (device, int32; outside [0, batch): it begins empty; parent NULL: i itself), with its
+ * n = len[parent[i]] rows, and needs room for `tokens` more.  `pages` and `page` are the pool's as
+ * in sj_cache, table is batch x width (rows table_row entries apart) and out_table out_batch x width
+ * (contiguous).  Row i of it has
+ *   - the parent's pages that are full, which sequences share,
+ *   - the parent's last, partly filled page if no other new sequence has that page full and i is
+ *     the first of those to go on with it; else a free page, to be filled by a copy,
+ *   - free pages up to row min(n + tokens, width * page), then -1.
+ * Entries outside [0, pages) among the parent's stay as they are.  A page is free unless a
+ * new sequence has it by the first or second rule: the pages of sequences that nobody continues,
+ * and those past a sequence's rows, are.  Free pages are given out from the
+ * lowest number on, in the order of sequences and rows, the copy first; where none is left the
+ * entry is -1, and lacking[i] (int32) counts these.  new_len[i] (int32) receives n, and
+ * copies[3 i ..] (int32) the page to copy from, the page to copy to and the rows to copy, or
+ * -1, -1, 0 (see sj_cache_copy).  The lengths are clamped as in all calls on caches.
+ * No output may overlap an input.  Errors as the joins'; SJ_E_INVAL also for page = 0,
+ * SJ_E_UNSUPPORTED for width * page > 2^30, pages or out_batch * width >= 2^31. */
+int sj_cache_pages(sj_ctx *ctx, const int32_t *table, int64_t table_row, uint32_t batch,
+                   uint32_t width, uint32_t pages, uint32_t page, const int32_t *len,
+                   const int32_t *parent, uint32_t out_batch, uint32_t tokens, int32_t *out_table,
+                   int32_t *new_len, int32_t *copies, int32_t *lacking);
+
+/* Copies pages within a cache: for each of the n entries of copies (device, int32 {from, to, rows})
+ * the first `rows` rows (at most page) of page `from`, of all heads, k and v, to page `to`.  Entries whose pages
+ * do not exist, or are the same, copy nothing.  No page may be copied to by two entries or be both copied
+ * to and from.  The cache's table is not used.  Errors as the joins'. */
+int sj_cache_copy(sj_ctx *ctx, const sj_cache *cache, const int32_t *copies, uint32_t n);
+
+/* The same within a cache in 8 bits, with the exponents of the blocks that the rows are in. */
+int sj_cache8_copy(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *copies, uint32_t n);
+
+/* Types of probabilities: SJ_F16, SJ_BF16 or fp32. */
+enum sj_float { SJ_F32 = 5 };
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers.
+ * Sequence b has nodes 0 .. T - 1 (T = t, or count[b] clamped to [0, t]): node 0 is the last token of
+ * its text, node n > 0 the drafted token tokens[b * t + n] (int64), which follows node parent[n] < n
+ * (int32, row b at parent + b * parent_seq, so 0 shares one tree; parent NULL: a chain, n - 1; a
+ * node whose parent is not in [0, n) is never reached).
+ * p(n, x) = target[b * target_stride[0] + n * target_stride[1] + x] is the target's probability of
+ * token x after node n, x < vocab, in `dtype`; what is not a positive finite number counts as 0.
+ * From node c = 0 the walk tries the nodes n > c that follow c, in ascending order:
+ *   - with draft (chains only; row n, strides draft_stride, the distribution that token n + 1 was drawn
+ *     from; t - 1 rows): n = c + 1 is accepted if u(n) draft(c, x) < p(c, x), x its token;
+ *   - without (tokens chosen without chance): n is accepted if p(c, x) > 0 and
+ *     u(n) left < p(c, x), where left is 1 less the p(c, .) of the tokens refused at c; a token
+ *     refused there already has p = 0.
+ * An accepted node becomes c.  Where nothing more is accepted the text goes on with a token drawn by u(0): the
+ * lowest x with sum_{y <= x} r(y) > u(0) sum r, where r = max(p(c, .) - draft(c, .), 0) after a
+ * refusal with draft, else p(c, .) with 0 for the tokens refused at c; if r is 0 everywhere r
+ * is p(c, .), and if that is 0 everywhere the token is -1.  So text that follows the
+ * rule is distributed as the target's.  u(n) = uniform[b * t + n] (fp32, in [0, 1); outside it counts
+ * as the nearer end).
+ * path (batch x t int32) receives the nodes 0, .. accepted, then -1; found (int32 per sequence) their
+ * number; next (int64 per sequence) the drawn token; a sequence of no nodes has found = 0 and next = -1.
+ * Arithmetic: products, differences and sums in double, in an order that does not depend
+ * on timing.  In a HIP graph as sj_attend.
+ * Errors as the joins'; SJ_E_INVAL also for t = 0, vocab = 0 or draft with parent; SJ_E_UNSUPPORTED for t
+ * > 1024, vocab or batch >= 2^31 / 1024. */
+int sj_verify(sj_ctx *ctx, int dtype, uint32_t batch, uint32_t t, uint32_t vocab,
+              const int64_t *tokens, const int32_t *parent, int64_t parent_seq, const int32_t *count,
+              const void *target, const int64_t target_stride[2], const void *draft,
+              const int64_t draft_stride[2], const float *uniform, int32_t *path, int32_t *found,
+              int64_t *next);
+
 /* Free the context and its scratch; NULL is a no-op. */
 void sj_destroy(sj_ctx *ctx);
 

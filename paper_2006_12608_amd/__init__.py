@@ -7,7 +7,8 @@ sj_join_hamming, sj_join_lsh, sj_lsh_sort, sj_lsh_collision, sj_lsh_plan, sj_jl,
 sj_get_stats, sj_last_error) with plain integer pointers; `join_ip`, `join_l2`, `count` and
 `join_lsh` (the LSH-bucketed join of Theorem 3) are conveniences over PyTorch
 device tensors, as are `rotary`, `cache_append`, `attend` and `cache_evict` around a
-cache of key and value rows (`kv_cache`).  This module only marshals
+cache of key and value rows (`kv_cache`, or `kv_cache8` in 8 bits), `cache_pages` and `cache_copy`
+for its pages, and `verify_drafts`.  This module only marshals
 arguments: every step of the join runs in the library's HIP kernels.  Import
 fails when libsj.so has not been built (python paper_2006_12608_amd/build.py).
 """
@@ -21,6 +22,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsj.so")
 
 SJ_F16, SJ_BF16, SJ_I8 = 1, 2, 3
+SJ_F32 = 5
 SJ_IP, SJ_L2 = 0, 1
 SJ_OK, SJ_E_INVAL, SJ_E_OVERFLOW, SJ_E_NOMEM, SJ_E_HIP, SJ_E_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 SJ_FLAG_TWO_PASS, SJ_FLAG_TIMING, SJ_FLAG_RECOMPUTE, SJ_FLAG_COSINE = 1, 2, 4, 8
@@ -53,6 +55,10 @@ class sj_cache(ctypes.Structure):
                 ("table", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
                 ("k_page", ctypes.c_int64), ("k_row", ctypes.c_int64), ("k_head", ctypes.c_int64),
                 ("v_page", ctypes.c_int64), ("v_row", ctypes.c_int64), ("v_head", ctypes.c_int64)]
+
+
+class sj_cache8(ctypes.Structure):
+    _fields_ = [("rows", sj_cache), ("exponents", ctypes.c_void_p), ("block", ctypes.c_uint32)]
 
 
 # allocation of an output half-way through a call, once its size is known
@@ -118,6 +124,21 @@ def _load():
     lib.sj_cache_evict.argtypes = [vp, cache, vp, vp, u32, u64, u32, u32, u32, cache, vp, vp, vp,
                                    u64]
     lib.sj_cache_evict.restype = i32
+    cache8 = ctypes.POINTER(sj_cache8)
+    lib.sj_cache8_append.argtypes = [vp, cache8, *lib.sj_cache_append.argtypes[2:]]
+    lib.sj_cache8_append.restype = i32
+    lib.sj_attend8.argtypes = [vp, cache8, *lib.sj_attend.argtypes[2:]]
+    lib.sj_attend8.restype = i32
+    lib.sj_cache_pages.argtypes = [vp, vp, ctypes.c_int64, u32, u32, u32, u32, vp, vp, u32, u32, vp,
+                                   vp, vp, vp]
+    lib.sj_cache_pages.restype = i32
+    lib.sj_cache_copy.argtypes = [vp, cache, vp, u32]
+    lib.sj_cache_copy.restype = i32
+    lib.sj_cache8_copy.argtypes = [vp, cache8, vp, u32]
+    lib.sj_cache8_copy.restype = i32
+    lib.sj_verify.argtypes = [vp, i32, u32, u32, u32, vp, vp, ctypes.c_int64, vp, vp, strides, vp,
+                              strides, vp, vp, vp, vp]
+    lib.sj_verify.restype = i32
     lib.sj_destroy.argtypes = [vp]
     lib.sj_destroy.restype = None
     lib.sj_get_stats.argtypes = [vp, ctypes.POINTER(sj_stats)]
@@ -266,6 +287,50 @@ def sj_cache_evict(ctx, src, length, weight, sets, w_cols, keep, sink, recent, d
                               sets, w_cols, keep, sink, recent,
                               None if dst is None else ctypes.byref(dst), index, new_len, w_out,
                               w_out_cols)
+
+
+def sj_cache8_append(ctx, cache, length, count, t, key, key_stride, value, value_stride, pos,
+                     turns, n_pairs, layout, factor, q=None, q_stride=(0, 0, 0), q_heads=0,
+                     q_out=None, q_out_stride=(0, 0, 0)):
+    """Returns the status; cache is an sj_cache8 structure (or None)."""
+    return lib.sj_cache8_append(ctx, None if cache is None else ctypes.byref(cache), length, count,
+                                t, key, _strides(*key_stride), value, _strides(*value_stride), pos,
+                                turns, n_pairs, layout, factor, q, _strides(*q_stride), q_heads,
+                                q_out, _strides(*q_out_stride))
+
+
+def sj_attend8(ctx, cache, length, count, t, q, q_stride, q_heads, tree, tree_stride, scale, out,
+               lse, w_in=None, w_out=None, w_cols=0):
+    """Returns the status; cache is an sj_cache8 structure (or None)."""
+    return lib.sj_attend8(ctx, None if cache is None else ctypes.byref(cache), length, count, t, q,
+                          _strides(*q_stride), q_heads, tree, _strides(*tree_stride), scale, out,
+                          lse, w_in, w_out, w_cols)
+
+
+def sj_cache_pages(ctx, table, table_row, batch, width, pages, page, length, parent, out_batch,
+                   tokens, out_table, new_len, copies, lacking):
+    """Returns the status; pointers are integers (device addresses)."""
+    return lib.sj_cache_pages(ctx, table, table_row, batch, width, pages, page, length, parent,
+                              out_batch, tokens, out_table, new_len, copies, lacking)
+
+
+def sj_cache_copy(ctx, cache, copies, n):
+    """Returns the status; cache is an sj_cache structure (or None)."""
+    return lib.sj_cache_copy(ctx, None if cache is None else ctypes.byref(cache), copies, n)
+
+
+def sj_cache8_copy(ctx, cache, copies, n):
+    """Returns the status; cache is an sj_cache8 structure (or None)."""
+    return lib.sj_cache8_copy(ctx, None if cache is None else ctypes.byref(cache), copies, n)
+
+
+def sj_verify(ctx, dtype, batch, t, vocab, tokens, parent, parent_seq, count, target, target_stride,
+              draft, draft_stride, uniform, path, found, next):
+    """Returns the status; strides are sequences of element strides, the other
+    arrays device addresses."""
+    return lib.sj_verify(ctx, dtype, batch, t, vocab, tokens, parent, parent_seq, count, target,
+                         _strides(*target_stride), draft, _strides(*draft_stride), uniform, path,
+                         found, next)
 
 
 def sj_get_stats(ctx) -> sj_stats:
@@ -671,6 +736,8 @@ class kv_cache:
     def __init__(self, k, v, table=None):
         self._describe(k, v, table)
 
+    eight = False
+
     k = property(lambda self: self._k, lambda self, x: self._describe(x, self._v, self._table))
     v = property(lambda self: self._v, lambda self, x: self._describe(self._k, x, self._table))
     table = property(lambda self: self._table, lambda self, x: self._describe(self._k, self._v, x))
@@ -679,6 +746,10 @@ class kv_cache:
         import torch
         if k.dtype not in (torch.float16, torch.bfloat16) or not k.is_cuda:
             raise ValueError("k must be a float16 or bfloat16 device tensor")
+        self._tensors(k, v, table, k.dtype)
+
+    def _tensors(self, k, v, table, dtype):
+        import torch
         _check_rows("k", k, (None,) * 4, k.dtype, k.device)
         _check_rows("v", v, tuple(k.shape), k.dtype, k.device)
         pages, page, heads, d = k.shape
@@ -686,12 +757,12 @@ class kv_cache:
             _check_rows("table", table, (None, None), torch.int32, k.device)
         self._k, self._v, self._table = k, v, table
         self.follows = _follows(k, v)
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device = dtype, k.device
         self.heads, self.d, self.page = heads, d, page
         self.batch, self.width = (pages, 1) if table is None else table.shape
         # (a table without columns has no address, but NULL would mean that there is none;
         # nothing is read of it)
-        self.raw = sj_cache(dtype_code(k), heads, d, pages, page, self.batch, self.width,
+        self.raw = sj_cache(SJ_F16 if dtype is torch.float16 else SJ_BF16, heads, d, pages, page, self.batch, self.width,
                             0 if table is None else table.stride(0),
                             None if table is None else (_ptr(table) or _ptr(k)),
                             _ptr(k), _ptr(v), *k.stride()[:3], *v.stride()[:3])
@@ -700,6 +771,51 @@ class kv_cache:
     def room(self) -> int:
         """Rows a sequence may hold."""
         return self.width * self.page
+
+
+class kv_cache8(kv_cache):
+    """A cache of key and value rows in 8 bits (sj_cache8): k and v are (pages, page, heads, d)
+    float8_e4m3fn device tensors, d a multiple of 8, and exponents a contiguous int8 tensor (pages, blocks
+    of a page, heads, 2): an element stands for its value times 2 to its block's and head's
+    exponent ([..., 0] for k, [..., 1] for v).  dtype (float16 or bfloat16) is the type of the
+    keys and values that cache_append rounds into it, of attend's queries and of its results.
+    Everything else is as in kv_cache; cache_evict takes no cache in 8 bits."""
+
+    eight = True
+
+    def __init__(self, k, v, exponents, table=None, *, dtype=None):
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError("dtype must be float16 or bfloat16")
+        self.dtype, self._exponents = dtype, exponents
+        self._describe(k, v, table)
+
+    exponents = property(lambda self: self._exponents, lambda self, x: self._assign(x))
+
+    def _assign(self, x):
+        before, self._exponents = self._exponents, x
+        try:
+            self._describe(self._k, self._v, self._table)
+        except ValueError:
+            self._exponents = before
+            raise
+
+    def _describe(self, k, v, table):
+        import torch
+        if k.dtype is not torch.float8_e4m3fn or not k.is_cuda:
+            raise ValueError("k must be a float8_e4m3fn device tensor")
+        if k.dim() == 4 and k.shape[3] % 8:
+            raise ValueError(f"d = {k.shape[3]} is no multiple of 8")
+        x = self._exponents
+        if x.dim() != 4 or k.dim() != 4:
+            _refuse("exponents", x, (k.shape[0], None, None, 2), torch.int8, k.device)
+        _check_whole("exponents", x, (k.shape[0], x.shape[1], k.shape[2], 2), torch.int8, k.device)
+        if x.shape[1] == 0 or k.shape[1] % x.shape[1]:
+            raise ValueError(f"{x.shape[1]} blocks do not divide pages of {k.shape[1]} rows")
+        self._tensors(k, v, table, self.dtype)
+        self.block = k.shape[1] // x.shape[1]
+        self.raw = sj_cache8(self.raw, _ptr(x), self.block)
 
 
 def rotary_turns(rot: int, base: float = 10000.0, *, linear: float = 1.0, ramp=None, device="cuda"):
@@ -770,7 +886,8 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     are (sequences, tokens, heads, d); lengths and counts int32 per sequence, pos
     int32 (sequences, tokens).  q (sequences, tokens, query heads, d), when
     given, is turned by the same positions and returned (in q_out, which may be
-    q).  There is no gradient: a backward pass through the result raises.  May be
+    q).  Into a kv_cache8 the turned keys and the values are rounded to 8 bits (sj_cache8_append); the
+    blocks of rows appended to must be of one sequence each.  There is no gradient: a backward pass through the result raises.  May be
     captured into a HIP graph, as rotary may."""
     import torch
     if cache.follows or key.requires_grad or value.requires_grad or _follows(q, q_out):
@@ -806,9 +923,10 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
             _check_rows("q_out", q_out, q.shape, q.dtype, dev)
         if q.numel():
             args = (q.data_ptr(), q.stride()[:3], q.shape[2], q_out.data_ptr(), q_out.stride()[:3])
-    st = sj_cache_append(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(counts), t,
-                         _ptr(key), key.stride()[:3], _ptr(value), value.stride()[:3], _ptr(pos),
-                         _ptr(turns), 0 if turns is None else turns.shape[0], code, factor, *args)
+    call = sj_cache8_append if cache.eight else sj_cache_append
+    st = call(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(counts), t, _ptr(key),
+              key.stride()[:3], _ptr(value), value.stride()[:3], _ptr(pos), _ptr(turns),
+              0 if turns is None else turns.shape[0], code, factor, *args)
     if st != SJ_OK:
         raise SjError(st, sj_last_error())
     return q_out
@@ -817,7 +935,7 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
 def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=None, weight=None,
            weight_out=None, out=None, ctx=None):
     """Attention of a few tokens of every sequence over its rows in the cache
-    (sj_attend).  q is (sequences, tokens, query heads, d); query head i reads cache head
+    (sj_attend, or sj_attend8 for a kv_cache8).  q is (sequences, tokens, query heads, d); query head i reads cache head
     i // (query heads / cache heads).  Token u of sequence b sees the
     lengths[b] rows before the call's tokens and, of the tokens' own rows (which
     follow them, appended beforehand), those that its mask names: bit w % 64 of
@@ -870,10 +988,11 @@ def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=N
     else:
         _check_whole("out", out, q.shape, cache.dtype, dev)
     lse = q.new_empty((B, t, q_heads), dtype=torch.float32)
-    st = sj_attend(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(counts), t, _ptr(q),
-                   q.stride()[:3], q_heads, _ptr(tree), tree_stride,
-                   cache.d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse),
-                   _ptr(weight), _ptr(weight_out), cols)
+    call = sj_attend8 if cache.eight else sj_attend
+    st = call(ctx or _current(dev), cache.raw, _ptr(lengths), _ptr(counts), t, _ptr(q),
+              q.stride()[:3], q_heads, _ptr(tree), tree_stride,
+              cache.d ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(weight),
+              _ptr(weight_out), cols)
     if st != SJ_OK:
         raise SjError(st, sj_last_error())
     return out, lse
@@ -890,6 +1009,8 @@ def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recen
     -1; the new lengths (int32); and the kept weights, then zeros (weight_out where
     given, else as wide as index).  In a HIP graph: see attend."""
     import torch
+    if cache.eight or into.eight:
+        raise ValueError("cache_evict takes no cache in 8 bits")
     if cache.follows or into.follows or _follows(weight, weight_out):
         if torch.is_grad_enabled():
             _lost("cache_evict")
@@ -913,3 +1034,108 @@ def cache_evict(cache, lengths, weight, into, *, keep: int, sink: int = 0, recen
     if st != SJ_OK:
         raise SjError(st, sj_last_error())
     return index, new, weight_out
+
+
+def cache_pages(table, lengths, tokens: int, *, pages: int, page: int, parent=None, ctx=None):
+    """The pages of sequences that go on, fork or end (sj_cache_pages).  table is the
+    (sequences, pages of a sequence) int32 device tensor of a cache whose pool has `pages` pages of
+    `page` rows, lengths int32 per sequence.  New sequence i continues sequence parent[i]
+    (int32, -1: begins empty; parent None: i itself), shares its full pages, has a partly filled last
+    page of its own, and free pages for `tokens` more rows.  A page that no new sequence
+    has is free, so sequences that nobody continues give theirs back.  Returns (table, lengths,
+    copies, lacking): the new table (new sequences, pages of a sequence) and lengths; copies
+    (new sequences, 3), the pages that cache_copy has to copy in every cache with this table before it
+    is used; and lacking, the pages that could not be given for want of free ones (their entries
+    are -1, and rows there do not exist).  One table may serve the caches of many layers:
+        table, lengths, copies, lacking = cache_pages(table, lengths, 16, pages=n, page=64,
+                                                      parent=parent)
+        for cache in layers:
+            cache_copy(cache, copies)
+            cache.table = table
+    In a HIP graph: see attend."""
+    import torch
+    dev = table.device
+    if not table.is_cuda:
+        raise ValueError("table must be a device tensor")
+    if table.numel() == 0:
+        table = table.new_empty(table.shape)    # (whose strides say nothing)
+    _check_rows("table", table, (lengths.shape[0], table.shape[-1]), torch.int32, dev)
+    _check_whole("lengths", lengths, (table.shape[0],), torch.int32, dev)
+    B, width = table.shape
+    out_batch = B
+    if parent is not None:
+        out_batch = parent.numel()
+        _check_whole("parent", parent, (out_batch,), torch.int32, dev)
+    if tokens < 0 or pages < 0 or page <= 0:
+        raise ValueError("tokens and pages must not be negative, page positive")
+    new_table, new = lengths.new_empty((out_batch, width)), lengths.new_empty((out_batch,))
+    copies, lacking = lengths.new_empty((out_batch, 3)), lengths.new_empty((out_batch,))
+    st = sj_cache_pages(ctx or _current(dev), _ptr(table), table.stride(0), B, width, pages, page,
+                        _ptr(lengths), _ptr(parent), out_batch, tokens, _ptr(new_table), _ptr(new),
+                        _ptr(copies), _ptr(lacking))
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+    return new_table, new, copies, lacking
+
+
+def cache_copy(cache, copies, *, ctx=None):
+    """Copies rows between pages of a cache, in 16 bits or 8 (sj_cache_copy, sj_cache8_copy): for each
+    row (from, to, rows) of copies (n, 3) int32 the first `rows` rows of page `from` to page
+    `to`; entries of pages that do not exist copy nothing.  No page may be copied to twice, or be
+    both copied to and from."""
+    import torch
+    if cache.follows and torch.is_grad_enabled():
+        _lost("cache_copy")
+    _check_whole("copies", copies, (copies.shape[0], 3), torch.int32, cache.device)
+    call = sj_cache8_copy if cache.eight else sj_cache_copy
+    st = call(ctx or _current(cache.device), cache.raw, _ptr(copies), copies.shape[0])
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+
+
+def verify_drafts(tokens, target, uniform, *, draft=None, parent=None, counts=None, ctx=None):
+    """Verification of drafted tokens against the target's probabilities, from given random
+    numbers (sj_verify).  tokens (sequences, nodes) int64: node 0 is the last token of a
+    sequence's text, the others are drafted; node n follows node parent[n] < n (int32 (nodes) or
+    (sequences, nodes); None: a chain).  target (sequences, nodes, vocabulary) float32, float16 or
+    bfloat16: the probabilities of what follows each node.  draft, of the same type: the
+    distributions (sequences, nodes - 1, vocabulary) that a chain's tokens were drawn from, node n + 1
+    from row n; without it tokens count as chosen without chance.  uniform (sequences, nodes)
+    float32: numbers in [0, 1), node n's decides on it, node 0's draws the token that follows the
+    accepted ones.  counts (int32 per sequence): nodes that exist.  Returns (path, found, next): path
+    (sequences, nodes) int32, the accepted nodes in order, node 0 first, then -1; found int32, how
+    many; next int64, the token drawn.  What follows the rule is distributed as the target's own
+    text.  In a HIP graph: see attend."""
+    import torch
+    codes = {torch.float32: SJ_F32, torch.float16: SJ_F16, torch.bfloat16: SJ_BF16}
+    dev = target.device
+    if target.dtype not in codes or not target.is_cuda:
+        raise ValueError("target must be a float32, float16 or bfloat16 device tensor")
+    if target.requires_grad or _follows(uniform, draft):
+        if torch.is_grad_enabled():
+            _lost("verify_drafts")
+    if tokens.dim() != 2:
+        _refuse("tokens", tokens, (None, None), torch.int64, dev)
+    B, t = tokens.shape
+    _check_whole("tokens", tokens, (B, t), torch.int64, dev)
+    _check_rows("target", target, (B, t, target.shape[-1]), target.dtype, dev)
+    _check_whole("uniform", uniform, (B, t), torch.float32, dev)
+    if draft is not None:
+        _check_rows("draft", draft, (B, t - 1, target.shape[2]), target.dtype, dev)
+        if parent is not None:
+            raise ValueError("draft goes with chains, not with parent")
+    parent_seq = 0
+    if parent is not None:
+        _check_whole("parent", parent, (t,) if parent.dim() == 1 else (B, t), torch.int32, dev)
+        parent_seq = 0 if parent.dim() == 1 else t
+    if counts is not None:
+        _check_whole("counts", counts, (B,), torch.int32, dev)
+    path = tokens.new_empty((B, t), dtype=torch.int32)
+    found, nxt = path.new_empty((B,)), tokens.new_empty((B,))
+    st = sj_verify(ctx or _current(dev), codes[target.dtype], B, t, target.shape[2], _ptr(tokens),
+                   _ptr(parent), parent_seq, _ptr(counts), _ptr(target), target.stride()[:2],
+                   _ptr(draft), (0, 0) if draft is None else draft.stride()[:2], _ptr(uniform),
+                   _ptr(path), _ptr(found), _ptr(nxt))
+    if st != SJ_OK:
+        raise SjError(st, sj_last_error())
+    return path, found, nxt

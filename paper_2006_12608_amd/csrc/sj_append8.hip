@@ -1,0 +1,266 @@
+// sj_append8.hip -- rows appended to a cache in 8 bits (sj_cache8_append): keys turned, and keys
+// and values rounded to e4m3 at a power of two for each block of rows and head.
+#include "sj_cache.h"
+#include "sj_turn.h"
+
+namespace sjc {
+
+namespace {
+
+constexpr uint32_t A8_GRID = 1u << 22;  // workgroups of a launch at most
+constexpr int A8_HELD = 8;              // 16-byte chunks of a block that a lane holds
+
+struct Append8Args {
+    Append8 r;
+    uint64_t first;             // of the launch's workgroups
+    uint32_t lanes_log;         // lanes of a row: d / 8 rounded up to a power of two
+    uint32_t units, groups;     // heads x {k, v}; workgroups of 4 of them
+    PageDiv by_blocks, by_groups;
+};
+
+template <int DT>
+struct Type8;
+template <>
+struct Type8<sjk::DT_F16> {
+    static constexpr uint32_t INF = 0x7c00u;
+    static constexpr int LEAST = -15, MOST = 7;
+};
+template <>
+struct Type8<sjk::DT_BF16> {
+    static constexpr uint32_t INF = 0x7f80u;
+    static constexpr int LEAST = -117, MOST = 119;
+};
+
+// The least e with x <= 448 2^e = 1.75 2^(e + 8), for a value of the 16-bit type, in its range.
+template <int DT>
+__device__ __forceinline__ int exponent_of(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return e < Type8<DT>::LEAST ? Type8<DT>::LEAST : (e > Type8<DT>::MOST ? Type8<DT>::MOST : e);
+}
+
+// 2^e, -126 <= e <= 127.
+__device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// x rounded to e4m3 in byte 0 or 1, 2 or 3 of a word, two at a time: between -448 and 448 first
+// (the type's largest), NaN for what is not finite.
+__device__ __forceinline__ float bound(float x, bool finite)
+{
+    return finite ? fminf(fmaxf(x, -448.f), 448.f) : __uint_as_float(0x7fc00000u);
+}
+
+__device__ __forceinline__ uint32_t four(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// Eight elements of a key row from element c on, turned and rounded to the 16-bit type.  The partner of
+// an element is in the same chunk (interleaved), or `pairs` elements on or back.
+template <int DT>
+__device__ __forceinline__ i32x4 turned8(const Turn &t, const uint16_t *row, i32x4 v, uint32_t c,
+                                         int left, uint64_t pos)
+{
+    const uint32_t rot = 2 * t.pairs;
+    if (c >= rot)
+        return v;
+    const bool half = t.layout == 0;
+    uint32_t mine[8], other[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        mine[e] = ((uint32_t)v[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+    if (half) {
+        const bool low = c + 8 <= t.pairs, high = c >= t.pairs && c + 8 <= rot;
+        if (low || high) {
+            const i32x4 w = load8(low ? row + c + t.pairs : row + c - t.pairs, 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                other[e] = ((uint32_t)w[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t i = c + e;
+                other[e] = i < rot && e < left ? row[i < t.pairs ? i + t.pairs : i - t.pairs] : 0;
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t i = c + e;
+        if (i >= rot)
+            break;
+        const bool first = half ? i < t.pairs : (i & 1) == 0;
+        const float2 cs = sine_of(t, pos, half ? (first ? i : i - t.pairs) : i >> 1);
+        const float x = to_float(DT, mine[e]);
+        const float y = to_float(DT, half ? other[e] : mine[e ^ 1]);
+        other[e] = to_bits(DT, first ? turn_a(x, y, cs.x, cs.y) : turn_b(y, x, cs.x, cs.y));
+        if (half)
+            mine[e] = other[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (!half && c + e < rot)
+            mine[e] = other[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] = (int)(mine[2 * e] | mine[2 * e + 1] << 16);
+    return v;
+}
+
+// A wave takes one block of a sequence's rows, one head, keys or values: the largest magnitude of
+// the new rows in it (a maximum of 16-bit integers), from that the exponent, the rows before
+// len[b] rounded to it where it grows, and the new rows' e4m3 values.
+template <int DT, bool TURN>
+__global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
+{
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    const Append8 &r = g.r;
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t id = (uint32_t)(g.first + blockIdx.x);
+    const uint32_t bj = g.by_groups.quot(id), unit = (id - bj * g.groups) * 4 + wave;
+    const uint32_t b = g.by_blocks.quot(bj), j = bj - b * r.blocks;
+    if (unit >= g.units)
+        return;
+    const uint32_t h = unit >> 1, kv = unit & 1, d = r.c.d, size = r.c.by_block.page;
+    const uint32_t len = clamp_rows(r.len[b], r.c.room);
+    const uint32_t count = r.count ? clamp_rows(r.count[b], r.t) : r.t;
+    const uint64_t all = (uint64_t)len + count;
+    const uint32_t end = all < r.c.room ? (uint32_t)all : r.c.room;
+    // (blocks do not cross pages, so a sequence's blocks are those of its rows)
+    const uint64_t row0 = ((uint64_t)r.c.by_block.quot(len) + j) * size;
+    if (row0 >= end)
+        return;
+    const Place p = place_of(r.c, b, (uint32_t)row0);
+    if (p.page < 0)
+        return;
+    const uint32_t from = len > row0 ? len - (uint32_t)row0 : 0;    // slots of the block
+    const uint32_t to = end - (uint32_t)row0 < size ? end - (uint32_t)row0 : size;
+    const Strided &x = kv ? r.value : r.key;
+    const int64_t page_s = kv ? r.c.v_page : r.c.k_page, row_s = kv ? r.c.v_row : r.c.k_row;
+    uint8_t *out = (uint8_t *)(kv ? r.c.v : r.c.k) + (int64_t)p.page * page_s +
+                   (int64_t)p.slot * row_s + (int64_t)h * (kv ? r.c.v_head : r.c.k_head);
+    const uint16_t *in = x.in + (int64_t)b * x.in_seq + (int64_t)h * x.in_head;
+    const uint32_t sub = lane >> g.lanes_log, c = 8 * (lane & ((1u << g.lanes_log) - 1));
+    const uint32_t step = 64u >> g.lanes_log;
+    const int left = (int)d - (int)c;
+    int8_t *at = (int8_t *)r.c.ex +
+                 2 * (((int64_t)p.page * r.c.blocks + r.c.by_block.quot(p.slot)) * r.c.heads + h) + kv;
+    const int was = *at;
+
+    auto get = [&](uint32_t s) -> i32x4 {       // eight elements of slot s, from < = s < to
+        const uint32_t u = (uint32_t)row0 + s - len;
+        const uint16_t *row = in + (int64_t)u * x.in_tok;
+        i32x4 v = load8(row + c, left);
+        if (TURN && kv == 0)
+            v = turned8<DT>(r.turn, row, v, c, left,
+                            (uint64_t)(int64_t)r.turn.pos[(uint64_t)b * r.t + u]);
+        return v;
+    };
+    u16x2 most = {0, 0};
+    auto look = [&](i32x4 v) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            u16x2 m = __builtin_bit_cast(u16x2, (uint32_t)v[e] & 0x7fff7fffu);
+            m.x = m.x >= Type8<DT>::INF ? 0 : m.x;
+            m.y = m.y >= Type8<DT>::INF ? 0 : m.y;
+            most = __builtin_elementwise_max(most, m);
+        }
+    };
+    i32x4 held[A8_HELD];
+#pragma unroll
+    for (int i = 0; i < A8_HELD; ++i) {
+        const uint32_t s = from + i * step + sub;
+        held[i] = s < to && left > 0 ? get(s) : i32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < A8_HELD; ++i)
+        look(held[i]);
+    for (uint32_t s = from + A8_HELD * step + sub; s < to; s += step)
+        if (left > 0)
+            look(get(s));
+    uint32_t top = most.x > most.y ? most.x : most.y;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = (uint32_t)__shfl_xor((int)top, o);
+        top = top > y ? top : y;
+    }
+    int e = exponent_of<DT>(to_float(DT, top));
+    if (from > 0) {
+        const int old = was < -126 ? -126 : (was > 126 ? 126 : was);
+        e = e > old ? e : old;
+        if (e > old) {      // the rows that are there
+            const float f = power(old - e < -126 ? -126 : old - e);
+            for (uint32_t s = sub; s < from; s += step) {
+                if (left <= 0)
+                    continue;
+                uint32_t w[2];
+                uint8_t *q = out + (int64_t)s * row_s + c;
+                __builtin_memcpy(w, q, 8);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false);
+                    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+                    w[k] = four(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+                }
+                __builtin_memcpy(q, w, 8);
+            }
+        }
+    }
+    const float f = power(-e);
+    auto put = [&](uint32_t s, i32x4 v) {
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float y[4];
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const uint32_t bits = ((uint32_t)v[2 * k + (z >> 1)] >> (16 * (z & 1))) & 0xffffu;
+                y[z] = bound(to_float(DT, bits) * f, (bits & 0x7fffu) < Type8<DT>::INF);
+            }
+            w[k] = four(y[0], y[1], y[2], y[3]);
+        }
+        __builtin_memcpy(out + (int64_t)s * row_s + c, w, 8);
+    };
+#pragma unroll
+    for (int i = 0; i < A8_HELD; ++i) {
+        const uint32_t s = from + i * step + sub;
+        if (s < to && left > 0)
+            put(s, held[i]);
+    }
+    for (uint32_t s = from + A8_HELD * step + sub; s < to; s += step)
+        if (left > 0)
+            put(s, get(s));
+    if (lane == 0)
+        *at = (int8_t)e;
+}
+
+}  // namespace
+
+hipError_t launch_append8(const Append8 &r, hipStream_t s)
+{
+    Append8Args g{};
+    g.r = r;
+    while ((8u << g.lanes_log) < r.c.d)
+        ++g.lanes_log;
+    g.units = 2 * r.c.heads;
+    g.groups = (g.units + 3) / 4;
+    g.by_blocks = PageDiv::of(r.blocks);
+    g.by_groups = PageDiv::of(g.groups);
+    const uint64_t total = (uint64_t)r.c.batch * r.blocks * g.groups;
+    hipError_t e = hipSuccess;
+    for (; g.first < total && e == hipSuccess; g.first += A8_GRID) {
+        const uint64_t left = total - g.first;
+        const dim3 grid((uint32_t)(left < A8_GRID ? left : A8_GRID));
+        const bool turn = r.turn.pairs != 0;
+        if (r.dtype == sjk::DT_F16)
+            (turn ? append8_blocks<sjk::DT_F16, true> : append8_blocks<sjk::DT_F16, false>)<<<grid, 256, 0, s>>>(g);
+        else
+            (turn ? append8_blocks<sjk::DT_BF16, true> : append8_blocks<sjk::DT_BF16, false>)<<<grid, 256, 0, s>>>(g);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+}  // namespace sjc

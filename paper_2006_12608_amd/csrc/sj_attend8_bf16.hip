@@ -1,0 +1,16 @@
+// sj_attend8_bf16.hip -- attention over a cache of e4m3 rows, queries and results in bfloat16.
+#include "sj_attend_kernels.h"
+
+namespace sjc {
+
+int attend8_occupancy_bf16(uint32_t d, uint32_t tile_rows)
+{
+    return attend_occupancy<sjk::DT_BF16, 1>(d, tile_rows);
+}
+
+hipError_t launch_attend8_bf16(const Attend &a, hipStream_t s)
+{
+    return launch_attend<sjk::DT_BF16, 1>(a, s);
+}
+
+}  // namespace sjc

@@ -22,6 +22,7 @@ namespace sjc {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int64_t i64x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -142,6 +143,88 @@ __device__ __forceinline__ i32x4 load_fit(const uint16_t *p, int left)
     return v;
 }
 
+// ---- elements of the cache: CE = 2 bytes, of the kernel's type, or 1, e4m3 times a power of two
+// for each block of rows and head (every value is one of the kernel's type, so that from here on
+// both are the same)
+
+template <int CE>
+struct Cells;
+template <>
+struct Cells<2> {
+    typedef uint16_t one;
+    typedef i32x4 eight;
+};
+template <>
+struct Cells<1> {
+    typedef uint8_t one;
+    typedef i32x2 eight;
+};
+
+template <int CE>
+__device__ __forceinline__ const typename Cells<CE>::one *cells(const uint16_t *p)
+{
+    return (const typename Cells<CE>::one *)p;
+}
+
+// Eight elements as they lie in the cache (d is a multiple of 8 where CE is 1).
+template <int FIT, int CE>
+__device__ __forceinline__ typename Cells<CE>::eight load_cells(const typename Cells<CE>::one *p,
+                                                                int left)
+{
+    if constexpr (CE == 2) {
+        return load_fit<FIT>(p, left);
+    } else {
+        static_assert(FIT != FIT_ANY, "chunks of 8");
+        i32x2 v = {0, 0};
+        if (FIT == FIT_WHOLE || left > 0)
+            __builtin_memcpy(&v, p, 8);
+        return v;
+    }
+}
+
+// The two exponents of the block of a row that exists: k's in the low byte, v's in the high one.
+template <int CE>
+__device__ __forceinline__ uint32_t load_exponents(const Cache &c, const Place &p, uint32_t h)
+{
+    if constexpr (CE == 2)
+        return 0;
+    return p.page < 0 ? 0
+                      : c.ex[((int64_t)p.page * c.blocks + c.by_block.quot(p.slot)) * c.heads + h];
+}
+
+// 2^e of one of them (e below -126: 2^-126).
+__device__ __forceinline__ float power_k(uint32_t ex)
+{
+    const int e = (int)(int8_t)ex;
+    return __uint_as_float((uint32_t)((e < -126 ? -126 : e) + 127) << 23);
+}
+
+__device__ __forceinline__ float power_v(uint32_t ex) { return power_k(ex >> 8); }
+
+// The elements' values in the kernel's type (a conversion takes two of them and the scale).
+template <int DT>
+__device__ __forceinline__ i32x4 widen(const i32x4 &v, float)
+{
+    return v;
+}
+
+template <int DT>
+__device__ __forceinline__ i32x4 widen(const i32x2 &v, float scale)
+{
+    i32x4 y;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        if constexpr (DT == sjk::DT_F16) {
+            y[2 * e] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], scale, false));
+            y[2 * e + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[e], scale, true));
+        } else {
+            y[2 * e] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e], scale, false));
+            y[2 * e + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e], scale, true));
+        }
+    }
+    return y;
+}
+
 // Eight elements of a query, negated for a negative scale: the scores' order is then
 // that of the products, and the maximum can be taken before the scale.
 template <int FIT>
@@ -208,7 +291,7 @@ __device__ __forceinline__ uint64_t seen64(const Attend &a, uint32_t b, const Ro
 // products leave out what is not finite in these rows, since 0 x inf and 0 x NaN would
 // reach the queries that do not see them; added up afterwards, what a query does
 // see of them decides its output whatever the weights are.
-template <class F>
+template <int CE, class F>
 __device__ __forceinline__ void own_rows(const Attend &a, uint32_t b, uint32_t h, const Rows &r,
                                          uint32_t u, uint32_t from, uint32_t to, F f)
 {
@@ -216,7 +299,7 @@ __device__ __forceinline__ void own_rows(const Attend &a, uint32_t b, uint32_t h
     for (uint32_t n = from > r.len ? from : r.len; n < to; ++n) {
         const Place p = place_of(a.c, b, n);
         if (p.page >= 0 && sees(a, b, r, u, n))
-            f(a.c.v + (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row +
+            f(cells<CE>(a.c.v) + (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row +
               (int64_t)h * a.c.v_head);
     }
 }
@@ -226,6 +309,12 @@ template <int DT>
 __device__ __forceinline__ float odd_part(uint16_t x)
 {
     return (x & Elem<DT>::EXP) == Elem<DT>::EXP ? bits_to_float(x, DT) : 0.f;
+}
+
+template <int DT>
+__device__ __forceinline__ float odd_part(uint8_t x)
+{
+    return (x & 0x7fu) == 0x7fu ? __uint_as_float(0x7fc00000u) : 0.f;
 }
 
 // For each of the query rows r0 .. r0 + n - 1 of q_rows, which of the 64 rows from row0 on it
@@ -452,10 +541,11 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
 // 5.4 TB/s, or 231 with the scores kept (33 MB); 32 sequences of 200 to 8192 rows, 550 MB, in
 // 116 (4.7 TB/s).  One sequence of 2048 rows: 10 us, of which most is the latency of the chain
 // lengths, page numbers, rows, join.
-template <int DT, int DC, int NQ, int FIT>
+template <int DT, int DC, int NQ, int FIT, int CE>
 __global__ void __launch_bounds__(256) attend_split(const Attend a)
 {
     typedef Elem<DT> E;
+    typedef typename Cells<CE>::one Cell;
     constexpr int QT = AT_Q * NQ, D = 32 * DC;
     constexpr int RS = 2 * D + 32;              // bytes of a V row in LDS
     constexpr int OS = D + 4;                   // floats of a query's sums in LDS
@@ -530,22 +620,23 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             O[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const uint16_t *kb = a.c.k + (int64_t)h * a.c.k_head, *vb = a.c.v + (int64_t)h * a.c.v_head;
+    const Cell *kb = cells<CE>(a.c.k) + (int64_t)h * a.c.k_head;
+    const Cell *vb = cells<CE>(a.c.v) + (int64_t)h * a.c.v_head;
     uint8_t *const my = lds + wave * WAVE_LDS;
 
     // place of row lane % 32 of a block: absent rows read page 0, row 0 (their
     // scores and values are replaced below)
     auto place = [&](const Entry &e) { return place_of(a.c, b, e, to); };
-    i32x4 K[2][DC], V[NV];
+    typename Cells<CE>::eight K[2][DC], V[NV];
     auto load_k = [&](const Place &p) {
         const int64_t off = p.page < 0 ? 0
                                        : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const uint16_t *r = kb + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
+            const Cell *r = kb + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
 #pragma unroll
             for (int c = 0; c < DC; ++c)
-                K[t][c] = load_fit<FIT>(r + 32 * c, (int)d - (int)(32 * c + 8 * g4));
+                K[t][c] = load_cells<FIT, CE>(r + 32 * c, (int)d - (int)(32 * c + 8 * g4));
         }
     };
     const uint32_t v_row = lane / (4 * DC), v_col = 8 * (lane % (4 * DC));
@@ -554,8 +645,8 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                                        : (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint16_t *r = vb + shfl64(off, VR * i + (int)v_row) + v_col;
-            V[i] = load_fit<FIT>(r, (int)d - (int)v_col);
+            const Cell *r = vb + shfl64(off, VR * i + (int)v_row) + v_col;
+            V[i] = load_cells<FIT, CE>(r, (int)d - (int)v_col);
         }
     };
 
@@ -564,8 +655,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     __syncthreads();
     uint32_t blk = first + wave;
     Place cur = {-1, 0u}, nxt = {-1, 0u};
+    uint32_t ex = 0;        // of row lane % 32
     if (blk < last) {
         cur = place(first_at);
+        ex = load_exponents<CE>(a.c, cur, h);
         load_k(cur);
         load_v(cur);
     }
@@ -577,28 +670,36 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 
         f32x4 s[NQ][2];
 #pragma unroll
-        for (int j = 0; j < NQ; ++j)
+        for (int t = 0; t < 2; ++t) {
+            const float two = CE == 1 ? power_k((uint32_t)__shfl((int)ex, (int)q16 + 16 * t)) : 1.f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int j = 0; j < NQ; ++j)
                 s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < DC; ++c)
-                    s[j][t] = E::mma(K[t][c], Q[j][c], s[j][t]);
+            for (int c = 0; c < DC; ++c) {
+                const i32x4 k8 = widen<DT>(K[t][c], two);
+#pragma unroll
+                for (int j = 0; j < NQ; ++j)
+                    s[j][t] = E::mma(k8, Q[j][c], s[j][t]);
             }
+        }
         ahead = entry(blk + 2 * AT_WAVES);
+        const uint32_t nex = load_exponents<CE>(a.c, nxt, h);
         load_k(nxt);        // (past the end: page 0, row 0; a branch would cost full waits)
 
         // V to LDS; rows that do not exist as zeros (0 x NaN would reach every query)
         uint32_t odd = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            i32x4 v8 = widen<DT>(
+                V[i], CE == 1 ? power_v((uint32_t)__shfl((int)ex, VR * i + (int)v_row)) : 1.f);
             if (tail || there != 0xffffffffu) {
                 if (!((there >> (VR * i + v_row)) & 1))
-                    V[i] = i32x4{0, 0, 0, 0};
-                odd |= drop_odd8<DT>(V[i], blk * AT_ROWS + VR * i + v_row >= rows.len);
+                    v8 = i32x4{0, 0, 0, 0};
+                odd |= drop_odd8<DT>(v8, blk * AT_ROWS + VR * i + v_row >= rows.len);
                 asm volatile("");       // (a branch, not selects in every round)
             }
-            *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = V[i];
+            *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = v8;
         }
         load_v(nxt);
 
@@ -662,6 +763,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                 O[j][i] = E::mma(vt, P[j], O[j][i]);
         }
         cur = nxt;
+        ex = nex;
     }
 
     // join the lanes of a query, then the waves; the scale 2^LIFT ends here
@@ -715,7 +817,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                 for (uint32_t w = 0; w < AT_WAVES; ++w)
                     o += *(const f32x4 *)((const float *)(lds + w * WAVE_LDS) + qi * OS + c);
                 if (odd_any && live)
-                    own_rows(a, b, h, rows, u, first * AT_ROWS, to, [&](const uint16_t *v) {
+                    own_rows<CE>(a, b, h, rows, u, first * AT_ROWS, to, [&](const Cell *v) {
 #pragma unroll
                         for (uint32_t e = 0; e < 4; ++e)
                             if (c + e < d)
@@ -782,10 +884,11 @@ __device__ __forceinline__ uint32_t swz(uint32_t row, uint32_t chunk)
         return chunk ^ (((row & 3) << 2) | ((row >> 2) & 3));
 }
 
-template <int DT, int DC, int QW, int FIT>
+template <int DT, int DC, int QW, int FIT, int CE>
 __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_tiles(const Attend a)
 {
     typedef Elem<DT> E;
+    typedef typename Cells<CE>::one Cell;
     constexpr uint32_t NT = QW == 8 ? 512 : 256, D = 32 * DC, QT = 32 * QW, RW = QW == 8 ? 1 : 4 / QW;
     constexpr uint32_t BN = DC == 8 ? 32 : 64;      // rows of a tile
     constexpr uint32_t WR = BN / RW;                // of these, one wave's
@@ -799,6 +902,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     __shared__ float stat[4][32][2];
     __shared__ uint32_t odd_any;
     __shared__ i64x2 where[8][BN];
+    __shared__ int64_t ex_at[CE == 1 ? 8 : 1][BN];  // places of the rows' exponents
     __shared__ uint64_t exist[8];
 
     const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
@@ -850,7 +954,8 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
             O[i][r] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    const uint16_t *kb = a.c.k + (int64_t)h * a.c.k_head, *vb = a.c.v + (int64_t)h * a.c.v_head;
+    const Cell *kb = cells<CE>(a.c.k) + (int64_t)h * a.c.k_head;
+    const Cell *vb = cells<CE>(a.c.v) + (int64_t)h * a.c.v_head;
     // places in a tile: chunk 2 k + half of row q32 of K (the same for every 32 rows), and of V
     // columns 32 z + 16 (g % 2) + 4 (l16 % 4) .. of rows 4 half + l16 / 4 and 8 further (the same
     // for every 16 rows)
@@ -883,6 +988,11 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                 o = i64x2{(int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row,
                           (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row};
             where[i & 7][lane] = o;
+            if constexpr (CE == 1)
+                ex_at[i & 7][lane] =
+                    p.page < 0 ? 0
+                               : ((int64_t)p.page * a.c.blocks + a.c.by_block.quot(p.slot)) *
+                                         a.c.heads + h;
         }
         if (lane == 0)
             exist[i & 7] = there;
@@ -892,17 +1002,23 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
         return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x) |
                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32;
     };
-    i32x4 kr[NL], vr[NL];
+    typename Cells<CE>::eight kr[NL], vr[NL];
+    uint32_t xr[NL] = {};
     auto fetch = [&](uint32_t i) {
         const int left = (int)d - (int)(8 * chunk);
         i64x2 o[NL];
 #pragma unroll
         for (int x = 0; x < NL; ++x)
             o[x] = where[i & 7][RPL * x + row_at];
+        if constexpr (CE == 1) {
+#pragma unroll
+            for (int x = 0; x < NL; ++x)
+                xr[x] = a.c.ex[ex_at[i & 7][RPL * x + row_at]];
+        }
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
-            kr[x] = load_fit<FIT>(kb + o[x][0] + 8 * chunk, left);
-            vr[x] = load_fit<FIT>(vb + o[x][1] + 8 * chunk, left);
+            kr[x] = load_cells<FIT, CE>(kb + o[x][0] + 8 * chunk, left);
+            vr[x] = load_cells<FIT, CE>(vb + o[x][1] + 8 * chunk, left);
         }
     };
     // (the swizzle repeats every 16 rows, and RPL is a multiple of 8: one place, or two)
@@ -912,13 +1028,19 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
         to_at[x] = (RPL * x + row_at) * (2 * D) + 16 * swz<DC>(RPL * x + row_at, chunk);
     auto stash = [&](uint32_t i, uint32_t buf, uint64_t there) {
         uint8_t *kt = lds + buf * 2 * TILE, *vt = kt + TILE;
+        i32x4 k8[NL], v8[NL];
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+            k8[x] = widen<DT>(kr[x], power_k(xr[x]));
+            v8[x] = widen<DT>(vr[x], power_v(xr[x]));
+        }
         if (from + i * BN + BN > rows.len || there != ~(uint64_t)0) {
             uint32_t odd = 0;
 #pragma unroll
             for (int x = 0; x < NL; ++x) {
                 if (!((there >> (RPL * x + row_at)) & 1))
-                    vr[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
-                odd |= drop_odd8<DT>(vr[x], from + i * BN + RPL * x + row_at >= rows.len);
+                    v8[x] = i32x4{0, 0, 0, 0};  // (0 x NaN would reach every query)
+                odd |= drop_odd8<DT>(v8[x], from + i * BN + RPL * x + row_at >= rows.len);
             }
             if (odd)
                 odd_any = 1;
@@ -927,8 +1049,8 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
             const uint32_t at = to_at[x & 1] + (x >> 1) * 2 * RPL * (2 * D);
-            *(i32x4 *)(kt + at) = kr[x];
-            *(i32x4 *)(vt + at) = vr[x];
+            *(i32x4 *)(kt + at) = k8[x];
+            *(i32x4 *)(vt + at) = v8[x];
         }
     };
 
@@ -1128,7 +1250,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + (r_mine - a.by_group.quot(r_mine) * a.group);
     const uint64_t part = ((uint64_t)slot * units + unit) * QT + 32 * qw + q32;
     if (odd_any && live)
-        own_rows(a, b, h, rows, tok, from, to, [&](const uint16_t *v) {
+        own_rows<CE>(a, b, h, rows, tok, from, to, [&](const Cell *v) {
 #pragma unroll
             for (int z = 0; z < DC; ++z)
 #pragma unroll
@@ -1312,7 +1434,7 @@ __global__ void __launch_bounds__(256) attend_join(const Attend a, uint32_t QT, 
 // lane l with query rows 8 (r / 4) + 4 (l / 32) + r % 4 in register r, so the sum stays in
 // the lane until the end.  Two buffers of query rows, the next one's on their way
 // while one is worked on.
-template <int DT, int DC, int FIT>
+template <int DT, int DC, int FIT, int CE>
 __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 {
     typedef Elem<DT> E;
@@ -1337,14 +1459,17 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
         const bool masked = row0 + WROWS > rows.len || there != ~(uint64_t)0;
         const int64_t off =
             p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
+        const uint32_t ex = load_exponents<CE>(a.c, p, h);
         i32x4 K[WT][2 * DC];
 #pragma unroll
         for (int t = 0; t < (int)WT; ++t) {
-            const uint16_t *r =
-                a.c.k + (int64_t)h * a.c.k_head + shfl64(off, (int)l32 + 32 * t) + 8 * half;
+            const auto *r = cells<CE>(a.c.k) + (int64_t)h * a.c.k_head +
+                            shfl64(off, (int)l32 + 32 * t) + 8 * half;
+            const float two = CE == 1 ? power_k((uint32_t)__shfl((int)ex, (int)l32 + 32 * t)) : 1.f;
 #pragma unroll
             for (int k = 0; k < 2 * DC; ++k)
-                K[t][k] = load_fit<FIT>(r + 16 * k, (int)d - (int)(16 * k + 8 * half));
+                K[t][k] = widen<DT>(
+                    load_cells<FIT, CE>(r + 16 * k, (int)d - (int)(16 * k + 8 * half)), two);
         }
         uint32_t q_at[2 * DC];      // chunk 2 k + half of query row l32 (the same for every 32)
 #pragma unroll
@@ -1454,7 +1579,7 @@ __global__ void __launch_bounds__(256) attend_weights(const Attend a)
 template <int DC>
 constexpr uint32_t kWeighRows = DC == 8 ? 128 : 256;
 
-template <int DT, int DC, int FIT>
+template <int DT, int DC, int FIT, int CE>
 __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 {
     typedef Elem<DT> E;
@@ -1530,22 +1655,24 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
     for (uint32_t k = 0; k < 2 * DC; ++k)
         q_at[k] = l32 * (2 * D) + 16 * swz<DC>(l32, 2 * k + half);
 
-    const uint16_t *kb = a.c.k + (int64_t)h * a.c.k_head + 8 * half;
+    const auto *kb = cells<CE>(a.c.k) + (int64_t)h * a.c.k_head + 8 * half;
     const uint32_t n_blk = (to - from + WROWS - 1) / WROWS;
     auto entry = [&](uint32_t i) {
         return entry_of(a.c, a.len, b, from + i * WROWS + (lane & (WROWS - 1)));
     };
-    i32x4 K[2][WT][2 * DC];
+    typename Cells<CE>::eight K[2][WT][2 * DC];
+    uint32_t ex[2];
     auto load_k = [&](const Place &p, auto set_) {      // absent rows read page 0, row 0
         constexpr int set = decltype(set_)::value;
         const int64_t off =
             p.page < 0 ? 0 : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
+        ex[set] = load_exponents<CE>(a.c, p, h);
 #pragma unroll
         for (int t = 0; t < (int)WT; ++t) {
-            const uint16_t *r = kb + shfl64(off, (int)l32 + 32 * t);
+            const auto *r = kb + shfl64(off, (int)l32 + 32 * t);
 #pragma unroll
             for (int k = 0; k < 2 * DC; ++k)
-                K[set][t][k] = load_fit<FIT>(r + 16 * k, (int)d - (int)(16 * k + 8 * half));
+                K[set][t][k] = load_cells<FIT, CE>(r + 16 * k, (int)d - (int)(16 * k + 8 * half));
         }
     };
     auto add = [&](uint32_t n) -> float {               // (a load whether it is needed or not)
@@ -1568,6 +1695,15 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
         for (int t = 0; t < (int)WT; ++t) {
             w[t] = 0.f;
             w0[t] = add(row0 + 32 * t + l32);
+        }
+        i32x4 K8[WT][2 * DC];
+#pragma unroll
+        for (int t = 0; t < (int)WT; ++t) {
+            const float two =
+                CE == 1 ? power_k((uint32_t)__shfl((int)ex[set], (int)l32 + 32 * t)) : 1.f;
+#pragma unroll
+            for (int k = 0; k < 2 * DC; ++k)
+                K8[t][k] = widen<DT>(K[set][t][k], two);
         }
         load_k(nxt, std::integral_constant<int, 1 - set>());
         if (masked)
@@ -1592,7 +1728,7 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
             for (uint32_t k = 0; k < 2 * DC; ++k)
 #pragma unroll
                 for (int t = 0; t < (int)WT; ++t)
-                    s[t] = E::mma(qf[k], K[set][t][k], s[t]);
+                    s[t] = E::mma(qf[k], K8[t][k], s[t]);
             __builtin_amdgcn_sched_barrier(0);
             read_q(q + 1 < n_q ? q0 + 32 : 0);
             f32x4 z[4];
@@ -1631,21 +1767,21 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 constexpr uint32_t kStrips = 1u << 20;     // of columns that one launch weighs at most
 
 // The kernel for tiles of qt query rows.
-template <int DT, int DC, int FIT>
+template <int DT, int DC, int FIT, int CE>
 void (*attend_kernel(uint32_t qt))(const Attend)
 {
     if (qt == 16)
-        return attend_split<DT, DC, 1, FIT>;
+        return attend_split<DT, DC, 1, FIT, CE>;
     if (qt == 32)
-        return attend_split<DT, DC, 2, FIT>;
+        return attend_split<DT, DC, 2, FIT, CE>;
     if (qt == 64 && DC != 8)
-        return attend_tiles<DT, DC, DC != 8 ? 2 : 4, FIT>;
+        return attend_tiles<DT, DC, DC != 8 ? 2 : 4, FIT, CE>;
     if (qt == 256 && DC != 8)
-        return attend_tiles<DT, DC, DC != 8 ? 8 : 4, FIT>;
-    return attend_tiles<DT, DC, 4, FIT>;
+        return attend_tiles<DT, DC, DC != 8 ? 8 : 4, FIT, CE>;
+    return attend_tiles<DT, DC, 4, FIT, CE>;
 }
 
-template <int DT, int DC, int FIT>
+template <int DT, int DC, int FIT, int CE>
 hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
 {
     const uint32_t qt = attend_tile_rows(a.t * a.group, a.c.d);
@@ -1654,7 +1790,7 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     if (rows) {
         // (a multiple of 8 workgroups: the tiled kernel deals them out by XCD)
         const dim3 grid((a.slots * a.c.heads * a.tiles + 7) / 8 * 8);
-        attend_kernel<DT, DC, FIT>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
+        attend_kernel<DT, DC, FIT, CE>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
         if (a.scores || !(a.arrivals || a.whole)) {
@@ -1680,42 +1816,44 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
         Attend w = a;       // (its own cut of the rows: a workgroup a share and head)
         w.want = a.w_want;
         w.slots = a.w_want > a.c.batch ? a.w_want : a.c.batch;
-        attend_weights_held<DT, DC, FIT><<<dim3(w.slots * a.c.heads), 256, 0, s>>>(w);
+        attend_weights_held<DT, DC, FIT, CE><<<dim3(w.slots * a.c.heads), 256, 0, s>>>(w);
         return hipGetLastError();
     }
     const uint32_t w_rows = DC == 8 ? 128 : 256;
     const dim3 wg((uint32_t)((a.w_cols + w_rows - 1) / w_rows), a.c.batch * a.c.heads);
-    attend_weights<DT, DC, FIT><<<wg, 256, 0, s>>>(a);
+    attend_weights<DT, DC, FIT, CE><<<wg, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <int DT, int DC>
+template <int DT, int DC, int CE>
 hipError_t launch_attend_fit(const Attend &a, hipStream_t s)
 {
     if (a.c.d == 32 * DC)
-        return launch_attend_dc<DT, DC, FIT_WHOLE>(a, s);
-    return a.c.d % 8 == 0 ? launch_attend_dc<DT, DC, FIT_CHUNKS>(a, s)
-                          : launch_attend_dc<DT, DC, FIT_ANY>(a, s);
+        return launch_attend_dc<DT, DC, FIT_WHOLE, CE>(a, s);
+    if (CE == 1 || a.c.d % 8 == 0)
+        return launch_attend_dc<DT, DC, FIT_CHUNKS, CE>(a, s);
+    return launch_attend_dc<DT, DC, CE == 1 ? FIT_CHUNKS : FIT_ANY, CE>(a, s);
 }
 
-template <int DT>
+template <int DT, int CE>
 hipError_t launch_attend(const Attend &a, hipStream_t s)
 {
     const uint32_t d = a.c.d;
-    return d <= 64 ? launch_attend_fit<DT, 2>(a, s)
-                   : (d <= 128 ? launch_attend_fit<DT, 4>(a, s) : launch_attend_fit<DT, 8>(a, s));
+    return d <= 64 ? launch_attend_fit<DT, 2, CE>(a, s)
+                   : (d <= 128 ? launch_attend_fit<DT, 4, CE>(a, s) : launch_attend_fit<DT, 8, CE>(a, s));
 }
 
 // Workgroups of the kernel for d and qt that one CU holds at once.
-template <int DT>
+template <int DT, int CE>
 int attend_occupancy(uint32_t d, uint32_t qt)
 {
+    constexpr int FIT = CE == 1 ? FIT_CHUNKS : FIT_ANY;
     static int known[3][5];
     int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : (qt == 128 ? 3 : 4)))];
     if (n == 0) {
-        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, FIT_ANY>(qt)
-                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, FIT_ANY>(qt)
-                                            : (const void *)attend_kernel<DT, 8, FIT_ANY>(qt));
+        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, FIT, CE>(qt)
+                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, FIT, CE>(qt)
+                                            : (const void *)attend_kernel<DT, 8, FIT, CE>(qt));
         int x = 0;
         if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&x, k, qt == 256 ? 512 : 256, 0) != hipSuccess)
             (void)hipGetLastError();

@@ -39,6 +39,11 @@ struct Cache {
     uint32_t room;          // width * page: rows a sequence may hold (< 2^31)
     PageDiv div;
     uint32_t batch, heads, d;
+    // of a cache in 8 bits: k and v point at e4m3 elements (strides in elements), and ex at the
+    // exponents of each page, block of rows and head, k's in the low byte and v's in the high one
+    const uint16_t *ex;
+    uint32_t blocks;        // of a page
+    PageDiv by_block;       // rows of a block
 };
 
 // Page number and place in the page of row n (< room) of sequence b; the number
@@ -175,6 +180,11 @@ int attend_occupancy_f16(uint32_t d, uint32_t tile_rows);
 int attend_occupancy_bf16(uint32_t d, uint32_t tile_rows);
 hipError_t launch_attend_f16(const Attend &a, hipStream_t s);
 hipError_t launch_attend_bf16(const Attend &a, hipStream_t s);
+// The same over a cache in 8 bits (d a multiple of 8).
+int attend8_occupancy_f16(uint32_t d, uint32_t tile_rows);
+int attend8_occupancy_bf16(uint32_t d, uint32_t tile_rows);
+hipError_t launch_attend8_f16(const Attend &a, hipStream_t s);
+hipError_t launch_attend8_bf16(const Attend &a, hipStream_t s);
 
 // --------------------------------------------------------- rotary and appending
 
@@ -238,5 +248,68 @@ inline uint64_t evict_hist_values(uint64_t sets, uint32_t chunks)
 inline uint64_t evict_state_values(uint64_t sets, uint32_t chunks) { return sets * chunks * 8; }
 
 hipError_t launch_evict(const Evict &e, hipStream_t s);
+
+// ------------------------------------------------------------- appending in 8 bits
+
+struct Append8 {
+    int dtype;
+    Turn turn;              // of keys
+    Cache c;
+    uint32_t t, blocks;     // tokens; blocks of a sequence that they may touch
+    const int32_t *len, *count;
+    Strided key, value;     // out unused
+};
+
+hipError_t launch_append8(const Append8 &r, hipStream_t s);
+
+// ------------------------------------------------------------------------- pages
+
+struct Pages {
+    const int32_t *table, *len, *parent;    // parent may be null
+    int64_t table_row;
+    uint32_t batch, width, pages, room, out_batch, tokens;
+    PageDiv div;
+    int32_t *out_table, *new_len, *copies, *lacking;
+    uint32_t *used;         // a bit a page, zeros between calls
+    int32_t *holder;        // a page: the first sequence that goes on with it partly filled
+    uint32_t *base;         // a sequence: pages given out before it
+    int32_t *kept;          // a sequence: whether its last page stays with it
+    int32_t *free;          // the pages to give out
+    uint32_t *n_free;       // how many there are
+};
+
+// Scratch of a call in 4-byte values: holder, base, kept, free, n_free.
+hipError_t launch_pages(const Pages &p, hipStream_t s);
+
+struct Copy {
+    Cache c;
+    uint32_t size;          // bytes of an element
+    const int32_t *copies;
+    uint32_t n;
+};
+
+hipError_t launch_copy(const Copy &c, hipStream_t s);
+
+// ------------------------------------------------------------------ drafted tokens
+
+struct Verify {
+    int dtype;
+    uint32_t batch, t, vocab;
+    const int64_t *tokens;
+    const int32_t *parent, *count;      // may be null
+    int64_t parent_seq;
+    const void *target, *draft;         // draft may be null
+    int64_t p_seq, p_row, q_seq, q_row; // strides in elements
+    const float *uniform;
+    int32_t *path, *found;
+    int64_t *next;
+    uint32_t chunks;                    // of VE_CHUNK tokens of the vocabulary
+    double *sums;                       // per sequence and chunk: of r, of p
+    uint32_t *arrivals;                 // per sequence, zeros between calls
+};
+
+constexpr uint32_t VE_CHUNK = 4096, VE_MOST = 1024;   // tokens of a workgroup; nodes at most
+
+hipError_t launch_verify(const Verify &v, hipStream_t s);
 
 }  // namespace sjc

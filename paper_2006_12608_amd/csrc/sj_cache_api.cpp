@@ -1,5 +1,6 @@
 // sj_cache_api.cpp -- host side of the calls on a cache of key and value rows
-// (sj_rotary, sj_cache_append, sj_attend, sj_cache_evict; contracts in include/sj.h):
+// (sj_rotary, sj_cache_append, sj_attend, sj_cache_evict, the two for caches in 8 bits, pages and
+// their copies, and the verification of drafted tokens; contracts in include/sj.h):
 // argument checks, scratch, and the kernels on the context's stream.  Nothing
 // here waits for the device but the replacement of scratch that a call outgrows.
 #include <hip/hip_runtime.h>
@@ -28,7 +29,7 @@ struct Axis {
 // The device array that element 0 and these strided axes reach, d adjacent elements
 // at each place.
 int check_strided(const sj_ctx *c, const void *p, const Axis *axes, int n_axes, uint64_t d,
-                  const char *name)
+                  const char *name, uint32_t size = 2)
 {
     uint64_t last = 0;
     for (int i = 0; i < n_axes; ++i) {
@@ -44,9 +45,9 @@ int check_strided(const sj_ctx *c, const void *p, const Axis *axes, int n_axes, 
             last += (axes[i].n - 1) * (uint64_t)axes[i].stride;
         }
     }
-    if ((uintptr_t)p % 2 != 0)
-        return fail(SJ_E_INVAL, "%s must be 2-byte aligned", name);
-    return check_device_ptr(c, p, (size_t)(last + d) * 2, name);
+    if ((uintptr_t)p % size != 0)
+        return fail(SJ_E_INVAL, "%s must be %u-byte aligned", name, size);
+    return check_device_ptr(c, p, (size_t)(last + d) * size, name);
 }
 
 // Scratch and counters of one call.  While the context's stream is captured nothing may be
@@ -80,8 +81,9 @@ int check_array(const sj_ctx *c, const void *p, uint64_t bytes, uint32_t align, 
     return check_device_ptr(c, p, (size_t)bytes, name);
 }
 
-// Checks a cache and translates it for the kernels.
-int check_cache(const sj_ctx *c, const sj_cache *s, const char *name, sjc::Cache *out)
+// Checks a cache of elements of `size` bytes and translates it for the kernels.
+int check_cache(const sj_ctx *c, const sj_cache *s, const char *name, sjc::Cache *out,
+                uint32_t size = 2)
 {
     if (!s)
         return fail(SJ_E_INVAL, "%s is NULL", name);
@@ -100,8 +102,8 @@ int check_cache(const sj_ctx *c, const sj_cache *s, const char *name, sjc::Cache
     int st;
     const Axis k[3] = {{s->pages, s->k_page}, {s->page, s->k_row}, {s->heads, s->k_head}};
     const Axis v[3] = {{s->pages, s->v_page}, {s->page, s->v_row}, {s->heads, s->v_head}};
-    if ((st = check_strided(c, s->k, k, 3, s->d, "k")) != SJ_OK ||
-        (st = check_strided(c, s->v, v, 3, s->d, "v")) != SJ_OK)
+    if ((st = check_strided(c, s->k, k, 3, s->d, "k", size)) != SJ_OK ||
+        (st = check_strided(c, s->v, v, 3, s->d, "v", size)) != SJ_OK)
         return st;
     if (s->table && s->batch && width) {
         if (s->table_row < 0 || s->table_row > kMaxStride)
@@ -113,7 +115,30 @@ int check_cache(const sj_ctx *c, const sj_cache *s, const char *name, sjc::Cache
     }
     *out = sjc::Cache{(const uint16_t *)s->k, (const uint16_t *)s->v, s->k_page, s->k_row, s->k_head,
                       s->v_page, s->v_row, s->v_head, s->table, s->table_row, width, s->pages,
-                      width * s->page, sjc::PageDiv::of(s->page), s->batch, s->heads, s->d};
+                      width * s->page, sjc::PageDiv::of(s->page), s->batch, s->heads, s->d,
+                      nullptr, 1, sjc::PageDiv::of(s->page)};
+    return SJ_OK;
+}
+
+// The same of a cache in 8 bits.
+int check_cache8(const sj_ctx *c, const sj_cache8 *s, const char *name, sjc::Cache *out)
+{
+    if (!s)
+        return fail(SJ_E_INVAL, "%s is NULL", name);
+    int st;
+    if ((st = check_cache(c, &s->rows, name, out, 1)) != SJ_OK)
+        return st;
+    if (s->rows.d % 8 != 0)
+        return fail(SJ_E_UNSUPPORTED, "%s: d = %u is no multiple of 8", name, s->rows.d);
+    if (s->block == 0 || s->rows.page % s->block != 0)
+        return fail(SJ_E_INVAL, "%s: blocks of %u rows do not divide pages of %u", name, s->block,
+                    s->rows.page);
+    out->blocks = s->rows.page / s->block;
+    if ((st = check_array(c, s->exponents, (uint64_t)s->rows.pages * out->blocks * s->rows.heads * 2, 2,
+                          "exponents")) != SJ_OK)
+        return st;
+    out->ex = (const uint16_t *)s->exponents;
+    out->by_block = sjc::PageDiv::of(s->block);
     return SJ_OK;
 }
 
@@ -178,20 +203,23 @@ extern "C" int sj_rotary(sj_ctx *c, int dtype, const void *x, const int64_t x_st
     return SJ_OK;
 }
 
-extern "C" int sj_cache_append(sj_ctx *c, const sj_cache *cache, const int32_t *len,
-                               const int32_t *count, uint32_t t, const void *key,
-                               const int64_t key_stride[3], const void *value,
-                               const int64_t value_stride[3], const int32_t *pos,
-                               const int64_t *turns, uint32_t n_pairs, int layout, double factor,
-                               const void *q, const int64_t q_stride[3], uint32_t q_heads,
-                               void *q_out, const int64_t q_out_stride[3])
+namespace {
+
+// sj_cache_append (cache) and sj_cache8_append (cache8).
+int append_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool eight, const int32_t *len,
+                const int32_t *count, uint32_t t, const void *key, const int64_t key_stride[3],
+                const void *value, const int64_t value_stride[3], const int32_t *pos,
+                const int64_t *turns, uint32_t n_pairs, int layout, double factor, const void *q,
+                const int64_t q_stride[3], uint32_t q_heads, void *q_out,
+                const int64_t q_out_stride[3])
 {
     g_err.clear();
     if (!c)
         return fail(SJ_E_INVAL, "context is NULL");
     sjc::Rotary r{};
     int st;
-    if ((st = check_cache(c, cache, "cache", &r.c)) != SJ_OK)
+    if ((st = eight ? check_cache8(c, cache8, "cache", &r.c)
+                    : check_cache(c, cache, "cache", &r.c)) != SJ_OK)
         return st;
     const uint32_t B = r.c.batch, d = r.c.d;
     if (!key_stride || !value_stride || (q && (!q_stride || !q_out_stride)))
@@ -232,7 +260,7 @@ extern "C" int sj_cache_append(sj_ctx *c, const sj_cache *cache, const int32_t *
                q_out_stride[0], q_out_stride[1], q_out_stride[2], q_heads};
     }
     SJ_HIP(hipSetDevice(c->device));
-    r.dtype = cache->dtype;
+    r.dtype = eight ? cache8->rows.dtype : cache->dtype;
     r.turn = {pos, turns, n_pairs, layout, (float)factor, false};
     r.batch = B;
     r.t = t;
@@ -243,14 +271,68 @@ extern "C" int sj_cache_append(sj_ctx *c, const sj_cache *cache, const int32_t *
              r.c.heads};
     r.value = {(const uint16_t *)value, nullptr, value_stride[0], value_stride[1], value_stride[2],
                0, 0, 0, r.c.heads};
-    SJ_HIP(sjc::launch_rotary(r, c->stream));
+    if (!eight) {
+        SJ_HIP(sjc::launch_rotary(r, c->stream));
+        return SJ_OK;
+    }
+    // (the blocks that t rows may touch, beginning anywhere in the first)
+    const uint32_t block = cache8->block;
+    const uint64_t blocks = ((uint64_t)t + block - 2) / block + 1;
+    if (B * blocks * ((2 * (uint64_t)r.c.heads + 3) / 4) >= kMaxCells)
+        return fail(SJ_E_UNSUPPORTED, "%u x %u tokens of %u heads are too many", B, t, r.c.heads);
+    sjc::Append8 w{};
+    w.dtype = r.dtype;
+    w.turn = r.turn;
+    w.c = r.c;
+    w.t = t;
+    w.blocks = (uint32_t)blocks;
+    w.len = len;
+    w.count = count;
+    w.key = r.key;
+    w.value = r.value;
+    if (q) {
+        r.c.batch = 0;      // (the queries alone)
+        SJ_HIP(sjc::launch_rotary(r, c->stream));
+    }
+    if (r.c.room)
+        SJ_HIP(sjc::launch_append8(w, c->stream));
     return SJ_OK;
 }
 
-extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, const int32_t *count,
-                         uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
-                         const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,
-                         float *lse, const float *w_in, float *w_out, uint64_t w_cols)
+}  // namespace
+
+extern "C" int sj_cache_append(sj_ctx *c, const sj_cache *cache, const int32_t *len,
+                               const int32_t *count, uint32_t t, const void *key,
+                               const int64_t key_stride[3], const void *value,
+                               const int64_t value_stride[3], const int32_t *pos,
+                               const int64_t *turns, uint32_t n_pairs, int layout, double factor,
+                               const void *q, const int64_t q_stride[3], uint32_t q_heads,
+                               void *q_out, const int64_t q_out_stride[3])
+{
+    return append_rows(c, cache, nullptr, false, len, count, t, key, key_stride, value, value_stride, pos,
+                       turns, n_pairs, layout, factor, q, q_stride, q_heads, q_out, q_out_stride);
+}
+
+extern "C" int sj_cache8_append(sj_ctx *c, const sj_cache8 *cache, const int32_t *len,
+                               const int32_t *count, uint32_t t, const void *key,
+                               const int64_t key_stride[3], const void *value,
+                               const int64_t value_stride[3], const int32_t *pos,
+                               const int64_t *turns, uint32_t n_pairs, int layout, double factor,
+                               const void *q, const int64_t q_stride[3], uint32_t q_heads,
+                               void *q_out, const int64_t q_out_stride[3])
+{
+    return append_rows(c, nullptr, cache, true, len, count, t, key, key_stride, value, value_stride, pos,
+                       turns, n_pairs, layout, factor, q, q_stride, q_heads, q_out, q_out_stride);
+}
+
+
+namespace {
+
+// sj_attend (cache) and sj_attend8 (cache8).
+int attend_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool eight, const int32_t *len,
+                const int32_t *count, uint32_t t, const void *q, const int64_t q_stride[3],
+                uint32_t q_heads, const uint64_t *tree, const int64_t tree_stride[2], double scale,
+                void *out, float *lse, const float *w_in, float *w_out, uint64_t w_cols)
 {
     g_err.clear();
     const Alone alone(c);
@@ -258,8 +340,10 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
         return fail(SJ_E_INVAL, "context is NULL");
     sjc::Attend a{};
     int st;
-    if ((st = check_cache(c, cache, "cache", &a.c)) != SJ_OK)
+    if ((st = eight ? check_cache8(c, cache8, "cache", &a.c)
+                    : check_cache(c, cache, "cache", &a.c)) != SJ_OK)
         return st;
+    const bool f16 = (eight ? cache8->rows.dtype : cache->dtype) == SJ_F16;
     const uint32_t B = a.c.batch, d = a.c.d;
     if (q_heads == 0 || q_heads % a.c.heads != 0)
         return fail(SJ_E_INVAL, "%u query heads do not divide over %u cache heads", q_heads,
@@ -338,8 +422,8 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     const uint32_t rows = t * a.group, qt = sjc::attend_tile_rows(rows, d);
     const uint32_t dp = d <= 64 ? 64 : (d <= 128 ? 128 : 256);
     a.tiles = rows == 0 ? 1 : (rows + qt - 1) / qt;
-    const int per_cu = cache->dtype == SJ_F16 ? sjc::attend_occupancy_f16(d, qt)
-                                              : sjc::attend_occupancy_bf16(d, qt);
+    const int per_cu = (eight ? (f16 ? sjc::attend8_occupancy_f16 : sjc::attend8_occupancy_bf16)
+                              : (f16 ? sjc::attend_occupancy_f16 : sjc::attend_occupancy_bf16))(d, qt);
     const uint64_t units = (uint64_t)a.c.heads * a.tiles, held = (uint64_t)c->num_cus * per_cu;
     a.want = held / units > 0 ? (uint32_t)(held / units) : 1;
     // (no more workgroups than shares of the least size could use)
@@ -378,10 +462,31 @@ extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, c
     a.part_ml = (float *)(s + off_ml);
     a.part_o = (float *)(s + off_o);
     a.scores = keep ? (float *)(s + off_s) : nullptr;
-    SJ_HIP(cache->dtype == SJ_F16 ? sjc::launch_attend_f16(a, c->stream)
-                                  : sjc::launch_attend_bf16(a, c->stream));
+    SJ_HIP((eight ? (f16 ? sjc::launch_attend8_f16 : sjc::launch_attend8_bf16)
+                  : (f16 ? sjc::launch_attend_f16 : sjc::launch_attend_bf16))(a, c->stream));
     return SJ_OK;
 }
+
+}  // namespace
+
+extern "C" int sj_attend(sj_ctx *c, const sj_cache *cache, const int32_t *len, const int32_t *count,
+                         uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
+                         const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,
+                         float *lse, const float *w_in, float *w_out, uint64_t w_cols)
+{
+    return attend_rows(c, cache, nullptr, false, len, count, t, q, q_stride, q_heads, tree, tree_stride,
+                       scale, out, lse, w_in, w_out, w_cols);
+}
+
+extern "C" int sj_attend8(sj_ctx *c, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
+                         uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
+                         const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,
+                         float *lse, const float *w_in, float *w_out, uint64_t w_cols)
+{
+    return attend_rows(c, nullptr, cache, true, len, count, t, q, q_stride, q_heads, tree, tree_stride,
+                       scale, out, lse, w_in, w_out, w_cols);
+}
+
 
 extern "C" int sj_cache_evict(sj_ctx *c, const sj_cache *src, const int32_t *len,
                               const float *weight, uint32_t sets, uint64_t w_cols, uint32_t keep,
@@ -446,5 +551,210 @@ extern "C" int sj_cache_evict(sj_ctx *c, const sj_cache *src, const int32_t *len
         e.state = (uint32_t *)((uint8_t *)c->scratch + off);
     }
     SJ_HIP(sjc::launch_evict(e, c->stream));
+    return SJ_OK;
+}
+
+extern "C" int sj_cache_pages(sj_ctx *c, const int32_t *table, int64_t table_row, uint32_t batch,
+                              uint32_t width, uint32_t pages, uint32_t page, const int32_t *len,
+                              const int32_t *parent, uint32_t out_batch, uint32_t tokens,
+                              int32_t *out_table, int32_t *new_len, int32_t *copies,
+                              int32_t *lacking)
+{
+    g_err.clear();
+    const Alone alone(c);
+    if (!c)
+        return fail(SJ_E_INVAL, "context is NULL");
+    if (page == 0)
+        return fail(SJ_E_INVAL, "page must be positive");
+    if ((uint64_t)width * page > kMaxRows || page >= kMaxCells || pages >= kMaxCells ||
+        batch >= kMaxCells || (uint64_t)out_batch * width >= kMaxCells || out_batch > (1u << 22))
+        return fail(SJ_E_UNSUPPORTED, "%u sequences of %u pages of %u rows are too many", out_batch,
+                    width, page);
+    if (out_batch == 0)
+        return SJ_OK;
+    int st;
+    if (batch && width) {
+        if (table_row < 0 || table_row > kMaxStride)
+            return fail(SJ_E_INVAL, "table_row is negative or too large");
+        if ((st = check_array(c, table, ((uint64_t)(batch - 1) * (uint64_t)table_row + width) * 4, 4,
+                              "table")) != SJ_OK)
+            return st;
+    }
+    const uint64_t n = out_batch;
+    if ((st = check_array(c, len, (uint64_t)batch * 4, 4, "len")) != SJ_OK ||
+        (parent && (st = check_array(c, parent, n * 4, 4, "parent")) != SJ_OK) ||
+        (st = check_array(c, out_table, n * width * 4, 4, "out_table")) != SJ_OK ||
+        (st = check_array(c, new_len, n * 4, 4, "new_len")) != SJ_OK ||
+        (st = check_array(c, copies, n * 12, 4, "copies")) != SJ_OK ||
+        (st = check_array(c, lacking, n * 4, 4, "lacking")) != SJ_OK)
+        return st;
+    if ((out_table == table && width) || new_len == len)
+        return fail(SJ_E_INVAL, "out_table must not be table, and new_len not len");
+    SJ_HIP(hipSetDevice(c->device));
+    // scratch: [holders][base][kept][pages given out][their number]; no more pages are given out
+    // than there are, nor than the table's entries
+    const uint64_t given = n * width < pages ? n * width : pages;
+    const size_t off_base = align_up((size_t)pages * 4), off_kept = off_base + align_up((size_t)n * 4);
+    const size_t off_free = off_kept + align_up((size_t)n * 4);
+    const size_t off_n = off_free + align_up((size_t)given * 4);
+    if ((st = grow_both(c, off_n + 256, ((size_t)pages + 31) / 32 + 1)) != SJ_OK)
+        return st;
+    uint8_t *s = (uint8_t *)c->scratch;
+    sjc::Pages p{};
+    p.table = table;
+    p.len = len;
+    p.parent = parent;
+    p.table_row = table_row;
+    p.batch = batch;
+    p.width = width;
+    p.pages = pages;
+    p.room = width * page;
+    p.out_batch = out_batch;
+    p.tokens = tokens;
+    p.div = sjc::PageDiv::of(page);
+    p.out_table = out_table;
+    p.new_len = new_len;
+    p.copies = copies;
+    p.lacking = lacking;
+    p.used = c->arrivals;
+    p.holder = (int32_t *)s;
+    p.base = (uint32_t *)(s + off_base);
+    p.kept = (int32_t *)(s + off_kept);
+    p.free = (int32_t *)(s + off_free);
+    p.n_free = (uint32_t *)(s + off_n);
+    SJ_HIP(sjc::launch_pages(p, c->stream));
+    return SJ_OK;
+}
+
+namespace {
+
+int copy_rows(sj_ctx *c, sjc::Copy &k, const int32_t *copies, uint32_t n)
+{
+    const uint64_t chunks = ((uint64_t)k.c.d * k.size + 15) / 16;
+    if ((uint64_t)k.c.div.page * k.c.heads * chunks >= kMaxCells - 65536)
+        return fail(SJ_E_UNSUPPORTED, "pages of %u rows of %u heads are too long", k.c.div.page,
+                    k.c.heads);
+    if (n == 0 || k.c.pages == 0)
+        return SJ_OK;
+    int st;
+    if ((st = check_array(c, copies, (uint64_t)n * 12, 4, "copies")) != SJ_OK)
+        return st;
+    k.copies = copies;
+    k.n = n;
+    SJ_HIP(hipSetDevice(c->device));
+    SJ_HIP(sjc::launch_copy(k, c->stream));
+    return SJ_OK;
+}
+
+}  // namespace
+
+extern "C" int sj_cache_copy(sj_ctx *c, const sj_cache *cache, const int32_t *copies, uint32_t n)
+{
+    g_err.clear();
+    if (!c)
+        return fail(SJ_E_INVAL, "context is NULL");
+    if (!cache)
+        return fail(SJ_E_INVAL, "cache is NULL");
+    sjc::Copy k{};
+    k.size = 2;
+    sj_cache pool = *cache;     // (whatever sequences there are)
+    pool.table = nullptr;
+    pool.batch = 0;
+    const int st = check_cache(c, &pool, "cache", &k.c);
+    return st != SJ_OK ? st : copy_rows(c, k, copies, n);
+}
+
+extern "C" int sj_cache8_copy(sj_ctx *c, const sj_cache8 *cache, const int32_t *copies, uint32_t n)
+{
+    g_err.clear();
+    if (!c)
+        return fail(SJ_E_INVAL, "context is NULL");
+    if (!cache)
+        return fail(SJ_E_INVAL, "cache is NULL");
+    sjc::Copy k{};
+    k.size = 1;
+    sj_cache8 pool = *cache;
+    pool.rows.table = nullptr;
+    pool.rows.batch = 0;
+    const int st = check_cache8(c, &pool, "cache", &k.c);
+    return st != SJ_OK ? st : copy_rows(c, k, copies, n);
+}
+
+extern "C" int sj_verify(sj_ctx *c, int dtype, uint32_t batch, uint32_t t, uint32_t vocab,
+                         const int64_t *tokens, const int32_t *parent, int64_t parent_seq,
+                         const int32_t *count, const void *target, const int64_t target_stride[2],
+                         const void *draft, const int64_t draft_stride[2], const float *uniform,
+                         int32_t *path, int32_t *found, int64_t *next)
+{
+    g_err.clear();
+    const Alone alone(c);
+    if (!c)
+        return fail(SJ_E_INVAL, "context is NULL");
+    if (dtype != SJ_F16 && dtype != SJ_BF16 && dtype != SJ_F32)
+        return fail(SJ_E_INVAL, "dtype %d is none of SJ_F16, SJ_BF16 and SJ_F32", dtype);
+    if (t == 0 || vocab == 0)
+        return fail(SJ_E_INVAL, "t and vocab must be positive");
+    if (draft && parent)
+        return fail(SJ_E_INVAL, "draft goes with chains, not with parent");
+    if (!target_stride || (draft && !draft_stride))
+        return fail(SJ_E_INVAL, "strides are NULL");
+    sjc::Verify v{};
+    v.chunks = (vocab + sjc::VE_CHUNK - 1) / sjc::VE_CHUNK;
+    if (t > sjc::VE_MOST || vocab >= kMaxCells || batch >= kMaxCells / 1024 ||
+        (uint64_t)batch * v.chunks >= kMaxCells)
+        return fail(SJ_E_UNSUPPORTED, "%u sequences of %u nodes and %u tokens are too many", batch, t,
+                    vocab);
+    if (batch == 0)
+        return SJ_OK;
+    const uint64_t n = (uint64_t)batch * t;
+    const uint32_t size = dtype == SJ_F32 ? 4 : 2;
+    const Axis ap[2] = {{batch, target_stride[0]}, {t, target_stride[1]}};
+    int st;
+    if ((st = check_array(c, tokens, n * 8, 8, "tokens")) != SJ_OK ||
+        (count && (st = check_array(c, count, (uint64_t)batch * 4, 4, "count")) != SJ_OK) ||
+        (st = check_strided(c, target, ap, 2, vocab, "target", size)) != SJ_OK ||
+        (st = check_array(c, uniform, n * 4, 4, "uniform")) != SJ_OK ||
+        (st = check_array(c, path, n * 4, 4, "path")) != SJ_OK ||
+        (st = check_array(c, found, (uint64_t)batch * 4, 4, "found")) != SJ_OK ||
+        (st = check_array(c, next, (uint64_t)batch * 8, 8, "next")) != SJ_OK)
+        return st;
+    if (draft && t > 1) {
+        const Axis aq[2] = {{batch, draft_stride[0]}, {t - 1, draft_stride[1]}};
+        if ((st = check_strided(c, draft, aq, 2, vocab, "draft", size)) != SJ_OK)
+            return st;
+    }
+    if (parent) {
+        if (parent_seq < 0 || parent_seq > kMaxStride)
+            return fail(SJ_E_INVAL, "parent_seq is negative or too large");
+        if ((st = check_array(c, parent, ((uint64_t)(batch - 1) * (uint64_t)parent_seq + t) * 4, 4,
+                              "parent")) != SJ_OK)
+            return st;
+    }
+    SJ_HIP(hipSetDevice(c->device));
+    if ((st = grow_both(c, (size_t)batch * v.chunks * 16, batch)) != SJ_OK)
+        return st;
+    v.dtype = dtype;
+    v.batch = batch;
+    v.t = t;
+    v.vocab = vocab;
+    v.tokens = tokens;
+    v.parent = parent;
+    v.count = count;
+    v.parent_seq = parent_seq;
+    v.target = target;
+    v.draft = t > 1 ? draft : nullptr;
+    v.p_seq = target_stride[0];
+    v.p_row = target_stride[1];
+    if (draft) {
+        v.q_seq = draft_stride[0];
+        v.q_row = draft_stride[1];
+    }
+    v.uniform = uniform;
+    v.path = path;
+    v.found = found;
+    v.next = next;
+    v.sums = (double *)c->scratch;
+    v.arrivals = c->arrivals;
+    SJ_HIP(sjc::launch_verify(v, c->stream));
     return SJ_OK;
 }

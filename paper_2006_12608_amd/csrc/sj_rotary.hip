@@ -2,6 +2,7 @@
 // (sj_cache_append): pair i of a head turned by pos * f_i, with f_i in turns of
 // 2^-64 so that the phase of any position is one 64-bit product.
 #include "sj_cache.h"
+#include "sj_turn.h"
 
 namespace sjc {
 
@@ -21,30 +22,6 @@ struct RotaryArgs {
     uint32_t q_items, k_items, items;  // (head, chunk) items of a token: queries, keys, all
     PageDiv by_items, by_q, by_k, by_v, by_t, by_pairs;
 };
-
-__device__ __forceinline__ float to_float(int dt, uint32_t x)
-{
-    return dt == sjk::DT_F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)x)
-                             : __uint_as_float(x << 16);
-}
-
-__device__ __forceinline__ uint32_t to_bits(int dt, float x)
-{
-    return dt == sjk::DT_F16 ? (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x)
-                             : (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x);
-}
-
-// The turned pair.  Which product is fused with the sum is said, not left to the compiler, so that
-// all variants, and the two items of a chunk that is moved back, round alike.
-__device__ __forceinline__ float turn_a(float a, float b, float c, float s)
-{
-    return __builtin_fmaf(a, c, -(b * s));
-}
-
-__device__ __forceinline__ float turn_b(float a, float b, float c, float s)
-{
-    return __builtin_fmaf(b, c, a * s);
-}
 
 // One 8-pair chunk: lo and hi hold its 16 elements, (a_0 .. a_7) and (b_0 .. b_7) in the
 // half layout, (a_0, b_0, a_1, ..) in the interleaved one.
@@ -200,13 +177,7 @@ __global__ void __launch_bounds__(256) rotary_rows(const RotaryArgs g)
     for (uint32_t y = threadIdx.x; y < mine * stride; y += 256) {
         const uint32_t u = g.by_pairs.quot(y), p = y - u * stride;
         if (p < pairs) {
-            const uint64_t phase =
-                (uint64_t)(int64_t)r.turn.pos[tok0 + u] * (uint64_t)r.turn.turns[p];
-            // signed fraction of a turn; 2^-31 half turns a unit
-            const float half = (float)(int32_t)(phase >> 32) * 4.656612873077393e-10f;
-            float s, c;
-            sincospif(half, &s, &c);
-            table[y] = float2{c * r.turn.factor, (r.turn.inverse ? -s : s) * r.turn.factor};
+            table[y] = sine_of(r.turn, (uint64_t)(int64_t)r.turn.pos[tok0 + u], p);
         }
     }
     __syncthreads();

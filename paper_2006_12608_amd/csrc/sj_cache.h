@@ -304,7 +304,7 @@ struct Verify {
     int32_t *path, *found;
     int64_t *next;
     uint32_t chunks;                    // of VE_CHUNK tokens of the vocabulary
-    double *sums;                       // per sequence and chunk: of r, of p
+    double *sums;                       // per sequence and chunk
     uint32_t *arrivals;                 // per sequence, zeros between calls
 };
 

@@ -731,7 +731,7 @@ extern "C" int sj_verify(sj_ctx *c, int dtype, uint32_t batch, uint32_t t, uint3
             return st;
     }
     SJ_HIP(hipSetDevice(c->device));
-    if ((st = grow_both(c, (size_t)batch * v.chunks * 16, batch)) != SJ_OK)
+    if ((st = grow_both(c, (size_t)batch * v.chunks * 8, batch)) != SJ_OK)
         return st;
     v.dtype = dtype;
     v.batch = batch;

@@ -38,100 +38,127 @@ constexpr uint32_t VE_EACH = VE_CHUNK / 256;    // tokens of a thread, side by s
 // Where a sequence's walk ended.
 struct Walk {
     uint32_t node, nodes;   // the last accepted one; nodes of the sequence
+    uint32_t found;         // accepted nodes, in path
     bool refused;           // a drafted token was refused there, with draft
     uint32_t gone;          // tokens refused there, without draft
 };
 
-struct Shared {
-    double p[VE_MOST];      // of a node's token after its parent
-    int64_t token[VE_MOST];
-    float u[VE_MOST], q[VE_MOST];
-    int32_t parent[VE_MOST], path[VE_MOST];
-    int64_t gone[VE_MOST];
-    uint32_t found;
+// What is known of node n, a lane each.
+struct Node {
+    float p, q, u;          // probabilities of its token after its parent; random number
+    int32_t parent;         // -1: never reached
+    int64_t token;
 };
 
-// The sequence's walk, by every workgroup for itself: the probabilities of the drafted tokens are
-// gathered at once, a thread a node; a wave then goes from node to node with ballots over 64 of
-// them at a time.
+__device__ __forceinline__ float number(float u)
+{
+    return u > 0.f ? (u < 1.f ? u : 0x1.fffffep-1f) : 0.f;
+}
+
 template <int DT>
-__device__ __forceinline__ Walk walk(const Verify &v, uint32_t b, Shared &sh)
+__device__ __forceinline__ Node node_of(const Verify &v, uint32_t b, uint32_t n, uint32_t T)
 {
     typedef typename Prob<DT>::one one;
-    __shared__ Walk out;
-    const uint32_t T = v.count ? clamp_rows(v.count[b], v.t) : v.t;
-    for (uint32_t n = threadIdx.x; n < T; n += 256) {
-        const int32_t from = v.parent ? v.parent[(int64_t)b * v.parent_seq + n] : (int32_t)n - 1;
-        const bool real = n > 0 && (uint32_t)from < n;
-        const int64_t x = v.tokens[(uint64_t)b * v.t + n];
-        const bool known = real && (uint64_t)x < v.vocab;
-        const one *p = (const one *)v.target + (int64_t)b * v.p_seq;
-        sh.p[n] = known ? clean(Prob<DT>::of(p[(int64_t)from * v.p_row + x])) : 0.f;
-        if (v.draft) {
-            const one *q = (const one *)v.draft + (int64_t)b * v.q_seq;
-            sh.q[n] = known ? clean(Prob<DT>::of(q[(int64_t)from * v.q_row + x])) : 0.f;
-        }
-        const float u = v.uniform[(uint64_t)b * v.t + n];
-        sh.u[n] = u > 0.f ? (u < 1.f ? u : 0x1.fffffep-1f) : 0.f;
-        sh.parent[n] = real ? from : -1;
-        sh.token[n] = x;
+    Node k = {0.f, 0.f, 0.f, -1, -1};
+    if (n == 0 || n >= T)
+        return k;
+    const int32_t from = v.parent ? v.parent[(int64_t)b * v.parent_seq + n] : (int32_t)n - 1;
+    k.token = v.tokens[(uint64_t)b * v.t + n];
+    k.u = number(v.uniform[(uint64_t)b * v.t + n]);
+    if ((uint32_t)from >= n)
+        return k;
+    k.parent = from;
+    if ((uint64_t)k.token < v.vocab) {
+        k.p = clean(Prob<DT>::of(((const one *)v.target)[(int64_t)b * v.p_seq + (int64_t)from * v.p_row + k.token]));
+        if (v.draft)
+            k.q = clean(Prob<DT>::of(((const one *)v.draft)[(int64_t)b * v.q_seq + (int64_t)from * v.q_row + k.token]));
     }
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        const uint32_t lane = threadIdx.x;
-        Walk w = {0, T, false, 0};
-        uint32_t found = T ? 1 : 0;
-        double left = 1.0;
-        if (lane == 0)
-            sh.path[0] = 0;
+    return k;
+}
+
+__device__ __forceinline__ int64_t shfl_token(int64_t x, uint32_t lane)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, (int)lane);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), (int)lane);
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+__device__ __forceinline__ float lane_value(float x, uint32_t lane)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), (int)lane));
+}
+
+// The sequence's walk, by a wave: 64 nodes at a time, the next ones' values on their way. A chain
+// ends at its first refusal; in a tree the wave goes from node to node by ballots of those that
+// follow the present one.
+template <int DT>
+__device__ __forceinline__ Walk walk(const Verify &v, uint32_t b, int32_t *path, int64_t *gone)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t T = v.count ? clamp_rows(v.count[b], v.t) : v.t;
+    Walk w = {0, T, T ? 1u : 0u, false, 0};
+    if (lane == 0)
+        path[0] = 0;
+    Node next = node_of<DT>(v, b, lane, T);
+    if (!v.parent) {
         for (uint32_t n0 = 0; n0 < T; n0 += 64) {
-            const uint32_t n = n0 + lane;
-            const int32_t mine = n < T && n > 0 ? sh.parent[n] : -1;
-            uint64_t tries = __ballot(mine == (int32_t)w.node && mine >= 0);
-            while (tries) {
-                const uint32_t c = n0 + (uint32_t)__ffsll((unsigned long long)tries) - 1;
-                tries &= tries - 1;
-                const double u = (double)sh.u[c];
-                double p = sh.p[c];
-                bool yes;
-                if (v.draft) {
-                    yes = u * (double)sh.q[c] < p;
-                } else {
-                    const int64_t x = sh.token[c];
-                    for (uint32_t g = 0; g < w.gone; g += 64)
-                        if (__ballot(g + lane < w.gone && sh.gone[g + lane] == x))
-                            p = 0.0;
-                    yes = p > 0.0 && u * left < p;
-                }
-                if (yes) {
-                    w.node = c;
-                    w.refused = false;
-                    w.gone = 0;
-                    left = 1.0;
-                    if (lane == 0)
-                        sh.path[found] = (int32_t)c;
-                    ++found;
-                    tries = __ballot(mine == (int32_t)c);
-                } else if (v.draft) {
-                    w.refused = true;
-                } else {
-                    left -= p;
-                    if (lane == 0)
-                        sh.gone[w.gone] = sh.token[c];
-                    ++w.gone;
-                    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                }
+            const Node k = next;
+            next = node_of<DT>(v, b, n0 + 64 + lane, T);
+            const bool yes = v.draft ? (double)k.u * (double)k.q < (double)k.p : k.u < k.p;
+            const uint64_t no = __ballot(n0 + lane > 0 && n0 + lane < T && !yes);
+            const uint32_t first = no ? n0 + (uint32_t)__ffsll((unsigned long long)no) - 1 : T;
+            if (n0 + lane < first)
+                path[n0 + lane] = (int32_t)(n0 + lane);
+            if (no) {
+                w.node = first - 1;
+                w.found = first;
+                w.refused = v.draft != nullptr;
+                w.gone = v.draft ? 0 : 1;
+                if (n0 + lane == first)
+                    gone[0] = k.token;
+                return w;
             }
         }
-        if (lane == 0) {
-            sh.found = found;
-            out = w;
-        }
+        w.node = T ? T - 1 : 0;
+        w.found = T;
+        return w;
     }
-    __syncthreads();
-    return out;
+    double left = 1.0;
+    for (uint32_t n0 = 0; n0 < T; n0 += 64) {
+        const Node k = next;
+        next = node_of<DT>(v, b, n0 + 64 + lane, T);
+        uint64_t tries = __ballot(k.parent == (int32_t)w.node), refused = 0;
+        while (tries) {
+            const uint32_t c = (uint32_t)__ffsll((unsigned long long)tries) - 1;
+            tries &= tries - 1;
+            const int64_t x = shfl_token(k.token, c);
+            double p = (double)lane_value(k.p, c);
+            uint64_t again = __ballot((refused >> lane) & 1 && k.token == x);
+            for (uint32_t g = 0; g < w.gone; g += 64)
+                again |= __ballot(g + lane < w.gone && gone[g + lane] == x);
+            p = again ? 0.0 : p;
+            if (p > 0.0 && (double)lane_value(k.u, c) * left < p) {
+                w.node = n0 + c;
+                w.gone = 0;
+                left = 1.0;
+                refused = 0;
+                if (lane == 0)
+                    path[w.found] = (int32_t)(n0 + c);
+                ++w.found;
+                tries = __ballot(k.parent == (int32_t)w.node);
+            } else {
+                left -= p;
+                refused |= (uint64_t)1 << c;
+            }
+        }
+        if ((refused >> lane) & 1)
+            gone[w.gone + (uint32_t)__popcll(refused & (((uint64_t)1 << lane) - 1))] = k.token;
+        w.gone += (uint32_t)__popcll(refused);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+    return w;
 }
 
 // The weights r and p of this thread's tokens of a chunk.
@@ -140,8 +167,8 @@ struct Weights {
     float p[VE_EACH], q[VE_EACH];
     uint32_t gone;          // bit k: token k was refused
 
-    __device__ __forceinline__ void load(const Verify &v, uint32_t b, const Walk &w, const Shared &sh,
-                                         uint32_t chunk)
+    __device__ __forceinline__ void load(const Verify &v, uint32_t b, const Walk &w,
+                                         const int64_t *refused, uint32_t chunk)
     {
         typedef typename Prob<DT>::one one;
         const uint32_t x0 = chunk * VE_CHUNK + threadIdx.x * VE_EACH;
@@ -168,16 +195,56 @@ struct Weights {
         }
         gone = 0;
         for (uint32_t g = 0; g < w.gone; ++g) {
-            const uint64_t k = (uint64_t)sh.gone[g] - x0;
+            const uint64_t k = (uint64_t)refused[g] - x0;
             gone |= k < VE_EACH ? 1u << k : 0u;
         }
     }
-    __device__ __forceinline__ double r(uint32_t k) const
+    // r of token k, or p where `plain`
+    __device__ __forceinline__ double of(uint32_t k, bool plain) const
     {
-        const double x = (double)p[k] - (double)q[k];
-        return (gone >> k) & 1 || x < 0.0 ? 0.0 : x;
+        const double x = (double)p[k] - (plain ? 0.0 : (double)q[k]);
+        return (!plain && (gone >> k) & 1) || x < 0.0 ? 0.0 : x;
+    }
+    __device__ __forceinline__ double sum(bool plain) const
+    {
+        double x = 0.0;
+#pragma unroll
+        for (uint32_t k = 0; k < VE_EACH; ++k)
+            x += of(k, plain);
+        return x;
     }
 };
+
+// Number of the first thread for which `yes` holds; 256 if none.  (`last`: of the last one.)
+__device__ __forceinline__ uint32_t first_thread(bool yes, uint32_t *found)
+{
+    const uint64_t m = __ballot(yes);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        found[threadIdx.x >> 6] =
+            m ? (threadIdx.x & 192) + (uint32_t)__ffsll((unsigned long long)m) - 1 : 256;
+    __syncthreads();
+    uint32_t x = found[3];
+#pragma unroll
+    for (int i = 2; i >= 0; --i)
+        x = found[i] < 256 ? found[i] : x;
+    return x;
+}
+
+__device__ __forceinline__ uint32_t last_thread(bool yes, uint32_t *found)
+{
+    const uint64_t m = __ballot(yes);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        found[threadIdx.x >> 6] =
+            m ? (threadIdx.x & 192) + 63 - (uint32_t)__clzll((long long)m) : 256;
+    __syncthreads();
+    uint32_t x = found[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+        x = found[i] < 256 ? found[i] : x;
+    return x;
+}
 
 // Sum of x over the threads before this one, and over all; always in the same order.
 __device__ __forceinline__ double add_before(double x, double *waves, double *all)
@@ -202,6 +269,9 @@ __device__ __forceinline__ double add_before(double x, double *waves, double *al
     return before + (incl - x);
 }
 
+// (Stores count as loads do.)
+__device__ __forceinline__ void wait_stores() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 __device__ __forceinline__ void put_sum(double *p, double x)
 {
     __hip_atomic_store((uint64_t *)p, __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED,
@@ -214,120 +284,129 @@ __device__ __forceinline__ double get_sum(const double *p)
                                                         __HIP_MEMORY_SCOPE_AGENT));
 }
 
-// A workgroup sums the weights of one chunk of the vocabulary in double; the last one of a
-// sequence to arrive finds the chunk, thread and token where the sums pass the threshold.
+// A workgroup sums the weights of one chunk of the vocabulary in double, after walking through its
+// sequence's nodes (every workgroup for itself); the last one of a sequence to arrive finds the
+// chunk, thread and token where the sums pass the threshold, and reads that chunk again.
 template <int DT>
 __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
 {
-    __shared__ Shared sh;
-    __shared__ double waves[4];
-    __shared__ uint32_t arrived, hit, last;
-    __shared__ double before_hit;
+    extern __shared__ int64_t lists[];      // tokens refused (t), then the path (t)
+    __shared__ Walk walked;
+    __shared__ double waves[4], before;
+    __shared__ uint32_t found[4], at_chunk, arrived;
     const Verify &v = g.v;
     const uint32_t id = (uint32_t)(g.first + blockIdx.x);
     const uint32_t b = g.by_chunks.quot(id), chunk = id - b * v.chunks, tid = threadIdx.x;
-    const Walk w = walk<DT>(v, b, sh);
-    Weights<DT> y;
-    double all, all_p;
-    if (w.nodes > 0) {
-        y.load(v, b, w, sh, chunk);
-        double r = 0.0, p = 0.0;
-#pragma unroll
-        for (uint32_t k = 0; k < VE_EACH; ++k) {
-            r += y.r(k);
-            p += (double)y.p[k];
-        }
-        add_before(r, waves, &all);
-        add_before(p, waves, &all_p);
-    } else {
-        all = all_p = 0.0;
+    int64_t *const gone = lists;
+    int32_t *const path = (int32_t *)(lists + v.t);
+    const float u = number(v.uniform[(uint64_t)b * v.t]);
+    if (tid < 64) {
+        const Walk w = walk<DT>(v, b, path, gone);
+        if (tid == 0)
+            walked = w;
     }
-    double *sums = v.sums + (uint64_t)b * v.chunks * 2;
+    __syncthreads();
+    const Walk w = walked;
+    Weights<DT> y;
+    double all = 0.0;
+    if (w.nodes > 0) {
+        y.load(v, b, w, gone, chunk);
+        add_before(y.sum(false), waves, &all);
+    }
+    double *const sums = v.sums + (uint64_t)b * v.chunks;
     if (tid == 0) {
-        put_sum(sums + 2 * chunk, all);
-        put_sum(sums + 2 * chunk + 1, all_p);
-        __builtin_amdgcn_s_waitcnt(0x0f70);     // (stored before it is counted)
+        put_sum(sums + chunk, all);
+        wait_stores();      // (before it is counted)
         arrived = __hip_atomic_fetch_add(&v.arrivals[b], 1u, __ATOMIC_RELAXED,
                                          __HIP_MEMORY_SCOPE_AGENT);
         if (arrived == v.chunks - 1)
             __hip_atomic_store(&v.arrivals[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        hit = v.chunks;
-        last = 0;
     }
     __syncthreads();
     if (arrived != v.chunks - 1)
         return;
     for (uint32_t n = tid; n < v.t; n += 256)
-        v.path[(uint64_t)b * v.t + n] = n < sh.found ? sh.path[n] : -1;
-    if (tid == 0)
-        v.found[b] = (int32_t)sh.found;
+        v.path[(uint64_t)b * v.t + n] = n < w.found ? path[n] : -1;
+    if (tid == 0) {
+        v.found[b] = (int32_t)w.found;
+        if (w.nodes == 0)
+            v.next[b] = -1;
+    }
+    if (w.nodes == 0)
+        return;
     // the chunks' sums, a run of them a thread
     const uint32_t run = (v.chunks + 255) / 256, c0 = tid * run;
     const uint32_t c1 = c0 + run < v.chunks ? c0 + run : v.chunks;
-    double r = 0.0, p = 0.0, total, total_p;
-    for (uint32_t c = c0; c < c1; ++c) {
-        r += get_sum(sums + 2 * c);
-        p += get_sum(sums + 2 * c + 1);
-    }
-    double begin = add_before(r, waves, &total);
-    const double begin_p = add_before(p, waves, &total_p);
-    const bool plain = !(total > 0.0);
-    if (plain) {
-        begin = begin_p;
-        total = total_p;
-    }
+    double mine = 0.0, total;
+    for (uint32_t c = c0; c < c1; ++c)
+        mine += get_sum(sums + c);
+    double begin = add_before(mine, waves, &total);
+    bool plain = false;
     if (!(total > 0.0)) {
-        if (tid == 0)
-            v.next[b] = -1;
-        return;
-    }
-    const double threshold = (double)sh.u[0] * total;
-    // the first chunk whose sums pass it; where rounding leaves none, the last with a sum
-    auto sum_of = [&](uint32_t c) { return get_sum(sums + 2 * c + (plain ? 1 : 0)); };
-    double at = begin;
-    for (uint32_t c = c0; c < c1; ++c) {
-        const double x = sum_of(c);
-        if (x > 0.0) {
-            atomicMax(&last, c);
-            if (at + x > threshold)
-                atomicMin(&hit, c);
+        // nothing left of what may be drawn: p itself, summed here (probabilities that add up
+        // to 1 do not come to this, but for rounding)
+        plain = true;
+        for (uint32_t c = 0; c < v.chunks; ++c) {
+            y.load(v, b, w, gone, c);
+            add_before(y.sum(true), waves, &all);
+            if (tid == 0)
+                put_sum(sums + c, all);
         }
-        at += x;
-    }
-    __syncthreads();
-    const uint32_t there = hit < v.chunks ? hit : last;
-    if (there >= c0 && there < c1) {
-        at = begin;
-        for (uint32_t c = c0; c < there; ++c)
-            at += sum_of(c);
-        before_hit = at;
-    }
-    __syncthreads();
-    if (tid == 0) {
-        hit = 0xffffffffu;
-        last = 0;
-    }
-    __syncthreads();
-    y.load(v, b, w, sh, there);
-    double mine = 0.0, unused;
-#pragma unroll
-    for (uint32_t k = 0; k < VE_EACH; ++k)
-        mine += plain ? (double)y.p[k] : y.r(k);
-    double sum = before_hit + add_before(mine, waves, &unused);
-#pragma unroll
-    for (uint32_t k = 0; k < VE_EACH; ++k) {
-        const double x = plain ? (double)y.p[k] : y.r(k);
-        sum += x;
-        if (x > 0.0) {
-            const uint32_t token = there * VE_CHUNK + tid * VE_EACH + k;
-            atomicMax(&last, token);
-            if (sum > threshold)
-                atomicMin(&hit, token);
+        wait_stores();
+        __syncthreads();
+        mine = 0.0;
+        for (uint32_t c = c0; c < c1; ++c)
+            mine += get_sum(sums + c);
+        begin = add_before(mine, waves, &total);
+        if (!(total > 0.0)) {
+            if (tid == 0)
+                v.next[b] = -1;
+            return;
         }
     }
+    // the first run whose sums pass the threshold and, where rounding leaves none, the last with a
+    // sum; in it the chunk, in the chunk the thread, of the thread the token, by the same rule
+    const double threshold = (double)u * total;
+    uint32_t who = first_thread(mine > 0.0 && begin + mine > threshold, found);
+    who = who < 256 ? who : last_thread(mine > 0.0, found);
+    if (tid == who) {
+        uint32_t last = c0;
+        double sum = begin, at = begin;
+        for (uint32_t c = c0; c < c1; ++c) {
+            const double x = get_sum(sums + c);
+            if (x > 0.0) {
+                last = c;
+                at = sum;
+                if (sum + x > threshold)
+                    break;
+            }
+            sum += x;
+        }
+        at_chunk = last;
+        before = at;
+    }
     __syncthreads();
-    if (tid == 0)
-        v.next[b] = (int64_t)(hit != 0xffffffffu ? hit : last);
+    const uint32_t there = at_chunk;
+    y.load(v, b, w, gone, there);
+    mine = y.sum(plain);
+    begin = before + add_before(mine, waves, &all);
+    who = first_thread(mine > 0.0 && begin + mine > threshold, found);
+    who = who < 256 ? who : last_thread(mine > 0.0, found);
+    if (tid == who) {
+        uint32_t last = 0;
+        double sum = begin;
+        bool passed = false;
+#pragma unroll
+        for (uint32_t k = 0; k < VE_EACH; ++k) {
+            const double x = y.of(k, plain);
+            if (x > 0.0 && !passed) {
+                last = k;
+                passed = sum + x > threshold;
+            }
+            sum += x;
+        }
+        v.next[b] = (int64_t)there * VE_CHUNK + tid * VE_EACH + last;
+    }
 }
 
 }  // namespace
@@ -342,12 +421,13 @@ hipError_t launch_verify(const Verify &v, hipStream_t s)
     for (; g.first < total && e == hipSuccess; g.first += step) {
         const uint64_t left = total - g.first;
         const dim3 grid((uint32_t)(left < step ? left : step));
+        const size_t lds = (size_t)v.t * 12;
         if (v.dtype == 5)
-            verify_chunks<5><<<grid, 256, 0, s>>>(g);
+            verify_chunks<5><<<grid, 256, lds, s>>>(g);
         else if (v.dtype == sjk::DT_F16)
-            verify_chunks<sjk::DT_F16><<<grid, 256, 0, s>>>(g);
+            verify_chunks<sjk::DT_F16><<<grid, 256, lds, s>>>(g);
         else
-            verify_chunks<sjk::DT_BF16><<<grid, 256, 0, s>>>(g);
+            verify_chunks<sjk::DT_BF16><<<grid, 256, lds, s>>>(g);
         e = hipGetLastError();
     }
     return e;

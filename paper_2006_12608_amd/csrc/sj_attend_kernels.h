@@ -182,6 +182,26 @@ __device__ __forceinline__ typename Cells<CE>::eight load_cells(const typename C
     }
 }
 
+// Sixteen elements of a cache in 8 bits (d is a multiple of 8).
+template <int FIT>
+__device__ __forceinline__ i32x4 load_cells16(const uint8_t *p, int left)
+{
+    i32x4 v = {0, 0, 0, 0};
+    if (FIT == FIT_WHOLE || left >= 16) {
+        __builtin_memcpy(&v, p, 16);
+    } else if (left > 0) {
+        i32x2 w;
+        __builtin_memcpy(&w, p, 8);
+        v = i32x4{w[0], w[1], 0, 0};
+    }
+    return v;
+}
+
+__device__ __forceinline__ i32x2 half_of(const i32x4 &v, int x)
+{
+    return x ? i32x2{v[2], v[3]} : i32x2{v[0], v[1]};
+}
+
 // The two exponents of the block of a row that exists: k's in the low byte, v's in the high one.
 template <int CE>
 __device__ __forceinline__ uint32_t load_exponents(const Cache &c, const Place &p, uint32_t h)
@@ -549,8 +569,11 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     constexpr int QT = AT_Q * NQ, D = 32 * DC;
     constexpr int RS = 2 * D + 32;              // bytes of a V row in LDS
     constexpr int OS = D + 4;                   // floats of a query's sums in LDS
-    constexpr int NV = 2 * DC;                  // 16-byte loads of V per lane and block
-    constexpr int VR = 16 / DC;                 // rows of V per load
+    constexpr int NV = 2 * DC;                  // 16-column tiles of V's products
+    constexpr int VL = 4 * DC / (CE == 1 ? 2 : 1);  // lanes of a row of V; 16 bytes each
+    constexpr int NL = VL / 2;                  // loads of V per lane and block
+    constexpr int VR = 64 / VL;                 // rows of V per load
+    constexpr int KL = CE == 1 ? DC / 2 : DC;   // loads of K per lane and row
     constexpr int WAVE_LDS = AT_ROWS * RS;
     static_assert(AT_Q * OS * 4 <= WAVE_LDS, "the sums of a query tile fit in the wave's V");
     __shared__ __align__(16) uint8_t lds[AT_WAVES * WAVE_LDS];
@@ -592,6 +615,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         ahead = entry(first + wave + AT_WAVES);
     }
 
+    // Elements of a product's step c that lane group g4 holds.  In 8 bits a lane loads 16 elements at
+    // once, which are those of two steps; the order of a product's terms is free.
+    auto at_elem = [&](int c) { return 64 * (c / 2) + 16 * (int)g4 + 8 * (c % 2); };
+
     // queries: lane l holds query l % 16 of each tile in operand layout
     i32x4 Q[NQ][DC];
     uint32_t tok[NQ];
@@ -603,9 +630,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         const uint16_t *p = a.q + (int64_t)b * a.q_seq + (int64_t)tok[j] * a.q_tok +
                             (int64_t)(h * a.group + (there ? r % a.group : 0)) * a.q_head + 8 * g4;
 #pragma unroll
-        for (int c = 0; c < DC; ++c)
-            Q[j][c] = there ? load_q8<FIT>(a, p + 32 * c, (int)d - (int)(32 * c + 8 * g4))
-                            : i32x4{0, 0, 0, 0};
+        for (int c = 0; c < DC; ++c) {
+            const int o = CE == 1 ? at_elem(c) - 8 * (int)g4 : 32 * c;
+            Q[j][c] = there ? load_q8<FIT>(a, p + o, (int)d - (o + 8 * (int)g4)) : i32x4{0, 0, 0, 0};
+        }
     }
 
     wait_loads();
@@ -627,26 +655,33 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     // place of row lane % 32 of a block: absent rows read page 0, row 0 (their
     // scores and values are replaced below)
     auto place = [&](const Entry &e) { return place_of(a.c, b, e, to); };
-    typename Cells<CE>::eight K[2][DC], V[NV];
+    i32x4 K[2][KL], V[NL];
     auto load_k = [&](const Place &p) {
         const int64_t off = p.page < 0 ? 0
                                        : (int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const Cell *r = kb + shfl64(off, (int)q16 + 16 * t) + 8 * g4;
+            const Cell *r = kb + shfl64(off, (int)q16 + 16 * t);
 #pragma unroll
-            for (int c = 0; c < DC; ++c)
-                K[t][c] = load_cells<FIT, CE>(r + 32 * c, (int)d - (int)(32 * c + 8 * g4));
+            for (int c = 0; c < KL; ++c) {
+                if constexpr (CE == 1)
+                    K[t][c] = load_cells16<FIT>(r + at_elem(2 * c), (int)d - at_elem(2 * c));
+                else
+                    K[t][c] = load_fit<FIT>(r + 8 * g4 + 32 * c, (int)d - (int)(32 * c + 8 * g4));
+            }
         }
     };
-    const uint32_t v_row = lane / (4 * DC), v_col = 8 * (lane % (4 * DC));
+    const uint32_t v_row = lane / VL, v_col = 16 / CE * (lane % VL);
     auto load_v = [&](const Place &p) {
         const int64_t off = p.page < 0 ? 0
                                        : (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < NL; ++i) {
             const Cell *r = vb + shfl64(off, VR * i + (int)v_row) + v_col;
-            V[i] = load_cells<FIT, CE>(r, (int)d - (int)v_col);
+            if constexpr (CE == 1)
+                V[i] = load_cells16<FIT>(r, (int)d - (int)v_col);
+            else
+                V[i] = load_fit<FIT>(r, (int)d - (int)v_col);
         }
     };
 
@@ -677,7 +712,11 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                 s[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < DC; ++c) {
-                const i32x4 k8 = widen<DT>(K[t][c], two);
+                i32x4 k8;
+                if constexpr (CE == 1)
+                    k8 = widen<DT>(half_of(K[t][c / 2], c % 2), two);
+                else
+                    k8 = K[t][c];
 #pragma unroll
                 for (int j = 0; j < NQ; ++j)
                     s[j][t] = E::mma(k8, Q[j][c], s[j][t]);
@@ -690,16 +729,24 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         // V to LDS; rows that do not exist as zeros (0 x NaN would reach every query)
         uint32_t odd = 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            i32x4 v8 = widen<DT>(
-                V[i], CE == 1 ? power_v((uint32_t)__shfl((int)ex, VR * i + (int)v_row)) : 1.f);
-            if (tail || there != 0xffffffffu) {
-                if (!((there >> (VR * i + v_row)) & 1))
-                    v8 = i32x4{0, 0, 0, 0};
-                odd |= drop_odd8<DT>(v8, blk * AT_ROWS + VR * i + v_row >= rows.len);
-                asm volatile("");       // (a branch, not selects in every round)
+        for (int i = 0; i < NL; ++i) {
+            const uint32_t r = VR * i + v_row;
+            const float two = CE == 1 ? power_v((uint32_t)__shfl((int)ex, (int)r)) : 1.f;
+#pragma unroll
+            for (int x = 0; x < 2 / CE; ++x) {
+                i32x4 v8;
+                if constexpr (CE == 1)
+                    v8 = widen<DT>(half_of(V[i], x), two);
+                else
+                    v8 = V[i];
+                if (tail || there != 0xffffffffu) {
+                    if (!((there >> r) & 1))
+                        v8 = i32x4{0, 0, 0, 0};
+                    odd |= drop_odd8<DT>(v8, blk * AT_ROWS + r >= rows.len);
+                    asm volatile("");       // (a branch, not selects in every round)
+                }
+                *(i32x4 *)(my + r * RS + 2 * v_col + 16 * x) = v8;
             }
-            *(i32x4 *)(my + (VR * i + v_row) * RS + 2 * v_col) = v8;
         }
         load_v(nxt);
 

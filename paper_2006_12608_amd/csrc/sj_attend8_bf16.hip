@@ -3,9 +3,9 @@
 
 namespace sjc {
 
-int attend8_occupancy_bf16(uint32_t d, uint32_t tile_rows)
+int attend8_occupancy_bf16(uint32_t d, uint32_t tile_rows, uint32_t heads)
 {
-    return attend_occupancy<sjk::DT_BF16, 1>(d, tile_rows);
+    return attend_occupancy<sjk::DT_BF16, 1>(d, tile_rows, heads);
 }
 
 hipError_t launch_attend8_bf16(const Attend &a, hipStream_t s)

@@ -17,7 +17,7 @@ uint32_t attend_tile_rows(uint32_t rows, uint32_t d)
 
 int attend_occupancy_f16(uint32_t d, uint32_t tile_rows)
 {
-    return attend_occupancy<sjk::DT_F16, 2>(d, tile_rows);
+    return attend_occupancy<sjk::DT_F16, 2>(d, tile_rows, 1);
 }
 
 hipError_t launch_attend_f16(const Attend &a, hipStream_t s)

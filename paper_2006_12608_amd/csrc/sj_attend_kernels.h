@@ -472,22 +472,26 @@ __device__ __forceinline__ f32x2 get2(const float *p)
     return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 
+__device__ __forceinline__ bool last_to_arrive(uint32_t *counter, uint32_t n)
+{
+    __shared__ uint32_t arrived;
+    wait_loads();       // (stores count as loads do)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (arrived == n - 1)
+            __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return arrived == n - 1;
+}
+
 template <int DT, uint32_t QT, uint32_t D>
 __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t h, uint32_t unit,
                                           uint32_t slot, uint32_t shares, uint32_t count)
 {
     typedef Elem<DT> E;
-    __shared__ uint32_t arrived;
-    wait_loads();       // (stores count as loads do)
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        uint32_t *n = a.arrivals + (uint64_t)b * a.c.heads * a.tiles + unit;
-        arrived = __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (arrived == shares - 1)
-            __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (arrived != shares - 1)
+    if (!last_to_arrive(a.arrivals + (uint64_t)b * a.c.heads * a.tiles + unit, shares))
         return;
     const uint64_t first = (uint64_t)slot * a.c.heads * a.tiles + unit;
     const uint64_t step = (uint64_t)a.c.heads * a.tiles;
@@ -537,6 +541,120 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
     }
 }
 
+// For more shares than a workgroup joins at once: n results, of the slots first_slot, first_slot + every,
+// ..., of query rows of `unit` are joined into that of the first one or, where `whole`, into the
+// output.  Where there are 8 or 4 query rows, the threads of the others take every second or
+// fourth result of theirs.
+constexpr uint32_t AT_JOIN = 32;
+
+template <int DT, uint32_t QT, uint32_t D>
+__device__ __forceinline__ void join_parts(const Attend &a, uint32_t b, uint32_t h, uint32_t unit,
+                                           uint32_t first_slot, uint32_t every, uint32_t n,
+                                           uint32_t count, bool whole)
+{
+    typedef Elem<DT> E;
+    const uint64_t units = (uint64_t)a.c.heads * a.tiles;
+    const uint64_t first = first_slot * units + unit, step = every * units;
+    for (uint32_t q0 = 0; q0 < QT; q0 += 16) {
+        const uint32_t r0 = unit % a.tiles * QT + q0, all = a.t * a.group;
+        const uint32_t here = r0 < all ? all - r0 : 0;
+        const uint32_t log = here > 8 ? 0 : (here > 4 ? 1 : 2), groups = 1u << log;
+        const uint32_t qi = threadIdx.x >> (4 + log), x = threadIdx.x & 15;
+        const uint32_t group = (threadIdx.x >> 4) & (groups - 1), lanes = 16 << log;
+        const uint32_t r = r0 + qi, u = a.by_group.quot(r);
+        auto at = [&](uint32_t s) { return (first + s * step) * QT + q0 + qi; };
+        if (r >= all)
+            continue;
+        float top = -INFINITY;
+        for (uint32_t s = threadIdx.x & (lanes - 1); s < n; s += lanes)
+            top = fmaxf(top, get2(a.part_ml + 2 * at(s))[0]);
+#pragma unroll
+        for (uint32_t o = 1; o < 64; o <<= 1)
+            if (o < lanes)
+                top = fmaxf(top, __shfl_xor(top, o));
+        const float base = top == -INFINITY ? 0.f : top;
+        f32x4 o[D / 64] = {};
+        float l = 0.f;
+#pragma unroll 8
+        for (uint32_t s = group; s < n; s += groups) {
+            const uint64_t p = at(s);
+            const f32x2 ml = get2(a.part_ml + 2 * p);
+            const float f = exp2_(ml[0] - base);
+            l += ml[1] * f;
+#pragma unroll
+            for (uint32_t k = 0; k < D / 64; ++k) {
+                const float *y = a.part_o + p * D + 64 * k + 4 * x;
+                const f32x2 lo = get2(y), hi = get2(y + 2);
+                o[k] += f32x4{lo[0], lo[1], hi[0], hi[1]} * f;
+            }
+        }
+#pragma unroll
+        for (uint32_t g = 1; g < 4; g <<= 1)
+            if (g < groups) {
+                l += __shfl_xor(l, 16 * g);
+#pragma unroll
+                for (uint32_t k = 0; k < D / 64; ++k)
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e)
+                        o[k][e] += __shfl_xor(o[k][e], 16 * g);
+            }
+        if (group)
+            continue;
+        if (!whole) {       // (the threads of a row are of one wave, which has read all it joins)
+            float *y = a.part_o + at(0) * D + 4 * x;
+#pragma unroll
+            for (uint32_t k = 0; k < D / 64; ++k) {
+                put2(y + 64 * k, o[k][0], o[k][1]);
+                put2(y + 64 * k + 2, o[k][2], o[k][3]);
+            }
+            if (x == 0)
+                put2(a.part_ml + 2 * at(0), top, l);
+            continue;
+        }
+        const bool live = u < count && l != 0.f;
+        const float inv = live ? 1.f / l : 0.f;
+        const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group;
+#pragma unroll
+        for (uint32_t k = 0; k < D / 64; ++k)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const uint32_t c = 64 * k + 4 * x + e;
+                if (c < a.c.d)
+                    a.out[row * a.c.d + c] =
+                        __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[k][e] * inv : 0.f));
+            }
+        if (x == 0)
+            a.lse[row] = live ? (top + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
+    }
+}
+
+// Joins the shares of HW heads in two steps, AT_JOIN neighbours at a time and then those
+// results, each by the last workgroup to arrive.  (Two sequences of 131072 rows, 96 to 128 shares of
+// 4 query rows each: 125 us in one step, 117 in two; heads of 64 90 and 77.)
+template <int DT, uint32_t QT, uint32_t D, int HW>
+__device__ __forceinline__ void join_steps(const Attend &a, uint32_t b, uint32_t h0, uint32_t tile,
+                                           uint32_t slot, const Share &sh)
+{
+    const uint32_t units = a.c.heads * a.tiles, unit = h0 * a.tiles + tile;
+    const uint32_t from = sh.share / AT_JOIN * AT_JOIN, groups = (sh.shares + AT_JOIN - 1) / AT_JOIN;
+    const uint32_t n = sh.shares - from < AT_JOIN ? sh.shares - from : AT_JOIN;
+    const uint32_t first = slot - sh.share;         // the sequence's first share
+    // counters: a sequence's, then a slot's
+    // (the call has B units and then slots units counters)
+    uint32_t *const steps = a.arrivals + (uint64_t)a.c.batch * units;
+    if (n > 1 && !last_to_arrive(steps + (uint64_t)(first + from) * units + unit, n))
+        return;
+    if (n > 1 || groups == 1)
+        for (uint32_t y = 0; y < HW; ++y)
+            join_parts<DT, QT, D>(a, b, h0 + y, unit + y * a.tiles, first + from, 1, n, sh.rows.count,
+                                  groups == 1);
+    if (groups == 1 || !last_to_arrive(a.arrivals + (uint64_t)b * units + unit, groups))
+        return;
+    for (uint32_t y = 0; y < HW; ++y)
+        join_parts<DT, QT, D>(a, b, h0 + y, unit + y * a.tiles, first, AT_JOIN, groups, sh.rows.count,
+                              true);
+}
+
 // ------------------------------------------------------------- the split kernel
 //
 // A workgroup takes one share of a sequence's rows for one cache head and its up to
@@ -561,9 +679,14 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
 // 5.4 TB/s, or 231 with the scores kept (33 MB); 32 sequences of 200 to 8192 rows, 550 MB, in
 // 116 (4.7 TB/s).  One sequence of 2048 rows: 10 us, of which most is the latency of the chain
 // lengths, page numbers, rows, join.
-template <int DT, int DC, int NQ, int FIT, int CE>
+//
+// HW > 1: the workgroup takes HW heads at once, AT_WAVES / HW waves each, so that their shorter rows,
+// side by side in memory, are asked for together (8 bits: 128 bytes a row and head of 128, and 4.0 TB/s
+// alone against 4.6 where the rows of a head are adjacent instead).
+template <int DT, int DC, int NQ, int FIT, int CE, int HW>
 __global__ void __launch_bounds__(256) attend_split(const Attend a)
 {
+    constexpr uint32_t STREAMS = AT_WAVES / HW;
     typedef Elem<DT> E;
     typedef typename Cells<CE>::one Cell;
     constexpr int QT = AT_Q * NQ, D = 32 * DC;
@@ -582,9 +705,10 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
 
     const uint32_t lane = threadIdx.x & 63;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t units = a.c.heads * a.tiles;
+    const uint32_t units = a.c.heads / HW * a.tiles;
     const uint32_t unit = blockIdx.x % units, slot = blockIdx.x / units;
-    const uint32_t h = unit / a.tiles, tile = unit % a.tiles;
+    const uint32_t h0 = unit / a.tiles * HW, tile = unit % a.tiles;
+    const uint32_t h = h0 + wave % HW, stream = wave / HW;
     Share sh;
     if (slot >= a.slots || !find_share(a, slot, &sh))
         return;
@@ -610,9 +734,9 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         return entry_of(a.c, a.len, b, blk * AT_ROWS + (lane & 31));
     };
     Entry first_at = {0, 0u}, ahead = {0, 0u};
-    if (first + wave < last) {
-        first_at = entry(first + wave);
-        ahead = entry(first + wave + AT_WAVES);
+    if (first + stream < last) {
+        first_at = entry(first + stream);
+        ahead = entry(first + stream + STREAMS);
     }
 
     // Elements of a product's step c that lane group g4 holds.  In 8 bits a lane loads 16 elements at
@@ -688,7 +812,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
     if (threadIdx.x == 0)
         odd_any = 0;
     __syncthreads();
-    uint32_t blk = first + wave;
+    uint32_t blk = first + stream;
     Place cur = {-1, 0u}, nxt = {-1, 0u};
     uint32_t ex = 0;        // of row lane % 32
     if (blk < last) {
@@ -697,7 +821,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         load_k(cur);
         load_v(cur);
     }
-    for (; blk < last; blk += AT_WAVES) {
+    for (; blk < last; blk += STREAMS) {
         nxt = place(ahead);
         // bit r: row r of the block exists
         const uint32_t there = (uint32_t)__ballot(cur.page >= 0);
@@ -722,7 +846,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
                     s[j][t] = E::mma(k8, Q[j][c], s[j][t]);
             }
         }
-        ahead = entry(blk + 2 * AT_WAVES);
+        ahead = entry(blk + 2 * STREAMS);
         const uint32_t nex = load_exponents<CE>(a.c, nxt, h);
         load_k(nxt);        // (past the end: page 0, row 0; a branch would cost full waits)
 
@@ -827,13 +951,12 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         }
     }
     __syncthreads();
-    const uint64_t part = (uint64_t)slot * units + unit;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
         float top = -INFINITY;
 #pragma unroll
-        for (uint32_t w = 0; w < AT_WAVES; ++w)
-            top = fmaxf(top, stat[w][AT_Q * j + q16][0]);
+        for (uint32_t w = 0; w < STREAMS; ++w)
+            top = fmaxf(top, stat[wave % HW + HW * w][AT_Q * j + q16][0]);
         const float f = exp2_(m[j] - (top == -INFINITY ? 0.f : top)) * DOWN;
         if (j)
             __syncthreads();
@@ -844,62 +967,72 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
         __syncthreads();
         // 256 threads: query threadIdx.x / 16, columns 4 (threadIdx.x % 16) + 64 k
         const uint32_t qi = threadIdx.x >> 4, c0 = 4 * (threadIdx.x & 15);
-        float tot = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (uint32_t w = 0; w < AT_WAVES; ++w)
-            tot = fmaxf(tot, stat[w][AT_Q * j + qi][0]);
-        const float base = tot == -INFINITY ? 0.f : tot;
-#pragma unroll
-        for (uint32_t w = 0; w < AT_WAVES; ++w)
-            sum += stat[w][AT_Q * j + qi][1] * exp2_(stat[w][AT_Q * j + qi][0] - base);
         const uint32_t r = tile * QT + AT_Q * j + qi;
         const uint32_t u = r / a.group;
-        if (r < q_rows) {
-            const bool live = u < rows.count;
-            const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r % a.group;
 #pragma unroll
-            for (uint32_t c = c0; c < (uint32_t)D; c += 64) {
-                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t y = 0; y < HW; ++y) {     // the workgroup's heads
+            const uint32_t hy = h0 + y;
+            float tot = -INFINITY, sum = 0.f;
 #pragma unroll
-                for (uint32_t w = 0; w < AT_WAVES; ++w)
-                    o += *(const f32x4 *)((const float *)(lds + w * WAVE_LDS) + qi * OS + c);
-                if (odd_any && live)
-                    own_rows<CE>(a, b, h, rows, u, first * AT_ROWS, to, [&](const Cell *v) {
+            for (uint32_t w = y; w < AT_WAVES; w += HW)
+                tot = fmaxf(tot, stat[w][AT_Q * j + qi][0]);
+            const float base = tot == -INFINITY ? 0.f : tot;
+#pragma unroll
+            for (uint32_t w = y; w < AT_WAVES; w += HW)
+                sum += stat[w][AT_Q * j + qi][1] * exp2_(stat[w][AT_Q * j + qi][0] - base);
+            if (r < q_rows) {
+                const bool live = u < rows.count;
+                const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + hy * a.group + r % a.group;
+                const uint64_t part = ((uint64_t)slot * a.c.heads + hy) * a.tiles + tile;
+#pragma unroll
+                for (uint32_t c = c0; c < (uint32_t)D; c += 64) {
+                    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (uint32_t w = y; w < AT_WAVES; w += HW)
+                        o += *(const f32x4 *)((const float *)(lds + w * WAVE_LDS) + qi * OS + c);
+                    if (odd_any && live)
+                        own_rows<CE>(a, b, hy, rows, u, first * AT_ROWS, to, [&](const Cell *v) {
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e)
+                                if (c + e < d)
+                                    o[e] += odd_part<DT>(v[c + e]);
+                        });
+                    if (shares > 1) {
+                        float *p = a.part_o + (part * QT + AT_Q * j + qi) * D + c;
+                        if (a.arrivals) {
+                            put2(p, o[0], o[1]);
+                            put2(p + 2, o[2], o[3]);
+                        } else {
+                            *(f32x4 *)p = o;
+                        }
+                    } else {
+                        const float inv = live && sum != 0.f ? 1.f / sum : 0.f;
 #pragma unroll
                         for (uint32_t e = 0; e < 4; ++e)
-                            if (c + e < d)
-                                o[e] += odd_part<DT>(v[c + e]);
-                    });
-                if (shares > 1) {
-                    float *p = a.part_o + (part * QT + AT_Q * j + qi) * D + c;
-                    if (a.arrivals) {
-                        put2(p, o[0], o[1]);
-                        put2(p + 2, o[2], o[3]);
-                    } else {
-                        *(f32x4 *)p = o;
+                            if (FIT == FIT_WHOLE || c + e < d)
+                                a.out[row * d + c + e] = __builtin_bit_cast(
+                                    uint16_t,
+                                    (typename E::one)(live && sum != 0.f ? o[e] * inv : 0.f));
                     }
-                } else {
-                    const float inv = live && sum != 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e)
-                        if (FIT == FIT_WHOLE || c + e < d)
-                            a.out[row * d + c + e] = __builtin_bit_cast(
-                                uint16_t, (typename E::one)(live && sum != 0.f ? o[e] * inv : 0.f));
                 }
-            }
-            if (c0 == 0) {
-                if (shares > 1) {
-                    put2(a.part_ml + (part * QT + AT_Q * j + qi) * 2, tot, sum);
-                } else {
-                    a.lse[row] = live && sum != 0.f
-                                     ? (tot + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f
-                                     : -INFINITY;
+                if (c0 == 0) {
+                    if (shares > 1) {
+                        put2(a.part_ml + (part * QT + AT_Q * j + qi) * 2, tot, sum);
+                    } else {
+                        a.lse[row] = live && sum != 0.f
+                                         ? (tot + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f
+                                         : -INFINITY;
+                    }
                 }
             }
         }
     }
-    if (shares > 1 && a.arrivals)
-        join_last<DT, QT, D>(a, b, h, unit, slot - sh.share, shares, rows.count);
+    if (shares > 1 && a.arrivals) {
+        if constexpr (CE == 1)
+            join_steps<DT, QT, D, HW>(a, b, h0, tile, slot, sh);
+        else
+            join_last<DT, QT, D>(a, b, h, unit, slot - sh.share, shares, rows.count);
+    }
 }
 
 // ------------------------------------------------------------- the tiled kernel
@@ -1814,13 +1947,20 @@ __global__ void __launch_bounds__(256, 2) attend_weights_held(const Attend a)
 constexpr uint32_t kStrips = 1u << 20;     // of columns that one launch weighs at most
 
 // The kernel for tiles of qt query rows.
-template <int DT, int DC, int FIT, int CE>
-void (*attend_kernel(uint32_t qt))(const Attend)
+template <int DT, int DC, int FIT, int CE, int HW>
+void (*split_kernel(uint32_t qt))(const Attend)
 {
-    if (qt == 16)
-        return attend_split<DT, DC, 1, FIT, CE>;
-    if (qt == 32)
-        return attend_split<DT, DC, 2, FIT, CE>;
+    return qt == 16 ? attend_split<DT, DC, 1, FIT, CE, HW> : attend_split<DT, DC, 2, FIT, CE, HW>;
+}
+
+template <int DT, int DC, int FIT, int CE>
+void (*attend_kernel(uint32_t qt, uint32_t hw))(const Attend)
+{
+    if (qt <= 32) {
+        if (CE == 1 && hw == 2)
+            return split_kernel<DT, DC, FIT, CE, CE == 1 ? 2 : 1>(qt);
+        return split_kernel<DT, DC, FIT, CE, 1>(qt);
+    }
     if (qt == 64 && DC != 8)
         return attend_tiles<DT, DC, DC != 8 ? 2 : 4, FIT, CE>;
     if (qt == 256 && DC != 8)
@@ -1836,8 +1976,8 @@ hipError_t launch_attend_dc(const Attend &a, hipStream_t s)
     hipError_t e;
     if (rows) {
         // (a multiple of 8 workgroups: the tiled kernel deals them out by XCD)
-        const dim3 grid((a.slots * a.c.heads * a.tiles + 7) / 8 * 8);
-        attend_kernel<DT, DC, FIT, CE>(qt)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
+        const dim3 grid((a.slots * (a.c.heads / a.heads_at_once) * a.tiles + 7) / 8 * 8);
+        attend_kernel<DT, DC, FIT, CE>(qt, a.heads_at_once)<<<grid, qt == 256 ? 512 : 256, 0, s>>>(a);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
         if (a.scores || !(a.arrivals || a.whole)) {
@@ -1892,15 +2032,15 @@ hipError_t launch_attend(const Attend &a, hipStream_t s)
 
 // Workgroups of the kernel for d and qt that one CU holds at once.
 template <int DT, int CE>
-int attend_occupancy(uint32_t d, uint32_t qt)
+int attend_occupancy(uint32_t d, uint32_t qt, uint32_t hw)
 {
     constexpr int FIT = CE == 1 ? FIT_CHUNKS : FIT_ANY;
-    static int known[3][5];
-    int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : (qt == 128 ? 3 : 4)))];
+    static int known[3][5][2];
+    int &n = known[d <= 64 ? 0 : (d <= 128 ? 1 : 2)][qt == 16 ? 0 : (qt == 32 ? 1 : (qt == 64 ? 2 : (qt == 128 ? 3 : 4)))][hw - 1];
     if (n == 0) {
-        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, FIT, CE>(qt)
-                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, FIT, CE>(qt)
-                                            : (const void *)attend_kernel<DT, 8, FIT, CE>(qt));
+        const void *k = d <= 64 ? (const void *)attend_kernel<DT, 2, FIT, CE>(qt, hw)
+                                : (d <= 128 ? (const void *)attend_kernel<DT, 4, FIT, CE>(qt, hw)
+                                            : (const void *)attend_kernel<DT, 8, FIT, CE>(qt, hw));
         int x = 0;
         if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&x, k, qt == 256 ? 512 : 256, 0) != hipSuccess)
             (void)hipGetLastError();

@@ -159,6 +159,7 @@ struct Attend {
     // work split: a sequence's rows are cut into shares, one workgroup per share,
     // cache head and tile of query rows
     uint32_t tiles;                // tiles of query rows per cache head
+    uint32_t heads_at_once;        // cache heads of a workgroup
     uint32_t want;                 // shares there should be at most
     uint32_t w_want;               // the same for the weights' kernel, a workgroup a share and head
     uint32_t slots;                // most shares there can be
@@ -181,8 +182,8 @@ int attend_occupancy_bf16(uint32_t d, uint32_t tile_rows);
 hipError_t launch_attend_f16(const Attend &a, hipStream_t s);
 hipError_t launch_attend_bf16(const Attend &a, hipStream_t s);
 // The same over a cache in 8 bits (d a multiple of 8).
-int attend8_occupancy_f16(uint32_t d, uint32_t tile_rows);
-int attend8_occupancy_bf16(uint32_t d, uint32_t tile_rows);
+int attend8_occupancy_f16(uint32_t d, uint32_t tile_rows, uint32_t heads_at_once);
+int attend8_occupancy_bf16(uint32_t d, uint32_t tile_rows, uint32_t heads_at_once);
 hipError_t launch_attend8_f16(const Attend &a, hipStream_t s);
 hipError_t launch_attend8_bf16(const Attend &a, hipStream_t s);
 

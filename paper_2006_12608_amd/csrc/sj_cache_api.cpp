@@ -422,13 +422,25 @@ int attend_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     const uint32_t rows = t * a.group, qt = sjc::attend_tile_rows(rows, d);
     const uint32_t dp = d <= 64 ? 64 : (d <= 128 ? 128 : 256);
     a.tiles = rows == 0 ? 1 : (rows + qt - 1) / qt;
-    const int per_cu = (eight ? (f16 ? sjc::attend8_occupancy_f16 : sjc::attend8_occupancy_bf16)
-                              : (f16 ? sjc::attend_occupancy_f16 : sjc::attend_occupancy_bf16))(d, qt);
+    // Two heads at once where rows are 8 bits and shares of one head each would more than fill the
+    // GPU (32 sequences of 200 to 8192 rows of 8 heads of 128: 76 us one at a time, 69 two, 73
+    // four; heads of 64: 54, 41, 50; one sequence of 2048 rows of 2 heads, which cannot fill it: 12
+    // and 16).
+    a.heads_at_once = 1;
+    const uint64_t least = sjc::AT_ROWS * sjc::AT_WAVES;
+    if (eight && qt <= 32 && a.c.heads % 2 == 0 &&
+        B * ((a.c.room + least - 1) / least) * a.c.heads * a.tiles > 8 * (uint64_t)c->num_cus)
+        a.heads_at_once = 2;
+    int per_cu;
+    if (eight)
+        per_cu = (f16 ? sjc::attend8_occupancy_f16 : sjc::attend8_occupancy_bf16)(d, qt, a.heads_at_once);
+    else
+        per_cu = (f16 ? sjc::attend_occupancy_f16 : sjc::attend_occupancy_bf16)(d, qt);
     const uint64_t units = (uint64_t)a.c.heads * a.tiles, held = (uint64_t)c->num_cus * per_cu;
-    a.want = held / units > 0 ? (uint32_t)(held / units) : 1;
+    const uint64_t groups = units / a.heads_at_once;
+    a.want = held / groups > 0 ? (uint32_t)(held / groups) : 1;
     // (no more workgroups than shares of the least size could use)
-    const uint64_t room_shares =
-        (uint64_t)B * ((a.c.room + sjc::AT_ROWS * sjc::AT_WAVES - 1) / (sjc::AT_ROWS * sjc::AT_WAVES) + 1);
+    const uint64_t room_shares = B * ((a.c.room + least - 1) / least + 1);
     a.slots = a.want > B ? a.want : B;
     a.slots = a.slots < room_shares ? a.slots : (uint32_t)room_shares;
     a.w_want = 2 * c->num_cus / a.c.heads > 0 ? 2 * c->num_cus / a.c.heads : 1;
@@ -452,8 +464,8 @@ int attend_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     const uint64_t s_bytes = (uint64_t)B * a.c.heads * rows * a.s_cols * 4;
     const bool keep = w_out && rows <= 16 && s_bytes > 0 && s_bytes <= kMaxScores;
     const bool counted = qt <= 32 && !keep && !a.whole;
-    if ((st = grow_both(c, off_s + (keep ? (size_t)s_bytes : 0), counted ? (size_t)B * units : 0)) !=
-        SJ_OK)
+    const size_t counters = counted ? (size_t)(B + (eight ? a.slots : 0)) * units : 0;
+    if ((st = grow_both(c, off_s + (keep ? (size_t)s_bytes : 0), counters)) != SJ_OK)
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     a.plan = (uint32_t *)s;

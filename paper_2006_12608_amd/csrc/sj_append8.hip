@@ -14,7 +14,7 @@ struct Append8Args {
     Append8 r;
     uint64_t first;             // of the launch's workgroups
     uint32_t lanes_log;         // lanes of a row: d / 8 rounded up to a power of two
-    uint32_t units, groups;     // heads x {k, v}; workgroups of 4 of them
+    uint32_t units, groups;     // heads x {k, v}; workgroups for them
     PageDiv by_blocks, by_groups;
 };
 
@@ -108,18 +108,21 @@ __device__ __forceinline__ i32x4 turned8(const Turn &t, const uint16_t *row, i32
     return v;
 }
 
-// A wave takes one block of a sequence's rows, one head, keys or values: the largest magnitude of
-// the new rows in it (a maximum of 16-bit integers), from that the exponent, the rows before
-// len[b] rounded to it where it grows, and the new rows' e4m3 values.
-template <int DT, bool TURN>
+// A wave (or all four of a workgroup, where a block has more than A8_HELD chunks a lane: 2 x 1184 tokens
+// in blocks of 64 rows of 256, 17 -> 6 us) takes one block of a sequence's rows, one head, keys or
+// values: the largest magnitude of the new rows in it (a maximum of 16-bit integers), from that
+// the exponent, the rows before len[b] rounded to it where it grows, and the new rows' e4m3
+// values.  Bound by HBM (2 bytes in, 1 out: 8 x 2048 tokens of 8 heads of 128, 101 MB, in 23 us), for
+// a token or two by the chain lengths, page, exponent, rows.
+template <int DT, bool TURN, uint32_t WAVES>
 __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
 {
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     const Append8 &r = g.r;
-    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t tid = threadIdx.x & (64 * WAVES - 1);    // of the unit's threads
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t id = (uint32_t)(g.first + blockIdx.x);
-    const uint32_t bj = g.by_groups.quot(id), unit = (id - bj * g.groups) * 4 + wave;
+    const uint32_t bj = g.by_groups.quot(id), unit = (id - bj * g.groups) * (4 / WAVES) + wave / WAVES;
     const uint32_t b = g.by_blocks.quot(bj), j = bj - b * r.blocks;
     if (unit >= g.units)
         return;
@@ -142,8 +145,8 @@ __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
     uint8_t *out = (uint8_t *)(kv ? r.c.v : r.c.k) + (int64_t)p.page * page_s +
                    (int64_t)p.slot * row_s + (int64_t)h * (kv ? r.c.v_head : r.c.k_head);
     const uint16_t *in = x.in + (int64_t)b * x.in_seq + (int64_t)h * x.in_head;
-    const uint32_t sub = lane >> g.lanes_log, c = 8 * (lane & ((1u << g.lanes_log) - 1));
-    const uint32_t step = 64u >> g.lanes_log;
+    const uint32_t sub = tid >> g.lanes_log, c = 8 * (tid & ((1u << g.lanes_log) - 1));
+    const uint32_t step = (64 * WAVES) >> g.lanes_log;
     const int left = (int)d - (int)c;
     int8_t *at = (int8_t *)r.c.ex +
                  2 * (((int64_t)p.page * r.c.blocks + r.c.by_block.quot(p.slot)) * r.c.heads + h) + kv;
@@ -169,22 +172,36 @@ __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
         }
     };
     i32x4 held[A8_HELD];
+    auto load = [&](uint32_t s0) {
 #pragma unroll
-    for (int i = 0; i < A8_HELD; ++i) {
-        const uint32_t s = from + i * step + sub;
-        held[i] = s < to && left > 0 ? get(s) : i32x4{0, 0, 0, 0};
+        for (int i = 0; i < A8_HELD; ++i) {
+            const uint32_t s = s0 + i * step + sub;
+            held[i] = s < to && left > 0 ? get(s) : i32x4{0, 0, 0, 0};
+        }
+    };
+    // (the first ones are loaded last, and stay)
+    const uint32_t round = A8_HELD * step, rounds = (to - from + round - 1) / round;
+    for (uint32_t y = rounds; y-- > 0;) {
+        load(from + y * round);
+#pragma unroll
+        for (int i = 0; i < A8_HELD; ++i)
+            look(held[i]);
     }
-#pragma unroll
-    for (int i = 0; i < A8_HELD; ++i)
-        look(held[i]);
-    for (uint32_t s = from + A8_HELD * step + sub; s < to; s += step)
-        if (left > 0)
-            look(get(s));
     uint32_t top = most.x > most.y ? most.x : most.y;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t y = (uint32_t)__shfl_xor((int)top, o);
         top = top > y ? top : y;
+    }
+    if constexpr (WAVES == 4) {
+        __shared__ uint32_t tops[4];
+        if ((threadIdx.x & 63) == 0)
+            tops[wave] = top;
+        __syncthreads();
+        top = tops[0];
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+            top = top > tops[w] ? top : tops[w];
     }
     int e = exponent_of<DT>(to_float(DT, top));
     if (from > 0) {
@@ -223,17 +240,26 @@ __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
         }
         __builtin_memcpy(out + (int64_t)s * row_s + c, w, 8);
     };
+    for (uint32_t y = 0; y < rounds; ++y) {
+        if (y)
+            load(from + y * round);
 #pragma unroll
-    for (int i = 0; i < A8_HELD; ++i) {
-        const uint32_t s = from + i * step + sub;
-        if (s < to && left > 0)
-            put(s, held[i]);
+        for (int i = 0; i < A8_HELD; ++i) {
+            const uint32_t s = from + y * round + i * step + sub;
+            if (s < to && left > 0)
+                put(s, held[i]);
+        }
     }
-    for (uint32_t s = from + A8_HELD * step + sub; s < to; s += step)
-        if (left > 0)
-            put(s, get(s));
-    if (lane == 0)
+    if (tid == 0)
         *at = (int8_t)e;
+}
+
+template <int DT>
+void (*append8_kernel(bool turn, bool all))(const Append8Args)
+{
+    if (turn)
+        return all ? append8_blocks<DT, true, 4> : append8_blocks<DT, true, 1>;
+    return all ? append8_blocks<DT, false, 4> : append8_blocks<DT, false, 1>;
 }
 
 }  // namespace
@@ -245,7 +271,8 @@ hipError_t launch_append8(const Append8 &r, hipStream_t s)
     while ((8u << g.lanes_log) < r.c.d)
         ++g.lanes_log;
     g.units = 2 * r.c.heads;
-    g.groups = (g.units + 3) / 4;
+    const bool all = (r.c.by_block.page << g.lanes_log) > 64u * A8_HELD;
+    g.groups = all ? g.units : (g.units + 3) / 4;
     g.by_blocks = PageDiv::of(r.blocks);
     g.by_groups = PageDiv::of(g.groups);
     const uint64_t total = (uint64_t)r.c.batch * r.blocks * g.groups;
@@ -253,11 +280,10 @@ hipError_t launch_append8(const Append8 &r, hipStream_t s)
     for (; g.first < total && e == hipSuccess; g.first += A8_GRID) {
         const uint64_t left = total - g.first;
         const dim3 grid((uint32_t)(left < A8_GRID ? left : A8_GRID));
-        const bool turn = r.turn.pairs != 0;
         if (r.dtype == sjk::DT_F16)
-            (turn ? append8_blocks<sjk::DT_F16, true> : append8_blocks<sjk::DT_F16, false>)<<<grid, 256, 0, s>>>(g);
+            append8_kernel<sjk::DT_F16>(r.turn.pairs != 0, all)<<<grid, 256, 0, s>>>(g);
         else
-            (turn ? append8_blocks<sjk::DT_BF16, true> : append8_blocks<sjk::DT_BF16, false>)<<<grid, 256, 0, s>>>(g);
+            append8_kernel<sjk::DT_BF16>(r.turn.pairs != 0, all)<<<grid, 256, 0, s>>>(g);
         e = hipGetLastError();
     }
     return e;

@@ -166,7 +166,8 @@ __device__ __forceinline__ const typename Cells<CE>::one *cells(const uint16_t *
     return (const typename Cells<CE>::one *)p;
 }
 
-// Eight elements as they lie in the cache (d is a multiple of 8 where CE is 1).
+// Eight elements as they lie in the cache.  Where CE is 1, d is a multiple of 8, and FIT_ANY stands for
+// d = 8.
 template <int FIT, int CE>
 __device__ __forceinline__ typename Cells<CE>::eight load_cells(const typename Cells<CE>::one *p,
                                                                 int left)
@@ -174,7 +175,6 @@ __device__ __forceinline__ typename Cells<CE>::eight load_cells(const typename C
     if constexpr (CE == 2) {
         return load_fit<FIT>(p, left);
     } else {
-        static_assert(FIT != FIT_ANY, "chunks of 8");
         i32x2 v = {0, 0};
         if (FIT == FIT_WHOLE || left > 0)
             __builtin_memcpy(&v, p, 8);
@@ -182,23 +182,30 @@ __device__ __forceinline__ typename Cells<CE>::eight load_cells(const typename C
     }
 }
 
-// Sixteen elements of a cache in 8 bits (d is a multiple of 8).
+// Sixteen elements of a cache in 8 bits.  A last half chunk is loaded with the eight elements before it
+// and put right where it is used (half_of), since loads of two sizes would be waited for where they
+// are made; d = 8 (FIT_ANY) has none before.
 template <int FIT>
 __device__ __forceinline__ i32x4 load_cells16(const uint8_t *p, int left)
 {
     i32x4 v = {0, 0, 0, 0};
-    if (FIT == FIT_WHOLE || left >= 16) {
-        __builtin_memcpy(&v, p, 16);
-    } else if (left > 0) {
-        i32x2 w;
-        __builtin_memcpy(&w, p, 8);
+    if (FIT == FIT_ANY) {
+        i32x2 w = {0, 0};
+        if (left > 0)
+            __builtin_memcpy(&w, p, 8);
         v = i32x4{w[0], w[1], 0, 0};
+    } else if (FIT == FIT_WHOLE || left > 0) {
+        __builtin_memcpy(&v, p - (FIT != FIT_WHOLE && left == 8 ? 8 : 0), 16);
     }
     return v;
 }
 
-__device__ __forceinline__ i32x2 half_of(const i32x4 &v, int x)
+// Half x of it.
+template <int FIT>
+__device__ __forceinline__ i32x2 half_of(const i32x4 &v, int x, int left)
 {
+    if (FIT == FIT_CHUNKS && left == 8)
+        return x ? i32x2{0, 0} : i32x2{v[2], v[3]};
     return x ? i32x2{v[2], v[3]} : i32x2{v[0], v[1]};
 }
 
@@ -838,7 +845,8 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             for (int c = 0; c < DC; ++c) {
                 i32x4 k8;
                 if constexpr (CE == 1)
-                    k8 = widen<DT>(half_of(K[t][c / 2], c % 2), two);
+                    k8 = widen<DT>(
+                        half_of<FIT>(K[t][c / 2], c % 2, (int)d - at_elem(c & ~1)), two);
                 else
                     k8 = K[t][c];
 #pragma unroll
@@ -860,7 +868,7 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             for (int x = 0; x < 2 / CE; ++x) {
                 i32x4 v8;
                 if constexpr (CE == 1)
-                    v8 = widen<DT>(half_of(V[i], x), two);
+                    v8 = widen<DT>(half_of<FIT>(V[i], x, (int)d - (int)v_col), two);
                 else
                     v8 = V[i];
                 if (tail || there != 0xffffffffu) {
@@ -2017,9 +2025,9 @@ hipError_t launch_attend_fit(const Attend &a, hipStream_t s)
 {
     if (a.c.d == 32 * DC)
         return launch_attend_dc<DT, DC, FIT_WHOLE, CE>(a, s);
-    if (CE == 1 || a.c.d % 8 == 0)
+    if (CE == 1 ? DC != 2 || a.c.d != 8 : a.c.d % 8 == 0)
         return launch_attend_dc<DT, DC, FIT_CHUNKS, CE>(a, s);
-    return launch_attend_dc<DT, DC, CE == 1 ? FIT_CHUNKS : FIT_ANY, CE>(a, s);
+    return launch_attend_dc<DT, DC, CE == 1 && DC != 2 ? FIT_CHUNKS : FIT_ANY, CE>(a, s);
 }
 
 template <int DT, int CE>

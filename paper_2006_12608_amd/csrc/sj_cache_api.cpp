@@ -278,7 +278,7 @@ int append_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     // (the blocks that t rows may touch, beginning anywhere in the first)
     const uint32_t block = cache8->block;
     const uint64_t blocks = ((uint64_t)t + block - 2) / block + 1;
-    if (B * blocks * ((2 * (uint64_t)r.c.heads + 3) / 4) >= kMaxCells)
+    if (B * blocks * 2 * r.c.heads >= kMaxCells)
         return fail(SJ_E_UNSUPPORTED, "%u x %u tokens of %u heads are too many", B, t, r.c.heads);
     sjc::Append8 w{};
     w.dtype = r.dtype;

@@ -71,6 +71,11 @@ class Case8(Case):
 
 
 EIGHTS = [s for s in SHAPES if s[4] % 8 == 0]
+# heads of 8, of a half chunk of 16, and of few query rows over many rows, whose shares are joined in steps
+EIGHTS += [(2, 3, 2, 2, 8, 16, [40, 5]), (1, 20, 2, 2, 8, 16, [300]), (2, 2, 4, 4, 24, 16, [700, 33]),
+           (1, 1, 4, 4, 56, 16, [9000]), (2, 1, 2, 4, 128, 64, [9000, 12000]), (1, 3, 4, 4, 72, 64, [20000]),
+           (1, 6, 2, 4, 64, 16, [14000]), (1, 1, 3, 4, 128, 64, [30000]), (1, 1, 2, 7, 232, 64, [9000]),
+           (1, 1, 16, 8, 64, 64, [6000])]
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])

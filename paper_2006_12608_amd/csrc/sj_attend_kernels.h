@@ -479,26 +479,22 @@ __device__ __forceinline__ f32x2 get2(const float *p)
     return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 
-__device__ __forceinline__ bool last_to_arrive(uint32_t *counter, uint32_t n)
-{
-    __shared__ uint32_t arrived;
-    wait_loads();       // (stores count as loads do)
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        arrived = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (arrived == n - 1)
-            __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    return arrived == n - 1;
-}
-
 template <int DT, uint32_t QT, uint32_t D>
 __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t h, uint32_t unit,
                                           uint32_t slot, uint32_t shares, uint32_t count)
 {
     typedef Elem<DT> E;
-    if (!last_to_arrive(a.arrivals + (uint64_t)b * a.c.heads * a.tiles + unit, shares))
+    __shared__ uint32_t arrived;
+    wait_loads();       // (stores count as loads do)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t *n = a.arrivals + (uint64_t)b * a.c.heads * a.tiles + unit;
+        arrived = __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (arrived == shares - 1)
+            __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (arrived != shares - 1)
         return;
     const uint64_t first = (uint64_t)slot * a.c.heads * a.tiles + unit;
     const uint64_t step = (uint64_t)a.c.heads * a.tiles;
@@ -546,120 +542,6 @@ __device__ __forceinline__ void join_last(const Attend &a, uint32_t b, uint32_t 
         if (x == 0)
             a.lse[row] = live ? (top + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
     }
-}
-
-// For more shares than a workgroup joins at once: n results, of the slots first_slot, first_slot + every,
-// ..., of query rows of `unit` are joined into that of the first one or, where `whole`, into the
-// output.  Where there are 8 or 4 query rows, the threads of the others take every second or
-// fourth result of theirs.
-constexpr uint32_t AT_JOIN = 32;
-
-template <int DT, uint32_t QT, uint32_t D>
-__device__ __forceinline__ void join_parts(const Attend &a, uint32_t b, uint32_t h, uint32_t unit,
-                                           uint32_t first_slot, uint32_t every, uint32_t n,
-                                           uint32_t count, bool whole)
-{
-    typedef Elem<DT> E;
-    const uint64_t units = (uint64_t)a.c.heads * a.tiles;
-    const uint64_t first = first_slot * units + unit, step = every * units;
-    for (uint32_t q0 = 0; q0 < QT; q0 += 16) {
-        const uint32_t r0 = unit % a.tiles * QT + q0, all = a.t * a.group;
-        const uint32_t here = r0 < all ? all - r0 : 0;
-        const uint32_t log = here > 8 ? 0 : (here > 4 ? 1 : 2), groups = 1u << log;
-        const uint32_t qi = threadIdx.x >> (4 + log), x = threadIdx.x & 15;
-        const uint32_t group = (threadIdx.x >> 4) & (groups - 1), lanes = 16 << log;
-        const uint32_t r = r0 + qi, u = a.by_group.quot(r);
-        auto at = [&](uint32_t s) { return (first + s * step) * QT + q0 + qi; };
-        if (r >= all)
-            continue;
-        float top = -INFINITY;
-        for (uint32_t s = threadIdx.x & (lanes - 1); s < n; s += lanes)
-            top = fmaxf(top, get2(a.part_ml + 2 * at(s))[0]);
-#pragma unroll
-        for (uint32_t o = 1; o < 64; o <<= 1)
-            if (o < lanes)
-                top = fmaxf(top, __shfl_xor(top, o));
-        const float base = top == -INFINITY ? 0.f : top;
-        f32x4 o[D / 64] = {};
-        float l = 0.f;
-#pragma unroll 8
-        for (uint32_t s = group; s < n; s += groups) {
-            const uint64_t p = at(s);
-            const f32x2 ml = get2(a.part_ml + 2 * p);
-            const float f = exp2_(ml[0] - base);
-            l += ml[1] * f;
-#pragma unroll
-            for (uint32_t k = 0; k < D / 64; ++k) {
-                const float *y = a.part_o + p * D + 64 * k + 4 * x;
-                const f32x2 lo = get2(y), hi = get2(y + 2);
-                o[k] += f32x4{lo[0], lo[1], hi[0], hi[1]} * f;
-            }
-        }
-#pragma unroll
-        for (uint32_t g = 1; g < 4; g <<= 1)
-            if (g < groups) {
-                l += __shfl_xor(l, 16 * g);
-#pragma unroll
-                for (uint32_t k = 0; k < D / 64; ++k)
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e)
-                        o[k][e] += __shfl_xor(o[k][e], 16 * g);
-            }
-        if (group)
-            continue;
-        if (!whole) {       // (the threads of a row are of one wave, which has read all it joins)
-            float *y = a.part_o + at(0) * D + 4 * x;
-#pragma unroll
-            for (uint32_t k = 0; k < D / 64; ++k) {
-                put2(y + 64 * k, o[k][0], o[k][1]);
-                put2(y + 64 * k + 2, o[k][2], o[k][3]);
-            }
-            if (x == 0)
-                put2(a.part_ml + 2 * at(0), top, l);
-            continue;
-        }
-        const bool live = u < count && l != 0.f;
-        const float inv = live ? 1.f / l : 0.f;
-        const uint64_t row = ((uint64_t)b * a.t + u) * a.q_heads + h * a.group + r - u * a.group;
-#pragma unroll
-        for (uint32_t k = 0; k < D / 64; ++k)
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-                const uint32_t c = 64 * k + 4 * x + e;
-                if (c < a.c.d)
-                    a.out[row * a.c.d + c] =
-                        __builtin_bit_cast(uint16_t, (typename E::one)(live ? o[k][e] * inv : 0.f));
-            }
-        if (x == 0)
-            a.lse[row] = live ? (top + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : -INFINITY;
-    }
-}
-
-// Joins the shares of HW heads in two steps, AT_JOIN neighbours at a time and then those
-// results, each by the last workgroup to arrive.  (Two sequences of 131072 rows, 96 to 128 shares of
-// 4 query rows each: 125 us in one step, 117 in two; heads of 64 90 and 77.)
-template <int DT, uint32_t QT, uint32_t D, int HW>
-__device__ __forceinline__ void join_steps(const Attend &a, uint32_t b, uint32_t h0, uint32_t tile,
-                                           uint32_t slot, const Share &sh)
-{
-    const uint32_t units = a.c.heads * a.tiles, unit = h0 * a.tiles + tile;
-    const uint32_t from = sh.share / AT_JOIN * AT_JOIN, groups = (sh.shares + AT_JOIN - 1) / AT_JOIN;
-    const uint32_t n = sh.shares - from < AT_JOIN ? sh.shares - from : AT_JOIN;
-    const uint32_t first = slot - sh.share;         // the sequence's first share
-    // counters: a sequence's, then a slot's
-    // (the call has B units and then slots units counters)
-    uint32_t *const steps = a.arrivals + (uint64_t)a.c.batch * units;
-    if (n > 1 && !last_to_arrive(steps + (uint64_t)(first + from) * units + unit, n))
-        return;
-    if (n > 1 || groups == 1)
-        for (uint32_t y = 0; y < HW; ++y)
-            join_parts<DT, QT, D>(a, b, h0 + y, unit + y * a.tiles, first + from, 1, n, sh.rows.count,
-                                  groups == 1);
-    if (groups == 1 || !last_to_arrive(a.arrivals + (uint64_t)b * units + unit, groups))
-        return;
-    for (uint32_t y = 0; y < HW; ++y)
-        join_parts<DT, QT, D>(a, b, h0 + y, unit + y * a.tiles, first, AT_JOIN, groups, sh.rows.count,
-                              true);
 }
 
 // ------------------------------------------------------------- the split kernel
@@ -1035,12 +917,9 @@ __global__ void __launch_bounds__(256) attend_split(const Attend a)
             }
         }
     }
-    if (shares > 1 && a.arrivals) {
-        if constexpr (CE == 1)
-            join_steps<DT, QT, D, HW>(a, b, h0, tile, slot, sh);
-        else
+    if constexpr (HW == 1)
+        if (shares > 1 && a.arrivals)
             join_last<DT, QT, D>(a, b, h, unit, slot - sh.share, shares, rows.count);
-    }
 }
 
 // ------------------------------------------------------------- the tiled kernel
@@ -1090,7 +969,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     __shared__ float stat[4][32][2];
     __shared__ uint32_t odd_any;
     __shared__ i64x2 where[8][BN];
-    __shared__ int64_t ex_at[CE == 1 ? 8 : 1][BN];  // places of the rows' exponents
+    __shared__ f32x2 scales[CE == 1 ? 8 : 1][BN];   // 2^exponent of the rows, of k and of v
     __shared__ uint64_t exist[8];
 
     const uint32_t lane = threadIdx.x & 63, tid = threadIdx.x;
@@ -1167,6 +1046,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     // Offsets of tile i's rows, for the threads that load them, and which rows exist; absent
     // rows read page 0, row 0.  Waves 0 .. 3 (and 4 .. 7, alike)
     // do one tile of four each.
+    uint32_t ex = 0;
     auto post = [&](uint32_t i, const Entry &e) {
         const Place p = place_of(a.c, b, e, to);
         const uint64_t there = __ballot(p.page >= 0);
@@ -1176,14 +1056,15 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                 o = i64x2{(int64_t)p.page * a.c.k_page + (int64_t)p.slot * a.c.k_row,
                           (int64_t)p.page * a.c.v_page + (int64_t)p.slot * a.c.v_row};
             where[i & 7][lane] = o;
-            if constexpr (CE == 1)
-                ex_at[i & 7][lane] =
-                    p.page < 0 ? 0
-                               : ((int64_t)p.page * a.c.blocks + a.c.by_block.quot(p.slot)) *
-                                         a.c.heads + h;
         }
+        ex = load_exponents<CE>(a.c, p, h);
         if (lane == 0)
             exist[i & 7] = there;
+    };
+    // (their exponents two tiles later, when they are there; a tile is stashed three after its post)
+    auto post_scales = [&](uint32_t i) {
+        if (CE == 1 && lane < BN)
+            scales[i & 7][lane] = f32x2{power_k(ex), power_v(ex)};
     };
     auto exists = [&](uint32_t i) -> uint64_t {
         const uint64_t x = exist[i & 7];
@@ -1191,18 +1072,12 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32;
     };
     typename Cells<CE>::eight kr[NL], vr[NL];
-    uint32_t xr[NL] = {};
     auto fetch = [&](uint32_t i) {
         const int left = (int)d - (int)(8 * chunk);
         i64x2 o[NL];
 #pragma unroll
         for (int x = 0; x < NL; ++x)
             o[x] = where[i & 7][RPL * x + row_at];
-        if constexpr (CE == 1) {
-#pragma unroll
-            for (int x = 0; x < NL; ++x)
-                xr[x] = a.c.ex[ex_at[i & 7][RPL * x + row_at]];
-        }
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
             kr[x] = load_cells<FIT, CE>(kb + o[x][0] + 8 * chunk, left);
@@ -1219,8 +1094,9 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
         i32x4 k8[NL], v8[NL];
 #pragma unroll
         for (int x = 0; x < NL; ++x) {
-            k8[x] = widen<DT>(kr[x], power_k(xr[x]));
-            v8[x] = widen<DT>(vr[x], power_v(xr[x]));
+            const f32x2 two = CE == 1 ? scales[i & 7][RPL * x + row_at] : f32x2{1.f, 1.f};
+            k8[x] = widen<DT>(kr[x], two[0]);
+            v8[x] = widen<DT>(vr[x], two[1]);
         }
         if (from + i * BN + BN > rows.len || there != ~(uint64_t)0) {
             uint32_t odd = 0;
@@ -1250,6 +1126,7 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     Entry ahead = {0, 0u};
     if (n_tiles > 0) {
         post(wave & 3, entry(wave & 3));
+        post_scales(wave & 3);
         ahead = entry(4 + (wave & 3));
         __syncthreads();
         there = exists(0);
@@ -1264,6 +1141,8 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
             post(i + 4 + (wave & 3), ahead);
             ahead = entry(i + 8 + (wave & 3));
         }
+        if (CE == 1 && (i & 3) == 2)
+            post_scales(i + 2 + (wave & 3));
         const uint64_t there1 = exists(i + 1);
         stash(i + 1, 1 - buf, there1);
         fetch(i + 2);       // (past the end: page 0, row 0; a branch would cost full waits)

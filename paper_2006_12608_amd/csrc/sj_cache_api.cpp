@@ -423,14 +423,15 @@ int attend_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     const uint32_t dp = d <= 64 ? 64 : (d <= 128 ? 128 : 256);
     a.tiles = rows == 0 ? 1 : (rows + qt - 1) / qt;
     // Two heads at once where rows are 8 bits and shares of one head each would more than fill the
-    // GPU (32 sequences of 200 to 8192 rows of 8 heads of 128: 76 us one at a time, 69 two, 73
+    // GPU (32 sequences of 200 to 8192 rows of 8 heads of 128: 77 us one at a time, 68 two, 73
     // four; heads of 64: 54, 41, 50; one sequence of 2048 rows of 2 heads, which cannot fill it: 12
-    // and 16).
-    a.heads_at_once = 1;
+    // and 16).  A kernel of its own joins these shares: where the last workgroup does, it reads
+    // twice the heads' results alone (2 x 131072 rows 125 and 113 us; 2 x 10865 to 19681 rows of 16
+    // heads of 72 with 18 query rows 74 and 38).
     const uint64_t least = sjc::AT_ROWS * sjc::AT_WAVES;
-    if (eight && qt <= 32 && a.c.heads % 2 == 0 &&
-        B * ((a.c.room + least - 1) / least) * a.c.heads * a.tiles > 8 * (uint64_t)c->num_cus)
-        a.heads_at_once = 2;
+    const bool fills = eight && qt <= 32 &&
+                       B * ((a.c.room + least - 1) / least) * a.c.heads * a.tiles > 8 * (uint64_t)c->num_cus;
+    a.heads_at_once = fills && a.c.heads % 2 == 0 ? 2 : 1;
     int per_cu;
     if (eight)
         per_cu = (f16 ? sjc::attend8_occupancy_f16 : sjc::attend8_occupancy_bf16)(d, qt, a.heads_at_once);
@@ -463,9 +464,9 @@ int attend_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     a.s_cols = (uint32_t)((cols + 31) / 32 * 32);
     const uint64_t s_bytes = (uint64_t)B * a.c.heads * rows * a.s_cols * 4;
     const bool keep = w_out && rows <= 16 && s_bytes > 0 && s_bytes <= kMaxScores;
-    const bool counted = qt <= 32 && !keep && !a.whole;
-    const size_t counters = counted ? (size_t)(B + (eight ? a.slots : 0)) * units : 0;
-    if ((st = grow_both(c, off_s + (keep ? (size_t)s_bytes : 0), counters)) != SJ_OK)
+    const bool counted = qt <= 32 && !keep && !a.whole && !fills;
+    if ((st = grow_both(c, off_s + (keep ? (size_t)s_bytes : 0), counted ? (size_t)B * units : 0)) !=
+        SJ_OK)
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     a.plan = (uint32_t *)s;

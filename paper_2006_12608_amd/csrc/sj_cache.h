@@ -271,15 +271,16 @@ struct Pages {
     uint32_t batch, width, pages, room, out_batch, tokens;
     PageDiv div;
     int32_t *out_table, *new_len, *copies, *lacking;
-    uint32_t *used;         // a bit a page, zeros between calls
-    int32_t *holder;        // a page: the first sequence that goes on with it partly filled
+    // zeros between calls:
+    uint32_t *arrived;      // workgroups
+    uint32_t *used;         // a bit a page
+    uint32_t *holder;       // a page: ~i for the first sequence i that goes on with it partly filled
     uint32_t *base;         // a sequence: pages given out before it
     int32_t *kept;          // a sequence: whether its last page stays with it
     int32_t *free;          // the pages to give out
     uint32_t *n_free;       // how many there are
 };
 
-// Scratch of a call in 4-byte values: holder, base, kept, free, n_free.
 hipError_t launch_pages(const Pages &p, hipStream_t s);
 
 struct Copy {

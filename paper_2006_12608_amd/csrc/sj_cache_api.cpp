@@ -604,13 +604,12 @@ extern "C" int sj_cache_pages(sj_ctx *c, const int32_t *table, int64_t table_row
     if ((out_table == table && width) || new_len == len)
         return fail(SJ_E_INVAL, "out_table must not be table, and new_len not len");
     SJ_HIP(hipSetDevice(c->device));
-    // scratch: [holders][base][kept][pages given out][their number]; no more pages are given out
-    // than there are, nor than the table's entries
-    const uint64_t given = n * width < pages ? n * width : pages;
-    const size_t off_base = align_up((size_t)pages * 4), off_kept = off_base + align_up((size_t)n * 4);
-    const size_t off_free = off_kept + align_up((size_t)n * 4);
+    // scratch: [base][kept][pages given out][their number]; no more pages are given out than there
+    // are, nor than the table's entries.  Counters: [workgroups][bits][holders]
+    const uint64_t given = n * width < pages ? n * width : pages, words = ((uint64_t)pages + 31) / 32;
+    const size_t off_kept = align_up((size_t)n * 4), off_free = off_kept + align_up((size_t)n * 4);
     const size_t off_n = off_free + align_up((size_t)given * 4);
-    if ((st = grow_both(c, off_n + 256, ((size_t)pages + 31) / 32 + 1)) != SJ_OK)
+    if ((st = grow_both(c, off_n + 256, (size_t)(1 + words + pages))) != SJ_OK)
         return st;
     uint8_t *s = (uint8_t *)c->scratch;
     sjc::Pages p{};
@@ -629,9 +628,10 @@ extern "C" int sj_cache_pages(sj_ctx *c, const int32_t *table, int64_t table_row
     p.new_len = new_len;
     p.copies = copies;
     p.lacking = lacking;
-    p.used = c->arrivals;
-    p.holder = (int32_t *)s;
-    p.base = (uint32_t *)(s + off_base);
+    p.arrived = c->arrivals;
+    p.used = c->arrivals + 1;
+    p.holder = c->arrivals + 1 + words;
+    p.base = (uint32_t *)s;
     p.kept = (int32_t *)(s + off_kept);
     p.free = (int32_t *)(s + off_free);
     p.n_free = (uint32_t *)(s + off_n);

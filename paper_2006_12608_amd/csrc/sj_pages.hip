@@ -8,6 +8,7 @@ namespace {
 
 constexpr uint32_t PG_THREADS = 1024, PG_WAVES = PG_THREADS / 64;
 constexpr uint32_t PG_ENTRIES = 4096;   // table entries of a workgroup
+constexpr uint32_t PG_WORDS = 8;        // words of marks that a thread looks through at once
 
 // What new sequence i goes on with: n rows, `whole` full pages, and in the table row `from`
 // the number of its last, partly filled one (-1: none, or one that does not exist).
@@ -35,28 +36,14 @@ __device__ __forceinline__ Heir heir_of(const Pages &p, uint32_t i)
     return h;
 }
 
-// Marks the pages that sequences share, one bit each, and makes the partly filled ones ready
-// for their first holder.  (A neighbour with the same parent has marked its pages already.)
-__global__ void __launch_bounds__(256) pages_mark(const Pages p, uint32_t groups)
-{
-    const uint32_t i = blockIdx.x / groups, w0 = blockIdx.x % groups * PG_ENTRIES;
-    const Heir h = heir_of(p, i);
-    if (w0 == 0 && threadIdx.x == 0 && h.last >= 0)
-        p.holder[h.last] = 0x7fffffff;
-    if (i > 0 && (p.parent ? p.parent[i] == p.parent[i - 1] : false))
-        return;
-    const uint32_t end = h.whole < w0 + PG_ENTRIES ? h.whole : w0 + PG_ENTRIES;
-    for (uint32_t w = w0 + threadIdx.x; w < end; w += 256) {
-        const uint32_t x = (uint32_t)h.from[w];
-        if (x < p.pages)
-            atomicOr(&p.used[x >> 5], 1u << (x & 31));
-    }
-}
-
 __device__ __forceinline__ uint32_t load_again(const uint32_t *p)
 {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+
+// Waits for the wave's atomics, which are done where all XCDs see them.  (A fence would write back a
+// whole cache, in every workgroup: 83 us instead of 15 for 256 sequences.)
+__device__ __forceinline__ void wait_marks() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // Sum of x over the threads before this one, and over all.
 __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t *waves, uint32_t *all)
@@ -75,19 +62,11 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t *waves, uint
     return before + incl - x;
 }
 
-// One workgroup: who keeps a partly filled page, how many pages each sequence is given and how
-// many before it, and the free pages in ascending order, as many as are needed.  Leaves the bits at
-// zero for the next call.
-__global__ void __launch_bounds__(PG_THREADS) pages_give(const Pages p)
+// Who keeps a partly filled page, how many pages each sequence is given and how many before it,
+// and the free pages in ascending order, as many as are needed.  Leaves the bits at zero for the
+// next call.
+__device__ __forceinline__ void give(const Pages &p, uint32_t *waves)
 {
-    __shared__ uint32_t waves[PG_WAVES];
-    for (uint32_t i = threadIdx.x; i < p.out_batch; i += PG_THREADS) {
-        const Heir h = heir_of(p, i);
-        if (h.last >= 0)
-            atomicMin(&p.holder[h.last], (int32_t)i);
-    }
-    __threadfence();
-    __syncthreads();
     uint32_t needed = 0;
     for (uint32_t i0 = 0; i0 < p.out_batch; i0 += PG_THREADS) {
         const uint32_t i = i0 + threadIdx.x;
@@ -99,7 +78,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_give(const Pages p)
                 const uint32_t x = (uint32_t)h.last;
                 // (only its holder sets the page's bit here, and reads it before)
                 keeps = !((load_again(&p.used[x >> 5]) >> (x & 31)) & 1) &&
-                        load_again((const uint32_t *)&p.holder[x]) == i;
+                        load_again(&p.holder[x]) == ~i;
                 if (keeps)
                     atomicOr(&p.used[x >> 5], 1u << (x & 31));
             }
@@ -113,30 +92,74 @@ __global__ void __launch_bounds__(PG_THREADS) pages_give(const Pages p)
             p.base[i] = needed + before;
         needed += all;
     }
-    __threadfence();
+    wait_marks();
     __syncthreads();
+    // a run of PG_WORDS words a thread
     const uint32_t words = (uint32_t)(((uint64_t)p.pages + 31) / 32);
     uint32_t found = 0;
-    for (uint32_t w0 = 0; w0 < words; w0 += PG_THREADS) {
-        const uint32_t w = w0 + threadIdx.x;
-        uint32_t bits = 0;
-        if (w < words) {
-            bits = ~load_again(&p.used[w]);
-            if (w == words - 1 && (p.pages & 31))
-                bits &= (1u << (p.pages & 31)) - 1;
-            p.used[w] = 0;
+    for (uint32_t w0 = 0; w0 < words; w0 += PG_THREADS * PG_WORDS) {
+        const uint32_t w = w0 + threadIdx.x * PG_WORDS;
+        uint32_t bits[PG_WORDS], n = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < PG_WORDS; ++k)
+            bits[k] = w + k < words ? ~load_again(&p.used[w + k]) : 0;
+#pragma unroll
+        for (uint32_t k = 0; k < PG_WORDS; ++k) {
+            if (w + k == words - 1 && (p.pages & 31))
+                bits[k] &= (1u << (p.pages & 31)) - 1;
+            if (w + k < words)
+                p.used[w + k] = 0;
+            n += (uint32_t)__popc(bits[k]);
         }
         uint32_t all;
-        uint32_t at = found + sum_before((uint32_t)__popc(bits), waves, &all);
-        for (; bits && at < needed; ++at, bits &= bits - 1)
-            p.free[at] = (int32_t)(32 * w + (uint32_t)__ffs(bits) - 1);
+        uint32_t at = found + sum_before(n, waves, &all);
+#pragma unroll
+        for (uint32_t k = 0; k < PG_WORDS; ++k)
+            for (; bits[k] && at < needed; ++at, bits[k] &= bits[k] - 1)
+                p.free[at] = (int32_t)(32 * (w + k) + (uint32_t)__ffs(bits[k]) - 1);
         found += all;
     }
     if (threadIdx.x == 0)
         *p.n_free = found;
 }
 
-// The new table, the copies and the numbers of each sequence.
+// Marks the pages that sequences share, one bit each, and for the partly filled ones the first
+// sequence that holds them (~i at most; 0: none).  A neighbour with the same parent has marked its pages
+// already.  The last workgroup to arrive gives the pages out.  Bound by latency, of the chain
+// parent, length, table, marks and of one workgroup's scans: 32 sequences and 20000 pages 21 us
+// in three launches, 15 in two; 256 sequences forked from 16 and 200000 pages 38 and 34, half of it the marks of 31000 pages.
+__global__ void __launch_bounds__(PG_THREADS) pages_give(const Pages p, uint32_t groups)
+{
+    __shared__ uint32_t waves[PG_WAVES], arrived;
+    const uint32_t i = blockIdx.x / groups, w0 = blockIdx.x % groups * PG_ENTRIES;
+    const Heir h = heir_of(p, i);
+    if (w0 == 0 && threadIdx.x == 0 && h.last >= 0)
+        atomicMax(&p.holder[h.last], ~i);
+    if (i == 0 || !p.parent || p.parent[i] != p.parent[i - 1]) {
+        uint32_t x[PG_ENTRIES / PG_THREADS];
+#pragma unroll
+        for (uint32_t k = 0; k < PG_ENTRIES / PG_THREADS; ++k) {
+            const uint32_t w = w0 + k * PG_THREADS + threadIdx.x;
+            x[k] = w < h.whole ? (uint32_t)h.from[w] : ~0u;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < PG_ENTRIES / PG_THREADS; ++k)
+            if (x[k] < p.pages)
+                atomicOr(&p.used[x[k] >> 5], 1u << (x[k] & 31));
+    }
+    wait_marks();       // (before the workgroup is counted)
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        arrived = __hip_atomic_fetch_add(p.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (arrived == gridDim.x - 1)
+            __hip_atomic_store(p.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (arrived == gridDim.x - 1)
+        give(p, waves);
+}
+
+// The new table, the copies and the numbers of each sequence; the holders are 0 again.
 __global__ void __launch_bounds__(256) pages_table(const Pages p, uint32_t groups)
 {
     const uint32_t i = blockIdx.x / groups, w0 = blockIdx.x % groups * PG_ENTRIES;
@@ -161,6 +184,8 @@ __global__ void __launch_bounds__(256) pages_table(const Pages p, uint32_t group
         const uint32_t need = (copy ? 1 : 0) + (h.ends > begins ? h.ends - begins : 0);
         const uint32_t left = base < n_free ? n_free - base : 0;
         const bool made = copy && left > 0;
+        if (h.last >= 0)
+            p.holder[h.last] = 0;
         p.new_len[i] = (int32_t)h.n;
         p.lacking[i] = (int32_t)(need - (need < left ? need : left));
         p.copies[3 * (uint64_t)i] = made ? h.last : -1;
@@ -272,12 +297,9 @@ __global__ void __launch_bounds__(256) copy_pages(const CopyArgs g)
 hipError_t launch_pages(const Pages &p, hipStream_t s)
 {
     const uint32_t groups = p.width ? (p.width + PG_ENTRIES - 1) / PG_ENTRIES : 1;
-    pages_mark<<<dim3(p.out_batch * groups), 256, 0, s>>>(p, groups);
-    hipError_t e = hipGetLastError();
+    pages_give<<<dim3(p.out_batch * groups), PG_THREADS, 0, s>>>(p, groups);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
-        return e;
-    pages_give<<<1, PG_THREADS, 0, s>>>(p);
-    if ((e = hipGetLastError()) != hipSuccess)
         return e;
     pages_table<<<dim3(p.out_batch * groups), 256, 0, s>>>(p, groups);
     return hipGetLastError();

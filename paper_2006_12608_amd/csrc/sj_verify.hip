@@ -56,11 +56,11 @@ __device__ __forceinline__ float number(float u)
 }
 
 template <int DT>
-__device__ __forceinline__ Node node_of(const Verify &v, uint32_t b, uint32_t n, uint32_t T)
+__device__ __forceinline__ Node node_of(const Verify &v, uint32_t b, uint32_t n)
 {
     typedef typename Prob<DT>::one one;
     Node k = {0.f, 0.f, 0.f, -1, -1};
-    if (n == 0 || n >= T)
+    if (n == 0 || n >= v.t)     // (nodes past the sequence's own are looked up beside its count)
         return k;
     const int32_t from = v.parent ? v.parent[(int64_t)b * v.parent_seq + n] : (int32_t)n - 1;
     k.token = v.tokens[(uint64_t)b * v.t + n];
@@ -99,11 +99,11 @@ __device__ __forceinline__ Walk walk(const Verify &v, uint32_t b, int32_t *path,
     Walk w = {0, T, T ? 1u : 0u, false, 0};
     if (lane == 0)
         path[0] = 0;
-    Node next = node_of<DT>(v, b, lane, T);
+    Node next = node_of<DT>(v, b, lane);
     if (!v.parent) {
         for (uint32_t n0 = 0; n0 < T; n0 += 64) {
             const Node k = next;
-            next = node_of<DT>(v, b, n0 + 64 + lane, T);
+            next = node_of<DT>(v, b, n0 + 64 + lane);
             const bool yes = v.draft ? (double)k.u * (double)k.q < (double)k.p : k.u < k.p;
             const uint64_t no = __ballot(n0 + lane > 0 && n0 + lane < T && !yes);
             const uint32_t first = no ? n0 + (uint32_t)__ffsll((unsigned long long)no) - 1 : T;
@@ -126,8 +126,9 @@ __device__ __forceinline__ Walk walk(const Verify &v, uint32_t b, int32_t *path,
     double left = 1.0;
     for (uint32_t n0 = 0; n0 < T; n0 += 64) {
         const Node k = next;
-        next = node_of<DT>(v, b, n0 + 64 + lane, T);
-        uint64_t tries = __ballot(k.parent == (int32_t)w.node), refused = 0;
+        next = node_of<DT>(v, b, n0 + 64 + lane);
+        const int32_t parent = n0 + lane < T ? k.parent : -1;
+        uint64_t tries = __ballot(parent == (int32_t)w.node), refused = 0;
         while (tries) {
             const uint32_t c = (uint32_t)__ffsll((unsigned long long)tries) - 1;
             tries &= tries - 1;
@@ -145,7 +146,7 @@ __device__ __forceinline__ Walk walk(const Verify &v, uint32_t b, int32_t *path,
                 if (lane == 0)
                     path[w.found] = (int32_t)(n0 + c);
                 ++w.found;
-                tries = __ballot(k.parent == (int32_t)w.node);
+                tries = __ballot(parent == (int32_t)w.node);
             } else {
                 left -= p;
                 refused |= (uint64_t)1 << c;
@@ -369,7 +370,10 @@ __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
     const double threshold = (double)u * total;
     uint32_t who = first_thread(mine > 0.0 && begin + mine > threshold, found);
     who = who < 256 ? who : last_thread(mine > 0.0, found);
-    if (tid == who) {
+    if (tid == who && run == 1) {
+        at_chunk = c0;
+        before = begin;
+    } else if (tid == who) {
         uint32_t last = c0;
         double sum = begin, at = begin;
         for (uint32_t c = c0; c < c1; ++c) {

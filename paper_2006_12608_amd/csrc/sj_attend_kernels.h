@@ -963,6 +963,10 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
     constexpr uint32_t CPR = 4 * DC;                // 16-byte chunks of a row
     constexpr int NL = BN * CPR / NT;              // loads per thread of K, of V
     constexpr uint32_t RPL = NT / CPR;             // rows per load of the workgroup
+    // 8 bits: 16 elements a load, two chunks, where there are loads enough
+    constexpr bool WIDE = CE == 1 && NL % 2 == 0;
+    constexpr int NW = WIDE ? NL / 2 : 1;
+    constexpr uint32_t RPW = WIDE ? 2 * RPL : RPL;
     constexpr uint32_t TILE = BN * D * 2;           // bytes
     static_assert(WR % 32 == 0, "whole products");
     __shared__ __align__(16) uint8_t lds[4 * TILE]; // K, V of two tiles
@@ -1072,7 +1076,19 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32;
     };
     typename Cells<CE>::eight kr[NL], vr[NL];
+    i32x4 kw[NW], vw[NW];
+    const uint32_t row_w = tid / (CPR / 2), chunk_w = tid % (CPR / 2);
+    const int left_w = (int)d - (int)(16 * chunk_w);
     auto fetch = [&](uint32_t i) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int x = 0; x < NW; ++x) {
+                const i64x2 o = where[i & 7][RPW * x + row_w];
+                kw[x] = load_cells16<FIT>((const uint8_t *)kb + o[0] + 16 * chunk_w, left_w);
+                vw[x] = load_cells16<FIT>((const uint8_t *)vb + o[1] + 16 * chunk_w, left_w);
+            }
+            return;
+        }
         const int left = (int)d - (int)(8 * chunk);
         i64x2 o[NL];
 #pragma unroll
@@ -1089,8 +1105,38 @@ __global__ void __launch_bounds__(QW == 8 ? 512 : 256, DC == 8 ? 1 : 2) attend_t
 #pragma unroll
     for (uint32_t x = 0; x < 2; ++x)
         to_at[x] = (RPL * x + row_at) * (2 * D) + 16 * swz<DC>(RPL * x + row_at, chunk);
+    uint32_t to_w[2];       // (of the two chunks; RPW is a multiple of 16)
+#pragma unroll
+    for (uint32_t y = 0; y < 2; ++y)
+        to_w[y] = row_w * (2 * D) + 16 * swz<DC>(row_w, 2 * chunk_w + y);
     auto stash = [&](uint32_t i, uint32_t buf, uint64_t there) {
         uint8_t *kt = lds + buf * 2 * TILE, *vt = kt + TILE;
+        if constexpr (WIDE) {
+            static_assert(!WIDE || RPW % 16 == 0, "places repeat");
+            const bool look = from + i * BN + BN > rows.len || there != ~(uint64_t)0;
+            uint32_t odd = 0;
+#pragma unroll
+            for (int x = 0; x < NW; ++x) {
+                const uint32_t r = RPW * x + row_w;
+                const f32x2 two = scales[i & 7][r];
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const i32x4 k8 = widen<DT>(half_of<FIT>(kw[x], y, left_w), two[0]);
+                    i32x4 v8 = widen<DT>(half_of<FIT>(vw[x], y, left_w), two[1]);
+                    if (look) {
+                        if (!((there >> r) & 1))
+                            v8 = i32x4{0, 0, 0, 0};     // (0 x NaN would reach every query)
+                        odd |= drop_odd8<DT>(v8, from + i * BN + r >= rows.len);
+                        asm volatile("");       // (a branch, not selects in every round)
+                    }
+                    *(i32x4 *)(kt + to_w[y] + x * RPW * (2 * D)) = k8;
+                    *(i32x4 *)(vt + to_w[y] + x * RPW * (2 * D)) = v8;
+                }
+            }
+            if (odd)
+                odd_any = 1;
+            return;
+        }
         i32x4 k8[NL], v8[NL];
 #pragma unroll
         for (int x = 0; x < NL; ++x) {

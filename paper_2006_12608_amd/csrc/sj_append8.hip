@@ -13,7 +13,8 @@ constexpr int A8_HELD = 8;              // 16-byte chunks of a block that a lane
 struct Append8Args {
     Append8 r;
     uint64_t first;             // of the launch's workgroups
-    uint32_t lanes_log;         // lanes of a row: d / 8 rounded up to a power of two
+    PageDiv by_lanes;           // lanes of a row: d / 8
+    uint32_t step1, step4;      // rows that a wave, and four, have lanes for
     uint32_t units, groups;     // heads x {k, v}; workgroups for them
     PageDiv by_blocks, by_groups;
 };
@@ -145,9 +146,10 @@ __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
     uint8_t *out = (uint8_t *)(kv ? r.c.v : r.c.k) + (int64_t)p.page * page_s +
                    (int64_t)p.slot * row_s + (int64_t)h * (kv ? r.c.v_head : r.c.k_head);
     const uint16_t *in = x.in + (int64_t)b * x.in_seq + (int64_t)h * x.in_head;
-    const uint32_t sub = tid >> g.lanes_log, c = 8 * (tid & ((1u << g.lanes_log) - 1));
-    const uint32_t step = (64 * WAVES) >> g.lanes_log;
-    const int left = (int)d - (int)c;
+    // (as many rows side by side as fit in the threads; those left over do nothing)
+    const uint32_t sub = g.by_lanes.quot(tid), c = 8 * (tid - sub * g.by_lanes.page);
+    const uint32_t step = WAVES == 1 ? g.step1 : g.step4;
+    const int left = sub < step ? (int)d - (int)c : 0;
     int8_t *at = (int8_t *)r.c.ex +
                  2 * (((int64_t)p.page * r.c.blocks + r.c.by_block.quot(p.slot)) * r.c.heads + h) + kv;
     const int was = *at;
@@ -171,21 +173,27 @@ __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
             most = __builtin_elementwise_max(most, m);
         }
     };
+    // (the first A8_HELD chunks of a lane stay, others are loaded again)
     i32x4 held[A8_HELD];
-    auto load = [&](uint32_t s0) {
+    const uint32_t round = A8_HELD * step;
+    auto load = [&](i32x4 *v, uint32_t s0) {
 #pragma unroll
         for (int i = 0; i < A8_HELD; ++i) {
             const uint32_t s = s0 + i * step + sub;
-            held[i] = s < to && left > 0 ? get(s) : i32x4{0, 0, 0, 0};
+            v[i] = s < to && left > 0 ? get(s) : i32x4{0, 0, 0, 0};
         }
     };
-    // (the first ones are loaded last, and stay)
-    const uint32_t round = A8_HELD * step, rounds = (to - from + round - 1) / round;
-    for (uint32_t y = rounds; y-- > 0;) {
-        load(from + y * round);
+    auto look_all = [&](const i32x4 *v) {
 #pragma unroll
         for (int i = 0; i < A8_HELD; ++i)
-            look(held[i]);
+            look(v[i]);
+    };
+    load(held, from);
+    look_all(held);
+    for (uint32_t s0 = from + round; s0 < to; s0 += round) {
+        i32x4 more[A8_HELD];
+        load(more, s0);
+        look_all(more);
     }
     uint32_t top = most.x > most.y ? most.x : most.y;
 #pragma unroll
@@ -240,15 +248,19 @@ __global__ void __launch_bounds__(256) append8_blocks(const Append8Args g)
         }
         __builtin_memcpy(out + (int64_t)s * row_s + c, w, 8);
     };
-    for (uint32_t y = 0; y < rounds; ++y) {
-        if (y)
-            load(from + y * round);
+    auto put_all = [&](const i32x4 *v, uint32_t s0) {
 #pragma unroll
         for (int i = 0; i < A8_HELD; ++i) {
-            const uint32_t s = from + y * round + i * step + sub;
+            const uint32_t s = s0 + i * step + sub;
             if (s < to && left > 0)
-                put(s, held[i]);
+                put(s, v[i]);
         }
+    };
+    put_all(held, from);
+    for (uint32_t s0 = from + round; s0 < to; s0 += round) {
+        i32x4 more[A8_HELD];
+        load(more, s0);
+        put_all(more, s0);
     }
     if (tid == 0)
         *at = (int8_t)e;
@@ -268,10 +280,12 @@ hipError_t launch_append8(const Append8 &r, hipStream_t s)
 {
     Append8Args g{};
     g.r = r;
-    while ((8u << g.lanes_log) < r.c.d)
-        ++g.lanes_log;
+    const uint32_t lanes = r.c.d / 8;
+    g.by_lanes = PageDiv::of(lanes);
+    g.step1 = 64 / lanes;
+    g.step4 = 256 / lanes;
     g.units = 2 * r.c.heads;
-    const bool all = (r.c.by_block.page << g.lanes_log) > 64u * A8_HELD;
+    const bool all = r.c.by_block.page > g.step1 * A8_HELD;
     g.groups = all ? g.units : (g.units + 3) / 4;
     g.by_blocks = PageDiv::of(r.blocks);
     g.by_groups = PageDiv::of(g.groups);

@@ -888,7 +888,7 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     given, is turned by the same positions and returned (in q_out, which may be
     q).  Into a kv_cache8 the turned keys and the values are rounded to 8 bits (sj_cache8_append); the
     blocks of rows appended to must be of one sequence each.  There is no gradient: a backward pass through the result raises.  May be
-    captured into a HIP graph, as rotary may."""
+    captured into a HIP graph, as rotary may (into a kv_cache8: see attend)."""
     import torch
     if cache.follows or key.requires_grad or value.requires_grad or _follows(q, q_out):
         if torch.is_grad_enabled():

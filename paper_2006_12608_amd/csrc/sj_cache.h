@@ -252,9 +252,11 @@ hipError_t launch_evict(const Evict &e, hipStream_t s);
 
 // ------------------------------------------------------------- appending in 8 bits
 
+constexpr uint32_t A8_SINES = 2048;     // rows x pairs of a block that a workgroup turns
+
 struct Append8 {
     int dtype;
-    Turn turn;              // of keys
+    Turn turn;              // of keys (no pairs where a block has more than A8_SINES)
     Cache c;
     uint32_t t, blocks;     // tokens; blocks of a sequence that they may touch
     const int32_t *len, *count;

@@ -276,7 +276,7 @@ int append_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
         return SJ_OK;
     }
     // (the blocks that t rows may touch, beginning anywhere in the first)
-    const uint32_t block = cache8->block;
+    const uint32_t block = cache8->block, heads = r.c.heads;
     const uint64_t blocks = ((uint64_t)t + block - 2) / block + 1;
     if (B * blocks * 2 * r.c.heads >= kMaxCells)
         return fail(SJ_E_UNSUPPORTED, "%u x %u tokens of %u heads are too many", B, t, r.c.heads);
@@ -290,9 +290,20 @@ int append_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     w.count = count;
     w.key = r.key;
     w.value = r.value;
-    if (q) {
-        r.c.batch = 0;      // (the queries alone)
+    r.c.batch = 0;
+    if (q)                  // (the queries alone)
         SJ_HIP(sjc::launch_rotary(r, c->stream));
+    if ((uint64_t)block * n_pairs > sjc::A8_SINES || (layout == SJ_HALF && n_pairs % 8 != 0)) {
+        // long blocks, halves that begin inside a chunk: the keys are turned on the way into scratch
+        const uint64_t cells = (uint64_t)B * t * heads * d;
+        if ((st = grow_both(c, (size_t)cells * 2, 0)) != SJ_OK)
+            return st;
+        const int64_t row = (int64_t)heads * d;
+        r.x = {(const uint16_t *)key, (uint16_t *)c->scratch, key_stride[0], key_stride[1],
+               key_stride[2], row * t, row, d, heads};
+        SJ_HIP(sjc::launch_rotary(r, c->stream));
+        w.key = {(const uint16_t *)c->scratch, nullptr, row * t, row, d, 0, 0, 0, heads};
+        w.turn.pairs = 0;
     }
     if (r.c.room)
         SJ_HIP(sjc::launch_append8(w, c->stream));
@@ -321,6 +332,7 @@ extern "C" int sj_cache8_append(sj_ctx *c, const sj_cache8 *cache, const int32_t
                                const void *q, const int64_t q_stride[3], uint32_t q_heads,
                                void *q_out, const int64_t q_out_stride[3])
 {
+    const Alone alone(c);
     return append_rows(c, nullptr, cache, true, len, count, t, key, key_stride, value, value_stride, pos,
                        turns, n_pairs, layout, factor, q, q_stride, q_heads, q_out, q_out_stride);
 }

@@ -264,13 +264,15 @@ def test_append8_strides(order):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
-@pytest.mark.parametrize("d,rot,T", [(64, 64, 1), (128, 64, 20), (72, 40, 7), (80, 38, 33), (256, 252, 3)])
-def test_append8_turned(dtype, layout, d, rot, T):
+@pytest.mark.parametrize("d,rot,T,page,block", [(64, 64, 1, 16, 8), (128, 64, 20, 16, 8), (72, 40, 7, 16, 8),
+                                                (80, 38, 33, 16, 8), (256, 252, 3, 16, 8), (128, 128, 70, 64, 16),
+                                                (128, 112, 90, 128, 64), (96, 96, 50, 100, 50), (64, 64, 300, 64, 64)])
+def test_append8_turned(dtype, layout, d, rot, T, page, block):
     """Turned keys are the ones that a cache in 16 bits gets, rounded to 8; so are the queries."""
     import torch
     import paper_2006_12608_amd as sj
     say("append8 turned", dtype, layout, d, rot, T)
-    c = Case8(12, dtype, 3, T, 2, 2, d, 16, [0, 9, 16], 8)
+    c = Case8(12, dtype, 3, T, 2, 2, d, page, [0, 9, 16], block)
     turns = sj.rotary_turns(rot)
     key = dev(c.rng.standard_normal((3, T, 2, d)), dtype)
     pos = torch.randint(-5, 100000, (3, T), dtype=torch.int32, device="cuda")

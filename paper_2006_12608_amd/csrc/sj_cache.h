@@ -280,7 +280,7 @@ struct Pages {
     uint32_t *base;         // a sequence: pages given out before it
     int32_t *kept;          // a sequence: whether its last page stays with it
     int32_t *free;          // the pages to give out
-    uint32_t *n_free;       // how many there are
+    uint32_t *n_free;       // how many were found (enough, or all)
 };
 
 hipError_t launch_pages(const Pages &p, hipStream_t s);

@@ -8,7 +8,7 @@ namespace {
 
 constexpr uint32_t PG_THREADS = 1024, PG_WAVES = PG_THREADS / 64;
 constexpr uint32_t PG_ENTRIES = 4096;   // table entries of a workgroup
-constexpr uint32_t PG_WORDS = 8;        // words of marks that a thread looks through at once
+constexpr uint32_t PG_SEQS = 16;        // sequences of a workgroup at most
 
 // What new sequence i goes on with: n rows, `whole` full pages, and in the table row `from`
 // the number of its last, partly filled one (-1: none, or one that does not exist).
@@ -94,58 +94,57 @@ __device__ __forceinline__ void give(const Pages &p, uint32_t *waves)
     }
     wait_marks();
     __syncthreads();
-    // a run of PG_WORDS words a thread
+    // 32 marks a thread, until there are enough (longer runs a thread are written down one by one: 9 us
+    // more for 1300 pages in runs of 256)
     const uint32_t words = (uint32_t)(((uint64_t)p.pages + 31) / 32);
     uint32_t found = 0;
-    for (uint32_t w0 = 0; w0 < words; w0 += PG_THREADS * PG_WORDS) {
-        const uint32_t w = w0 + threadIdx.x * PG_WORDS;
-        uint32_t bits[PG_WORDS], n = 0;
-#pragma unroll
-        for (uint32_t k = 0; k < PG_WORDS; ++k)
-            bits[k] = w + k < words ? ~load_again(&p.used[w + k]) : 0;
-#pragma unroll
-        for (uint32_t k = 0; k < PG_WORDS; ++k) {
-            if (w + k == words - 1 && (p.pages & 31))
-                bits[k] &= (1u << (p.pages & 31)) - 1;
-            if (w + k < words)
-                p.used[w + k] = 0;
-            n += (uint32_t)__popc(bits[k]);
-        }
+    for (uint32_t w0 = 0; w0 < words && found < needed; w0 += PG_THREADS) {
+        const uint32_t w = w0 + threadIdx.x;
+        uint32_t bits = w < words ? ~load_again(p.used + w) : 0;
+        if (w == words - 1 && p.pages % 32)
+            bits &= (1u << p.pages % 32) - 1;
         uint32_t all;
-        uint32_t at = found + sum_before(n, waves, &all);
-#pragma unroll
-        for (uint32_t k = 0; k < PG_WORDS; ++k)
-            for (; bits[k] && at < needed; ++at, bits[k] &= bits[k] - 1)
-                p.free[at] = (int32_t)(32 * (w + k) + (uint32_t)__ffs(bits[k]) - 1);
+        uint32_t at = found + sum_before((uint32_t)__popc(bits), waves, &all);
+        for (; bits && at < needed; ++at, bits &= bits - 1)
+            p.free[at] = (int32_t)(32 * w + (uint32_t)__ffs(bits) - 1);
         found += all;
     }
+    __syncthreads();
+    for (uint32_t w = threadIdx.x; w < words; w += PG_THREADS)
+        p.used[w] = 0;
     if (threadIdx.x == 0)
         *p.n_free = found;
 }
 
 // Marks the pages that sequences share, one bit each, and for the partly filled ones the first
 // sequence that holds them (~i at most; 0: none).  A neighbour with the same parent has marked its pages
-// already.  The last workgroup to arrive gives the pages out.  Bound by latency, of the chain
-// parent, length, table, marks and of one workgroup's scans: 32 sequences and 20000 pages 21 us
-// in three launches, 15 in two; 256 sequences forked from 16 and 200000 pages 38 and 34, half of it the marks of 31000 pages.
-__global__ void __launch_bounds__(PG_THREADS) pages_give(const Pages p, uint32_t groups)
+// already.  The last workgroup to arrive gives the pages out.  A workgroup takes `seqs` sequences, so that
+// few are counted.  Bound by latency, of the chain parent, length, table, marks and of one
+// workgroup's scans: 32 sequences and 20000 pages 21 us in three launches, 15 in two; 256 sequences
+// forked from 16 and 200000 pages 38 and 20.
+__global__ void __launch_bounds__(PG_THREADS) pages_give(const Pages p, uint32_t groups, uint32_t seqs)
 {
     __shared__ uint32_t waves[PG_WAVES], arrived;
-    const uint32_t i = blockIdx.x / groups, w0 = blockIdx.x % groups * PG_ENTRIES;
-    const Heir h = heir_of(p, i);
-    if (w0 == 0 && threadIdx.x == 0 && h.last >= 0)
-        atomicMax(&p.holder[h.last], ~i);
-    if (i == 0 || !p.parent || p.parent[i] != p.parent[i - 1]) {
-        uint32_t x[PG_ENTRIES / PG_THREADS];
+    const uint32_t each = PG_THREADS / seqs, tid = threadIdx.x % each;
+    const uint32_t i = blockIdx.x / groups * seqs + threadIdx.x / each;
+    const uint32_t w0 = blockIdx.x % groups * PG_ENTRIES;
+    if (i < p.out_batch) {
+        const Heir h = heir_of(p, i);
+        if (w0 == 0 && tid == 0 && h.last >= 0)
+            atomicMax(&p.holder[h.last], ~i);
+        if (i == 0 || !p.parent || p.parent[i] != p.parent[i - 1]) {
+            const uint32_t end = h.whole < w0 + PG_ENTRIES ? h.whole : w0 + PG_ENTRIES;
+            for (uint32_t w = w0 + tid; w < end; w += 4 * each) {
+                uint32_t x[4];
 #pragma unroll
-        for (uint32_t k = 0; k < PG_ENTRIES / PG_THREADS; ++k) {
-            const uint32_t w = w0 + k * PG_THREADS + threadIdx.x;
-            x[k] = w < h.whole ? (uint32_t)h.from[w] : ~0u;
+                for (uint32_t k = 0; k < 4; ++k)
+                    x[k] = w + k * each < end ? (uint32_t)h.from[w + k * each] : ~0u;
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k)
+                    if (x[k] < p.pages)
+                        atomicOr(&p.used[x[k] >> 5], 1u << (x[k] & 31));
+            }
         }
-#pragma unroll
-        for (uint32_t k = 0; k < PG_ENTRIES / PG_THREADS; ++k)
-            if (x[k] < p.pages)
-                atomicOr(&p.used[x[k] >> 5], 1u << (x[k] & 31));
     }
     wait_marks();       // (before the workgroup is counted)
     __syncthreads();
@@ -297,7 +296,10 @@ __global__ void __launch_bounds__(256) copy_pages(const CopyArgs g)
 hipError_t launch_pages(const Pages &p, hipStream_t s)
 {
     const uint32_t groups = p.width ? (p.width + PG_ENTRIES - 1) / PG_ENTRIES : 1;
-    pages_give<<<dim3(p.out_batch * groups), PG_THREADS, 0, s>>>(p, groups);
+    uint32_t seqs = 1;      // (32 workgroups, or a sequence each)
+    while (seqs < PG_SEQS && p.out_batch > 32 * seqs)
+        seqs *= 2;
+    pages_give<<<dim3((p.out_batch + seqs - 1) / seqs * groups), PG_THREADS, 0, s>>>(p, groups, seqs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;

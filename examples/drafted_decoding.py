@@ -7,7 +7,12 @@ to its own ancestors, and keeps the path that the model itself would have taken:
 tokens a step, and the same text as one token at a time.  The softmax weight that each cache
 row draws is accumulated, and where a cache is full its heaviest rows move to other pages.
 
+With a temperature the text is sampled: the drafted tokens are verified against the model's
+probabilities.  With --bits 8 the caches hold 8 bits and take their pages from a pool instead of
+evicting, and --samples continues every prompt several times, over shared pages.
+
     python examples/drafted_decoding.py [--steps 32] [--batch 4] [--budget 512]
+    python examples/drafted_decoding.py --bits 8 --samples 4 --temperature 20
 """
 import argparse
 import os
@@ -47,6 +52,7 @@ class Tree:
             sees.append((sees[parent[n]] if n else 0) | 1 << n)
         sees = [s - 2 ** 64 if s >= 2 ** 63 else s for s in sees]
         self.mask = torch.tensor(sees, device=device).view(1, self.size, 1)
+        self.up = torch.tensor(parent, dtype=torch.int32, device=device)
         self.depth = torch.tensor(depth, dtype=torch.int32, device=device)
 
 
@@ -110,6 +116,33 @@ class Caches:
         self.lengths = lengths
 
 
+class Pool:
+    """Per layer a cache in 8 bits, all with one table, whose pages are given out from a pool as
+    the sequences grow, fork and end."""
+
+    def __init__(self, model, batch, room, pages):
+        width = -(-room // PAGE)
+        shape = (pages, PAGE, model.heads, model.d)
+        self.room, self.pages, self.weight = width * PAGE, pages, [None] * model.layers
+        self.table = torch.full((batch, width), -1, dtype=torch.int32, device="cuda")
+        self.lengths = torch.zeros(batch, dtype=torch.int32, device="cuda")
+
+        def cache():
+            k, v = (torch.zeros(shape, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+                    for _ in "kv")
+            exponents = torch.zeros(pages, 1, model.heads, 2, dtype=torch.int8, device="cuda")
+            return sj.kv_cache8(k, v, exponents, self.table, dtype=model.embed.dtype)
+        self.used = [cache() for _ in range(model.layers)]
+
+    def reserve(self, tokens, parent=None):
+        """Pages for so many more rows of every sequence, or of those that continue `parent`."""
+        self.table, self.lengths, copies, self.lacking = sj.cache_pages(
+            self.table, self.lengths, tokens, pages=self.pages, page=PAGE, parent=parent)
+        for cache in self.used:
+            sj.cache_copy(cache, copies)
+            cache.table = self.table
+
+
 def forward(model, caches, tokens, pos, counts=None, tree=None):
     """Logits of a block of tokens.  Without a tree the block becomes part of the text and adds
     to the rows' weights; with one, returns also its keys, values and weights per layer."""
@@ -123,7 +156,7 @@ def forward(model, caches, tokens, pos, counts=None, tree=None):
             o, _ = sj.attend(caches.used[i], caches.lengths, q, counts=counts,
                              weight=caches.weight[i])
         else:
-            w = torch.empty_like(caches.weight[i])
+            w = None if caches.weight[i] is None else torch.empty_like(caches.weight[i])
             o, _ = sj.attend(caches.used[i], caches.lengths, q, tree.mask, weight_out=w)
             drafted.append((k, v, w))
         x = x + o.flatten(2) @ model.out[i]
@@ -133,6 +166,8 @@ def forward(model, caches, tokens, pos, counts=None, tree=None):
 def read_prompts(model, caches, prompts, chunk=64):
     """The prompts' tokens but the last of each, in blocks."""
     sizes = [len(p) - 1 for p in prompts]
+    if isinstance(caches, Pool):
+        caches.reserve(max(sizes))
     for at in range(0, max(sizes), chunk):
         counts = [min(max(n - at, 0), chunk) for n in sizes]
         block = [(p[at:at + c] + [0] * chunk)[:chunk] for p, c in zip(prompts, counts)]
@@ -142,17 +177,10 @@ def read_prompts(model, caches, prompts, chunk=64):
         caches.lengths = caches.lengths + counts
 
 
-def step(model, caches, tree, last, pos):
-    """One draft and its verification: the tokens accepted, per sequence.  last and pos: the
-    text's last tokens, not yet in the cache, and their positions."""
-    drafts = [last]
-    for n in range(1, tree.size):
-        drafts.append(model.follow[drafts[tree.parent[n]], tree.rank[n]])
-    tokens = torch.stack(drafts, 1)
-    where = (pos[:, None] + tree.depth).int()
-    logits, drafted = forward(model, caches, tokens, where, tree=tree)
-    best = logits.argmax(-1)
-    paths, said = [], []
+def greedy(tree, tokens, logits):
+    """The path that the model's likeliest tokens take through the drafts, as nodes and then -1, its
+    length, and the token after it (verify_drafts without chance)."""
+    best, paths, after = logits.argmax(-1), [], []
     for tok, nxt in zip(tokens.tolist(), best.tolist()):
         path, n = [0], 0
         while n is not None:
@@ -160,12 +188,34 @@ def step(model, caches, tree, last, pos):
             n = next((c for c in tree.children[n] if tok[c] == text), None)
             if n is not None:
                 path.append(n)
-        paths.append(path)
-        said.append([tok[n] for n in path[1:]] + [text])
+        paths.append(path + [-1] * (tree.size - len(path)))
+        after.append(text)
+    path = torch.tensor(paths, dtype=torch.int32, device="cuda")
+    return path, (path >= 0).sum(1, dtype=torch.int32), torch.tensor(after, device="cuda")
+
+
+def step(model, caches, tree, last, pos, temperature=0.0):
+    """One draft and its verification: the tokens accepted, per sequence.  last and pos: the
+    text's last tokens, not yet in the cache, and their positions."""
+    if isinstance(caches, Pool):
+        caches.reserve(tree.size)
+    drafts = [last]
+    for n in range(1, tree.size):
+        drafts.append(model.follow[drafts[tree.parent[n]], tree.rank[n]])
+    tokens = torch.stack(drafts, 1)
+    where = (pos[:, None] + tree.depth).int()
+    logits, drafted = forward(model, caches, tokens, where, tree=tree)
+    if temperature > 0:
+        p = torch.softmax(logits.float() / temperature, -1)
+        path, counts, after = sj.verify_drafts(tokens, p, torch.rand(tokens.shape, device="cuda"),
+                                               parent=tree.up)
+    else:
+        path, counts, after = greedy(tree, tokens, logits)
+    said = [[tok[n] for n in way[1:k]] + [x] for tok, way, k, x in
+            zip(tokens.tolist(), path.tolist(), counts.tolist(), after.tolist())]
     # the accepted rows close up at the front of the drafted ones
-    longest = max(map(len, paths))
-    counts = torch.tensor([len(p) for p in paths], dtype=torch.int32, device="cuda")
-    path = torch.tensor([p + [0] * (longest - len(p)) for p in paths], device="cuda")
+    longest = max(map(len, said))
+    path = path[:, :longest].clamp(min=0).long()
     rows = path[:, :, None, None]
     own = caches.lengths[:, None].long()
     columns = torch.arange(caches.room, device="cuda")
@@ -175,6 +225,8 @@ def step(model, caches, tree, last, pos):
                         v.gather(1, rows.expand(shape)), pos=where.gather(1, path),
                         turns=model.turns, counts=counts)
         old = caches.weight[i]
+        if old is None:
+            continue
         accepted = w.gather(2, (own + path)[:, None].expand(-1, model.heads, -1))
         accepted *= torch.arange(longest, device="cuda") < counts[:, None, None]
         new = torch.where(columns < own[:, None], old + w, 0.)
@@ -184,25 +236,36 @@ def step(model, caches, tree, last, pos):
     return said
 
 
-def decode(model, prompts, steps, budget, fans=(3, 2, 1, 1), sink=4):
-    """Continues the prompts: (texts, evictions, seconds of the steps)."""
+def decode(model, prompts, steps, budget, fans=(3, 2, 1, 1), sink=4, temperature=0.0, bits=16,
+           samples=1):
+    """Continues the prompts, each `samples` times: (texts, evictions, seconds of the steps)."""
     tree = Tree(fans, "cuda")
     chunk = 64
-    room = max(budget, max(map(len, prompts)) + chunk) + tree.size
-    caches = Caches(model, len(prompts), room)
+    longest = max(map(len, prompts))
+    if bits == 8:
+        room = longest + chunk + steps * tree.size
+        pages = len(prompts) * samples * (-(-room // PAGE) + 1)
+        caches = Pool(model, len(prompts), room, pages)
+    else:
+        if samples != 1:
+            raise ValueError("samples share the pages of caches in 8 bits")
+        caches = Caches(model, len(prompts), max(budget, longest + chunk) + tree.size)
     read_prompts(model, caches, prompts, chunk)
-    texts = [list(p) for p in prompts]
-    evictions, upper = 0, max(map(len, prompts)) - 1
+    texts = [list(p) for p in prompts for _ in range(samples)]
+    if samples != 1:
+        parent = torch.arange(len(texts), dtype=torch.int32, device="cuda") // samples
+        caches.reserve(tree.size, parent)
+    evictions, upper = 0, longest - 1
     torch.cuda.synchronize()
     begin = time.perf_counter()
     for _ in range(steps):
-        if upper + tree.size > caches.room:
+        if bits == 16 and upper + tree.size > caches.room:
             caches.evict(budget // 2, sink, recent=budget // 8)
             evictions += 1
             upper = budget // 2
         last = torch.tensor([t[-1] for t in texts], device="cuda")
         pos = torch.tensor([len(t) - 1 for t in texts], device="cuda")
-        said = step(model, caches, tree, last, pos)
+        said = step(model, caches, tree, last, pos, temperature)
         for t, s in zip(texts, said):
             t += s
         upper += max(map(len, said))
@@ -215,18 +278,22 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=32)
     ap.add_argument("--batch", type=int, default=4)
     ap.add_argument("--prompt", type=int, default=300, help="tokens of the longest prompt")
-    ap.add_argument("--budget", type=int, default=512, help="cache rows of a sequence")
+    ap.add_argument("--budget", type=int, default=512, help="cache rows of a sequence (16 bits)")
+    ap.add_argument("--temperature", type=float, default=0.0, help="0: the likeliest tokens")
+    ap.add_argument("--bits", type=int, default=16, choices=(8, 16), help="of the caches")
+    ap.add_argument("--samples", type=int, default=1, help="answers to each prompt (8 bits)")
     args = ap.parse_args(argv)
     model = Model()
     g = torch.Generator().manual_seed(3)
     vocab = model.embed.shape[0]
     prompts = [torch.randint(vocab, (max(args.prompt - 37 * b, 2),), generator=g).tolist()
                for b in range(args.batch)]
-    decode(model, prompts, 2, args.budget)          # loads the libraries
-    texts, evictions, seconds = decode(model, prompts, args.steps, args.budget)
-    said = sum(len(t) - len(p) for t, p in zip(texts, prompts))
-    print(f"{said} tokens in {args.steps} steps of {args.batch} sequences, "
-          f"{said / (args.steps * args.batch):.2f} a step and sequence, {evictions} evictions, "
+    how = dict(temperature=args.temperature, bits=args.bits, samples=args.samples)
+    decode(model, prompts, 2, args.budget, **how)   # loads the libraries
+    texts, evictions, seconds = decode(model, prompts, args.steps, args.budget, **how)
+    said = sum(map(len, texts)) - args.samples * sum(map(len, prompts))
+    print(f"{said} tokens in {args.steps} steps of {len(texts)} sequences, "
+          f"{said / (args.steps * len(texts)):.2f} a step and sequence, {evictions} evictions, "
           f"{1e3 * seconds / args.steps:.2f} ms a step")
 
 

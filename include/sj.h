@@ -478,8 +478,9 @@ int sj_cache8_append(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, co
                      const int64_t q_out_stride[3]);
 
 /* sj_attend over a cache in 8 bits: the definitions, arithmetic and errors of sj_attend with k_n
- * and v_n the 16-bit values that the elements stand for (an exponent that the append would not
- * set may leave the type's range: such values round as the type does). */
+ * and v_n the 16-bit values that the elements stand for.  (With exponents outside the range that the
+ * append sets they may not be values of the type; the results are then unspecified, the accesses
+ * are not.) */
 int sj_attend8(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
                uint32_t t, const void *q, const int64_t q_stride[3], uint32_t q_heads,
                const uint64_t *tree, const int64_t tree_stride[2], double scale, void *out,
@@ -511,7 +512,8 @@ int sj_cache_pages(sj_ctx *ctx, const int32_t *table, int64_t table_row, uint32_
 /* Copies pages within a cache: for each of the n entries of copies (device, int32 {from, to, rows})
  * the first `rows` rows (at most page) of page `from`, of all heads, k and v, to page `to`.  Entries whose pages
  * do not exist, or are the same, copy nothing.  No page may be copied to by two entries or be both copied
- * to and from.  The cache's table is not used.  Errors as the joins'. */
+ * to and from.  The cache's table is not used.  Errors as the joins'; SJ_E_UNSUPPORTED for more than
+ * 65535 heads. */
 int sj_cache_copy(sj_ctx *ctx, const sj_cache *cache, const int32_t *copies, uint32_t n);
 
 /* The same within a cache in 8 bits, with the exponents of the blocks that the rows are in. */

@@ -1066,8 +1066,8 @@ def cache_pages(table, lengths, tokens: int, *, pages: int, page: int, parent=No
     if parent is not None:
         out_batch = parent.numel()
         _check_whole("parent", parent, (out_batch,), torch.int32, dev)
-    if tokens < 0 or pages < 0 or page <= 0:
-        raise ValueError("tokens and pages must not be negative, page positive")
+    if not (0 <= tokens < 2 ** 32 and 0 <= pages < 2 ** 32 and 0 < page < 2 ** 32):
+        raise ValueError("tokens and pages must not be negative, page positive, all below 2^32")
     new_table, new = lengths.new_empty((out_batch, width)), lengths.new_empty((out_batch,))
     copies, lacking = lengths.new_empty((out_batch, 3)), lengths.new_empty((out_batch,))
     st = sj_cache_pages(ctx or _current(dev), _ptr(table), table.stride(0), B, width, pages, page,

@@ -656,7 +656,7 @@ namespace {
 int copy_rows(sj_ctx *c, sjc::Copy &k, const int32_t *copies, uint32_t n)
 {
     const uint64_t chunks = ((uint64_t)k.c.d * k.size + 15) / 16;
-    if ((uint64_t)k.c.div.page * k.c.heads * chunks >= kMaxCells - 65536)
+    if (k.c.heads > 65535 || (uint64_t)k.c.div.page * k.c.heads * chunks >= kMaxCells - 65536)
         return fail(SJ_E_UNSUPPORTED, "pages of %u rows of %u heads are too long", k.c.div.page,
                     k.c.heads);
     if (n == 0 || k.c.pages == 0)

@@ -376,6 +376,51 @@ def test_refusals():
     assert sj.sj_attend8(ctx, r, *args) == sj.SJ_E_INVAL
 
 
+def test_pools_without_pages_and_calls_without_tokens():
+    import torch
+    import paper_2006_12608_amd as sj
+    say("empty8")
+    none = torch.empty(0, 16, 2, 64, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    ex = torch.empty(0, 2, 2, 2, dtype=torch.int8, device="cuda")
+    table = torch.full((3, 4), -1, dtype=torch.int32, device="cuda")
+    lens = torch.tensor([0, 5, -1], dtype=torch.int32, device="cuda")
+    x = torch.randn(3, 2, 2, 64, device="cuda").bfloat16()
+    cache = sj.kv_cache8(none, none, ex, table)
+    sj.cache_append(cache, lens, x, x)
+    w = torch.full((3, 2, 9), 7.0, device="cuda")
+    out, lse = sj.attend(cache, lens, x, weight_out=w)
+    assert (out == 0).all() and (lse == -np.inf).all() and (w == 0).all()
+    sj.cache_copy(cache, torch.zeros(2, 3, dtype=torch.int32, device="cuda"))
+    c = Case8(16, "bf16", 2, 3, 2, 2, 64, 16, [3, 4], 8)
+    sj.cache_append(c.cache, dev(c.lens), c.dq[:, :0, :2], c.dq[:, :0, :2])
+    check_bytes(c)
+    out, lse = sj.attend(c.cache, dev(c.lens), c.dq[:, :0])
+    assert out.shape == (2, 0, 4, 64) and lse.shape == (2, 0, 4)
+
+
+@pytest.mark.parametrize("T,weights", [(1, False), (7, True), (60, True)])
+def test_attend8_into_its_queries_and_on_another_stream(T, weights):
+    """out may be q where no weights are asked for; a call on a side stream gives the same bits."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("attend8 streams", T)
+    c = Case8(17, "bf16", 4, T, 4, 4, 128, 64, [9000, 30, 7000, 12000], 16)
+    lens = dev(c.lens)
+    kw = dict(weight_out=torch.empty(4, 4, c.cache.room, device="cuda")) if weights else {}
+    want = sj.attend(c.cache, lens, c.dq, **kw)
+    first = [x.clone() for x in want] + [x.clone() for x in kw.values()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [*sj.attend(c.cache, lens, c.dq, **kw), *kw.values()]
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(first, got))
+    if not weights:
+        q = c.dq.clone()
+        out, lse = sj.attend(c.cache, lens, q, out=q)
+        assert out is q and torch.equal(q, first[0]) and torch.equal(lse, first[1])
+
+
 def test_gradients_are_not_lost_silently():
     import torch
     import paper_2006_12608_amd as sj

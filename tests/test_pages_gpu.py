@@ -108,7 +108,7 @@ def test_pages_strided_table_refusals_and_graph():
     got = sj.cache_pages(wide[:, 2:8], lens, 6, pages=50, page=4, parent=parent)
     want = ref8.pages(wide[:, 2:8].cpu().numpy(), [20, 5, 9, 0], 6, 50, 4, np.array([0, 0, 2]))
     assert all(np.array_equal(x.cpu().numpy(), y) for x, y in zip(got, want))
-    for bad in (dict(tokens=-1), dict(pages=-1), dict(page=0)):
+    for bad in (dict(tokens=-1), dict(pages=-1), dict(page=0), dict(tokens=2 ** 32), dict(pages=2 ** 33)):
         kw = dict(dict(tokens=1, pages=5, page=2), **bad)
         with pytest.raises(ValueError):
             sj.cache_pages(wide, lens, kw["tokens"], pages=kw["pages"], page=kw["page"])

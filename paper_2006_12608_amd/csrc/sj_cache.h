@@ -307,12 +307,12 @@ struct Verify {
     const float *uniform;
     int32_t *path, *found;
     int64_t *next;
-    uint32_t chunks;                    // of VE_CHUNK tokens of the vocabulary
+    uint32_t parts, chunks;             // of VE_CHUNK tokens; chunks of the vocabulary of so many parts
     double *sums;                       // per sequence and chunk
     uint32_t *arrivals;                 // per sequence, zeros between calls
 };
 
-constexpr uint32_t VE_CHUNK = 4096, VE_MOST = 1024;   // tokens of a workgroup; nodes at most
+constexpr uint32_t VE_CHUNK = 4096, VE_MOST = 1024;   // tokens that a workgroup takes at once; nodes at most
 
 hipError_t launch_verify(const Verify &v, hipStream_t s);
 

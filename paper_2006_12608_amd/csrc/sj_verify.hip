@@ -285,10 +285,12 @@ __device__ __forceinline__ double get_sum(const double *p)
                                                         __HIP_MEMORY_SCOPE_AGENT));
 }
 
-// A workgroup sums the weights of one chunk of the vocabulary in double, after walking through its
+// A workgroup sums the weights of one chunk of the vocabulary (PARTS x VE_CHUNK tokens) in double, after walking through its
 // sequence's nodes (every workgroup for itself); the last one of a sequence to arrive finds the
-// chunk, thread and token where the sums pass the threshold, and reads that chunk again.
-template <int DT>
+// chunk, thread and token where the sums pass the threshold, and reads that chunk again.  Bound
+// by latency for few sequences (count, tokens, probabilities, row, sums, row: 10 us for a chain over 32768
+// tokens); 64 chains over 131072 tokens, 67 MB, in 25 us, of which 6 are the last workgroups'.
+template <int DT, uint32_t PARTS>
 __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
 {
     extern __shared__ int64_t lists[];      // tokens refused (t), then the path (t)
@@ -311,8 +313,13 @@ __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
     Weights<DT> y;
     double all = 0.0;
     if (w.nodes > 0) {
-        y.load(v, b, w, gone, chunk);
-        add_before(y.sum(false), waves, &all);
+        double x = 0.0;
+#pragma unroll 1
+        for (uint32_t i = 0; i < PARTS; ++i) {
+            y.load(v, b, w, gone, chunk * PARTS + i);
+            x += y.sum(false);
+        }
+        add_before(x, waves, &all);
     }
     double *const sums = v.sums + (uint64_t)b * v.chunks;
     if (tid == 0) {
@@ -348,8 +355,13 @@ __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
         // to 1 do not come to this, but for rounding)
         plain = true;
         for (uint32_t c = 0; c < v.chunks; ++c) {
-            y.load(v, b, w, gone, c);
-            add_before(y.sum(true), waves, &all);
+            double x = 0.0;
+#pragma unroll 1
+            for (uint32_t i = 0; i < PARTS; ++i) {
+                y.load(v, b, w, gone, c * PARTS + i);
+                x += y.sum(true);
+            }
+            add_before(x, waves, &all);
             if (tid == 0)
                 put_sum(sums + c, all);
         }
@@ -390,12 +402,31 @@ __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
         before = at;
     }
     __syncthreads();
-    const uint32_t there = at_chunk;
-    y.load(v, b, w, gone, there);
-    mine = y.sum(plain);
-    begin = before + add_before(mine, waves, &all);
-    who = first_thread(mine > 0.0 && begin + mine > threshold, found);
-    who = who < 256 ? who : last_thread(mine > 0.0, found);
+    // the part of the chunk, likewise
+    uint32_t there = at_chunk * PARTS, pick = there;
+    double sofar = before, pick_begin = 0.0;
+    who = 256;
+#pragma unroll 1
+    for (const uint32_t end = there + PARTS;; ) {
+        y.load(v, b, w, gone, there);
+        mine = y.sum(plain);
+        begin = sofar + add_before(mine, waves, &all);
+        const uint32_t first = first_thread(mine > 0.0 && begin + mine > threshold, found);
+        const uint32_t last = last_thread(mine > 0.0, found);
+        if (last < 256) {
+            pick = there;
+            pick_begin = begin;
+            who = first < 256 ? first : last;
+        }
+        if (first < 256 || ++there == end)
+            break;
+        sofar += all;
+    }
+    if (pick != there) {
+        y.load(v, b, w, gone, pick);
+        there = pick;
+    }
+    begin = pick_begin;
     if (tid == who) {
         uint32_t last = 0;
         double sum = begin;
@@ -413,6 +444,12 @@ __global__ void __launch_bounds__(256) verify_chunks(const VerifyArgs g)
     }
 }
 
+template <int DT>
+void (*verify_kernel(uint32_t parts))(const VerifyArgs)
+{
+    return parts == 1 ? verify_chunks<DT, 1> : verify_chunks<DT, 2>;
+}
+
 }  // namespace
 
 hipError_t launch_verify(const Verify &v, hipStream_t s)
@@ -427,11 +464,11 @@ hipError_t launch_verify(const Verify &v, hipStream_t s)
         const dim3 grid((uint32_t)(left < step ? left : step));
         const size_t lds = (size_t)v.t * 12;
         if (v.dtype == 5)
-            verify_chunks<5><<<grid, 256, lds, s>>>(g);
+            verify_kernel<5>(v.parts)<<<grid, 256, lds, s>>>(g);
         else if (v.dtype == sjk::DT_F16)
-            verify_chunks<sjk::DT_F16><<<grid, 256, lds, s>>>(g);
+            verify_kernel<sjk::DT_F16>(v.parts)<<<grid, 256, lds, s>>>(g);
         else
-            verify_chunks<sjk::DT_BF16><<<grid, 256, lds, s>>>(g);
+            verify_kernel<sjk::DT_BF16>(v.parts)<<<grid, 256, lds, s>>>(g);
         e = hipGetLastError();
     }
     return e;

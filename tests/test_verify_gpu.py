@@ -85,7 +85,7 @@ def drafted(rng, B, T, V, parent=None, chance=True, sharp=2.0):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("B,T,V", [(1, 1, 1), (3, 2, 5), (4, 5, 4096), (2, 7, 4097), (5, 66, 100), (2, 4, 33001),
-                                   (40, 3, 777), (1, 5, 131072)])
+                                   (40, 3, 777), (1, 5, 131072), (400, 2, 20000)])
 def test_chains(dtype, B, T, V):
     say("chains", dtype, B, T, V)
     rng = np.random.default_rng(B + T + V)
@@ -145,6 +145,23 @@ def test_numbers_at_the_ends_and_probabilities_of_every_kind():
     nan = sj.verify_drafts(dev(tokens), put(p, "f32"), torch.full((B, T), float("nan"), device="cuda"))
     zero = sj.verify_drafts(dev(tokens), put(p, "f32"), torch.zeros((B, T), device="cuda"))
     assert all(torch.equal(x, y) for x, y in zip(nan, zero))
+
+
+@pytest.mark.parametrize("B,V", [(3, 9000), (400, 20000)])
+def test_nothing_left_but_the_targets_own(B, V):
+    """Drafts as likely as the target's, and tokens that neither gives: every one is refused, nothing is
+    left of the difference, and the token is drawn from the target itself."""
+    say("nothing left", B, V)
+    rng = np.random.default_rng(V)
+    p = softmax(rng.standard_normal((B, 2, V)))
+    p[..., ::3] = 0.0
+    p[:, :, :V // 2] *= rng.random((B, 2, 1)) < 0.5
+    tokens = 3 * rng.integers(0, V // 3, (B, 2))
+    target = put(p, "f32")
+    path, found, nxt = check(tokens, target, rng.random((B, 2)), target[:, :1].contiguous())
+    assert (found == 1).all() and (nxt % 3 != 0).all()
+    if B > 100:     # (three sequences may all be drawn from the upper half)
+        assert (nxt >= V // 2).any() and (nxt < V // 2).any()
 
 
 @pytest.mark.parametrize("kind", ["chain", "certain", "tree"])

@@ -47,13 +47,13 @@ __device__ __forceinline__ int exponent_of(float x)
 // 2^e, -126 <= e <= 127.
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// x rounded to e4m3 in byte 0 or 1, 2 or 3 of a word, two at a time: between -448 and 448 first
-// (the type's largest), NaN for what is not finite.
+// x between e4m3's least and largest values, -448 and 448, or NaN where it is not finite.
 __device__ __forceinline__ float bound(float x, bool finite)
 {
     return finite ? fminf(fmaxf(x, -448.f), 448.f) : __uint_as_float(0x7fc00000u);
 }
 
+// Four values rounded to e4m3, ties to even, in the bytes of a word.
 __device__ __forceinline__ uint32_t four(float a, float b, float c, float d)
 {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
@@ -61,8 +61,8 @@ __device__ __forceinline__ uint32_t four(float a, float b, float c, float d)
 }
 
 // Eight elements of a key row from element c on, turned and rounded to the 16-bit type.  The partner of
-// an element is `pairs`, a multiple of 8, elements on or back (HALF), or beside it; x cos -+ partner sin is turn_a and
-// turn_b, as they round.
+// an element is `pairs`, a multiple of 8, elements on or back (HALF), or beside it; x cos -+ partner sin
+// is turn_a and turn_b, as they round.
 template <int DT, bool HALF>
 __device__ __forceinline__ i32x4 turned8(uint32_t pairs, const uint16_t *row, i32x4 v, uint32_t c,
                                          const float2 *sines)
@@ -93,15 +93,16 @@ __device__ __forceinline__ i32x4 turned8(uint32_t pairs, const uint16_t *row, i3
 // in blocks of 64 rows of 256, 17 -> 6 us) takes one block of a sequence's rows, one head, keys or
 // values: the largest magnitude of the new rows in it (a maximum of 16-bit integers), from that
 // the exponent, the rows before len[b] rounded to it where it grows, and the new rows' e4m3
-// values.  Sines are computed once for the workgroup's heads, into LDS.  Bound by HBM (2 bytes in, 1 out: 8 x 2048 tokens of 8 heads of 128, 101 MB, in 23 us), for
-// a token or two by the chain lengths, page, exponent, rows.
+// values.  Sines are computed once for the workgroup's heads, into LDS.  Bound by HBM (2 bytes in, 1
+// out: 8 x 2048 tokens of 8 heads of 128, 101 MB, in 23 us), for a token or two by the chain
+// lengths, page, exponent, rows.
 // TURN: keys are turned in halves (1) or adjacent pairs (2).
 template <int DT, int TURN, uint32_t WAVES>
 __global__ void __launch_bounds__(256, 4) append8_blocks(const Append8Args g)
 {
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     constexpr int HELD = held_chunks(TURN != 0);
-    __shared__ float2 sines[TURN != 0 ? A8_SINES + 1 : 1];
+    __shared__ float2 sines[TURN != 0 ? A8_SINES : 1];
     const Append8 &r = g.r;
     const uint32_t tid = threadIdx.x & (64 * WAVES - 1);    // of the unit's threads
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

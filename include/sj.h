@@ -510,10 +510,10 @@ int sj_cache_pages(sj_ctx *ctx, const int32_t *table, int64_t table_row, uint32_
                    int32_t *new_len, int32_t *copies, int32_t *lacking);
 
 /* Copies pages within a cache: for each of the n entries of copies (device, int32 {from, to, rows})
- * the first `rows` rows (at most page) of page `from`, of all heads, k and v, to page `to`.  Entries whose pages
- * do not exist, or are the same, copy nothing.  No page may be copied to by two entries or be both copied
- * to and from.  The cache's table is not used.  Errors as the joins'; SJ_E_UNSUPPORTED for more than
- * 65535 heads. */
+ * the first `rows` rows (at most page) of page `from`, of all heads, k and v, to page `to`.  Entries
+ * whose pages do not exist, or are the same, copy nothing.  No page may be copied to by two entries
+ * or be both copied to and from.  The cache's table is not used.  Errors as the joins';
+ * SJ_E_UNSUPPORTED for more than 65535 heads. */
 int sj_cache_copy(sj_ctx *ctx, const sj_cache *cache, const int32_t *copies, uint32_t n);
 
 /* The same within a cache in 8 bits, with the exponents of the blocks that the rows are in. */
@@ -535,8 +535,8 @@ enum sj_float { SJ_F32 = 5 };
  *   - without (tokens chosen without chance): n is accepted if p(c, x) > 0 and
  *     u(n) left < p(c, x), where left is 1 less the p(c, .) of the tokens refused at c; a token
  *     refused there already has p = 0.
- * An accepted node becomes c.  Where nothing more is accepted the text goes on with a token drawn by u(0): the
- * lowest x with sum_{y <= x} r(y) > u(0) sum r, where r = max(p(c, .) - draft(c, .), 0) after a
+ * An accepted node becomes c.  Where nothing more is accepted the text goes on with a token drawn by
+ * u(0): the lowest x with sum_{y <= x} r(y) > u(0) sum r, where r = max(p(c, .) - draft(c, .), 0) after a
  * refusal with draft, else p(c, .) with 0 for the tokens refused at c; if r is 0 everywhere r
  * is p(c, .), and if that is 0 everywhere the token is -1.  So text that follows the
  * rule is distributed as the target's.  u(n) = uniform[b * t + n] (fp32, in [0, 1); outside it counts

@@ -762,7 +762,8 @@ class kv_cache:
         self.batch, self.width = (pages, 1) if table is None else table.shape
         # (a table without columns has no address, but NULL would mean that there is none;
         # nothing is read of it)
-        self.raw = sj_cache(SJ_F16 if dtype is torch.float16 else SJ_BF16, heads, d, pages, page, self.batch, self.width,
+        self.raw = sj_cache(SJ_F16 if dtype is torch.float16 else SJ_BF16, heads, d, pages, page,
+                            self.batch, self.width,
                             0 if table is None else table.stride(0),
                             None if table is None else (_ptr(table) or _ptr(k)),
                             _ptr(k), _ptr(v), *k.stride()[:3], *v.stride()[:3])
@@ -886,9 +887,10 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     are (sequences, tokens, heads, d); lengths and counts int32 per sequence, pos
     int32 (sequences, tokens).  q (sequences, tokens, query heads, d), when
     given, is turned by the same positions and returned (in q_out, which may be
-    q).  Into a kv_cache8 the turned keys and the values are rounded to 8 bits (sj_cache8_append); the
-    blocks of rows appended to must be of one sequence each.  There is no gradient: a backward pass through the result raises.  May be
-    captured into a HIP graph, as rotary may (into a kv_cache8: see attend)."""
+    q).  Into a kv_cache8 the turned keys and the values are rounded to 8 bits
+    (sj_cache8_append); the blocks of rows appended to must be of one sequence each.  There is no
+    gradient: a backward pass through the result raises.  May be captured into a HIP graph, as
+    rotary may (into a kv_cache8: see attend)."""
     import torch
     if cache.follows or key.requires_grad or value.requires_grad or _follows(q, q_out):
         if torch.is_grad_enabled():
@@ -935,8 +937,8 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
 def attend(cache, lengths, q, tree=None, *, scale: float | None = None, counts=None, weight=None,
            weight_out=None, out=None, ctx=None):
     """Attention of a few tokens of every sequence over its rows in the cache
-    (sj_attend, or sj_attend8 for a kv_cache8).  q is (sequences, tokens, query heads, d); query head i reads cache head
-    i // (query heads / cache heads).  Token u of sequence b sees the
+    (sj_attend, or sj_attend8 for a kv_cache8).  q is (sequences, tokens, query
+    heads, d); query head i reads cache head i // (query heads / cache heads).  Token u of sequence b sees the
     lengths[b] rows before the call's tokens and, of the tokens' own rows (which
     follow them, appended beforehand), those that its mask names: bit w % 64 of
     tree[b, u, w // 64] for token w (tree: int64 (sequences or 1, tokens,

@@ -69,9 +69,12 @@ __device__ __forceinline__ Node node_of(const Verify &v, uint32_t b, uint32_t n)
         return k;
     k.parent = from;
     if ((uint64_t)k.token < v.vocab) {
-        k.p = clean(Prob<DT>::of(((const one *)v.target)[(int64_t)b * v.p_seq + (int64_t)from * v.p_row + k.token]));
-        if (v.draft)
-            k.q = clean(Prob<DT>::of(((const one *)v.draft)[(int64_t)b * v.q_seq + (int64_t)from * v.q_row + k.token]));
+        const one *p = (const one *)v.target + (int64_t)b * v.p_seq + (int64_t)from * v.p_row;
+        k.p = clean(Prob<DT>::of(p[k.token]));
+        if (v.draft) {
+            const one *q = (const one *)v.draft + (int64_t)b * v.q_seq + (int64_t)from * v.q_row;
+            k.q = clean(Prob<DT>::of(q[k.token]));
+        }
     }
     return k;
 }
@@ -285,8 +288,8 @@ __device__ __forceinline__ double get_sum(const double *p)
                                                         __HIP_MEMORY_SCOPE_AGENT));
 }
 
-// A workgroup sums the weights of one chunk of the vocabulary (PARTS x VE_CHUNK tokens) in double, after walking through its
-// sequence's nodes (every workgroup for itself); the last one of a sequence to arrive finds the
+// A workgroup sums the weights of one chunk of the vocabulary (PARTS x VE_CHUNK tokens) in double,
+// after walking through its sequence's nodes (every workgroup for itself); the last one of a sequence to arrive finds the
 // chunk, thread and token where the sums pass the threshold, and reads that chunk again.  Bound
 // by latency for few sequences (count, tokens, probabilities, row, sums, row: 10 us for a chain over 32768
 // tokens); 64 chains over 131072 tokens, 67 MB, in 25 us, of which 6 are the last workgroups'.

@@ -468,7 +468,8 @@ typedef struct sj_cache8 {
  * becomes x / 2^e, rounded to nearest even and held between -448 and 448; infinities
  * and NaN become NaN and do not count for the exponents.  Keys are turned first, as
  * sj_cache_append turns them, and rounded to the 16-bit type.  The blocks that a call appends to
- * must be of one sequence each.  (Keys to be turned into blocks of more than 2048 rows x pairs, or in
+ * must be of one sequence each; a sequence without rows to append (count[b] <= 0, or no room left)
+ * neither reads nor writes its pages, whoever else has them.  (Keys to be turned into blocks of more than 2048 rows x pairs, or in
  * halves of a number of pairs that 8 does not divide, pass through device scratch.) */
 int sj_cache8_append(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
                      uint32_t t, const void *key, const int64_t key_stride[3], const void *value,

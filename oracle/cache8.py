@@ -59,6 +59,8 @@ def append(k8, v8, ex, row_of, lens, key, value, block, dtype, counts=None, room
                 continue
             p, s = r
             old, new = max(n0 - begin, 0), min(begin + block, end) - begin
+            if new <= old:      # nothing is appended
+                continue
             for h in range(heads):
                 for i, (pool, x) in enumerate(((k8, key), (v8, value))):
                     rows = x[b, begin + old - n0:begin + new - n0, h]

@@ -888,7 +888,8 @@ def cache_append(cache, lengths, key, value, *, pos=None, turns=None, q=None, la
     int32 (sequences, tokens).  q (sequences, tokens, query heads, d), when
     given, is turned by the same positions and returned (in q_out, which may be
     q).  Into a kv_cache8 the turned keys and the values are rounded to 8 bits
-    (sj_cache8_append); the blocks of rows appended to must be of one sequence each.  There is no
+    (sj_cache8_append); the blocks of rows appended to must be of one sequence each, and
+    sequences with a count of 0 leave theirs as they are.  There is no
     gradient: a backward pass through the result raises.  May be captured into a HIP graph, as
     rotary may (into a kv_cache8: see attend)."""
     import torch

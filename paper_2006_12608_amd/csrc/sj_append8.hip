@@ -116,7 +116,8 @@ __global__ void __launch_bounds__(256, 4) append8_blocks(const Append8Args g)
     const uint32_t end = all < r.c.room ? (uint32_t)all : r.c.room;
     // (blocks do not cross pages, so a sequence's blocks are those of its rows)
     const uint64_t row0 = ((uint64_t)r.c.by_block.quot(len) + j) * size;
-    if (row0 >= end)
+    // (a sequence that appends nothing writes nothing: its page may be another one's by now)
+    if (row0 >= end || len >= end)
         return;
     const Place p = place_of(r.c, b, (uint32_t)row0);
     if (p.page < 0)

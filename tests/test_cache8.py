@@ -100,3 +100,21 @@ def test_the_rule_keeps_the_targets_distribution():
     rest = np.maximum(p - q, 0)
     got = q * pass_ + (q * (1 - pass_)).sum() * rest / rest.sum()
     assert np.allclose(got, p)
+
+
+def test_a_call_that_appends_nothing_changes_nothing():
+    """Sequence 0 ends inside a block and appends no row: its bytes and exponents, the least ones of
+    int8 among them, stay, also where sequence 1 appends to the same page."""
+    rng = np.random.default_rng(1)
+    k8, v8 = (rng.integers(0, 126, (2, 4, 1, 8)).astype(np.uint8) for _ in "kv")
+    ex = np.full((2, 1, 1, 2), -120, np.int8)
+    before = [x.copy() for x in (k8, v8, ex)]
+    rows = rng.standard_normal((1, 2, 1, 8))
+    for count in (0, -1):
+        ref.append(k8, v8, ex, lambda b, n: (0, n), [3], rows, rows, 4, "bf16", [count])
+        assert all(np.array_equal(x, y) for x, y in zip((k8, v8, ex), before))
+    alone = [x.copy() for x in before]
+    rows = np.concatenate([rows * 0, rows * 512])
+    ref.append(*alone, lambda b, n: (0, n), [2], rows[1:], rows[1:], 4, "bf16")
+    ref.append(k8, v8, ex, lambda b, n: (0, n), [3, 2], rows, rows, 4, "bf16", [0, 2])
+    assert all(np.array_equal(x, y) for x, y in zip((k8, v8, ex), alone)) and ex[0, 0, 0, 0] > -10

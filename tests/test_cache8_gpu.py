@@ -253,6 +253,32 @@ def test_append8_counts_holes_and_the_room():
     appended(c, key, key * 3, counts=counts)
 
 
+@pytest.mark.parametrize("turn", [False, True])
+@pytest.mark.parametrize("page,block,T", [(16, 16, 3), (256, 128, 90)])
+def test_append8_idle_sequences_leave_the_pages_they_name(page, block, T, turn):
+    """Sequences that append nothing (a count of 0 or less) name the page that another one appends
+    much larger rows to, or hold rows at an exponent below the type's: they write nothing."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("append8 idle", page, block, T, turn)
+    heads, d = 16, 64
+    lens = [5, 7, 1, 15, 3, 9, 14, 4]
+    c = Case8(18, "bf16", 8, T, heads, 1, d, page, lens, block)
+    c.table[1:7] = c.table[0]
+    c.cache.table = dev(c.table)
+    c.ex[c.table[7, 0], 0] = -120
+    c.dex.copy_(dev(c.ex))
+    counts = np.array([T, 0, 0, -1, 0, -9, 0, 0], np.int32)
+    key = dev(c.rng.standard_normal((8, T, heads, d)) * 2.0 ** 14, "bf16")
+    before = c.ex.copy()
+    kw = {}
+    if turn:        # by nothing: turned rows are the rows
+        kw = dict(pos=torch.zeros(8, T, dtype=torch.int32, device="cuda"), turns=sj.rotary_turns(32))
+    appended(c, key, key.flip(2), counts=counts, **kw)
+    assert (c.ex[c.table[0, 0], 0] > before[c.table[0, 0], 0]).all()
+    assert (c.ex[c.table[7, 0], 0] == -120).all()
+
+
 @pytest.mark.parametrize("order", ["heads", "wide"])
 def test_append8_strides(order):
     say("append8 strides", order)

@@ -291,13 +291,15 @@ int append_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     w.key = r.key;
     w.value = r.value;
     r.c.batch = 0;
+    // long blocks, halves that begin inside a chunk: the keys are turned on the way into scratch, which is
+    // there before the first launch, since a call that is refused must not have turned the queries
+    const bool passes =
+        (uint64_t)block * n_pairs > sjc::A8_SINES || (layout == SJ_HALF && n_pairs % 8 != 0);
+    if (passes && (st = grow_both(c, (size_t)((uint64_t)B * t * heads * d * 2), 0)) != SJ_OK)
+        return st;
     if (q)                  // (the queries alone)
         SJ_HIP(sjc::launch_rotary(r, c->stream));
-    if ((uint64_t)block * n_pairs > sjc::A8_SINES || (layout == SJ_HALF && n_pairs % 8 != 0)) {
-        // long blocks, halves that begin inside a chunk: the keys are turned on the way into scratch
-        const uint64_t cells = (uint64_t)B * t * heads * d;
-        if ((st = grow_both(c, (size_t)cells * 2, 0)) != SJ_OK)
-            return st;
+    if (passes) {
         const int64_t row = (int64_t)heads * d;
         r.x = {(const uint16_t *)key, (uint16_t *)c->scratch, key_stride[0], key_stride[1],
                key_stride[2], row * t, row, d, heads};

@@ -312,6 +312,46 @@ def test_append8_turned(dtype, layout, d, rot, T, page, block):
     assert torch.equal(q.view(want_q.shape), want_q)
 
 
+@pytest.mark.parametrize("layout,rot,page", [("half", 38, 16), ("interleaved", 64, 256)])
+def test_append8_refused_in_a_capture_leaves_the_queries(layout, rot, page):
+    """Keys that pass through scratch: where it would grow during a capture the call is refused, and
+    nothing of it is in the graph; queries turned in place are turned once, by the call that is not
+    refused."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("append8 refused", layout, rot, page)
+    c = Case8(19, "bf16", 2, 5, 2, 2, 80, page, [3, 16], page)
+    turns = sj.rotary_turns(rot)
+    lens, key = dev(c.lens), c.dq[:, :, :2].clone()
+    pos = torch.arange(10, dtype=torch.int32, device="cuda").view(2, 5) + 1
+    q = c.dq.clone()
+    want = sj.rotary(q.view(10, 4, 80), pos.view(-1), turns, layout=layout).view(q.shape)
+    turned = sj.rotary(key.view(10, 2, 80), pos.view(-1), turns, layout=layout).view(key.shape)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    ctx = sj.sj_create(torch.cuda.current_device(), stream.cuda_stream)
+    args = (c.cache, lens, key, key)
+    kw = dict(pos=pos, turns=turns, q=q, q_out=q, layout=layout, ctx=ctx)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        with pytest.raises(sj.SjError, match="capture"):
+            sj.cache_append(*args, **kw)
+        seen = q + 0
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q, c.dq) and torch.equal(seen, c.dq)
+    check_bytes(c)
+    with torch.cuda.stream(stream):
+        sj.cache_append(*args, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(q, want)
+    ref8.append(c.b8[0], c.b8[1], c.ex, lambda b, n: ref.row_of(c.table, c.page, c.k8.shape[0], b, n),
+                c.lens, host(turned), host(key), c.block, c.dtype)
+    check_bytes(c)
+    del graph
+    sj.sj_destroy(ctx)
+
+
 def test_append8_then_attend_graph():
     """Append and attend captured together, replayed with other inputs, lengths and pages in place."""
     import torch

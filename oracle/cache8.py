@@ -65,7 +65,7 @@ def append(k8, v8, ex, row_of, lens, key, value, block, dtype, counts=None, room
                 for i, (pool, x) in enumerate(((k8, key), (v8, value))):
                     rows = x[b, begin + old - n0:begin + new - n0, h]
                     e = exponent(rows, dtype)
-                    was = int(ex[p, s // block, h, i])
+                    was = max(int(ex[p, s // block, h, i]), -126)
                     if old and was >= e:
                         e = was
                     elif old:

@@ -47,6 +47,9 @@ __device__ __forceinline__ int exponent_of(float x)
 // 2^e, -126 <= e <= 127.
 __device__ __forceinline__ float power(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// 2^-e, -127 <= e <= 127 (2^-127 is subnormal).
+__device__ __forceinline__ float power_less(int e) { return e < 127 ? power(-e) : 0x1p-127f; }
+
 // x between e4m3's least and largest values, -448 and 448, or NaN where it is not finite.
 __device__ __forceinline__ float bound(float x, bool finite)
 {
@@ -210,7 +213,7 @@ __global__ void __launch_bounds__(256, 4) append8_blocks(const Append8Args g)
         }
         int e = exponent_of<DT>(to_float(DT, top));
         if (from > 0) {
-            const int old = was < -126 ? -126 : (was > 126 ? 126 : was);
+            const int old = was < -126 ? -126 : was;
             e = e > old ? e : old;
             if (e > old) {      // the rows that are there
                 const float f = power(old - e < -126 ? -126 : old - e);
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(256, 4) append8_blocks(const Append8Args g)
                 }
             }
         }
-        const float f = power(-e);
+        const float f = power_less(e);
         auto put = [&](uint32_t s, i32x4 v) {
             uint32_t w[2];
 #pragma unroll

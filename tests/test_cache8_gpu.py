@@ -244,6 +244,31 @@ def test_append8_values_of_every_kind(dtype):
     appended(c, t, t.neg())
 
 
+@pytest.mark.parametrize("e", [127, 126, 125, 119, -118, -126, -127, -128])
+def test_append8_behind_rows_of_every_exponent(e):
+    """Exponents that the append does not set itself, at the ends of int8 (below -126: as -126): one that is
+    not less than the new rows' stays, the others' rows are rounded to the new one; what the rows
+    stand for is the same."""
+    say("append8 exponents", e)
+    c = Case8(20, "bf16", 3, 2, 2, 1, 32, 16, [5, 1, 14], 8)
+    for name, b in (("k8", c.b8[0]), ("v8", c.b8[1])):
+        b[...] = c.rng.integers(0, 0x40, b.shape)       # (below 2, so that values stay finite)
+        getattr(c, name).copy_(dev8(b))
+    c.ex[...] = e
+    c.dex.copy_(dev(c.ex))
+    x = np.zeros((3, 2, 2, 32))
+    x[0] = 3.2e38 * np.linspace(-1, 1, 32)
+    x[1] = 2.0 ** -120
+    key = dev(x, "bf16")
+    p, s = c.table[0, 0], slice(0, 5)
+    want = ref8.e4m3(c.b8[1][p, s]) * 2.0 ** max(e, -126)
+    appended(c, key, key)
+    top = 119 if e < 119 else e
+    assert (c.ex[p, 0] == top).all()
+    got = ref8.e4m3(bytes_of(c.v8)[p, s]) * 2.0 ** int(c.dex[p, 0, 0, 1])
+    assert (np.abs(got - want) <= (2.0 ** (top - 10) if e < 119 else 0)).all()
+
+
 def test_append8_counts_holes_and_the_room():
     say("append8 counts")
     c = Case8(9, "bf16", 7, 9, 2, 1, 64, 16, [0, 15, 20, 3, 14, -7, 30], 8, hole=(2, 1))

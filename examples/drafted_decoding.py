@@ -4,12 +4,14 @@ A small attention model with random weights continues a batch of ragged prompts.
 drafts a tree of likely tokens below the last one, appends their keys (turned by rotary
 positions) and values to the paged caches, lets every drafted token attend to the cache and
 to its own ancestors, and keeps the path that the model itself would have taken: so several
-tokens a step, and the same text as one token at a time.  The softmax weight that each cache
+tokens a step, and (caches in 16 bits) the same text as one token at a time.  The softmax weight that each cache
 row draws is accumulated, and where a cache is full its heaviest rows move to other pages.
 
 With a temperature the text is sampled: the drafted tokens are verified against the model's
 probabilities.  With --bits 8 the caches hold 8 bits and take their pages from a pool instead of
-evicting, and --samples continues every prompt several times, over shared pages.
+evicting, and --samples continues every prompt several times, over shared pages.  In 8 bits a row is
+rounded by the exponent of its block, which drafted rows may raise that are refused afterwards, so the text
+may differ from that of one token at a time.
 
     python examples/drafted_decoding.py [--steps 32] [--batch 4] [--budget 512]
     python examples/drafted_decoding.py --bits 8 --samples 4 --temperature 20

@@ -470,7 +470,8 @@ typedef struct sj_cache8 {
  * sj_cache_append turns them, and rounded to the 16-bit type.  The blocks that a call appends to
  * must be of one sequence each; a sequence without rows to append (count[b] <= 0, or no room left)
  * neither reads nor writes its pages, whoever else has them.  (Keys to be turned into blocks of more than 2048 rows x pairs, or in
- * halves of a number of pairs that 8 does not divide, pass through device scratch.) */
+ * halves of a number of pairs that 8 does not divide, pass through device scratch.)
+ * SJ_E_UNSUPPORTED also where batch x heads x the blocks that t rows may touch are 2^30 or more. */
 int sj_cache8_append(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
                      uint32_t t, const void *key, const int64_t key_stride[3], const void *value,
                      const int64_t value_stride[3], const int32_t *pos, const int64_t *turns,
@@ -504,7 +505,8 @@ int sj_attend8(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const in
  * copies[3 i ..] (int32) the page to copy from, the page to copy to and the rows to copy, or
  * -1, -1, 0 (see sj_cache_copy).  The lengths are clamped as in all calls on caches.
  * No output may overlap an input.  Errors as the joins'; SJ_E_INVAL also for page = 0,
- * SJ_E_UNSUPPORTED for width * page > 2^30, pages or out_batch * width >= 2^31. */
+ * SJ_E_UNSUPPORTED for width * page > 2^30, page, pages, batch or out_batch * width >= 2^31, and
+ * out_batch > 2^22. */
 int sj_cache_pages(sj_ctx *ctx, const int32_t *table, int64_t table_row, uint32_t batch,
                    uint32_t width, uint32_t pages, uint32_t page, const int32_t *len,
                    const int32_t *parent, uint32_t out_batch, uint32_t tokens, int32_t *out_table,
@@ -514,7 +516,8 @@ int sj_cache_pages(sj_ctx *ctx, const int32_t *table, int64_t table_row, uint32_
  * the first `rows` rows (at most page) of page `from`, of all heads, k and v, to page `to`.  Entries
  * whose pages do not exist, or are the same, copy nothing.  No page may be copied to by two entries
  * or be both copied to and from.  The cache's table is not used.  Errors as the joins';
- * SJ_E_UNSUPPORTED for more than 65535 heads. */
+ * SJ_E_UNSUPPORTED for more than 65535 heads, and for pages whose rows and heads have 2^31 - 65536 chunks
+ * of 16 bytes, begun ones counted, or more. */
 int sj_cache_copy(sj_ctx *ctx, const sj_cache *cache, const int32_t *copies, uint32_t n);
 
 /* The same within a cache in 8 bits, with the exponents of the blocks that the rows are in. */
@@ -540,14 +543,17 @@ enum sj_float { SJ_F32 = 5 };
  * u(0): the lowest x with sum_{y <= x} r(y) > u(0) sum r, where r = max(p(c, .) - draft(c, .), 0) after a
  * refusal with draft, else p(c, .) with 0 for the tokens refused at c; if r is 0 everywhere r
  * is p(c, .), and if that is 0 everywhere the token is -1.  So text that follows the
- * rule is distributed as the target's.  u(n) = uniform[b * t + n] (fp32, in [0, 1); outside it counts
- * as the nearer end).
+ * rule is distributed as the target's, as far as the rows of target (and draft) add up to 1: nothing is
+ * normalised but the last draw, and `left` takes the sum to be 1, which rows rounded to 16 bits miss by up
+ * to 2^-8 (bf16) or 2^-11 (fp16).  u(n) = uniform[b * t + n] (fp32, in [0, 1); outside it counts
+ * as the nearer end, NaN as 0).
  * path (batch x t int32) receives the nodes 0, .. accepted, then -1; found (int32 per sequence) their
  * number; next (int64 per sequence) the drawn token; a sequence of no nodes has found = 0 and next = -1.
  * Arithmetic: products, differences and sums in double, in an order that does not depend
  * on timing.  In a HIP graph as sj_attend.
  * Errors as the joins'; SJ_E_INVAL also for t = 0, vocab = 0 or draft with parent; SJ_E_UNSUPPORTED for t
- * > 1024, vocab or batch >= 2^31 / 1024. */
+ * > 1024, vocab >= 2^31, batch >= 2^21, and batch x the vocabulary's parts of 4096 tokens (8192 where
+ * batch x these are more than six a CU) >= 2^31. */
 int sj_verify(sj_ctx *ctx, int dtype, uint32_t batch, uint32_t t, uint32_t vocab,
               const int64_t *tokens, const int32_t *parent, int64_t parent_seq, const int32_t *count,
               const void *target, const int64_t target_stride[2], const void *draft,

@@ -441,7 +441,10 @@ int attend_rows(sj_ctx *c, const sj_cache *cache, const sj_cache8 *cache8, bool 
     // four; heads of 64: 54, 41, 50; one sequence of 2048 rows of 2 heads, which cannot fill it: 12
     // and 16).  A kernel of its own joins these shares: where the last workgroup does, it reads
     // twice the heads' results alone (2 x 131072 rows 125 and 113 us; 2 x 10865 to 19681 rows of 16
-    // heads of 72 with 18 query rows 74 and 38).
+    // heads of 72 with 18 query rows 74 and 38).  The host knows the table's room and not the lengths, so
+    // short sequences of a wide table are taken two heads at once too, with the kernel that joins
+    // (4 x 500 rows of 8 heads of 128: 11 us with room for 512 rows, 14 for 16384; 2048 rows of one
+    // sequence: 12, and 14 for 131072).
     const uint64_t least = sjc::AT_ROWS * sjc::AT_WAVES;
     const bool fills = eight && qt <= 32 &&
                        B * ((a.c.room + least - 1) / least) * a.c.heads * a.tiles > 8 * (uint64_t)c->num_cus;

@@ -466,11 +466,11 @@ typedef struct sj_cache8 {
  * otherwise the block takes the new one and the rows before len[b] are rounded to it (slots from
  * len[b] + count on are left as they were, and what they stand for changes with the exponent).  A row
  * becomes x / 2^e, rounded to nearest even and held between -448 and 448; infinities
- * and NaN become NaN and do not count for the exponents.  Keys are turned first, as
- * sj_cache_append turns them, and rounded to the 16-bit type.  The blocks that a call appends to
- * must be of one sequence each; a sequence without rows to append (count[b] <= 0, or no room left)
- * neither reads nor writes its pages, whoever else has them.  (Keys to be turned into blocks of more than 2048 rows x pairs, or in
- * halves of a number of pairs that 8 does not divide, pass through device scratch.)
+ * and NaN become NaN and do not count for the exponents.  Keys are turned first, as sj_cache_append turns
+ * them, and rounded to the 16-bit type.  The blocks that a call appends to must be of one sequence each;
+ * a sequence without rows to append (count[b] <= 0, or no room left) neither reads nor writes its pages,
+ * whoever else has them.  (Keys to be turned into blocks of more than 2048 rows x pairs, or in halves of
+ * a number of pairs that 8 does not divide, pass through device scratch.)
  * SJ_E_UNSUPPORTED also where batch x heads x the blocks that t rows may touch are 2^30 or more. */
 int sj_cache8_append(sj_ctx *ctx, const sj_cache8 *cache, const int32_t *len, const int32_t *count,
                      uint32_t t, const void *key, const int64_t key_stride[3], const void *value,

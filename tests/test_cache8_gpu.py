@@ -91,6 +91,86 @@ def test_attend8(dtype, shape, mask):
     check_attend(c, tree, weight)
 
 
+def widen_table(c, room):
+    """The same rows in a table with room for more, whose further pages do not exist."""
+    more = np.full((c.B, -(-room // c.page) - c.table.shape[1]), -1, np.int32)
+    c.table = np.concatenate([c.table, more], 1)
+    c.cache.table = dev(c.table)
+    return c
+
+
+# Room enough that a workgroup takes two heads (of an odd number: one), of 1 to 32 query rows, in one
+# share a sequence or several; heads of every variant
+WIDES = [
+    # B, T, heads, group, d, page, lens, room
+    (4, 1, 32, 4, 64, 64, [0, 1, 700, 310], 2560),
+    (3, 3, 32, 2, 128, 64, [300, 650, 33], 3000),
+    (3, 8, 16, 4, 72, 16, [40, 500, 0], 6000),
+    (2, 5, 16, 4, 256, 64, [400, 10], 9000),
+    (2, 2, 16, 8, 136, 48, [47, 300], 9000),
+    (2, 3, 32, 1, 8, 16, [200, 5], 5000),
+    (2, 7, 32, 3, 24, 16, [333, 128], 5000),
+    (1, 1, 31, 4, 56, 64, [900], 9000),
+    (2, 20, 31, 1, 64, 7, [300, 20], 5000),
+    (300, 1, 16, 2, 64, 16, [(7 * b) % 60 for b in range(300)], 128),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", WIDES, ids=lambda s: "x".join(map(str, s[:6])))
+@pytest.mark.parametrize("mask", ["chain", "tree"])
+def test_attend8_wide_tables(dtype, shape, mask):
+    import torch
+    import paper_2006_12608_amd as sj
+    B, T, heads, group, d, page, lens, room = shape
+    say("attend8 wide", dtype, shape[:6], mask)
+    assert B * -(-room // 128) * heads > 8 * 256
+    counts = [T, max(T - 2, 0)] * (B // 2) + [T] * (B % 2) if T > 4 else None
+    c = widen_table(Case8(31, dtype, B, T, heads, group, d, page, lens, 8 if page % 8 == 0 else 1,
+                          counts=counts), room)
+    tree = chain_tree(c.rng, B, T) if mask == "tree" else None
+    weight = c.rng.random((B, heads, c.cache.room + 5)).astype(np.float32)
+    check_attend(c, tree, weight)
+    check_attend(c, tree, None)
+    # into its queries, on another stream: the same bits
+    lens, q = dev(c.lens), c.dq.clone()
+    kw = dict(tree=None if tree is None else dev(tree.view(np.int64)),
+              counts=None if c.counts is None else dev(c.counts))
+    want = sj.attend(c.cache, lens, c.dq, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = sj.attend(c.cache, lens, q, out=q, **kw)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("heads,group", [(16, 2), (16, 5), (31, 1)])
+def test_attend8_wide_tables_hidden_rows_may_hold_anything(dtype, heads, group):
+    """NaN in one head of a drafted token's key and value reaches, of the head that shares its
+    workgroup too, nothing but the tokens that see it there."""
+    import torch
+    import paper_2006_12608_amd as sj
+    say("attend8 wide hidden", dtype, heads, group)
+    T = 6
+    c = widen_table(Case8(32, dtype, 1, T, heads, group, 64, 16, [300], 4), 20000)
+    tree = np.zeros((1, T, 1), np.uint64)
+    for t in range(T):
+        tree[0, t, 0] = sum(1 << w for w in range(t + 1) if w != 2 or t == 2)
+    r = ref.row_of(c.table, c.page, c.k.shape[0], 0, 302)
+    args = (c.cache, dev(c.lens), c.dq, dev(tree.view(np.int64)))
+    plain, _ = sj.attend(*args)
+    for x in (c.k8, c.v8):
+        x.view(torch.uint8)[r[0], r[1], 4] = 127
+    got, lse = sj.attend(*args, weight_out=torch.zeros((1, heads, c.cache.room), device="cuda"))
+    again, _ = sj.attend(*args)
+    hit = torch.zeros(got.shape, dtype=torch.bool, device="cuda")
+    hit[:, 2, 4 * group:5 * group] = True
+    for x in (got, again):
+        assert torch.isnan(x[hit]).all() and torch.equal(x[~hit], plain[~hit])
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("order", ["heads", "wide"])
 @pytest.mark.parametrize("table", ["mixed", None])
